@@ -459,6 +459,120 @@ int comet_beaver_mul(void* cuda_stream, const uint64_t* const X[2], const uint64
                      uint64_t* const D[2], uint64_t* const E[2], uint64_t* const Z[2], int64_t count);
 
 /* ---------------------------------------------------------------------------
+ * Linear layer, Section 2.1 "Multiplication" and "Addition" with the local truncation, for both parties:
+ *     E_i = X_i - A_i,  F_i = W_i - B_i                                     (messages)
+ *     z_i = C_i + E B_i^T + A_i F^T + i E F^T                               (scale 2f)
+ *     y_i = trunc_f(z_i + 2^f bias_i)                                       (scale f)
+ * and, with `quadratic`, the activation k2 y^2 + k1 y + k0 -- the kind that additive shares evaluate without a
+ * comparison -- on the dealer's pair (R, Q), Q = R * R element by element:
+ *     M_i = y_i - R_i                                                       (message),  m = M_0 + M_1
+ *     y_i <- trunc_f(k2 trunc_f(Q_i + 2 m R_i + i m^2) + k1 y_i) + i k0
+ * then, with a residual, Y_i = y_i + residual_i.  trunc_f is comet_truncate's rule.
+ *
+ * Stateless; X, A, E are [tokens, inner], W, B, F [cols, inner] (output-feature-major), C, residual, R, Q, M, Y
+ * [tokens, cols], bias [cols], each pair the two parties'; DEVICE pointers on the current device, 16-byte aligned,
+ * owned by the caller.  bias and residual may be null (both parties' or neither's).  k[0..2] are the coefficients as
+ * ring words at scale f.  What is written (E, F, M, Y and the workspace) must not overlap any other argument.
+ * The work is enqueued on `cuda_stream` (NULL = default stream) and the call does not wait for it.  Up to 32 rows, and
+ * up to 64 of a layer of 786432 weights or more, the product streams the weights (COMET_KERNEL_STREAM); beyond, it goes
+ * through operand planes (COMET_KERNEL_LIMB or COMET_KERNEL_RESIDUE) in `workspace`, 256-byte aligned and of at least
+ * the bytes that comet_linear_workspace reports for these sizes on this device (none for the first kind).  A captured
+ * call keeps its workspace's address; calls whose work may overlap in time need one each.
+ * The kernels' waits are bounded: comet_static_status says whether one ran out.  The first call on a device makes
+ * settings once; make it outside stream capture.
+ * Errors: INVALID_ARG (null or unaligned pointer, overlap, a `quadratic` that is neither 0 nor 1), SHAPE (inner not a
+ * multiple of 8, cols not of 4, a size outside [1, 2^20], more than 2^28 steps of 128 x 64 results x 32 inner indices,
+ * frac_bits outside [1, 31], workspace too small), CUDA. */
+typedef struct {
+    int32_t tokens, inner, cols;
+    int32_t frac_bits;
+    int32_t quadratic;              /* 0: no activation, 1: the quadratic                */
+    uint64_t k[3];
+    const uint64_t* X[2];
+    const uint64_t* A[2];
+    const uint64_t* W[2];
+    const uint64_t* B[2];
+    const uint64_t* C[2];
+    const uint64_t* bias[2];
+    const uint64_t* residual[2];
+    const uint64_t* R[2];
+    const uint64_t* Q[2];
+    uint64_t* E[2];
+    uint64_t* F[2];
+    uint64_t* M[2];                 /* with the activation only                          */
+    uint64_t* Y[2];
+    void* workspace;
+    int64_t workspace_bytes;
+} comet_linear_args;
+int comet_linear(void* cuda_stream, const comet_linear_args* args);
+/* Bytes of workspace that comet_linear takes for these sizes on the current device.  512 tokens of 2048 x 8192: 1.1 GB.
+ * Errors: INVALID_ARG, SHAPE, CUDA. */
+int comet_linear_workspace(int32_t tokens, int32_t inner, int32_t cols, int64_t* bytes_out);
+
+/* ---------------------------------------------------------------------------
+ * Root-mean-square norm of every row of shared queries and keys, gain, and rotation by position, for both parties, in
+ * one pass.  A row x is one head of one token, D = dim words at scale f; with heads = 1 it is the whole token.  It is
+ * composed of Section 2.1's "Multiplication" and "Addition"; trunc_b is the local truncation by b bits, div_d the same
+ * by a divisor d (party 0: s -> floor(s / d), party 1: s -> -floor(-s / d), as unsigned words), sums run over the row:
+ *   norm (steps >= 2), every value masked and opened once:
+ *     M_i = x_i - U_i (message), m = M_0 + M_1;   sq_i = row_words[0] + sum 2 m U_i + i sum m^2
+ *     s_i = div_{D 2^f}(sq_i) + i eps;   y_i = trunc_{f+1}(guess (3 i 2^f - trunc_f(s_i first))), first = floor(guess^2 / 2^f)
+ *     then steps - 1 times, with Eq. 1 for each product:  p = trunc_f(y y), w = 3 2^f - trunc_f(s p), y = trunc_{f+1}(y w)
+ *     x <- trunc_f(y x)
+ *   gain (not null):   D_i = x_i - A_i, G_i = gain_i - gain_mask_i (messages), x <- trunc_f(x gain) by Eq. 1 with C
+ *   rotation (rot_dim > 0), the public angles of row positions[token] of the tables, by pairs (a, b):
+ *     a <- trunc_f(a cos - b sin), b <- trunc_f(b cos + a sin)     pairs (j, j + rot_dim / 2), or (2j, 2j + 1) if interleaved;
+ *     words from rot_dim on stay as they are
+ * A rotation alone (steps = 0) is a local step without messages.  The Newton iteration converges to 1 / sqrt(s) where
+ * 0 < guess^2 s < 3 (as real numbers); far below the root y grows by half in every step, and at the end the error is squared, so
+ * s in (1/8, 8) with a guess of 0.55 takes some eight steps.  Where it does not converge the words are still the ones that
+ * the formulas above give.
+ *
+ * From the dealer, per row: row_words, 6 steps - 3 words: sum U^2; the mask a of s; for each of the steps - 1 rounds of
+ * Newton's the mask of y, its square, the mask of p, its product with a, the mask of w, its product with that of y; the
+ * mask v of the root.  UV = v U, C = A gain_mask.  A row's message S, 3 steps - 1 words: the openings of s; of y, p, w in every
+ * round; of the root.
+ * Shapes: X [tokens, heads, dim], a token's rows together, tokens x_stride words apart; U, UV, M, A, C, D, Z the same,
+ * dense; row_words, S [tokens, heads, words]; gain, gain_mask, G [gains, dim], where gains = 2 if 0 < q_heads < heads (the
+ * first for heads below q_heads, the second for the others), else 1; cos, sin [table_rows, rot_dim / 2], encoded at scale f;
+ * positions [tokens].
+ * A position outside [0, table_rows) is never followed: the rotated words of its token become zero and, if `bad_index_flag`
+ * (device int32, may be null) is given, it is set to 1.  The caller clears the flag.
+ * Stateless; DEVICE pointers on the current device, owned by the caller, 8-byte aligned (16-byte accesses are used where
+ * rot_dim is a multiple of 4, x_stride even and every pointer 16-byte aligned); what is written must not overlap any other argument.
+ * One kernel on `cuda_stream`; the call does not wait, allocates nothing, and may be captured.
+ * Errors: INVALID_ARG (null or unaligned pointer, overlap, nothing to do, a gain without a norm), SHAPE (dim odd or outside
+ * [2, 8192], tokens or heads < 1 or more than 2^27 rows, x_stride < heads * dim or > 2^32, q_heads outside [0, heads], rot_dim odd
+ * or outside [0, dim], table_rows < 1, steps outside {0, 2..24}, guess outside [1, 2^32), frac_bits outside [1, 31]), CUDA. */
+typedef struct {
+    int32_t tokens, heads, q_heads, dim;
+    int64_t x_stride;
+    int32_t frac_bits;
+    int32_t steps;                  /* Newton steps; 0: no norm                          */
+    uint64_t guess, eps;            /* public, at scale f                                */
+    int32_t rot_dim, interleaved;   /* 0: no rotation                                    */
+    int32_t table_rows;
+    const uint64_t* X[2];
+    const uint64_t* U[2];
+    const uint64_t* row_words[2];
+    const uint64_t* UV[2];
+    const uint64_t* gain[2];
+    const uint64_t* gain_mask[2];
+    const uint64_t* A[2];
+    const uint64_t* C[2];
+    const uint64_t* cos;
+    const uint64_t* sin;
+    const int32_t* positions;
+    uint64_t* M[2];
+    uint64_t* S[2];
+    uint64_t* D[2];
+    uint64_t* G[2];
+    uint64_t* Z[2];
+    int32_t* bad_index_flag;
+} comet_norm_rotate_args;
+int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args* args);
+
+/* ---------------------------------------------------------------------------
  * Allocation-free Pi_MatMul.  (The paper has no counterpart; this exists for
  * deployment reasons only.)
  *

@@ -12,7 +12,7 @@ from __future__ import annotations
 import ctypes
 import os
 import subprocess
-from typing import Optional
+from typing import Any, NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -35,6 +35,7 @@ EXPORTS = (
     "comet_beaver_mul", "comet_set_token_mask", "comet_get_components", "comet_kv_plan",
     "comet_add_bias", "comet_bind_shares", "comet_truncate_pair", "comet_synchronize", "comet_inject_timeout",
     "comet_pipe_probe", "comet_device_pointer", "comet_static_status", "comet_static_inject_timeout",
+    "comet_linear", "comet_linear_workspace", "comet_norm_rotate",
 )
 STATIC_SCRATCH_WORDS = 1 << 20
 ERR_SCRATCH_LIMIT = -7
@@ -54,6 +55,22 @@ class CometStats(ctypes.Structure):
                 ("kernel_launches", ctypes.c_int64), ("phase_ms", ctypes.c_double * 5),
                 ("phase_launches", ctypes.c_int64 * 5), ("n_components", ctypes.c_int32),
                 ("product_kernel", ctypes.c_int32), ("tensor_tile_macs", ctypes.c_int64)]
+
+
+class CometLinearArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "inner", "cols", "frac_bits", "quadratic")] + [
+        ("k", ctypes.c_uint64 * 3)] + [(n, ctypes.c_void_p * 2) for n in (
+            "X", "A", "W", "B", "C", "bias", "residual", "R", "Q", "E", "F", "M", "Y")] + [
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
+
+
+class CometNormRotateArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "heads", "q_heads", "dim")] + [("x_stride", ctypes.c_int64)] + [
+        (n, ctypes.c_int32) for n in ("frac_bits", "steps")] + [(n, ctypes.c_uint64) for n in ("guess", "eps")] + [
+        (n, ctypes.c_int32) for n in ("rot_dim", "interleaved", "table_rows")] + [(n, ctypes.c_void_p * 2) for n in (
+            "X", "U", "row_words", "UV", "gain", "gain_mask", "A", "C")] + [
+        (n, ctypes.c_void_p) for n in ("cos", "sin", "positions")] + [(n, ctypes.c_void_p * 2) for n in ("M", "S", "D", "G", "Z")] + [
+        ("bad_index_flag", ctypes.c_void_p)]
 
 
 class CometError(RuntimeError):
@@ -106,6 +123,9 @@ def _load():
     lib.comet_truncate_pair.argtypes = [vp, pair, pair, pair, pair, i64, i32]
     lib.comet_kv_plan.argtypes = [vp, vp, i32, i32, i64, i64, vp, vp, ctypes.POINTER(i32)]
     lib.comet_beaver_mul.argtypes = [vp, pair, pair, pair, pair, pair, pair, pair, pair, i64]
+    lib.comet_linear.argtypes = [vp, ctypes.POINTER(CometLinearArgs)]
+    lib.comet_linear_workspace.argtypes = [i32, i32, i32, ctypes.POINTER(i64)]
+    lib.comet_norm_rotate.argtypes = [vp, ctypes.POINTER(CometNormRotateArgs)]
     return lib
 
 
@@ -389,3 +409,89 @@ def add_bias(Z, bias, stream: Optional[torch.cuda.Stream] = None):
     code = _native.add_bias(stream, Z, bias)
     if code:
         raise CometError(code, "comet_add_bias")
+
+
+def _on_stream(call, stream, like, *args):
+    """A call that makes its results, and what it needs meanwhile, on the stream it works on: torch hands memory out per stream."""
+    device = like.device.index if isinstance(like, torch.Tensor) and like.is_cuda else None
+    if device is None or torch._C._cuda_getCurrentRawStream(device) == (stream.cuda_stream if stream is not None else 0):
+        return call(stream, *args)
+    with torch.cuda.stream(stream if stream is not None else torch.cuda.default_stream(device)):
+        return call(stream, *args)
+
+
+def linear_workspace(tokens: int, inner: int, cols: int) -> int:
+    """Bytes that `linear` takes for the length of a call on the current device (comet_linear_workspace)."""
+    out = ctypes.c_int64(0)
+    code = _lib.comet_linear_workspace(tokens, inner, cols, ctypes.byref(out))
+    if code != OK:
+        raise CometError(code, "comet_linear_workspace")
+    return out.value
+
+
+def linear(X, A, W, B, C, frac_bits: int, bias=None, act=None, residual=None, stream: Optional[torch.cuda.Stream] = None):
+    """Shared linear layer (comet_linear), both parties: Y = act(trunc(X W^T + bias)) + residual.
+
+    Every tensor argument is a pair (party 0, party 1) of contiguous CUDA tensors of 64-bit integers: X, A [T, K]; W, B [N, K];
+    C [T, N] with the dealer's C = A B^T; bias [N]; residual [T, N].  K is a multiple of 8, N of 4.  `act`: None, or
+    ((k0, k1, k2), R, Q) for k2 y^2 + k1 y + k0 with coefficients at scale f and the dealer's Q = R * R, [T, N].
+    Returns (E, F, M, Y): the messages (M is None without an activation) and the result's shares, new tensors.  The operand
+    planes of more than a few rows live in a tensor of linear_workspace(T, K, N) bytes for the length of the call.
+    A captured call is replayed on the memory that it was captured with.
+    """
+    code, E, F, M, Y = _on_stream(_native.linear, stream, X[0], X, A, W, B, C, frac_bits, bias, act, residual)
+    if code:
+        raise CometError(code, "comet_linear")
+    return E, F, M, Y
+
+
+class Norm(NamedTuple):
+    """Dealer's material and public numbers of a norm (comet_norm_rotate): pairs U [T, H, D] (masks of x), words
+    [T, H, 6 steps - 3] (a row's own), UV [T, H, D]; Newton's steps, its first guess and eps, both at scale f."""
+    U: Any
+    words: Any
+    UV: Any
+    steps: int
+    guess: int
+    eps: int = 0
+
+
+class Gain(NamedTuple):
+    """Shared gain and its triple: pairs weight, mask [gains, D], A, C [T, H, D] with C = A * mask."""
+    weight: Any
+    mask: Any
+    A: Any
+    C: Any
+
+
+class Rotation(NamedTuple):
+    """Public angles at scale f, 64-bit integers [rows, rotated / 2], and every token's row of them, int32 [T]."""
+    cos: torch.Tensor
+    sin: torch.Tensor
+    positions: torch.Tensor
+    interleaved: bool = False
+
+
+class NormMessages(NamedTuple):
+    """What a party sends: M = x - U, S (a row's openings), D and G (the gain's); pairs, or None where the part is absent."""
+    M: Any
+    S: Any
+    D: Any
+    G: Any
+
+
+def norm_rotate(X, frac_bits: int, norm: Optional[Norm] = None, gain: Optional[Gain] = None,
+                rotation: Optional[Rotation] = None, q_heads: Optional[int] = None,
+                stream: Optional[torch.cuda.Stream] = None, bad_index_flag=None):
+    """Root-mean-square norm of every head, gain and rotation by position (comet_norm_rotate), both parties, in one pass.
+
+    X: a pair of CUDA tensors of 64-bit integers [T, H, D], D even and at most 8192; a token's heads lie together, tokens may
+    lie further apart (a view of a stacked projection's result).  Heads below `q_heads` take the gain's first row, the others
+    its second; without `q_heads` there is one row.  A rotation may come alone.
+    Returns (NormMessages, Z): Z a pair of new tensors [T, H, D].
+    """
+    heads = X[0].shape[1] if q_heads is None else q_heads
+    code, M, S, D, G, Z = _on_stream(_native.norm_rotate, stream, X[0], X, frac_bits, norm, gain, rotation, heads, bad_index_flag)
+    if code:
+        raise CometError(code, "comet_norm_rotate")
+    return NormMessages(M, S, D, G), Z

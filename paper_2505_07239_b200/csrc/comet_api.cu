@@ -16,7 +16,9 @@
 #include <cuda_runtime.h>
 
 #include "kernels_limb.cuh"
+#include "kernels_linear.cuh"
 #include "kernels_mul.cuh"
+#include "kernels_norm.cuh"
 #include "kernels_open.cuh"
 #include "kernels_peak.cuh"
 #include "kernels_residue.cuh"
@@ -457,6 +459,33 @@ int join_side(comet_ctx* c) {
     return COMET_OK;
 }
 
+// Shared memory of the tensor-core path's kernels on the current device.
+cudaError_t tensor_kernel_attributes() {
+    cudaError_t err = cudaSuccess;
+    auto room = [&](auto* kernel, size_t bytes) {
+        if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    };
+    // the memory-side kernels may share an SM with a resident tensor-core CTA (which forces the largest
+    // shared-memory carve-out), so they ask for the same carve-out
+    auto carve = [&](auto* kernel) {
+        if (err == cudaSuccess)
+            err = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, (int)cudaSharedmemCarveoutMaxShared);
+    };
+    for (auto* kernel : {comet::combine_stream_kernel<16, comet::limb_stream::BW>, comet::combine_stream_kernel<32, comet::limb_stream::BW>,
+                         comet::combine_stream_kernel<16, comet::limb_stream::QROWS>, comet::combine_stream_kernel<32, comet::limb_stream::QROWS>})
+        room(kernel, comet::limb_stream::SMEM_BYTES);
+    room(comet::combine_limb_kernel, comet::limb::SMEM_BYTES);
+    carve(comet::combine_limb_kernel);
+    room(comet::combine_limb_grouped_kernel, comet::limb::SMEM_BYTES);
+    carve(comet::combine_limb_grouped_kernel);
+    room(comet::combine_residue_kernel, comet::residue::SMEM_BYTES);
+    for (auto* kernel : {comet::limb_exchange_kernel<false>, comet::limb_exchange_kernel<true>}) {
+        carve(kernel);
+        room(kernel, comet::limb::EX_SMEM_BYTES);
+    }
+    return err;
+}
+
 // Bytes of one set of operand planes: of limbs (tiles of `tile` rows), of residues.
 size_t limb_set(int rows, int K, int tile) {
     return (size_t)ceil_div(rows, tile) * ceil_div(K, comet::limb::KC) * tile * comet::limb::KC * comet::limb::PLANES;
@@ -697,8 +726,8 @@ cudaError_t residue_map(CUtensorMap* map, uint8_t* planes, int operand_rows, int
                       CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
-// Tensor-core path: both parties' product through residues, from the planes to Z.
-int residue_combine(comet_ctx* c, const Proj& pr) {
+// Tensor-core path: both parties' product through residues, from the planes to Z; `end`: what follows it in a linear layer.
+int residue_combine(comet_ctx* c, const Proj& pr, const comet::LinearEnd* end = nullptr) {
     namespace rs = comet::residue;
     const ResidueTiles t = residue_tiles(c->sm_count, pr.M, pr.N, pr.K);
     const int m_rows = t.swapped ? pr.N : pr.M, n_rows = t.swapped ? pr.M : pr.N;
@@ -737,9 +766,26 @@ int residue_combine(comet_ctx* c, const Proj& pr) {
         const int most = c->sm_count / 2, pairs = ceil_div(a.jobs, ceil_div(a.jobs, most));
         COMET_CUDA(c, launch_chained(comet::combine_residue_kernel, dim3(2 * pairs), dim3(rs::THREADS), rs::SMEM_BYTES, c->stream,
                                      &c->top_priority, a, maps));
-        COMET_CUDA(c, launch_chained(t.swapped ? comet::residue_recombine_kernel<true> : comet::residue_recombine_kernel<false>,
-                                     dim3(ew_grid(c, (int64_t)a.m_groups * a.n_chunks * 128, 256), 2), dim3(256), 0, c->stream,
-                                     nullptr, r));
+        const int recombine_grid = ew_grid(c, (int64_t)a.m_groups * a.n_chunks * 128, 256);
+        if (end) {
+            comet::LinearEnd e = *end;
+            for (int p = 0; p < 2; ++p) {
+                if (e.bias[p] && t.swapped) e.bias[p] += first;
+                if (e.residual[p]) e.residual[p] += at;
+                if (e.R[p]) {
+                    e.R[p] += at;
+                    e.Q[p] += at;
+                    e.M[p] += at;
+                }
+            }
+            const bool quadratic = e.R[0] != nullptr;
+            auto* const kernel = t.swapped ? (quadratic ? comet::linear_recombine_kernel<true, true> : comet::linear_recombine_kernel<true, false>)
+                                           : (quadratic ? comet::linear_recombine_kernel<false, true> : comet::linear_recombine_kernel<false, false>);
+            COMET_CUDA(c, launch_chained(kernel, dim3(recombine_grid, quadratic ? 1 : 2), dim3(256), 0, c->stream, nullptr, r, e));
+        } else {
+            COMET_CUDA(c, launch_chained(t.swapped ? comet::residue_recombine_kernel<true> : comet::residue_recombine_kernel<false>,
+                                         dim3(recombine_grid, 2), dim3(256), 0, c->stream, nullptr, r));
+        }
         c->stats.kernel_launches += 2;
     }
     c->stats.tensor_tile_macs = 2ll * 2 * t.mt * rs::BM * t.nt * t.n_tile * a.k32 * 32;
@@ -900,29 +946,7 @@ int comet_init(const comet_config* cfg, void* cuda_stream, comet_ctx** out) {
             c->residues.bytes = std::max(up ? residue_room(T, (int)gn) : 0, dn ? residue_room(T, d) : 0);
             reserve(device, &c->residues.at, c->residues.bytes);
         }
-        ok = ok && cudaFuncSetAttribute(comet::combine_limb_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                        (int)lb::SMEM_BYTES) == cudaSuccess;
-        // the memory-side kernels may share an SM with a resident tensor-core CTA (which forces the largest
-        // shared-memory carve-out), so they ask for the same carve-out
-        for (auto* kernel : {comet::combine_stream_kernel<16, comet::limb_stream::BW>, comet::combine_stream_kernel<32, comet::limb_stream::BW>,
-                             comet::combine_stream_kernel<16, comet::limb_stream::QROWS>, comet::combine_stream_kernel<32, comet::limb_stream::QROWS>})
-            ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                            (int)comet::limb_stream::SMEM_BYTES) == cudaSuccess;
-        ok = ok && cudaFuncSetAttribute(comet::combine_limb_kernel, cudaFuncAttributePreferredSharedMemoryCarveout,
-                                        (int)cudaSharedmemCarveoutMaxShared) == cudaSuccess;
-        ok = ok && cudaFuncSetAttribute(comet::combine_limb_grouped_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                        (int)lb::SMEM_BYTES) == cudaSuccess;
-        ok = ok && cudaFuncSetAttribute(comet::combine_limb_grouped_kernel,
-                                        cudaFuncAttributePreferredSharedMemoryCarveout,
-                                        (int)cudaSharedmemCarveoutMaxShared) == cudaSuccess;
-        ok = ok && cudaFuncSetAttribute(comet::combine_residue_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                        (int)comet::residue::SMEM_BYTES) == cudaSuccess;
-        for (auto* kernel : {comet::limb_exchange_kernel<false>, comet::limb_exchange_kernel<true>}) {
-            ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout,
-                                            (int)cudaSharedmemCarveoutMaxShared) == cudaSuccess;
-            ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                            (int)lb::EX_SMEM_BYTES) == cudaSuccess;
-        }
+        ok = ok && tensor_kernel_attributes() == cudaSuccess;
         ok = ok && cudaStreamCreateWithFlags(&c->side, cudaStreamNonBlocking) == cudaSuccess;
         ok = ok && cudaEventCreateWithFlags(&c->ev_fork, cudaEventDisableTiming) == cudaSuccess;
         ok = ok && cudaEventCreateWithFlags(&c->ev_join, cudaEventDisableTiming) == cudaSuccess;
@@ -1597,7 +1621,7 @@ constexpr int kMaxDevices = 64;
 struct StaticDevice {
     u64* scratch;      // device address of the array
     int* error;        // and of the error word
-    int sm_count;
+    int sm_count, top_priority;
 };
 std::mutex g_static_mutex;
 StaticDevice g_static_device[kMaxDevices] = {};    // per device ordinal
@@ -1613,11 +1637,9 @@ cudaError_t static_device(StaticDevice* out) {
     if (!d.scratch) {
         void *p = nullptr, *e = nullptr;
         err = cudaDeviceGetAttribute(&d.sm_count, cudaDevAttrMultiProcessorCount, dev);
-        for (auto* kernel : {comet::combine_stream_kernel<16, comet::limb_stream::BW>, comet::combine_stream_kernel<32, comet::limb_stream::BW>,
-                             comet::combine_stream_kernel<16, comet::limb_stream::QROWS>, comet::combine_stream_kernel<32, comet::limb_stream::QROWS>})
-            if (err == cudaSuccess)
-                err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                           (int)comet::limb_stream::SMEM_BYTES);
+        int least = 0;
+        if (err == cudaSuccess) err = cudaDeviceGetStreamPriorityRange(&least, &d.top_priority);
+        if (err == cudaSuccess) err = tensor_kernel_attributes();
         if (err == cudaSuccess) err = cudaGetSymbolAddress(&p, g_static_scratch);
         if (err == cudaSuccess) err = cudaGetSymbolAddress(&e, g_static_error);
         if (err != cudaSuccess) return err;
@@ -1968,6 +1990,325 @@ extern "C" int comet_add_bias(void* cuda_stream, uint64_t* const Z[2], const uin
     g.stride_pieces = (int)((long long)grid * 256 % g.pieces);
     auto* kernel = vec ? comet::add_bias_kernel<ulonglong2> : comet::add_bias_kernel<u64>;
     return launch_pass(kernel, dim3(grid), (cudaStream_t)cuda_stream, g);
+}
+
+// ---------------------------------------------------------------------------
+// Linear layer: Pi_MatMul, bias, truncation, activation, residual.  Stateless; the workspace is the caller's.
+// ---------------------------------------------------------------------------
+namespace {
+
+constexpr int64_t LINEAR_MAX_SIZE = 1 << 20;
+
+bool linear_sizes(int64_t T, int64_t K, int64_t N) {
+    namespace lb = comet::limb;
+    if (T < 1 || K < 8 || N < 4 || K % 8 || N % 4 || T > LINEAR_MAX_SIZE || K > LINEAR_MAX_SIZE || N > LINEAR_MAX_SIZE) return false;
+    // the tensor-core kernels count steps of work in 32 bits
+    const int64_t tiles = ((T + lb::BM - 1) / lb::BM) * ((N + lb::BN - 1) / lb::BN), steps = (K + lb::KC - 1) / lb::KC;
+    return tiles * steps <= 0x7fffffffll / 8;
+}
+
+// The kernel for few rows beats the planes up to 64 rows where a layer has STREAM_WORDS of weights in two products (see there).
+bool linear_streams(int64_t T, int64_t K, int64_t N) {
+    return T <= comet::limb_stream::BT || (T <= STREAM_TOKENS && 2 * K * N >= STREAM_WORDS);
+}
+
+// A context of one product: what the launching functions of the path read of one, its planes in the caller's workspace.  Returns
+// the bytes of that.
+constexpr size_t LINEAR_ALIGN = 256;
+size_t linear_context(comet_ctx* c, int sm_count, int T, int K, int N, uint8_t* workspace) {
+    std::memset(c, 0, sizeof(*c));
+    c->path = COMET_PATH_LIMB;
+    c->groups = 1;
+    c->sm_count = sm_count;
+    c->cfg.d_model = K;
+    c->cfg.block = N;                    // one active block of all features: a gather that moves nothing
+    c->n_active = N;
+    c->ids_held = true;
+    if (linear_streams(T, K, N)) {
+        c->stream_sync_words = ~(size_t)0;         // (none: Z <- C is a launch of its own)
+        return 0;
+    }
+    const bool residue = K <= comet::residue::MAX_DEPTH && residues_pay(sm_count, T, N, K);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        uint8_t* const piece = workspace ? workspace + at : nullptr;
+        at += (bytes + LINEAR_ALIGN - 1) / LINEAR_ALIGN * LINEAR_ALIGN;
+        return piece;
+    };
+    c->planes_left.bytes = 3 * (residue ? residue_set(T, K) : limb_set(T, K, comet::limb::BM));
+    c->planes_left.at = take(c->planes_left.bytes);
+    c->planes_right_up.bytes = 3 * (residue ? residue_set(N, K) : limb_set(N, K, comet::limb::BN));
+    c->planes_right_up.at = take(c->planes_right_up.bytes);
+    if (residue) {
+        c->residues.bytes = residue_room(T, N);
+        c->residues.at = take(c->residues.bytes);
+    }
+    return at;
+}
+
+struct Span {
+    uintptr_t begin, end;
+    Span(const void* p, int64_t count, size_t size = sizeof(u64))
+        : begin(reinterpret_cast<uintptr_t>(p)), end(begin + (p ? (uintptr_t)count * size : 0)) {}
+    bool meets(const Span& o) const { return begin < o.end && o.begin < end; }
+};
+// Whether one of the first `outputs` spans shares memory with any other span.
+bool outputs_overlap(const Span* span, int outputs, int count) {
+    for (int k = 0; k < outputs; ++k)
+        for (int j = k + 1; j < count; ++j)
+            if (span[k].meets(span[j])) return true;
+    return false;
+}
+
+bool pair_missing(const uint64_t* const p[2]) { return !p[0] || !p[1]; }
+bool pair_halved(const uint64_t* const p[2]) { return !p[0] != !p[1]; }
+bool pair_unaligned(const uint64_t* const p[2]) { return !aligned16(p[0]) || !aligned16(p[1]); }
+
+}  // namespace
+
+extern "C" int comet_linear_workspace(int32_t tokens, int32_t inner, int32_t cols, int64_t* bytes_out) {
+    if (!bytes_out) return COMET_ERR_INVALID_ARG;
+    if (!linear_sizes(tokens, inner, cols)) return COMET_ERR_SHAPE;
+    StaticDevice dev;
+    if (static_device(&dev) != cudaSuccess) {
+        cudaGetLastError();
+        return COMET_ERR_CUDA;
+    }
+    comet_ctx c;
+    *bytes_out = (int64_t)linear_context(&c, dev.sm_count, tokens, inner, cols, nullptr);
+    return COMET_OK;
+}
+
+extern "C" int comet_linear(void* cuda_stream, const comet_linear_args* g) {
+    if (!g) return COMET_ERR_INVALID_ARG;
+    if (pair_missing(g->X) || pair_missing(g->A) || pair_missing(g->W) || pair_missing(g->B) || pair_missing(g->C) ||
+        pair_missing(g->E) || pair_missing(g->F) || pair_missing(g->Y) || pair_halved(g->bias) || pair_halved(g->residual))
+        return COMET_ERR_INVALID_ARG;
+    if (g->quadratic != 0 && g->quadratic != 1) return COMET_ERR_INVALID_ARG;
+    if (g->quadratic && (pair_missing(g->R) || pair_missing(g->Q) || pair_missing(g->M))) return COMET_ERR_INVALID_ARG;
+    for (auto* p : {g->X, g->A, g->W, g->B, g->C, g->bias, g->residual})
+        if (pair_unaligned(p)) return COMET_ERR_INVALID_ARG;
+    for (auto* p : {g->E, g->F, g->Y})
+        if (pair_unaligned(p)) return COMET_ERR_INVALID_ARG;
+    if (g->quadratic && (pair_unaligned(g->R) || pair_unaligned(g->Q) || pair_unaligned(g->M))) return COMET_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(g->workspace) % LINEAR_ALIGN || g->workspace_bytes < 0) return COMET_ERR_INVALID_ARG;
+    if (g->frac_bits < 1 || g->frac_bits > 31) return COMET_ERR_SHAPE;
+    const int T = g->tokens, K = g->inner, N = g->cols;
+    if (!linear_sizes(T, K, N)) return COMET_ERR_SHAPE;
+    {
+        const int64_t left = (int64_t)T * K, right = (int64_t)N * K, out = (int64_t)T * N;
+        auto square = [&](const uint64_t* p) { return Span(g->quadratic ? p : nullptr, out); };
+        const Span span[] = {
+            // what is written: 9
+            {g->E[0], left}, {g->E[1], left}, {g->F[0], right}, {g->F[1], right}, {g->Y[0], out}, {g->Y[1], out}, square(g->M[0]),
+            square(g->M[1]), {g->workspace, g->workspace_bytes, 1},
+            // what is only read
+            {g->X[0], left}, {g->X[1], left}, {g->A[0], left}, {g->A[1], left}, {g->W[0], right}, {g->W[1], right},
+            {g->B[0], right}, {g->B[1], right}, {g->C[0], out}, {g->C[1], out}, {g->bias[0], N}, {g->bias[1], N},
+            {g->residual[0], out}, {g->residual[1], out}, square(g->R[0]), square(g->R[1]), square(g->Q[0]), square(g->Q[1])};
+        if (outputs_overlap(span, 9, sizeof(span) / sizeof(span[0]))) return COMET_ERR_INVALID_ARG;
+    }
+    StaticDevice dev;
+    if (static_device(&dev) != cudaSuccess) {
+        cudaGetLastError();
+        return COMET_ERR_CUDA;
+    }
+    comet_ctx ctx;
+    comet_ctx* const c = &ctx;
+    const size_t need = linear_context(c, dev.sm_count, T, K, N, static_cast<uint8_t*>(g->workspace));
+    if (need && !g->workspace) return COMET_ERR_INVALID_ARG;
+    if (g->workspace_bytes < (int64_t)need) return COMET_ERR_SHAPE;
+    c->stream = (cudaStream_t)cuda_stream;
+    c->top_priority = dev.top_priority;
+    c->d_error = dev.error;
+    c->h_count_dev = reinterpret_cast<int32_t*>(dev.error) - 3;       // both reports of a wait that ran out go to one word
+    for (int p = 0; p < 2; ++p) {
+        auto in = [](const uint64_t* q) { return const_cast<u64*>(reinterpret_cast<const u64*>(q)); };   // only ever read
+        c->buf[p][COMET_X] = in(g->X[p]);
+        c->buf[p][COMET_A_UP] = in(g->A[p]);
+        c->buf[p][COMET_W1] = in(g->W[p]);
+        c->buf[p][COMET_B_UP] = in(g->B[p]);
+        c->buf[p][COMET_C_UP] = in(g->C[p]);
+        c->buf[p][COMET_E_UP] = reinterpret_cast<u64*>(g->E[p]);
+        c->buf[p][COMET_F_UP] = reinterpret_cast<u64*>(g->F[p]);
+        c->buf[p][COMET_Z_UP] = reinterpret_cast<u64*>(g->Y[p]);
+    }
+    comet::LinearEpilogueArgs last;
+    std::memset(&last, 0, sizeof(last));
+    last.end.k0 = g->k[0]; last.end.k1 = g->k[1]; last.end.k2 = g->k[2];
+    last.end.f = g->frac_bits;
+    for (int p = 0; p < 2; ++p) {
+        last.end.bias[p] = reinterpret_cast<const u64*>(g->bias[p]);
+        last.end.residual[p] = reinterpret_cast<const u64*>(g->residual[p]);
+        if (g->quadratic) {
+            last.end.R[p] = reinterpret_cast<const u64*>(g->R[p]);
+            last.end.Q[p] = reinterpret_cast<const u64*>(g->Q[p]);
+            last.end.M[p] = reinterpret_cast<u64*>(g->M[p]);
+        }
+        last.Z[p] = reinterpret_cast<u64*>(g->Y[p]);
+    }
+    const Proj pr = proj_up(c, T);
+    int rc;
+    if (linear_streams(T, K, N)) {
+        rc = stream_product(c, pr);
+    } else if (through_residues(c, pr)) {
+        rc = limb_exchange(c, pr, true, true, true, false, c->stream);
+        if (rc == COMET_OK) rc = residue_combine(c, pr, &last.end);
+        if (rc == COMET_OK) return rc;
+    } else {
+        rc = limb_exchange(c, pr, false, true, true, true, c->stream);
+        if (rc == COMET_OK) rc = limb_combine(c, pr);
+    }
+    if (rc != COMET_OK) {
+        cudaGetLastError();
+        return rc;
+    }
+    last.pairs = (int64_t)T * N / 2;
+    last.row_pairs = N / 2;
+    const int grid = ew_grid(c, last.pairs, 256);
+    last.stride_pairs = (int)((long long)grid * 256 % last.row_pairs);
+    return launch_pass(comet::linear_epilogue_kernel, dim3(grid), c->stream, last);
+}
+
+// ---------------------------------------------------------------------------
+// Norms of heads, gain and position rotation.  Stateless.
+// ---------------------------------------------------------------------------
+namespace {
+
+// A thread takes four words of a row.  Up to 128 words: a warp for a row, or for two or four; beyond: a cluster of CTAs of at
+// most 256 threads.
+int launch_norm(const comet::NormArgs& a, bool vec, cudaStream_t stream) {
+    namespace nm = comet::norm;
+    const int quads = ceil_div(a.dim, 4);
+    const size_t row_bytes = 2 * nm::words(a.steps) * sizeof(u64);
+    cudaError_t err;
+    if (a.dim <= nm::GROUP_DIM) {
+        const int group = quads <= 8 ? 8 : quads <= 16 ? 16 : 32, rows = 32 * nm::GROUP_WARPS / group;
+        void (*kernel)(comet::NormArgs) = group == 8    ? (vec ? comet::norm_group_kernel<8, true> : comet::norm_group_kernel<8, false>)
+                                          : group == 16 ? (vec ? comet::norm_group_kernel<16, true> : comet::norm_group_kernel<16, false>)
+                                                        : (vec ? comet::norm_group_kernel<32, true> : comet::norm_group_kernel<32, false>);
+        err = launch_chained(kernel, dim3(ceil_div(a.rows, rows)), dim3(32 * nm::GROUP_WARPS), rows * row_bytes, stream, nullptr, a);
+    } else {
+        int cluster = 1;
+        while (ceil_div(quads, cluster) > nm::MAX_CTA_QUADS) cluster *= 2;
+        cudaLaunchConfig_t lc;
+        std::memset(&lc, 0, sizeof(lc));
+        lc.gridDim = dim3((unsigned)a.rows * cluster);
+        lc.blockDim = dim3(ceil_div(ceil_div(quads, cluster), 32) * 32);
+        lc.dynamicSmemBytes = row_bytes;
+        lc.stream = stream;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = cluster;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        lc.attrs = attr;
+        lc.numAttrs = 2;
+        err = cudaLaunchKernelEx(&lc, vec ? comet::norm_cluster_kernel<true> : comet::norm_cluster_kernel<false>, a);
+    }
+    if (err != cudaSuccess) cudaGetLastError();
+    return err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args* g) {
+    namespace nm = comet::norm;
+    if (!g) return COMET_ERR_INVALID_ARG;
+    if (pair_missing(g->X) || pair_missing(g->Z)) return COMET_ERR_INVALID_ARG;
+    const bool normed = g->steps != 0, gained = g->gain[0] || g->gain[1], turned = g->rot_dim != 0;
+    if (!normed && !turned) return COMET_ERR_INVALID_ARG;
+    if (gained && !normed) return COMET_ERR_INVALID_ARG;
+    if (normed && (pair_missing(g->U) || pair_missing(g->row_words) || pair_missing(g->UV) || pair_missing(g->M) || pair_missing(g->S)))
+        return COMET_ERR_INVALID_ARG;
+    if (gained && (pair_missing(g->gain) || pair_missing(g->gain_mask) || pair_missing(g->A) || pair_missing(g->C) ||
+                   pair_missing(g->D) || pair_missing(g->G)))
+        return COMET_ERR_INVALID_ARG;
+    if (turned && (!g->cos || !g->sin || !g->positions)) return COMET_ERR_INVALID_ARG;
+    if (g->interleaved != 0 && g->interleaved != 1) return COMET_ERR_INVALID_ARG;
+    if (g->frac_bits < 1 || g->frac_bits > 31) return COMET_ERR_SHAPE;
+    if (g->tokens < 1 || g->heads < 1 || g->dim < 2 || g->dim % 2 || g->dim > nm::MAX_DIM) return COMET_ERR_SHAPE;
+    const int64_t rows = (int64_t)g->tokens * g->heads, row = (int64_t)g->heads * g->dim, words = rows * g->dim;
+    if (rows > 1 << 27) return COMET_ERR_SHAPE;
+    if (g->x_stride < 0 || g->x_stride > 1ll << 32 || (g->tokens > 1 && g->x_stride < row)) return COMET_ERR_SHAPE;
+    if (g->q_heads < 0 || g->q_heads > g->heads) return COMET_ERR_SHAPE;
+    if (turned && (g->rot_dim < 0 || g->rot_dim % 2 || g->rot_dim > g->dim || g->table_rows < 1)) return COMET_ERR_SHAPE;
+    if (normed && (g->steps < 2 || g->steps > nm::MAX_STEPS)) return COMET_ERR_SHAPE;
+    if (normed && (g->guess < 1 || g->guess >> 32)) return COMET_ERR_SHAPE;
+    bool vec = g->rot_dim % 4 == 0 && (g->x_stride % 2 == 0 || g->tokens == 1);
+    {
+        const int64_t x_words = (int64_t)(g->tokens - 1) * g->x_stride + row;
+        const int64_t gains = g->q_heads > 0 && g->q_heads < g->heads ? 2 : 1;
+        const int64_t own = normed ? rows * nm::words(g->steps) : 0, sent = normed ? rows * nm::openings(g->steps) : 0;
+        const int64_t n_words = normed ? words : 0, g_words = gained ? words : 0, g_rows = gained ? gains * g->dim : 0;
+        const int64_t table = turned ? (int64_t)g->table_rows * (g->rot_dim / 2) : 0;
+        auto used = [](const void* p, int64_t n) { return Span(n ? p : nullptr, n); };
+        const Span span[] = {
+            // what is written: 11
+            {g->Z[0], words}, {g->Z[1], words}, used(g->M[0], n_words), used(g->M[1], n_words), used(g->D[0], g_words),
+            used(g->D[1], g_words), used(g->G[0], g_rows), used(g->G[1], g_rows), used(g->S[0], sent), used(g->S[1], sent),
+            {g->bad_index_flag, 1, sizeof(int32_t)},
+            // what is only read
+            {g->X[0], x_words}, {g->X[1], x_words}, used(g->U[0], n_words), used(g->U[1], n_words), used(g->UV[0], n_words),
+            used(g->UV[1], n_words), used(g->gain[0], g_rows), used(g->gain[1], g_rows), used(g->gain_mask[0], g_rows),
+            used(g->gain_mask[1], g_rows), used(g->A[0], g_words), used(g->A[1], g_words), used(g->C[0], g_words), used(g->C[1], g_words),
+            used(g->cos, table), used(g->sin, table), used(g->row_words[0], own), used(g->row_words[1], own),
+            {turned ? g->positions : nullptr, g->tokens, sizeof(int32_t)}};
+        constexpr int count = sizeof(span) / sizeof(span[0]);
+        if (outputs_overlap(span, 11, count)) return COMET_ERR_INVALID_ARG;
+        for (int k = 0; k < count; ++k) {
+            const bool narrow = k == 10 || k == count - 1, alone = k == 8 || k == 9 || k == count - 3 || k == count - 2;
+            if (span[k].begin % (narrow ? sizeof(int32_t) : sizeof(u64))) return COMET_ERR_INVALID_ARG;
+            if (!narrow && !alone) vec = vec && span[k].begin % 16 == 0;       // (a row's own words are read one by one)
+        }
+    }
+    comet::NormArgs a;
+    std::memset(&a, 0, sizeof(a));
+    for (int p = 0; p < 2; ++p) {
+        a.X[p] = reinterpret_cast<const u64*>(g->X[p]);
+        a.Z[p] = reinterpret_cast<u64*>(g->Z[p]);
+        if (normed) {
+            a.U[p] = reinterpret_cast<const u64*>(g->U[p]);
+            a.row_words[p] = reinterpret_cast<const u64*>(g->row_words[p]);
+            a.UV[p] = reinterpret_cast<const u64*>(g->UV[p]);
+            a.M[p] = reinterpret_cast<u64*>(g->M[p]);
+            a.S[p] = reinterpret_cast<u64*>(g->S[p]);
+        }
+        if (gained) {
+            a.gain[p] = reinterpret_cast<const u64*>(g->gain[p]);
+            a.gain_mask[p] = reinterpret_cast<const u64*>(g->gain_mask[p]);
+            a.A[p] = reinterpret_cast<const u64*>(g->A[p]);
+            a.C[p] = reinterpret_cast<const u64*>(g->C[p]);
+            a.Dm[p] = reinterpret_cast<u64*>(g->D[p]);
+            a.G[p] = reinterpret_cast<u64*>(g->G[p]);
+        }
+    }
+    a.cos = reinterpret_cast<const u64*>(g->cos);
+    a.sin = reinterpret_cast<const u64*>(g->sin);
+    a.positions = g->positions;
+    a.bad_index = g->bad_index_flag;
+    a.x_stride = g->x_stride;
+    a.guess = g->guess;
+    a.first = g->guess * g->guess >> g->frac_bits;
+    a.eps = g->eps;
+    a.divisor = (u64)g->dim << g->frac_bits;
+    a.divisor_bits = -1;
+    for (int b = 0; b < 64; ++b)
+        if (a.divisor == 1ull << b) a.divisor_bits = b;
+    a.rows = (int)rows;
+    a.heads = g->heads;
+    a.q_heads = g->q_heads < g->heads ? g->q_heads : 0;
+    a.dim = g->dim;
+    a.half = g->rot_dim / 2;
+    a.interleaved = g->interleaved;
+    a.table_rows = g->table_rows;
+    a.f = g->frac_bits;
+    a.steps = g->steps;
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    if (normed) return launch_norm(a, vec, stream);
+    const unsigned quads = (unsigned)ceil_div(a.dim, 4);
+    return launch_pass(vec ? comet::rotate_kernel<true> : comet::rotate_kernel<false>, dim3(shuffle_grid(rows * quads)), stream, a, quads);
 }
 
 // ---------------------------------------------------------------------------

@@ -365,6 +365,229 @@ PyObject* beaver_matmul_static(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// Tensors of ring words given to the calls below: 64-bit integers.
+bool ring_words(const at::Tensor& t) {
+    if (t.is_cuda() && (t.scalar_type() == at::kLong || t.scalar_type() == at::kUInt64)) return true;
+    return refuse(PyExc_AssertionError, "CUDA tensors of 64-bit integers are expected");
+}
+// The addresses of a pair of a given shape on the device of `like`.
+bool words_of(const Pair& t, at::IntArrayRef shape, const at::Tensor& like, const uint64_t* to[2]) {
+    for (int p = 0; p < 2; ++p) {
+        if (!ring_words(t[p])) return false;
+        if (t[p].device() != like.device()) return refuse(PyExc_AssertionError, "all tensors must be on one device");
+        if (t[p].sizes() != shape) return refuse(PyExc_AssertionError, "the tensors of both parties must have the documented shapes");
+        to[p] = words(t[p]);
+    }
+    return true;
+}
+// The same of an argument, which may be None where it is optional: the addresses stay null.
+bool as_words(PyObject* o, at::IntArrayRef shape, const at::Tensor& like, bool optional, Pair& out, const uint64_t* to[2]) {
+    return (o == Py_None && optional) || (as_pair(o, 8, out) && words_of(out, shape, like, to));
+}
+bool as_tuple(PyObject* o, Py_ssize_t n) {
+    return (PyTuple_Check(o) && PyTuple_GET_SIZE(o) == n) || refuse(PyExc_TypeError, "a tuple of the documented length is expected");
+}
+// A ring word: any integer, mod 2^64.
+bool as_word(PyObject* o, uint64_t* out) {
+    *out = PyLong_AsUnsignedLongLongMask(o);
+    return !(*out == ~0ull && PyErr_Occurred());
+}
+bool fits_int32(std::initializer_list<int64_t> values) {
+    for (int64_t v : values)
+        if (v < INT32_MIN || v > INT32_MAX) return false;
+    return true;
+}
+
+// A new contiguous tensor of ring words on the device of `like` (see empty_like).
+at::Tensor new_words(at::IntArrayRef shape, const at::Tensor& like) {
+    const c10::DeviceGuard guard(like.device());
+    return at::detail::empty_generic(shape, c10::GetAllocator(c10::DeviceType::CUDA), c10::DispatchKeySet(c10::DispatchKey::CUDA),
+                                     like.scalar_type(), std::nullopt);
+}
+void new_pair(at::IntArrayRef shape, const at::Tensor& like, at::Tensor t[2], uint64_t* to[2]) {
+    for (int p = 0; p < 2; ++p) {
+        t[p] = new_words(shape, like);
+        to[p] = words(t[p]);
+    }
+}
+// (code, [party 0, party 1] or None, ...)
+PyObject* answer_pairs(int code, std::initializer_list<const at::Tensor*> pairs) {
+    PyObject* out = PyTuple_New(1 + (Py_ssize_t)pairs.size());
+    if (!out) return nullptr;
+    PyTuple_SET_ITEM(out, 0, PyLong_FromLong(code));
+    Py_ssize_t i = 1;
+    for (const at::Tensor* t : pairs) {
+        PyObject* l = Py_None;
+        if (t[0].defined()) {
+            PyObject *a = THPVariable_Wrap(t[0]), *b = a ? THPVariable_Wrap(t[1]) : nullptr;
+            if (!b) Py_XDECREF(a);
+            l = b ? Py_BuildValue("[NN]", a, b) : nullptr;
+            if (!l) {
+                Py_DECREF(out);
+                return nullptr;
+            }
+        } else {
+            Py_INCREF(l);
+        }
+        PyTuple_SET_ITEM(out, i++, l);
+    }
+    return out;
+}
+
+// linear(stream, X, A, W, B, C, frac_bits, bias, act, residual) -> (code, E, F, M, Y); act: None or (coefficients, R, Q)
+PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        void* stream;
+        int64_t frac;
+        Pair X, A, W, B, C, bias, R, Q, residual;
+        if (!counted(n, 10) || !as_stream(args[0], &stream) || !as_pair(args[1], 8, X) || !as_pair(args[3], 8, W) ||
+            !as_int(args[6], &frac))
+            return nullptr;
+        const at::Tensor& x = X[0];
+        if (x.dim() != 2 || W[0].dim() != 2) {
+            refuse(PyExc_ValueError, "matrices are expected");
+            return nullptr;
+        }
+        const int64_t T = x.size(0), K = x.size(1), N = W[0].size(0);
+        comet_linear_args g;
+        std::memset(&g, 0, sizeof(g));
+        if (!words_of(X, {T, K}, x, g.X) || !as_words(args[2], {T, K}, x, false, A, g.A) || !words_of(W, {N, K}, x, g.W) ||
+            !as_words(args[4], {N, K}, x, false, B, g.B) || !as_words(args[5], {T, N}, x, false, C, g.C) ||
+            !as_words(args[7], {N}, x, true, bias, g.bias) || !as_words(args[9], {T, N}, x, true, residual, g.residual))
+            return nullptr;
+        if (args[8] != Py_None) {
+            if (!as_tuple(args[8], 3)) return nullptr;
+            PyObject* const k = PyTuple_GET_ITEM(args[8], 0);
+            if (!as_tuple(k, 3) || !as_words(PyTuple_GET_ITEM(args[8], 1), {T, N}, x, false, R, g.R) ||
+                !as_words(PyTuple_GET_ITEM(args[8], 2), {T, N}, x, false, Q, g.Q))
+                return nullptr;
+            for (int j = 0; j < 3; ++j)
+                if (!as_word(PyTuple_GET_ITEM(k, j), &g.k[j])) return nullptr;
+            g.quadratic = 1;
+        }
+        int code = fits_int32({T, K, N, frac}) ? COMET_OK : COMET_ERR_SHAPE;
+        g.tokens = (int32_t)T; g.inner = (int32_t)K; g.cols = (int32_t)N;
+        g.frac_bits = (int32_t)frac;
+        const c10::DeviceGuard guard(x.device());
+        if (code == COMET_OK) code = comet_linear_workspace(g.tokens, g.inner, g.cols, &g.workspace_bytes);
+        at::Tensor E[2], F[2], M[2], Y[2], workspace;
+        if (code == COMET_OK) {
+            new_pair({T, K}, x, E, g.E);
+            new_pair({N, K}, x, F, g.F);
+            if (g.quadratic) new_pair({T, N}, x, M, g.M);
+            new_pair({T, N}, x, Y, g.Y);
+            if (g.workspace_bytes) {
+                workspace = new_words({(g.workspace_bytes + 7) / 8}, x);
+                g.workspace = workspace.data_ptr();
+            }
+            code = unlocked([&] { return comet_linear(stream, &g); });
+        }
+        return answer_pairs(code, {E, F, M, Y});
+    });
+}
+
+// norm_rotate(stream, X, frac_bits, norm, gain, rotation, q_heads, bad_index_flag) -> (code, M, S, D, G, Z)
+//   norm: None or (U, words, UV, steps, guess, eps); gain: None or (weight, mask, A, C); rotation: None or (cos, sin, positions,
+//   interleaved)
+PyObject* norm_rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        static PyObject* const index[2] = {PyLong_FromLong(0), PyLong_FromLong(1)};
+        void* stream;
+        int64_t frac, q_heads;
+        Pair X, U, row_words, UV, weight, mask, A, C;
+        if (!counted(n, 8) || !as_stream(args[0], &stream) || !as_int(args[2], &frac) || !as_int(args[6], &q_heads)) return nullptr;
+        for (int p = 0; p < 2; ++p)
+            if (!(X.item[p] = PyObject_GetItem(args[1], index[p])) || !(X.t[p] = as_tensor(X.item[p])) || !ring_words(X[p])) return nullptr;
+        const at::Tensor& x = X[0];
+        if (x.dim() != 3 || X[1].sizes() != x.sizes() || X[1].device() != x.device()) {
+            refuse(PyExc_AssertionError, "rows of heads, [tokens, heads, dim], of both parties are expected");
+            return nullptr;
+        }
+        const int64_t T = x.size(0), H = x.size(1), D = x.size(2);
+        const int64_t stride = T > 1 ? x.stride(0) : H * D;
+        for (int p = 0; p < 2; ++p)
+            if ((D > 1 && X[p].stride(2) != 1) || (H > 1 && X[p].stride(1) != D) || (T > 1 && X[p].stride(0) != stride)) {
+                refuse(PyExc_AssertionError, "a token's heads must lie together, and both parties' tokens equally far apart");
+                return nullptr;
+            }
+        comet_norm_rotate_args g;
+        std::memset(&g, 0, sizeof(g));
+        g.X[0] = words(x);
+        g.X[1] = words(X[1]);
+        int64_t steps = 0, rot = 0, rows = 0, sent = 0;
+        const at::IntArrayRef like = x.sizes();
+        const at::Tensor none[2];
+        if (args[3] != Py_None) {
+            if (!as_tuple(args[3], 6) || !as_int(PyTuple_GET_ITEM(args[3], 3), &steps) || !as_word(PyTuple_GET_ITEM(args[3], 4), &g.guess) ||
+                !as_word(PyTuple_GET_ITEM(args[3], 5), &g.eps))
+                return nullptr;
+            if (steps < 2 || steps > INT32_MAX / 8) return answer_pairs(COMET_ERR_SHAPE, {none, none, none, none, none});
+            sent = 3 * steps - 1;
+            if (!as_words(PyTuple_GET_ITEM(args[3], 0), like, x, false, U, g.U) ||
+                !as_words(PyTuple_GET_ITEM(args[3], 1), {T, H, 6 * steps - 3}, x, false, row_words, g.row_words) ||
+                !as_words(PyTuple_GET_ITEM(args[3], 2), like, x, false, UV, g.UV))
+                return nullptr;
+        }
+        const int64_t gains = q_heads > 0 && q_heads < H ? 2 : 1;
+        if (args[4] != Py_None) {
+            if (!as_tuple(args[4], 4) || !as_words(PyTuple_GET_ITEM(args[4], 0), {gains, D}, x, false, weight, g.gain) ||
+                !as_words(PyTuple_GET_ITEM(args[4], 1), {gains, D}, x, false, mask, g.gain_mask) ||
+                !as_words(PyTuple_GET_ITEM(args[4], 2), like, x, false, A, g.A) ||
+                !as_words(PyTuple_GET_ITEM(args[4], 3), like, x, false, C, g.C))
+                return nullptr;
+        }
+        if (args[5] != Py_None) {
+            if (!as_tuple(args[5], 4)) return nullptr;
+            const at::Tensor *cos = as_tensor(PyTuple_GET_ITEM(args[5], 0)), *sin = cos ? as_tensor(PyTuple_GET_ITEM(args[5], 1)) : nullptr,
+                             *pos = sin ? as_tensor(PyTuple_GET_ITEM(args[5], 2)) : nullptr;
+            const int interleaved = pos ? PyObject_IsTrue(PyTuple_GET_ITEM(args[5], 3)) : -1;
+            if (interleaved < 0 || !ring_words(*cos) || !ring_words(*sin)) return nullptr;
+            if (cos->dim() != 2 || !cos->is_contiguous() || !sin->is_contiguous() || cos->sizes() != sin->sizes() ||
+                pos->scalar_type() != at::kInt || !pos->is_cuda() || !pos->is_contiguous() || pos->dim() != 1 || pos->size(0) != T ||
+                cos->device() != x.device() || sin->device() != x.device() || pos->device() != x.device()) {
+                refuse(PyExc_AssertionError, "tables [rows, rotated / 2] of 64-bit integers and int32 positions [tokens] are expected");
+                return nullptr;
+            }
+            rows = cos->size(0);
+            rot = 2 * cos->size(1);
+            g.cos = words(*cos);
+            g.sin = words(*sin);
+            g.positions = static_cast<const int32_t*>(pos->data_ptr());
+            g.interleaved = interleaved;
+        }
+        if (args[7] != Py_None) {
+            const at::Tensor* flag = as_tensor(args[7]);
+            if (!flag) return nullptr;
+            if (!flag->is_cuda() || flag->scalar_type() != at::kInt || flag->numel() < 1 || flag->device() != x.device()) {
+                refuse(PyExc_AssertionError, "the flag is an int32 on the tensors' device");
+                return nullptr;
+            }
+            g.bad_index_flag = static_cast<int32_t*>(flag->data_ptr());
+        }
+        if (!fits_int32({T, H, D, frac, q_heads, rows, rot}) || T < 1 || H < 1 || D < 1)
+            return answer_pairs(COMET_ERR_SHAPE, {none, none, none, none, none});
+        g.tokens = (int32_t)T; g.heads = (int32_t)H; g.q_heads = (int32_t)q_heads; g.dim = (int32_t)D;
+        g.x_stride = stride;
+        g.frac_bits = (int32_t)frac;
+        g.steps = (int32_t)steps;
+        g.rot_dim = (int32_t)rot;
+        g.table_rows = (int32_t)rows;
+        const c10::DeviceGuard guard(x.device());
+        at::Tensor M[2], S[2], Dm[2], G[2], Z[2];
+        if (steps) {
+            new_pair(like, x, M, g.M);
+            new_pair({T, H, sent}, x, S, g.S);
+        }
+        if (g.gain[0]) {
+            new_pair(like, x, Dm, g.D);
+            new_pair({gains, D}, x, G, g.G);
+        }
+        new_pair(like, x, Z, g.Z);
+        const int code = unlocked([&] { return comet_norm_rotate(stream, &g); });
+        return answer_pairs(code, {M, S, Dm, G, Z});
+    });
+}
+
 #define FAST(name, f) {name, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     FAST("bind_shares", bind_shares),
@@ -379,6 +602,8 @@ PyMethodDef methods[] = {
     FAST("truncate_pair", truncate_pair),
     FAST("add_bias", add_bias),
     FAST("beaver_matmul_static", beaver_matmul_static),
+    FAST("linear", linear),
+    FAST("norm_rotate", norm_rotate),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -441,3 +441,61 @@ def reshare(value: np.ndarray, seed: int, stream: str):
 def lib_layout(right_operand: np.ndarray) -> np.ndarray:
     """[inner, cols] (paper shape) -> [cols, inner] contiguous (library storage)."""
     return np.ascontiguousarray(right_operand.T)
+
+
+# ---------------------------------------------------------------------------
+# linear layers and norms of heads: the dealer's material and the public tables
+# ---------------------------------------------------------------------------
+def dealer_square_pair(seed: int, stream: str, shape) -> dict:
+    """The dealer's pair for one square per element: R uniform and Q = R * R mod 2^64, each split into two uniform
+    shares.  Returns {"R": (R, R0, R1), "Q": ...}."""
+    R = random_u64(seed, stream + "/R", int(np.prod(shape))).reshape(shape)
+    with np.errstate(over="ignore"):
+        Q = R * R
+    return {"R": (R, *split_shares(R, seed, stream + "/R")), "Q": (Q, *split_shares(Q, seed, stream + "/Q"))}
+
+
+def norm_row_words(steps: int) -> int:
+    """Words of dealer's material per row of a norm with this many Newton steps."""
+    return 6 * steps - 3
+
+
+def dealer_norm(seed: int, stream: str, tokens: int, heads: int, dim: int, steps: int) -> dict:
+    """Material of the norms of [tokens, heads] rows of `dim` words.  U: the masks of the rows; "words": per row the sum of
+    their squares, the mask a of the mean square, for each step behind the first the mask of y, its square, the mask of p, its
+    product with a, the mask of w, its product with that of y, and the mask v of the root; UV = v U.  Each (value, share 0,
+    share 1)."""
+    def draw(name, *shape):
+        return random_u64(seed, f"{stream}/{name}", int(np.prod(shape))).reshape(shape)
+
+    U = draw("U", tokens, heads, dim)
+    words = np.empty((tokens, heads, norm_row_words(steps)), U64)
+    with np.errstate(over="ignore"):
+        words[..., 0] = (U * U).sum(-1, dtype=U64)
+        a = draw("a", tokens, heads)
+        words[..., 1] = a
+        for k in range(steps - 1):
+            y, p, w = (draw(f"{name}{k}", tokens, heads) for name in "ypw")
+            for j, v in enumerate((y, y * y, p, a * p, w, y * w)):
+                words[..., 2 + 6 * k + j] = v
+        v = draw("v", tokens, heads)
+        words[..., -1] = v
+        UV = U * v[..., None]
+    return {name: (t, *split_shares(t, seed, f"{stream}/{name}/split")) for name, t in (("U", U), ("words", words), ("UV", UV))}
+
+
+def dealer_gain(seed: int, stream: str, tokens: int, heads: int, dim: int, gains: int, q_heads: int) -> dict:
+    """Triple of a product of [tokens, heads, dim] with a gain [gains, dim] (the second row for the heads from q_heads
+    on): A, mask uniform, C = A * mask of the head's gain row; each (value, share 0, share 1)."""
+    A = random_u64(seed, stream + "/A", tokens * heads * dim).reshape(tokens, heads, dim)
+    mask = random_u64(seed, stream + "/mask", gains * dim).reshape(gains, dim)
+    row = np.where(np.arange(heads) < q_heads, 0, gains - 1)
+    with np.errstate(over="ignore"):
+        C = A * mask[row][None]
+    return {name: (t, *split_shares(t, seed, f"{stream}/{name}/split")) for name, t in (("A", A), ("mask", mask), ("C", C))}
+
+
+def rotation_tables(rows: int, rot_dim: int, frac_bits: int, base: float = 10000.0):
+    """Public tables (cos, sin) [rows, rot_dim / 2] at scale f of the angles position * base^(-2j / rot_dim)."""
+    angle = np.arange(rows)[:, None] * base ** (-np.arange(rot_dim // 2) / (rot_dim // 2))
+    return encode(np.cos(angle), frac_bits), encode(np.sin(angle), frac_bits)
