@@ -486,6 +486,24 @@ cudaError_t tensor_kernel_attributes() {
     return err;
 }
 
+// The same for the kernels of comet_norm_rotate: room for the longest row words, three CTAs an SM with those of ten steps.
+cudaError_t norm_kernel_attributes() {
+    namespace nm = comet::norm;
+    cudaError_t err = cudaSuccess;
+    auto room = [&](auto* kernel, int rows) {
+        if (err == cudaSuccess)
+            err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       nm::PLACE_BYTES * nm::CLUSTER_THREADS + rows * nm::row_bytes(nm::MAX_STEPS));
+        if (err == cudaSuccess)
+            err = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, (int)cudaSharedmemCarveoutMaxShared);
+    };
+    for (auto* kernel : {comet::norm_group_kernel<8, true>, comet::norm_group_kernel<8, false>}) room(kernel, nm::GROUP_THREADS / 8);
+    for (auto* kernel : {comet::norm_group_kernel<16, true>, comet::norm_group_kernel<16, false>}) room(kernel, nm::GROUP_THREADS / 16);
+    for (auto* kernel : {comet::norm_group_kernel<32, true>, comet::norm_group_kernel<32, false>}) room(kernel, nm::GROUP_THREADS / 32);
+    for (auto* kernel : {comet::norm_cluster_kernel<true>, comet::norm_cluster_kernel<false>}) room(kernel, 1);
+    return err;
+}
+
 // Bytes of one set of operand planes: of limbs (tiles of `tile` rows), of residues.
 size_t limb_set(int rows, int K, int tile) {
     return (size_t)ceil_div(rows, tile) * ceil_div(K, comet::limb::KC) * tile * comet::limb::KC * comet::limb::PLANES;
@@ -1640,6 +1658,7 @@ cudaError_t static_device(StaticDevice* out) {
         int least = 0;
         if (err == cudaSuccess) err = cudaDeviceGetStreamPriorityRange(&least, &d.top_priority);
         if (err == cudaSuccess) err = tensor_kernel_attributes();
+        if (err == cudaSuccess) err = norm_kernel_attributes();
         if (err == cudaSuccess) err = cudaGetSymbolAddress(&p, g_static_scratch);
         if (err == cudaSuccess) err = cudaGetSymbolAddress(&e, g_static_error);
         if (err != cudaSuccess) return err;
@@ -2177,36 +2196,42 @@ namespace {
 
 // A thread takes four words of a row.  Up to 128 words: a warp for a row, or for two or four; beyond: a cluster of CTAs of at
 // most 256 threads.
+void (*norm_kernel(int dim, bool vec))(comet::NormArgs) {
+    const int quads = ceil_div(dim, 4);
+    if (dim > comet::norm::GROUP_DIM) return vec ? comet::norm_cluster_kernel<true> : comet::norm_cluster_kernel<false>;
+    if (quads <= 8) return vec ? comet::norm_group_kernel<8, true> : comet::norm_group_kernel<8, false>;
+    if (quads <= 16) return vec ? comet::norm_group_kernel<16, true> : comet::norm_group_kernel<16, false>;
+    return vec ? comet::norm_group_kernel<32, true> : comet::norm_group_kernel<32, false>;
+}
+
 int launch_norm(const comet::NormArgs& a, bool vec, cudaStream_t stream) {
     namespace nm = comet::norm;
     const int quads = ceil_div(a.dim, 4);
-    const size_t row_bytes = 2 * nm::words(a.steps) * sizeof(u64);
-    cudaError_t err;
+    const size_t row_bytes = nm::row_bytes(a.steps);
+    int cluster = 1;
+    while (ceil_div(quads, cluster) > nm::CLUSTER_THREADS) cluster *= 2;
+    cudaLaunchConfig_t lc;
+    std::memset(&lc, 0, sizeof(lc));
     if (a.dim <= nm::GROUP_DIM) {
-        const int group = quads <= 8 ? 8 : quads <= 16 ? 16 : 32, rows = 32 * nm::GROUP_WARPS / group;
-        void (*kernel)(comet::NormArgs) = group == 8    ? (vec ? comet::norm_group_kernel<8, true> : comet::norm_group_kernel<8, false>)
-                                          : group == 16 ? (vec ? comet::norm_group_kernel<16, true> : comet::norm_group_kernel<16, false>)
-                                                        : (vec ? comet::norm_group_kernel<32, true> : comet::norm_group_kernel<32, false>);
-        err = launch_chained(kernel, dim3(ceil_div(a.rows, rows)), dim3(32 * nm::GROUP_WARPS), rows * row_bytes, stream, nullptr, a);
+        const int rows = nm::GROUP_THREADS / (quads <= 8 ? 8 : quads <= 16 ? 16 : 32);
+        lc.gridDim = dim3(ceil_div(a.rows, rows));
+        lc.blockDim = dim3(nm::GROUP_THREADS);
+        lc.dynamicSmemBytes = nm::PLACE_BYTES * nm::GROUP_THREADS + rows * row_bytes;
     } else {
-        int cluster = 1;
-        while (ceil_div(quads, cluster) > nm::MAX_CTA_QUADS) cluster *= 2;
-        cudaLaunchConfig_t lc;
-        std::memset(&lc, 0, sizeof(lc));
         lc.gridDim = dim3((unsigned)a.rows * cluster);
         lc.blockDim = dim3(ceil_div(ceil_div(quads, cluster), 32) * 32);
-        lc.dynamicSmemBytes = row_bytes;
-        lc.stream = stream;
-        cudaLaunchAttribute attr[2];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = cluster;
-        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-        lc.attrs = attr;
-        lc.numAttrs = 2;
-        err = cudaLaunchKernelEx(&lc, vec ? comet::norm_cluster_kernel<true> : comet::norm_cluster_kernel<false>, a);
+        lc.dynamicSmemBytes = nm::PLACE_BYTES * lc.blockDim.x + row_bytes;
     }
+    lc.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = cluster > 1 ? 2 : 1;
+    const cudaError_t err = cudaLaunchKernelEx(&lc, norm_kernel(a.dim, vec), a);
     if (err != cudaSuccess) cudaGetLastError();
     return err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
 }
@@ -2306,7 +2331,14 @@ extern "C" int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args
     a.f = g->frac_bits;
     a.steps = g->steps;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    if (normed) return launch_norm(a, vec, stream);
+    if (normed) {
+        StaticDevice dev;                                        // (the kernels' shared memory is settled there)
+        if (static_device(&dev) != cudaSuccess) {
+            cudaGetLastError();
+            return COMET_ERR_CUDA;
+        }
+        return launch_norm(a, vec, stream);
+    }
     const unsigned quads = (unsigned)ceil_div(a.dim, 4);
     return launch_pass(vec ? comet::rotate_kernel<true> : comet::rotate_kernel<false>, dim3(shuffle_grid(rows * quads)), stream, a, quads);
 }

@@ -28,11 +28,13 @@ typedef unsigned long long u64;
 
 namespace norm {
 constexpr int MAX_STEPS = 24, MAX_DIM = 8192;
-constexpr int GROUP_WARPS = 4;                       // warps of a CTA that has a row per warp, or several
+constexpr int GROUP_THREADS = 128;                   // of a CTA that has several rows
+constexpr int CLUSTER_THREADS = 256;                 // at most, of a CTA of a cluster that has one
 constexpr int GROUP_DIM = 128;                       // longest row of one warp: four words a lane
-constexpr int MAX_CTA_QUADS = 256;                   // longer rows: a thread per four words, a cluster per row
+constexpr int PLACE_BYTES = 6 * 2 * 16;              // of shared memory that a thread's four words of UV, A and C of both parties take
 __host__ __device__ constexpr int words(int steps) { return 6 * steps - 3; }       // a row's own, from the dealer
 __host__ __device__ constexpr int openings(int steps) { return 3 * steps - 1; }    // a row's own, in its message
+constexpr int row_bytes(int steps) { return 2 * (words(steps) + openings(steps)) * 8; }    // of shared memory, both parties' of both
 }  // namespace norm
 
 struct NormArgs {
@@ -51,13 +53,18 @@ struct NormArgs {
     int f, steps, divisor_bits;          // divisor_bits: its logarithm, or -1
 };
 
-__device__ __forceinline__ u64 norm_negate(u64 v, int party) { return party ? 0ull - v : v; }
-__device__ __forceinline__ u64 norm_trunc(u64 v, int party, int bits) { return norm_negate(norm_negate(v, party) >> bits, party); }
+// v >> bits for 1 <= bits <= 32: two instructions, where a shift by any count takes twice as many.
+__device__ __forceinline__ u64 norm_shift(u64 v, int bits) {
+    const unsigned lo = (unsigned)v, hi = (unsigned)(v >> 32);
+    return (u64)__funnelshift_rc(hi, 0u, bits) << 32 | __funnelshift_rc(lo, hi, bits);
+}
 
-// Where a thread's four words of a row lie: pairs P and P + 1, P even, of the row's dim / 2.  A pair is (2P, 2P + 1), or
-// (P, P + half) where halves are rotated against each other.  VEC: two accesses of 16 bytes, else four of 8.
+// Where a thread's four words of a row lie.  A row is dim / 2 pairs, (2P, 2P + 1), or (P, P + half) for the P < half where
+// halves are rotated against each other; a thread has two pairs.  VEC: two accesses of 16 bytes, else four of 8.  Neighbouring
+// threads' accesses lie side by side: a thread's pairs are neighbours where a pair's members lie apart, else they lie apart
+// themselves.  (As neighbours throughout, 32-byte sectors are touched twice: rows of 4096 words, 203 tokens, 38.9 us.)
 struct NormPlace {
-    int pair, at[4];             // elements: first and second of either pair (VEC: at[0] and at[2] of the two accesses)
+    int pair[2], at[4];          // elements: first and second of either pair (VEC: at[0] and at[2] of the two accesses)
     bool has[2];                 // either pair exists (VEC: either access)
     bool split;                  // VEC: the accesses are the firsts and the seconds, not the pairs
     bool turned[2];              // either pair is rotated
@@ -65,159 +72,214 @@ struct NormPlace {
 template <bool VEC>
 __device__ __forceinline__ NormPlace norm_place(int quad, int dim, int half, int interleaved) {
     NormPlace p;
-    p.pair = 2 * quad;
-    p.has[0] = p.pair < dim / 2;
-    p.has[1] = p.pair + 1 < dim / 2;
-    p.split = !interleaved && p.pair < half;
+    const int pairs = dim / 2, apart = VEC && !interleaved ? half : 0;       // (VEC: half is even)
+    p.split = 2 * quad < apart;
+    const int rest = (pairs - apart + 1) / 2;                                // threads that have the other pairs
+    p.pair[0] = p.split ? 2 * quad : quad + apart / 2;
+    p.pair[1] = p.pair[0] + (p.split ? 1 : rest);
+    p.has[0] = p.split || p.pair[0] < apart + rest;
+    p.has[1] = p.has[0] && p.pair[1] < pairs;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const int P = p.pair + k;
-        p.turned[k] = P < half;
-        const bool apart = !interleaved && P < half;
-        p.at[2 * k] = apart ? P : 2 * P;
-        p.at[2 * k + 1] = apart ? P + half : 2 * P + 1;
+        const int P = p.pair[k];
+        p.turned[k] = p.has[k] && P < half;
+        const bool far = !interleaved && P < half;
+        p.at[2 * k] = far ? P : 2 * P;
+        p.at[2 * k + 1] = far ? P + half : 2 * P + 1;
     }
-    if (VEC && p.split) p.at[2] = p.pair + half;     // half is even: both pairs are apart
+    if (p.split) p.at[2] = p.pair[0] + half;
     return p;
 }
-// STREAMED: read once; else through L1, for what several rows read.
-template <bool VEC, bool STREAMED>
-__device__ __forceinline__ void norm_load(const u64* row, const NormPlace& p, u64 v[4]) {
+// The words of access k (VEC; else of pair k), through L1: what several rows read.
+template <bool VEC>
+__device__ __forceinline__ void norm_load2(const u64* row, const NormPlace& p, int k, u64 v[2]) {
     if (VEC) {
-        ulonglong2 a = make_ulonglong2(0ull, 0ull), b = a;
-        const ulonglong2 *pa = reinterpret_cast<const ulonglong2*>(row + p.at[0]), *pb = reinterpret_cast<const ulonglong2*>(row + p.at[2]);
-        if (p.has[0]) a = STREAMED ? __ldcs(pa) : __ldg(pa);
-        if (p.has[1]) b = STREAMED ? __ldcs(pb) : __ldg(pb);
-        v[0] = a.x;
-        v[1] = p.split ? b.x : a.y;
-        v[2] = p.split ? a.y : b.x;
-        v[3] = b.y;
+        const ulonglong2 w = __ldg(reinterpret_cast<const ulonglong2*>(row + p.at[2 * k]));
+        v[0] = w.x;
+        v[1] = w.y;
     } else {
+        v[0] = __ldg(row + p.at[2 * k]);
+        v[1] = __ldg(row + p.at[2 * k + 1]);
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void norm_store2(u64* row, const NormPlace& p, int k, const u64 v[2]) {
+    if (VEC) {
+        __stcs(reinterpret_cast<ulonglong2*>(row + p.at[2 * k]), make_ulonglong2(v[0], v[1]));
+    } else {
+        __stcs(row + p.at[2 * k], v[0]);
+        __stcs(row + p.at[2 * k + 1], v[1]);
+    }
+}
+// All four words, in the order of the accesses, read once.
+template <bool VEC>
+__device__ __forceinline__ void norm_load(const u64* row, const NormPlace& p, u64 v[4]) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = !p.has[k >> 1] ? 0ull : STREAMED ? __ldcs(row + p.at[k]) : __ldg(row + p.at[k]);
+    for (int k = 0; k < 2; ++k) {
+        v[2 * k] = v[2 * k + 1] = 0ull;
+        if (!p.has[k]) continue;
+        if (VEC) {
+            const ulonglong2 w = __ldcs(reinterpret_cast<const ulonglong2*>(row + p.at[2 * k]));
+            v[2 * k] = w.x;
+            v[2 * k + 1] = w.y;
+        } else {
+            v[2 * k] = __ldcs(row + p.at[2 * k]);
+            v[2 * k + 1] = __ldcs(row + p.at[2 * k + 1]);
+        }
     }
 }
 template <bool VEC>
 __device__ __forceinline__ void norm_store(u64* row, const NormPlace& p, const u64 v[4]) {
-    if (VEC) {
-        if (p.has[0]) __stcs(reinterpret_cast<ulonglong2*>(row + p.at[0]), make_ulonglong2(v[0], p.split ? v[2] : v[1]));
-        if (p.has[1]) __stcs(reinterpret_cast<ulonglong2*>(row + p.at[2]), make_ulonglong2(p.split ? v[1] : v[2], v[3]));
-    } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (p.has[k >> 1]) __stcs(row + p.at[k], v[k]);
-    }
+    for (int k = 0; k < 2; ++k)
+        if (p.has[k]) norm_store2<VEC>(row, p, k, v + 2 * k);
 }
 
 // Public angles of a thread's two pairs.  A position outside the tables is not followed: its pairs become zero.
 template <bool VEC>
 __device__ __forceinline__ void norm_angles(const NormArgs& a, int token, const NormPlace& p, u64 c[2], u64 s[2]) {
     c[0] = c[1] = s[0] = s[1] = 0ull;
-    if (!p.turned[0]) return;
+    if (!p.turned[0] && !p.turned[1]) return;
     const int at = __ldg(a.positions + token);
     if (at < 0 || at >= a.table_rows) {
         if (a.bad_index) *a.bad_index = 1;
         return;
     }
-    const size_t o = (size_t)at * a.half + p.pair;
-    if (VEC) {                                       // half is even
-        const ulonglong2 cc = __ldg(reinterpret_cast<const ulonglong2*>(a.cos + o)), ss = __ldg(reinterpret_cast<const ulonglong2*>(a.sin + o));
+    const size_t o = (size_t)at * a.half;
+    if (p.split) {                                   // (half is even)
+        const ulonglong2 cc = __ldg(reinterpret_cast<const ulonglong2*>(a.cos + o + p.pair[0]));
+        const ulonglong2 ss = __ldg(reinterpret_cast<const ulonglong2*>(a.sin + o + p.pair[0]));
         c[0] = cc.x; c[1] = cc.y; s[0] = ss.x; s[1] = ss.y;
     } else {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
             if (p.turned[k]) {
-                c[k] = __ldg(a.cos + o + k);
-                s[k] = __ldg(a.sin + o + k);
+                c[k] = __ldg(a.cos + o + p.pair[k]);
+                s[k] = __ldg(a.sin + o + p.pair[k]);
             }
     }
 }
-__device__ __forceinline__ void norm_rotate_words(u64 v[4], const NormPlace& p, const u64 c[2], const u64 s[2], int party, int f) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const u64 x = v[2 * k], y = v[2 * k + 1];
-        const u64 one = norm_trunc(x * c[k] - y * s[k], party, f), two = norm_trunc(y * c[k] + x * s[k], party, f);
-        v[2 * k] = p.turned[k] ? one : x;
-        v[2 * k + 1] = p.turned[k] ? two : y;
+// Party 1's shares are held negated: its truncation of a share x = -n is -(n >> b), the plain shift of what is held.
+__device__ __forceinline__ void norm_turn(u64& x, u64& y, u64 c, u64 s, int f) {
+    const u64 one = norm_shift(x * c - y * s, f), two = norm_shift(y * c + x * s, f);
+    x = one;
+    y = two;
+}
+__device__ __forceinline__ void norm_rotate_words(u64 v[4], const NormPlace& p, const u64 c[2], const u64 s[2], int f) {
+    if (p.split) {
+        norm_turn(v[0], v[2], c[0], s[0], f);
+        norm_turn(v[1], v[3], c[1], s[1], f);
+    } else {
+        if (p.turned[0]) norm_turn(v[0], v[1], c[0], s[0], f);
+        if (p.turned[1]) norm_turn(v[2], v[3], c[1], s[1], f);
     }
 }
 
-// The shares of the root of a row's mean square, on even lanes party 0's, on odd lanes party 1's (sq: that party's share of the
-// sum of squares without Q).  `w` holds the row's words, [party][words(steps)]; the openings take the place of words that have been
-// read: the first openings(steps) of each party are then its message.  Every pair of lanes computes the same; `write` for one.
-// Returns the opened y - v; *v_own becomes the party's share of v.  All lanes of the warp take part.
-__device__ __forceinline__ u64 norm_other(u64 v) { return __shfl_xor_sync(0xffffffffu, v, 1); }
-__device__ __forceinline__ u64 norm_root(const NormArgs& a, u64 sq, u64* w, bool write, int party, u64* v_own) {
+// The shares of the root of a row's mean square: even lanes work for party 0, odd ones for party 1, and a pair of lanes exchanges
+// its openings.  All of party 1's is held negated here, its words w too, which makes its truncation the plain shift:
+//   sq: the party's share of the sum of squares without Q;  w: its words of the row;  o: where its openings go, 3 steps - 1
+//   words (`write`: pairs of lanes that share a row let one of them do that).
+// Returns the opened y - v.  A chain of 3 steps products, each waiting for the one before, while the CTA waits for it: what a
+// step does not have to wait for is made ahead of it.
+__device__ __forceinline__ u64 norm_opened(u64 mine, int party) {
+    const u64 theirs = __shfl_xor_sync(0xffffffffu, mine, 1);
+    return party ? theirs - mine : mine - theirs;
+}
+__device__ __forceinline__ u64 norm_root(const NormArgs& a, u64 sq, const u64* __restrict__ w, u64* __restrict__ o, bool write, int party) {
     const int f = a.f;
-    const u64 three = party ? 3ull << f : 0ull;
-    w += party * norm::words(a.steps);
-    u64 sum = norm_negate(sq + w[0], party);
-    sum = a.divisor_bits >= 0 ? sum >> a.divisor_bits : sum / a.divisor;
-    const u64 s = norm_negate(sum, party) + (party ? a.eps : 0ull);
-    u64 y = norm_trunc(a.guess * (three - norm_trunc(s * a.first, party, f)), party, f + 1);
-    const u64 sa = w[1];
-    u64 mine = s - sa;
-    const u64 ds = mine + norm_other(mine);
-    __syncwarp();
-    if (write) w[0] = mine;
+    const u64 only = party ? ~0ull : 0ull, three = only & 3ull << f;     // the public terms are party 1's
+    u64 s = sq + w[0];
+    s = a.divisor_bits >= 0 ? s >> a.divisor_bits : s / a.divisor;
+    s -= only & a.eps;
+    u64 y = norm_shift(a.guess * (0ull - three - norm_shift(s * a.first, f)), f + 1);
+    const u64 t0 = s - w[1], ds = norm_opened(t0, party), sa = w[1] - (only & ds);
+    if (write) o[0] = t0;
     const u64* next = w + 2;
-    u64* out = w + 1;                // stays behind `next`
+    u64* out = o + 1;
+#pragma unroll 1
     for (int k = 1; k < a.steps; ++k) {
-        const u64 ya = next[0], yy = next[1], pb = next[2], apb = next[3], wb = next[4], yw = next[5];
-        next += 6;
-        const u64 oy = y - ya, d = oy + norm_other(oy);
-        const u64 p = norm_trunc(yy + d * (ya + ya + (party ? d : 0ull)), party, f);
-        const u64 op = p - pb, g = op + norm_other(op);
-        const u64 x = three - norm_trunc(apb + ds * pb + g * (sa + (party ? ds : 0ull)), party, f);
-        const u64 ow = x - wb, h = ow + norm_other(ow);
-        y = norm_trunc(yw + d * wb + h * (ya + (party ? d : 0ull)), party, f + 1);
-        __syncwarp();
+        const u64 ya = next[0], yy = next[1], pb = next[2], wb = next[4], yw = next[5], ap = next[3] + ds * pb, ya2 = ya + ya;
+        const u64 t1 = y - ya, d = norm_opened(t1, party), own = only & d;
+        const u64 p = norm_shift(yy + d * (ya2 - own), f);
+        const u64 t2 = p - pb, g = norm_opened(t2, party);
+        const u64 x = 0ull - three - norm_shift(ap + g * sa, f);
+        const u64 t3 = x - wb, h = norm_opened(t3, party);
+        y = norm_shift(yw + d * wb + h * (ya - own), f + 1);
         if (write) {
-            out[0] = oy;
-            out[1] = op;
-            out[2] = ow;
+            out[0] = t1;
+            out[1] = t2;
+            out[2] = t3;
         }
+        next += 6;
         out += 3;
     }
-    *v_own = *next;
-    mine = y - *v_own;
-    __syncwarp();
-    if (write) *out = mine;
-    return mine + norm_other(mine);
+    const u64 t4 = y - *next;
+    if (write) *out = t4;
+    return norm_opened(t4, party);
 }
 
-__device__ __forceinline__ void norm_fetch_word(u64* dst, const u64* src) {
+__device__ __forceinline__ void norm_fetch8(void* dst, const u64* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void norm_fetch16(void* dst, const u64* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
 }
 __device__ __forceinline__ void norm_fetch_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// A thread's four words of a row: `open` before the root, `finish` after it.
+// A thread's four words of a row: `open` before the root, `finish` after it.  What `finish` reads is on its way to this thread's
+// places in shared memory meanwhile (nobody else reads them): UV, A and C of both parties.
 template <bool VEC>
 struct NormQuad {
     NormPlace p;
     size_t at;                   // the row in the dense tensors
-    u64 m[4], U[2][4], UV[2][4], A[2][4], C[2][4], c[2], s[2];
+    u64 m[4], U[2][4];
+    ulonglong2* mine;            // pair k of array j, party i: mine[((3 i + j) 2 + k) stride]
+    int stride;
+
+    __device__ __forceinline__ void fetch(int array, const u64* row) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            ulonglong2* to = mine + (array * 2 + k) * stride;
+            if (!p.has[k]) continue;
+            if (VEC) {
+                norm_fetch16(to, row + p.at[2 * k]);
+            } else {
+                norm_fetch8(&to->x, row + p.at[2 * k]);
+                norm_fetch8(&to->y, row + p.at[2 * k + 1]);
+            }
+        }
+    }
+    __device__ __forceinline__ void fetched(int array, int k, u64 v[2]) const {
+        const ulonglong2 w = mine[(array * 2 + k) * stride];
+        v[0] = w.x;
+        v[1] = w.y;
+    }
 
     // Loads, the first message, and both parties' part of the sum of squares.
-    __device__ __forceinline__ void open(const NormArgs& a, int row, int token, int head, int quad, u64 sq[2]) {
+    // `beside` runs while the loads are under way.
+    template <typename F>
+    __device__ __forceinline__ void open(const NormArgs& a, int row, int token, int head, int quad, ulonglong2* place, int place_stride,
+                                         u64 sq[2], F&& beside) {
         p = norm_place<VEC>(quad, a.dim, a.half, a.interleaved);
         at = (size_t)row * a.dim;
+        mine = place;
+        stride = place_stride;
         const size_t x_at = (size_t)token * a.x_stride + (size_t)head * a.dim;
         u64 x[2][4];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            norm_load<VEC, true>(a.X[i] + x_at, p, x[i]);
-            norm_load<VEC, true>(a.U[i] + at, p, U[i]);
+            norm_load<VEC>(a.X[i] + x_at, p, x[i]);
+            norm_load<VEC>(a.U[i] + at, p, U[i]);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            norm_load<VEC, true>(a.UV[i] + at, p, UV[i]);
+            fetch(3 * i, a.UV[i] + at);
             if (a.gain[0]) {
-                norm_load<VEC, true>(a.A[i] + at, p, A[i]);
-                norm_load<VEC, true>(a.C[i] + at, p, C[i]);
+                fetch(3 * i + 1, a.A[i] + at);
+                fetch(3 * i + 2, a.C[i] + at);
             }
         }
-        if (a.half) norm_angles<VEC>(a, token, p, c, s);
+        beside();
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
 #pragma unroll
@@ -234,46 +296,61 @@ struct NormQuad {
         sq[0] *= 2;
     }
 
-    // root: the opened y - v; v: both parties' shares of v.  `tells`: this row writes the message of its gain.
-    __device__ __forceinline__ void finish(const NormArgs& a, int head, bool tells, u64 root, const u64 v[2]) {
+    // root: the opened y - v; v0, n1: party 0's share of v and party 1's, negated.  `tells`: this row writes the message of its
+    // gain.  An access at a time: the registers of both at once would not fit.
+    __device__ __forceinline__ void finish(const NormArgs& a, int token, int head, bool tells, u64 root, u64 v0, u64 n1) {
+        const size_t g_at = a.q_heads > 0 && head >= a.q_heads ? a.dim : 0;
+        norm_fetch_wait();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            U[0][k] = norm_trunc(UV[0][k] + m[k] * v[0] + root * U[0][k], 0, a.f);
-            U[1][k] = norm_trunc(UV[1][k] + m[k] * v[1] + root * (U[1][k] + m[k]), 1, a.f);
-        }
-        if (a.gain[0]) {
-            const size_t g_at = a.q_heads > 0 && head >= a.q_heads ? a.dim : 0;
-            u64 b[2][4], e[4], g[4];
+        for (int k = 0; k < 2; ++k) {
+            if (!p.has[k]) continue;
+            u64 *x0 = U[0] + 2 * k, *x1 = U[1] + 2 * k, t[2];
+            fetched(0, k, t);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                norm_load<VEC, false>(a.gain_mask[i] + g_at, p, b[i]);
-                norm_load<VEC, false>(a.gain[i] + g_at, p, g);
+            for (int j = 0; j < 2; ++j) x0[j] = norm_shift(t[j] + m[2 * k + j] * v0 + root * x0[j], a.f);
+            fetched(3, k, t);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    g[k] -= b[i][k];
-                    e[k] = i ? e[k] + g[k] : g[k];
-                }
-                if (tells) norm_store<VEC>(a.G[i] + g_at, p, g);
-            }
-            u64 d[4];
+            for (int j = 0; j < 2; ++j) x1[j] = norm_shift(m[2 * k + j] * n1 - t[j] - root * (x1[j] + m[2 * k + j]), a.f);          // negated
+            if (!a.gain[0]) continue;
+            u64 A[2][2], d[2], e[2], b[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
+                fetched(3 * i + 1, k, A[i]);
+                u64 o[2];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    U[i][k] -= A[i][k];
-                    d[k] = i ? d[k] + U[i][k] : U[i][k];
+                for (int j = 0; j < 2; ++j) {
+                    o[j] = i ? 0ull - (x1[j] + A[1][j]) : x0[j] - A[0][j];
+                    d[j] = i ? d[j] + o[j] : o[j];
                 }
-                norm_store<VEC>(a.Dm[i] + at, p, U[i]);
+                norm_store2<VEC>(a.Dm[i] + at, p, k, o);
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                U[0][k] = norm_trunc(C[0][k] + d[k] * b[0][k] + e[k] * A[0][k], 0, a.f);
-                U[1][k] = norm_trunc(C[1][k] + d[k] * b[1][k] + e[k] * (A[1][k] + d[k]), 1, a.f);
+            for (int i = 0; i < 2; ++i) {
+                norm_load2<VEC>(a.gain[i] + g_at, p, k, t);
+                norm_load2<VEC>(a.gain_mask[i] + g_at, p, k, b);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    t[j] -= b[j];
+                    e[j] = i ? e[j] + t[j] : t[j];
+                }
+                if (tells) norm_store2<VEC>(a.G[i] + g_at, p, k, t);
             }
+            fetched(5, k, t);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) x1[j] = norm_shift(0ull - t[j] - d[j] * b[j] - e[j] * (A[1][j] + d[j]), a.f);
+            norm_load2<VEC>(a.gain_mask[0] + g_at, p, k, b);
+            fetched(2, k, t);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) x0[j] = norm_shift(t[j] + d[j] * b[j] + e[j] * A[0][j], a.f);
         }
+        u64 c[2], s[2];
+        if (a.half) norm_angles<VEC>(a, token, p, c, s);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            if (a.half) norm_rotate_words(U[i], p, c, s, i, a.f);
+            if (a.half) norm_rotate_words(U[i], p, c, s, a.f);
+            if (i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) U[1][k] = 0ull - U[1][k];
             norm_store<VEC>(a.Z[i] + at, p, U[i]);
         }
     }
@@ -283,81 +360,103 @@ struct NormQuad {
 __device__ __forceinline__ bool norm_tells(const NormArgs& a, int token, int head) {
     return token == 0 && (head == 0 || head == a.q_heads);
 }
+// The sum over GROUP lanes of both parties' sq, in every lane: even lanes add up party 0's, odd lanes party 1's.
+template <int GROUP>
+__device__ __forceinline__ u64 norm_lane_sum(const u64 sq[2], int party) {
+    u64 sum = (party ? sq[1] : sq[0]) + __shfl_xor_sync(0xffffffffu, party ? sq[0] : sq[1], 1);
+#pragma unroll
+    for (int o = 2; o < GROUP; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return sum;
+}
 
-// Rows of up to GROUP_DIM words: GROUP lanes each, four words a lane.
+// Rows of up to GROUP_DIM words: GROUP lanes each, four words a lane; one warp works out the roots of all of the CTA's rows, a lane
+// a row.
 template <int GROUP, bool VEC>
-__global__ void __launch_bounds__(32 * norm::GROUP_WARPS, 4)
+__global__ void __launch_bounds__(norm::GROUP_THREADS, 5)
 norm_group_kernel(const __grid_constant__ NormArgs a) {
-    extern __shared__ u64 norm_smem[];
+    constexpr int ROWS = norm::GROUP_THREADS / GROUP;
+    extern __shared__ __align__(16) uint8_t norm_smem[];
+    __shared__ u64 sums[ROWS][2], root[ROWS];
+    ulonglong2* const places = reinterpret_cast<ulonglong2*>(norm_smem);
+    u64* const words = reinterpret_cast<u64*>(norm_smem + norm::PLACE_BYTES * norm::GROUP_THREADS);      // [party][row][count]
     const int sub = threadIdx.x / GROUP, lane = threadIdx.x % GROUP, party = threadIdx.x & 1;
     const int count = norm::words(a.steps), sent = norm::openings(a.steps);
-    u64* const w = norm_smem + sub * 2 * count;
-    const long long r = (long long)blockIdx.x * (32 * norm::GROUP_WARPS / GROUP) + sub;
-    const bool live = r < a.rows;
-    const int row = (int)(live ? r : a.rows - 1);            // groups past the last row have none of its words and write nothing
+    u64* const opened = words + 2 * ROWS * count;                                                         // [party][row][sent]
+    const int first = blockIdx.x * ROWS, rows = min(ROWS, a.rows - first);
+    const bool live = sub < rows;
+    const int row = first + (live ? sub : 0);                // groups past the last row have none of its words and write nothing
     const int token = row / a.heads, head = row - token * a.heads;
     pdl_wait();
     pdl_launch_dependents();
-    for (int i = 0; i < 2; ++i)
-        for (int k = lane; k < count; k += GROUP) norm_fetch_word(w + i * count + k, a.row_words[i] + (size_t)row * count + k);
     NormQuad<VEC> q;
     u64 sq[2];
-    q.open(a, row, token, head, live ? lane : a.dim, sq);
-    // even lanes keep party 0's sum, odd lanes party 1's
-    u64 sum = (party ? sq[1] : sq[0]) + norm_other(party ? sq[0] : sq[1]);
-#pragma unroll
-    for (int o = 2; o < GROUP; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    norm_fetch_wait();
-    __syncwarp();
-    u64 mine;
-    const u64 root = norm_root(a, sum, w, lane < 2, party, &mine), theirs = norm_other(mine);
-    const u64 v[2] = {party ? theirs : mine, party ? mine : theirs};
-    q.finish(a, head, live && norm_tells(a, token, head), root, v);
-    __syncwarp();
-    if (live)
-        for (int i = 0; i < 2; ++i)
-            for (int k = lane; k < sent; k += GROUP) a.S[i][(size_t)row * sent + k] = w[i * count + k];
+    q.open(a, row, token, head, live ? lane : a.dim, places + threadIdx.x, norm::GROUP_THREADS, sq, [&] {
+        for (int k = threadIdx.x; k < rows * count; k += norm::GROUP_THREADS) {
+            words[k] = __ldcs(a.row_words[0] + (size_t)first * count + k);
+            words[ROWS * count + k] = 0ull - __ldcs(a.row_words[1] + (size_t)first * count + k);
+        }
+    });
+    const u64 sum = norm_lane_sum<GROUP>(sq, party);
+    if (lane < 2) sums[sub][party] = party ? 0ull - sum : sum;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        const int r = min((int)threadIdx.x >> 1, ROWS - 1);
+        const bool mine = (int)threadIdx.x < 2 * rows;
+        const u64 opened_root = norm_root(a, sums[r][party], words + (party * ROWS + r) * count, opened + (party * ROWS + r) * sent, mine, party);
+        if (mine) root[r] = opened_root;
+    }
+    __syncthreads();
+    if (!live) return;
+    for (int i = 0; i < 2; ++i)
+        for (int k = lane; k < sent; k += GROUP) {
+            const u64 t = opened[(i * ROWS + sub) * sent + k];
+            __stcs(a.S[i] + (size_t)row * sent + k, i ? 0ull - t : t);
+        }
+    q.finish(a, token, head, norm_tells(a, token, head), root[sub], words[(sub + 1) * count - 1], words[(ROWS + sub + 1) * count - 1]);
 }
 
 // Longer rows: a cluster of CTAs per row, a thread per four words.
 template <bool VEC>
-__global__ void __launch_bounds__(norm::MAX_CTA_QUADS, 2)
+__global__ void __launch_bounds__(norm::CLUSTER_THREADS, 3)
 norm_cluster_kernel(const __grid_constant__ NormArgs a) {
-    extern __shared__ u64 norm_smem[];
-    __shared__ u64 partial[norm::MAX_CTA_QUADS / 32][2], cta_sum[2], told[3];
+    extern __shared__ __align__(16) uint8_t norm_smem[];
+    __shared__ u64 partial[norm::CLUSTER_THREADS / 32][2], cta_sum[2], root;
+    ulonglong2* const places = reinterpret_cast<ulonglong2*>(norm_smem);
+    u64* const words = reinterpret_cast<u64*>(norm_smem + norm::PLACE_BYTES * blockDim.x);               // [party][count]
     uint32_t rank, cluster;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(cluster));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, party = threadIdx.x & 1, warps = blockDim.x >> 5;
     const int count = norm::words(a.steps), sent = norm::openings(a.steps);
+    u64* const opened = words + 2 * count;                                                               // [party][sent]
     const int row = (int)(blockIdx.x / cluster), token = row / a.heads, head = row - token * a.heads;
     pdl_wait();
     pdl_launch_dependents();
-    if (warp == 0)
-        for (int i = 0; i < 2; ++i)
-            for (int k = lane; k < count; k += 32) norm_fetch_word(norm_smem + i * count + k, a.row_words[i] + (size_t)row * count + k);
     NormQuad<VEC> q;
     u64 sq[2];
-    q.open(a, row, token, head, (int)(rank * blockDim.x + threadIdx.x), sq);
-    u64 sum = (party ? sq[1] : sq[0]) + norm_other(party ? sq[0] : sq[1]);
-#pragma unroll
-    for (int o = 2; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    q.open(a, row, token, head, (int)(rank * blockDim.x + threadIdx.x), places + threadIdx.x, blockDim.x, sq, [&] {
+        for (int k = threadIdx.x; k < count; k += blockDim.x) {
+            words[k] = __ldcs(a.row_words[0] + (size_t)row * count + k);
+            words[count + k] = 0ull - __ldcs(a.row_words[1] + (size_t)row * count + k);
+        }
+    });
+    u64 sum = norm_lane_sum<32>(sq, party);
     if (lane < 2) partial[warp][party] = sum;
     __syncthreads();
     if (warp == 0) {
         sum = 0ull;
         for (int k = 0; k < warps; ++k) sum += partial[k][party];
         if (lane < 2) cta_sum[party] = sum;
+        __syncwarp();
     }
     if (cluster > 1) {
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (warp == 0) {
             sum = 0ull;
-            const uint32_t from = (uint32_t)__cvta_generic_to_shared(&cta_sum[party]);
             for (uint32_t k = 0; k < cluster; ++k) {
                 uint32_t there;
                 u64 v;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(from), "r"(k));
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(&cta_sum[party])), "r"(k));
                 asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(there) : "memory");
                 sum += v;
             }
@@ -367,19 +466,17 @@ norm_cluster_kernel(const __grid_constant__ NormArgs a) {
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     }
     if (warp == 0) {
-        norm_fetch_wait();
-        __syncwarp();
-        u64 mine;
-        const u64 root = norm_root(a, sum, norm_smem, lane < 2, party, &mine);
-        if (lane < 2) told[party] = mine;
-        if (lane == 0) told[2] = root;
+        const u64 opened_root = norm_root(a, party ? 0ull - sum : sum, words + party * count, opened + party * sent, lane < 2, party);
+        if (lane == 0) root = opened_root;
     }
     __syncthreads();
-    const u64 v[2] = {told[0], told[1]};
-    q.finish(a, head, norm_tells(a, token, head), told[2], v);
     if (warp == 0 && rank == 0)
         for (int i = 0; i < 2; ++i)
-            for (int k = lane; k < sent; k += 32) a.S[i][(size_t)row * sent + k] = norm_smem[i * count + k];
+            for (int k = lane; k < sent; k += 32) {
+                const u64 t = opened[i * sent + k];
+                __stcs(a.S[i] + (size_t)row * sent + k, i ? 0ull - t : t);
+            }
+    q.finish(a, token, head, norm_tells(a, token, head), root, words[count - 1], words[2 * count - 1]);
     __syncwarp();
     if (cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -396,11 +493,17 @@ rotate_kernel(const __grid_constant__ NormArgs a, unsigned quads) {
         const NormPlace p = norm_place<VEC>((int)(t - (u64)row * quads), a.dim, a.half, a.interleaved);
         u64 x[2][4], c[2], s[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) norm_load<VEC, true>(a.X[i] + (size_t)token * a.x_stride + (size_t)head * a.dim, p, x[i]);
+        for (int i = 0; i < 2; ++i) norm_load<VEC>(a.X[i] + (size_t)token * a.x_stride + (size_t)head * a.dim, p, x[i]);
         norm_angles<VEC>(a, token, p, c, s);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            norm_rotate_words(x[i], p, c, s, i, a.f);
+            auto negate = [&] {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[1][k] = 0ull - x[1][k];
+            };
+            if (i) negate();
+            norm_rotate_words(x[i], p, c, s, a.f);
+            if (i) negate();
             norm_store<VEC>(a.Z[i] + (size_t)row * a.dim, p, x[i]);
         }
     }
