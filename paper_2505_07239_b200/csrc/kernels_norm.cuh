@@ -369,6 +369,37 @@ __device__ __forceinline__ u64 norm_lane_sum(const u64 sq[2], int party) {
     return sum;
 }
 
+// The words of a CTA's rows, `total` of them behind one another, on their way to shared memory, party 1's negated: the first N a
+// thread are asked for before anything else and put there when the other loads are under way.
+template <int N>
+struct NormWords {
+    u64 v[N][2];
+    __device__ __forceinline__ void load(const NormArgs& a, int row, int total, int threads) {
+        const size_t at = (size_t)row * norm::words(a.steps);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int k = threadIdx.x + j * threads;
+            if (k < total)
+                for (int i = 0; i < 2; ++i) v[j][i] = __ldcs(a.row_words[i] + at + k);
+        }
+    }
+    __device__ __forceinline__ void store(const NormArgs& a, int row, int total, int threads, u64* w0, u64* w1) const {
+        const size_t at = (size_t)row * norm::words(a.steps);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int k = threadIdx.x + j * threads;
+            if (k < total) {
+                w0[k] = v[j][0];
+                w1[k] = 0ull - v[j][1];
+            }
+        }
+        for (int k = threadIdx.x + N * threads; k < total; k += threads) {
+            w0[k] = __ldcs(a.row_words[0] + at + k);
+            w1[k] = 0ull - __ldcs(a.row_words[1] + at + k);
+        }
+    }
+};
+
 // Rows of up to GROUP_DIM words: GROUP lanes each, four words a lane; one warp works out the roots of all of the CTA's rows, a lane
 // a row.
 template <int GROUP, bool VEC>
@@ -388,14 +419,12 @@ norm_group_kernel(const __grid_constant__ NormArgs a) {
     const int token = row / a.heads, head = row - token * a.heads;
     pdl_wait();
     pdl_launch_dependents();
+    NormWords<ROWS <= 4 ? 2 : ROWS / 2> early;
+    early.load(a, first, rows * count, norm::GROUP_THREADS);
     NormQuad<VEC> q;
     u64 sq[2];
-    q.open(a, row, token, head, live ? lane : a.dim, places + threadIdx.x, norm::GROUP_THREADS, sq, [&] {
-        for (int k = threadIdx.x; k < rows * count; k += norm::GROUP_THREADS) {
-            words[k] = __ldcs(a.row_words[0] + (size_t)first * count + k);
-            words[ROWS * count + k] = 0ull - __ldcs(a.row_words[1] + (size_t)first * count + k);
-        }
-    });
+    q.open(a, row, token, head, live ? lane : a.dim, places + threadIdx.x, norm::GROUP_THREADS, sq,
+           [&] { early.store(a, first, rows * count, norm::GROUP_THREADS, words, words + ROWS * count); });
     const u64 sum = norm_lane_sum<GROUP>(sq, party);
     if (lane < 2) sums[sub][party] = party ? 0ull - sum : sum;
     __syncthreads();
@@ -432,14 +461,12 @@ norm_cluster_kernel(const __grid_constant__ NormArgs a) {
     const int row = (int)(blockIdx.x / cluster), token = row / a.heads, head = row - token * a.heads;
     pdl_wait();
     pdl_launch_dependents();
+    NormWords<1> early;
+    early.load(a, row, count, blockDim.x);
     NormQuad<VEC> q;
     u64 sq[2];
-    q.open(a, row, token, head, (int)(rank * blockDim.x + threadIdx.x), places + threadIdx.x, blockDim.x, sq, [&] {
-        for (int k = threadIdx.x; k < count; k += blockDim.x) {
-            words[k] = __ldcs(a.row_words[0] + (size_t)row * count + k);
-            words[count + k] = 0ull - __ldcs(a.row_words[1] + (size_t)row * count + k);
-        }
-    });
+    q.open(a, row, token, head, (int)(rank * blockDim.x + threadIdx.x), places + threadIdx.x, blockDim.x, sq,
+           [&] { early.store(a, row, count, blockDim.x, words, words + count); });
     u64 sum = norm_lane_sum<32>(sq, party);
     if (lane < 2) partial[warp][party] = sum;
     __syncthreads();
