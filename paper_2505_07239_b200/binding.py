@@ -411,15 +411,6 @@ def add_bias(Z, bias, stream: Optional[torch.cuda.Stream] = None):
         raise CometError(code, "comet_add_bias")
 
 
-def _on_stream(call, stream, like, *args):
-    """A call that makes its results, and what it needs meanwhile, on the stream it works on: torch hands memory out per stream."""
-    device = like.device.index if isinstance(like, torch.Tensor) and like.is_cuda else None
-    if device is None or torch._C._cuda_getCurrentRawStream(device) == (stream.cuda_stream if stream is not None else 0):
-        return call(stream, *args)
-    with torch.cuda.stream(stream if stream is not None else torch.cuda.default_stream(device)):
-        return call(stream, *args)
-
-
 def linear_workspace(tokens: int, inner: int, cols: int) -> int:
     """Bytes that `linear` takes for the length of a call on the current device (comet_linear_workspace)."""
     out = ctypes.c_int64(0)
@@ -439,7 +430,7 @@ def linear(X, A, W, B, C, frac_bits: int, bias=None, act=None, residual=None, st
     planes of more than a few rows live in a tensor of linear_workspace(T, K, N) bytes for the length of the call.
     A captured call is replayed on the memory that it was captured with.
     """
-    code, E, F, M, Y = _on_stream(_native.linear, stream, X[0], X, A, W, B, C, frac_bits, bias, act, residual)
+    code, E, F, M, Y = _native.linear(stream, X, A, W, B, C, frac_bits, bias, act, residual)
     if code:
         raise CometError(code, "comet_linear")
     return E, F, M, Y
@@ -490,8 +481,7 @@ def norm_rotate(X, frac_bits: int, norm: Optional[Norm] = None, gain: Optional[G
     its second; without `q_heads` there is one row.  A rotation may come alone.
     Returns (NormMessages, Z): Z a pair of new tensors [T, H, D].
     """
-    heads = X[0].shape[1] if q_heads is None else q_heads
-    code, M, S, D, G, Z = _on_stream(_native.norm_rotate, stream, X[0], X, frac_bits, norm, gain, rotation, heads, bad_index_flag)
+    code, M, S, D, G, Z = _native.norm_rotate(stream, X, frac_bits, norm, gain, rotation, q_heads, bad_index_flag)
     if code:
         raise CometError(code, "comet_norm_rotate")
     return NormMessages(M, S, D, G), Z

@@ -22,6 +22,7 @@
 #include "kernels_open.cuh"
 #include "kernels_peak.cuh"
 #include "kernels_residue.cuh"
+#include "kernels_rows.cuh"
 #include "kernels_shuffle.cuh"
 #include "kernels_simt.cuh"
 #include "kernels_stream.cuh"
@@ -501,6 +502,18 @@ cudaError_t norm_kernel_attributes() {
     for (auto* kernel : {comet::norm_group_kernel<16, true>, comet::norm_group_kernel<16, false>}) room(kernel, nm::GROUP_THREADS / 16);
     for (auto* kernel : {comet::norm_group_kernel<32, true>, comet::norm_group_kernel<32, false>}) room(kernel, nm::GROUP_THREADS / 32);
     for (auto* kernel : {comet::norm_cluster_kernel<true>, comet::norm_cluster_kernel<false>}) room(kernel, 1);
+    return err;
+}
+
+cudaError_t rows_kernel_attributes() {
+    cudaError_t err = cudaSuccess;
+    for (auto* kernel : {comet::linear_rows_kernel<1>, comet::linear_rows_kernel<2>, comet::linear_rows_kernel<4>}) {
+        if (err == cudaSuccess)
+            err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       comet::rows::RING_BYTES + comet::rows::VECTOR_BYTES);
+        if (err == cudaSuccess)
+            err = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, (int)cudaSharedmemCarveoutMaxShared);
+    }
     return err;
 }
 
@@ -1659,6 +1672,7 @@ cudaError_t static_device(StaticDevice* out) {
         if (err == cudaSuccess) err = cudaDeviceGetStreamPriorityRange(&least, &d.top_priority);
         if (err == cudaSuccess) err = tensor_kernel_attributes();
         if (err == cudaSuccess) err = norm_kernel_attributes();
+        if (err == cudaSuccess) err = rows_kernel_attributes();
         if (err == cudaSuccess) err = cudaGetSymbolAddress(&p, g_static_scratch);
         if (err == cudaSuccess) err = cudaGetSymbolAddress(&e, g_static_error);
         if (err != cudaSuccess) return err;
@@ -2065,6 +2079,49 @@ size_t linear_context(comet_ctx* c, int sm_count, int T, int K, int N, uint8_t* 
     return at;
 }
 
+// Whether a layer of a few rows goes through linear_rows_kernel.  A token's multiply-adds on the ALUs cost it time beside the loads from
+// the second row on, and every chunk of the contraction index a staging of the rows; what it saves is two launches and the streaming
+// kernel's latency.  This kernel and the streaming kernel with its two passes, us: one row, 64 x 64 5.5 and 9.2, 768 x 768 11.3 and 14.7,
+// 1000 x 1364 16.4 and 23.2, 2048 x 2048 41.0 and 41.6, 4096 x 4096 140.6 and 139.3, 4096 x 11008 359 and 356; two rows, 512 x 512 8.5
+// and 12.6, 1024 x 768 18.1 and 18.8, 1536 x 768 20.8 and 19.5, 2048 x 128 14.0 and 12.6; four rows, 256 x 96 6.8 and 10.2, 512 x 256 10.6
+// either way, 512 x 512 12.6 either way, 768 x 512 15.4 and 13.3.  Nothing is gained on deeper layers (one row, 11008 x 4096 365 and
+// 354, 11008 x 64 30 and 17), nor where a feature does not fill a warp and there are many (24 x 50000 48 and 24).
+bool linear_in_rows(int64_t T, int64_t K, int64_t N) {
+    if (K < 64 && N > 8192) return false;
+    if (T <= 2) return T == 1 ? K <= 4096 : K <= 1024 && K * N <= 1 << 20;
+    return T <= comet::rows::MAX_ROWS && K <= 512 && K * N <= 1 << 17;
+}
+
+// One to four rows: a launch for the whole layer.
+int launch_rows(const comet_ctx* c, const Proj& pr, const comet::LinearEnd& end) {
+    namespace rw = comet::rows;
+    comet::RowsArgs a;
+    std::memset(&a, 0, sizeof(a));
+    for (int p = 0; p < 2; ++p) {
+        a.X[p] = c->buf[p][pr.idX];
+        a.A[p] = c->buf[p][pr.idA];
+        a.W[p] = c->buf[p][COMET_W1];
+        a.B[p] = c->buf[p][pr.idB];
+        a.C[p] = c->buf[p][pr.idC];
+        a.E[p] = c->buf[p][pr.idE];
+        a.F[p] = c->buf[p][pr.idF];
+        a.Y[p] = c->buf[p][pr.idZ];
+    }
+    a.end = end;
+    a.rows = pr.M; a.cols = pr.N; a.pairs = pr.K / 2;
+    const int rows = pr.M <= 2 ? pr.M : 4, chunk = std::min(rw::chunk_pairs(rows), a.pairs);
+    a.slices = chunk >= 384 ? 8 : chunk >= 192 ? 4 : chunk >= 96 ? 2 : 1;
+    // a CTA an SM, all of them with as many blocks
+    const int rounds = ceil_div(a.cols, c->sm_count * rw::MAX_BLOCK);
+    a.block = ceil_div(a.cols, c->sm_count * rounds);
+    a.blocks = ceil_div(a.cols, a.block);
+    const size_t smem = rw::RING_BYTES + (size_t)3 * 16 * rows * chunk;
+    auto* const kernel = rows == 1 ? comet::linear_rows_kernel<1> : rows == 2 ? comet::linear_rows_kernel<2> : comet::linear_rows_kernel<4>;
+    const cudaError_t err = launch_chained(kernel, dim3(std::min(a.blocks, c->sm_count)), dim3(rw::THREADS), smem, c->stream, nullptr, a);
+    if (err != cudaSuccess) cudaGetLastError();
+    return err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
+}
+
 struct Span {
     uintptr_t begin, end;
     Span(const void* p, int64_t count, size_t size = sizeof(u64))
@@ -2167,6 +2224,7 @@ extern "C" int comet_linear(void* cuda_stream, const comet_linear_args* g) {
         last.Z[p] = reinterpret_cast<u64*>(g->Y[p]);
     }
     const Proj pr = proj_up(c, T);
+    if (linear_in_rows(T, K, N)) return launch_rows(c, pr, last.end);
     int rc;
     if (linear_streams(T, K, N)) {
         rc = stream_product(c, pr);

@@ -11,6 +11,8 @@
 #include <ATen/EmptyTensor.h>
 #include <c10/core/Allocator.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/Stream.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -398,18 +400,80 @@ bool fits_int32(std::initializer_list<int64_t> values) {
     return true;
 }
 
-// A new contiguous tensor of ring words on the device of `like` (see empty_like).
-at::Tensor new_words(at::IntArrayRef shape, const at::Tensor& like) {
-    const c10::DeviceGuard guard(like.device());
-    return at::detail::empty_generic(shape, c10::GetAllocator(c10::DeviceType::CUDA), c10::DispatchKeySet(c10::DispatchKey::CUDA),
-                                     like.scalar_type(), std::nullopt);
-}
-void new_pair(at::IntArrayRef shape, const at::Tensor& like, at::Tensor t[2], uint64_t* to[2]) {
-    for (int p = 0; p < 2; ++p) {
-        t[p] = new_words(shape, like);
-        to[p] = words(t[p]);
+// For the length of a call: the tensors' device is the current one, and the stream that the call works on is torch's current one
+// there, because torch hands memory out per stream.
+struct OnStream {
+    c10::DeviceGuard device;
+    c10::impl::VirtualGuardImpl impl;
+    c10::Stream before, wanted;
+    OnStream(c10::Device d, c10::Stream s) : device(d), impl(c10::DeviceType::CUDA), before(impl.getStream(d)), wanted(s) {
+        if (before != wanted) impl.exchangeStream(wanted);
     }
+    ~OnStream() {
+        if (before != wanted) impl.exchangeStream(before);
+    }
+};
+// The stream of a CUDA stream object as torch names it; None: the device's default stream.
+bool stream_of(PyObject* o, c10::Device device, std::optional<c10::Stream>* out) {
+    if (o == Py_None) {
+        out->emplace(c10::Stream::DEFAULT, device);
+        return true;
+    }
+    static PyObject* const names[2] = {PyUnicode_InternFromString("stream_id"), PyUnicode_InternFromString("device_index")};
+    int64_t value[2];
+    for (int k = 0; k < 2; ++k) {
+        PyObject* v = PyObject_GetAttr(o, names[k]);
+        const bool ok = v && as_int(v, &value[k]);
+        Py_XDECREF(v);
+        if (!ok) return false;
+    }
+    if (value[1] != device.index()) return refuse(PyExc_AssertionError, "the stream must be one of the tensors' device");
+    out->emplace(c10::Stream::UNSAFE, device, value[0]);
+    return true;
 }
+
+// The results of a call, new contiguous tensors of ring words on the current stream.  Results of up to a megabyte together share
+// one piece of memory, which is as much as torch's allocator may keep for the smallest of them: ten tensors cost 7 us one by one.
+// Larger ones have memory of their own, so that messages can be let go of without the result.
+struct Results {
+    static constexpr size_t SHARED = 1 << 20, ALIGN = 256;
+    struct Item {
+        c10::SmallVector<int64_t, 3> shape;
+        at::Tensor* to;
+        uint64_t** at;
+        size_t bytes;
+    };
+    const at::Tensor& like;
+    c10::SmallVector<Item, 12> items;
+    size_t total = 0;
+    explicit Results(const at::Tensor& t) : like(t) {}
+    // Two tensors, and where their addresses go.
+    void pair(at::IntArrayRef shape, at::Tensor t[2], uint64_t* to[2]) {
+        size_t bytes = sizeof(uint64_t);
+        for (int64_t n : shape) bytes *= (size_t)n;
+        for (int p = 0; p < 2; ++p) items.push_back({c10::SmallVector<int64_t, 3>(shape.begin(), shape.end()), t + p, to + p, bytes});
+        total += 2 * ((bytes + ALIGN - 1) / ALIGN * ALIGN);
+    }
+    void make() {
+        c10::Allocator* const allocator = c10::GetAllocator(c10::DeviceType::CUDA);
+        const c10::DispatchKeySet keys(c10::DispatchKey::CUDA);
+        std::optional<c10::Storage> storage;
+        if (total <= SHARED) storage.emplace(c10::Storage::use_byte_size_t(), total, allocator->allocate(total), allocator, false);
+        size_t offset = 0;
+        for (Item& i : items) {
+            if (storage) {
+                *i.to = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(*storage), keys, like.dtype());
+                c10::TensorImpl* const impl = i.to->unsafeGetTensorImpl();
+                impl->set_storage_offset((int64_t)(offset / sizeof(uint64_t)));
+                impl->set_sizes_contiguous(i.shape);
+                offset += (i.bytes + ALIGN - 1) / ALIGN * ALIGN;
+            } else {
+                *i.to = at::detail::empty_generic(i.shape, allocator, keys, like.scalar_type(), std::nullopt);
+            }
+            *i.at = words(*i.to);
+        }
+    }
+};
 // (code, [party 0, party 1] or None, ...)
 PyObject* answer_pairs(int code, std::initializer_list<const at::Tensor*> pairs) {
     PyObject* out = PyTuple_New(1 + (Py_ssize_t)pairs.size());
@@ -468,17 +532,22 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
         int code = fits_int32({T, K, N, frac}) ? COMET_OK : COMET_ERR_SHAPE;
         g.tokens = (int32_t)T; g.inner = (int32_t)K; g.cols = (int32_t)N;
         g.frac_bits = (int32_t)frac;
-        const c10::DeviceGuard guard(x.device());
+        std::optional<c10::Stream> on;
+        if (!stream_of(args[0], x.device(), &on)) return nullptr;
+        const OnStream guard(x.device(), *on);
         if (code == COMET_OK) code = comet_linear_workspace(g.tokens, g.inner, g.cols, &g.workspace_bytes);
-        at::Tensor E[2], F[2], M[2], Y[2], workspace;
+        at::Tensor E[2], F[2], M[2], Y[2];
+        c10::DataPtr workspace;
         if (code == COMET_OK) {
-            new_pair({T, K}, x, E, g.E);
-            new_pair({N, K}, x, F, g.F);
-            if (g.quadratic) new_pair({T, N}, x, M, g.M);
-            new_pair({T, N}, x, Y, g.Y);
+            Results results(x);
+            results.pair({T, K}, E, g.E);
+            results.pair({N, K}, F, g.F);
+            if (g.quadratic) results.pair({T, N}, M, g.M);
+            results.pair({T, N}, Y, g.Y);
+            results.make();
             if (g.workspace_bytes) {
-                workspace = new_words({(g.workspace_bytes + 7) / 8}, x);
-                g.workspace = workspace.data_ptr();
+                workspace = c10::GetAllocator(c10::DeviceType::CUDA)->allocate((size_t)g.workspace_bytes);
+                g.workspace = workspace.get();
             }
             code = unlocked([&] { return comet_linear(stream, &g); });
         }
@@ -486,7 +555,7 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
-// norm_rotate(stream, X, frac_bits, norm, gain, rotation, q_heads, bad_index_flag) -> (code, M, S, D, G, Z)
+// norm_rotate(stream, X, frac_bits, norm, gain, rotation, q_heads or None, bad_index_flag or None) -> (code, M, S, D, G, Z)
 //   norm: None or (U, words, UV, steps, guess, eps); gain: None or (weight, mask, A, C); rotation: None or (cos, sin, positions,
 //   interleaved)
 PyObject* norm_rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -495,7 +564,7 @@ PyObject* norm_rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
         void* stream;
         int64_t frac, q_heads;
         Pair X, U, row_words, UV, weight, mask, A, C;
-        if (!counted(n, 8) || !as_stream(args[0], &stream) || !as_int(args[2], &frac) || !as_int(args[6], &q_heads)) return nullptr;
+        if (!counted(n, 8) || !as_stream(args[0], &stream) || !as_int(args[2], &frac)) return nullptr;
         for (int p = 0; p < 2; ++p)
             if (!(X.item[p] = PyObject_GetItem(args[1], index[p])) || !(X.t[p] = as_tensor(X.item[p])) || !ring_words(X[p])) return nullptr;
         const at::Tensor& x = X[0];
@@ -504,6 +573,8 @@ PyObject* norm_rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
             return nullptr;
         }
         const int64_t T = x.size(0), H = x.size(1), D = x.size(2);
+        q_heads = H;
+        if (args[6] != Py_None && !as_int(args[6], &q_heads)) return nullptr;
         const int64_t stride = T > 1 ? x.stride(0) : H * D;
         for (int p = 0; p < 2; ++p)
             if ((D > 1 && X[p].stride(2) != 1) || (H > 1 && X[p].stride(1) != D) || (T > 1 && X[p].stride(0) != stride)) {
@@ -572,17 +643,21 @@ PyObject* norm_rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
         g.steps = (int32_t)steps;
         g.rot_dim = (int32_t)rot;
         g.table_rows = (int32_t)rows;
-        const c10::DeviceGuard guard(x.device());
+        std::optional<c10::Stream> on;
+        if (!stream_of(args[0], x.device(), &on)) return nullptr;
+        const OnStream guard(x.device(), *on);
         at::Tensor M[2], S[2], Dm[2], G[2], Z[2];
+        Results results(x);
         if (steps) {
-            new_pair(like, x, M, g.M);
-            new_pair({T, H, sent}, x, S, g.S);
+            results.pair(like, M, g.M);
+            results.pair({T, H, sent}, S, g.S);
         }
         if (g.gain[0]) {
-            new_pair(like, x, Dm, g.D);
-            new_pair({gains, D}, x, G, g.G);
+            results.pair(like, Dm, g.D);
+            results.pair({gains, D}, G, g.G);
         }
-        new_pair(like, x, Z, g.Z);
+        results.pair(like, Z, g.Z);
+        results.make();
         const int code = unlocked([&] { return comet_norm_rotate(stream, &g); });
         return answer_pairs(code, {M, S, Dm, G, Z});
     });

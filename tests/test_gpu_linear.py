@@ -88,7 +88,54 @@ def test_shapes_match_the_oracle(cb, T, K, N):
     assert cb.static_status() == 0
 
 
-@pytest.mark.parametrize("T,K,N", [(5, 64, 36), (64, 72, 68), (90, 264, 132), (512, 1024, 1028)])
+# one to four rows, in one launch or not: blocks of one feature and of several, a second round of blocks, a ragged last one; a
+# contraction index of one pair and more, slices with and without words, one chunk and more, lanes and chunks not filled
+FEW = [(1, 8, 8192), (1, 8, 8196), (1, 40, 4), (1, 64, 4800), (1, 72, 9600), (1, 96, 148), (1, 136, 152), (1, 200, 596), (1, 392, 36),
+       (1, 768, 1188), (1, 1000, 68), (1, 1792, 20), (1, 1800, 148), (1, 3592, 12), (1, 4096, 300), (1, 4104, 8), (2, 8, 12), (2, 96, 8200),
+       (2, 192, 296), (2, 904, 44), (2, 1024, 1024), (2, 1024, 1028), (2, 1032, 8), (3, 8, 4), (3, 64, 2048), (3, 392, 180), (3, 512, 256),
+       (3, 520, 8), (4, 16, 8), (4, 200, 640), (4, 384, 340), (4, 512, 100), (4, 256, 516)]
+
+
+@pytest.mark.parametrize("T,K,N", FEW)
+def test_few_rows(cb, T, K, N):
+    case = ring_case(T * 5 + N, T, K, N, (12, 13, 16)[N % 3], bias=True, act=True, residual=True)
+    compare(cb.linear(**on_gpu(case)), layers.linear(**case))
+    bare = dict(case, bias=None, act=None, residual=None)
+    compare(cb.linear(**on_gpu(bare)), layers.linear(**bare))
+
+
+def test_few_rows_behind_one_another_and_replayed(cb):
+    """The product of each call reads what the call before wrote."""
+    f, seed = 16, 8
+    sizes = [(2, 264, 520), (2, 520, 520), (2, 520, 100)]
+    cases = [ring_case(seed + k, *s, f, True, "tame", False) for k, s in enumerate(sizes)]
+    gpu = [on_gpu(c) for c in cases]
+
+    def chain(stream):
+        x, out = gpu[0]["X"], []
+        for g in gpu:
+            out.append(cb.linear(**dict(g, X=x), stream=stream))
+            x = out[-1][3]
+        return out
+
+    graph = torch.cuda.CUDAGraph()
+    chain(None)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        captured = chain(torch.cuda.current_stream())
+    eager = chain(None)
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    for k, c in enumerate(cases):
+        ref = layers.linear(**c)
+        compare(eager[k], ref)
+        compare(captured[k], ref)
+        if k + 1 < len(cases):
+            cases[k + 1]["X"] = ref["Y"]
+
+
+@pytest.mark.parametrize("T,K,N", [(1, 264, 36), (2, 64, 36), (4, 128, 36), (5, 64, 36), (64, 72, 68), (90, 264, 132), (512, 1024, 1028)])
 @pytest.mark.parametrize("bias", [False, True])
 @pytest.mark.parametrize("act", [None, "tame", "wild"])
 @pytest.mark.parametrize("residual", [False, True])
@@ -185,7 +232,7 @@ def test_calls_on_two_streams_at_once(cb):
             compare(result, ref)
 
 
-@pytest.mark.parametrize("T,K,N", [(9, 64, 36), (90, 264, 132), (512, 1024, 1024)])
+@pytest.mark.parametrize("T,K,N", [(1, 768, 300), (9, 64, 36), (90, 264, 132), (512, 1024, 1024)])
 def test_captured_and_replayed(cb, T, K, N):
     case, other = ring_case(3, T, K, N, 13, True, "tame", True), ring_case(4, T, K, N, 13, True, "tame", True)
     g, g_other = on_gpu(case), on_gpu(other)
