@@ -432,41 +432,46 @@ bool stream_of(PyObject* o, c10::Device device, std::optional<c10::Stream>* out)
     return true;
 }
 
-// The results of a call, new contiguous tensors of ring words on the current stream.  Results of up to a megabyte together share
-// one piece of memory, which is as much as torch's allocator may keep for the smallest of them: ten tensors cost 7 us one by one.
-// Larger ones have memory of their own, so that messages can be let go of without the result.
+// What a call makes, new contiguous tensors of ring words on the current stream.  Its messages share one piece of memory and its
+// result another, up to 32 MiB each: ten tensors cost 7 us one by one.  Who keeps a result does not keep the messages with it;
+// larger ones have memory of their own.
 struct Results {
-    static constexpr size_t SHARED = 1 << 20, ALIGN = 256;
+    static constexpr size_t SHARED = 32 << 20, ALIGN = 256;
+    enum { MESSAGE, RESULT, KINDS };
     struct Item {
         c10::SmallVector<int64_t, 3> shape;
         at::Tensor* to;
         uint64_t** at;
         size_t bytes;
+        int kind;
     };
     const at::Tensor& like;
     c10::SmallVector<Item, 12> items;
-    size_t total = 0;
+    size_t total[KINDS] = {0, 0};
     explicit Results(const at::Tensor& t) : like(t) {}
+    static size_t padded(size_t bytes) { return (bytes + ALIGN - 1) / ALIGN * ALIGN; }
     // Two tensors, and where their addresses go.
-    void pair(at::IntArrayRef shape, at::Tensor t[2], uint64_t* to[2]) {
+    void pair(int kind, at::IntArrayRef shape, at::Tensor t[2], uint64_t* to[2]) {
         size_t bytes = sizeof(uint64_t);
         for (int64_t n : shape) bytes *= (size_t)n;
-        for (int p = 0; p < 2; ++p) items.push_back({c10::SmallVector<int64_t, 3>(shape.begin(), shape.end()), t + p, to + p, bytes});
-        total += 2 * ((bytes + ALIGN - 1) / ALIGN * ALIGN);
+        for (int p = 0; p < 2; ++p) items.push_back({c10::SmallVector<int64_t, 3>(shape.begin(), shape.end()), t + p, to + p, bytes, kind});
+        total[kind] += 2 * padded(bytes);
     }
     void make() {
         c10::Allocator* const allocator = c10::GetAllocator(c10::DeviceType::CUDA);
         const c10::DispatchKeySet keys(c10::DispatchKey::CUDA);
-        std::optional<c10::Storage> storage;
-        if (total <= SHARED) storage.emplace(c10::Storage::use_byte_size_t(), total, allocator->allocate(total), allocator, false);
-        size_t offset = 0;
+        std::optional<c10::Storage> storage[KINDS];
+        size_t offset[KINDS] = {0, 0};
+        for (int k = 0; k < KINDS; ++k)
+            if (total[k] && total[k] <= SHARED)
+                storage[k].emplace(c10::Storage::use_byte_size_t(), total[k], allocator->allocate(total[k]), allocator, false);
         for (Item& i : items) {
-            if (storage) {
-                *i.to = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(*storage), keys, like.dtype());
+            if (storage[i.kind]) {
+                *i.to = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(*storage[i.kind]), keys, like.dtype());
                 c10::TensorImpl* const impl = i.to->unsafeGetTensorImpl();
-                impl->set_storage_offset((int64_t)(offset / sizeof(uint64_t)));
+                impl->set_storage_offset((int64_t)(offset[i.kind] / sizeof(uint64_t)));
                 impl->set_sizes_contiguous(i.shape);
-                offset += (i.bytes + ALIGN - 1) / ALIGN * ALIGN;
+                offset[i.kind] += padded(i.bytes);
             } else {
                 *i.to = at::detail::empty_generic(i.shape, allocator, keys, like.scalar_type(), std::nullopt);
             }
@@ -540,10 +545,10 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
         c10::DataPtr workspace;
         if (code == COMET_OK) {
             Results results(x);
-            results.pair({T, K}, E, g.E);
-            results.pair({N, K}, F, g.F);
-            if (g.quadratic) results.pair({T, N}, M, g.M);
-            results.pair({T, N}, Y, g.Y);
+            results.pair(Results::MESSAGE, {T, K}, E, g.E);
+            results.pair(Results::MESSAGE, {N, K}, F, g.F);
+            if (g.quadratic) results.pair(Results::MESSAGE, {T, N}, M, g.M);
+            results.pair(Results::RESULT, {T, N}, Y, g.Y);
             results.make();
             if (g.workspace_bytes) {
                 workspace = c10::GetAllocator(c10::DeviceType::CUDA)->allocate((size_t)g.workspace_bytes);
@@ -649,14 +654,14 @@ PyObject* norm_rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
         at::Tensor M[2], S[2], Dm[2], G[2], Z[2];
         Results results(x);
         if (steps) {
-            results.pair(like, M, g.M);
-            results.pair({T, H, sent}, S, g.S);
+            results.pair(Results::MESSAGE, like, M, g.M);
+            results.pair(Results::MESSAGE, {T, H, sent}, S, g.S);
         }
         if (g.gain[0]) {
-            results.pair(like, Dm, g.D);
-            results.pair({gains, D}, G, g.G);
+            results.pair(Results::MESSAGE, like, Dm, g.D);
+            results.pair(Results::MESSAGE, {gains, D}, G, g.G);
         }
-        results.pair(like, Z, g.Z);
+        results.pair(Results::RESULT, like, Z, g.Z);
         results.make();
         const int code = unlocked([&] { return comet_norm_rotate(stream, &g); });
         return answer_pairs(code, {M, S, Dm, G, Z});
