@@ -473,11 +473,12 @@ int comet_beaver_mul(void* cuda_stream, const uint64_t* const X[2], const uint64
  * [tokens, cols], bias [cols], each pair the two parties'; DEVICE pointers on the current device, 16-byte aligned,
  * owned by the caller.  bias and residual may be null (both parties' or neither's).  k[0..2] are the coefficients as
  * ring words at scale f.  What is written (E, F, M, Y and the workspace) must not overlap any other argument.
- * The work is enqueued on `cuda_stream` (NULL = default stream) and the call does not wait for it.  Up to 32 rows, and
- * up to 64 of a layer of 786432 weights or more, the product streams the weights (COMET_KERNEL_STREAM); beyond, it goes
- * through operand planes (COMET_KERNEL_LIMB or COMET_KERNEL_RESIDUE) in `workspace`, 256-byte aligned and of at least
- * the bytes that comet_linear_workspace reports for these sizes on this device (none for the first kind).  A captured
- * call keeps its workspace's address; calls whose work may overlap in time need one each.
+ * The work is enqueued on `cuda_stream` (NULL = default stream) and the call does not wait for it.  One row, and up to
+ * four of a small layer, take one launch on the integer ALUs; up to 32 rows, and up to 64 of a layer of 786432 weights or
+ * more, the product streams the weights (COMET_KERNEL_STREAM); beyond, it goes through operand planes (COMET_KERNEL_LIMB
+ * or COMET_KERNEL_RESIDUE).  `workspace` is 256-byte aligned and has at least the bytes that comet_linear_workspace
+ * reports for these sizes on this device (none for some).  A captured call keeps its workspace's address; calls whose
+ * work may overlap in time need one each.
  * The kernels' waits are bounded: comet_static_status says whether one ran out.  The first call on a device makes
  * settings once; make it outside stream capture.
  * Errors: INVALID_ARG (null or unaligned pointer, overlap, a `quadratic` that is neither 0 nor 1), SHAPE (inner not a

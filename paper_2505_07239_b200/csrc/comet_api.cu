@@ -52,6 +52,7 @@ struct comet_ctx {
     Planes planes_right_up;       // B_0, B_1, F of the up-projection
     Planes planes_right_dn;       // B'_0, B'_1, F' of the down-projection
     Planes residues;              // of one product: what the kernel on residues hands to the recombination
+    Planes stream_parts;          // of a product without a context: the streaming kernel's sums in parts, or nothing
     int* d_error;                     // = d_count + 1
     // the weight side of the down-projection is opened on a second stream while the up-projection's
     // tensor-core kernel runs (it only needs the mask, W2 and B'_i)
@@ -353,10 +354,27 @@ int stream_features(int M, int N, int K, int sm_count) {
     return (long long)ceil_div(M, ls::BT) * ceil_div(N, ls::QROWS) * ceil_div(K, ls::KC) <= sm_count ? ls::QROWS : ls::BW;
 }
 
+// How the streaming kernel's work is cut where it leaves its sums in parts: a CTA per part.  parts = 0: not so, because equal ranges of
+// all tiles' steps would be more than half a step shorter than these parts' longest, which takes as long as the launch that is saved.
+struct StreamParts {
+    int parts, steps;
+};
+StreamParts stream_parts(int sm_count, int M, int N, int K) {
+    namespace ls = comet::limb_stream;
+    const int64_t tiles = (int64_t)ceil_div(M, ls::BT) * ceil_div(N, stream_features(M, N, K, sm_count));
+    const int kb = ceil_div(K, ls::KC);
+    if (tiles > sm_count || kb > ls::MAX_SEGMENT_STEPS) return StreamParts{0, 0};       // (a part is one segment)
+    const int steps = ceil_div(kb, std::min(kb, (int)(sm_count / tiles)));
+    const int64_t all = tiles * kb;
+    if (steps > 1 && (2 * steps - 1) * (int64_t)sm_count > 2 * all) return StreamParts{0, 0};
+    const int parts = ceil_div(kb, steps);
+    return parts <= 32 ? StreamParts{parts, steps} : StreamParts{0, 0};             // 64 of them: 15.7 and 14.0 us a layer
+}
+
 // The streaming kernel.  Without `sync` words (they belong to one stream's order, so a call without a context has none) Z <- C
 // is a launch of its own before it; the product's CTAs are set up while the copy runs.
 int launch_stream(comet::StreamArgs& args, const comet::BlockIds& held, int sm_count, cudaStream_t stream,
-                  const int* priority, cudaError_t* err) {
+                  const int* priority, cudaError_t* err, uint8_t* sums = nullptr) {
     namespace ls = comet::limb_stream;
     *err = cudaSuccess;
     args.mt = ceil_div(args.M, ls::BT);
@@ -374,6 +392,24 @@ int launch_stream(comet::StreamArgs& args, const comet::BlockIds& held, int sm_c
     args.cta_cost = steps > sm_count ? (unsigned)(cost / grid) : 0u;
     args.cta_extra = (unsigned)(cost % grid);
     comet::LimbMaps maps;
+    if (sums) {                                          // in parts, [2][parts][M][N]
+        const StreamParts cut = stream_parts(sm_count, args.M, args.N, args.K);
+        args.parts = cut.parts;
+        args.part_steps = cut.steps;
+        const cuuint64_t size[3] = {(cuuint64_t)args.N, (cuuint64_t)args.M, (cuuint64_t)cut.parts};
+        const cuuint64_t pitch[2] = {(cuuint64_t)args.N * sizeof(u64), (cuuint64_t)args.N * args.M * sizeof(u64)};
+        const cuuint32_t box[3] = {32, ls::OUT_TOKENS, 1}, step[3] = {1, 1, 1};
+        for (int p = 0; p < 2; ++p) {
+            *err = tensor_map(&maps.z[p], CU_TENSOR_MAP_DATA_TYPE_UINT64, 3, sums + p * cut.parts * pitch[1], size, pitch, box, step,
+                              CU_TENSOR_MAP_SWIZZLE_NONE);
+            if (*err != cudaSuccess) return COMET_ERR_CUDA;
+        }
+        auto* const kernel = small ? (args.M <= 16 ? comet::combine_stream_kernel<16, ls::QROWS, true> : comet::combine_stream_kernel<32, ls::QROWS, true>)
+                                   : (args.M <= 16 ? comet::combine_stream_kernel<16, ls::BW, true> : comet::combine_stream_kernel<32, ls::BW, true>);
+        *err = launch_chained(kernel, dim3((unsigned)(args.mt * args.nt * cut.parts)), dim3(ls::THREADS), ls::SMEM_BYTES, stream, priority,
+                              args, maps, held);
+        return *err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
+    }
     for (int p = 0; p < 2; ++p) {
         *err = result_map(&maps.z[p], args.Z[p], args.M, args.N, ls::OUT_TOKENS, 32, CU_TENSOR_MAP_SWIZZLE_NONE);
         if (*err != cudaSuccess) return COMET_ERR_CUDA;
@@ -427,7 +463,7 @@ int stream_product(comet_ctx* c, const Proj& pr) {
     cudaError_t err;
     {
         PhaseTimer timer(c, COMET_PHASE_COMBINE, 1);
-        const int rc = launch_stream(a, c->held, c->sm_count, c->stream, &c->top_priority, &err);
+        const int rc = launch_stream(a, c->held, c->sm_count, c->stream, &c->top_priority, &err, c->stream_parts.at);
         if (rc == COMET_ERR_CUDA) c->last_cuda_error = (int)err;
         if (rc != COMET_OK) return rc;
     }
@@ -474,6 +510,9 @@ cudaError_t tensor_kernel_attributes() {
     };
     for (auto* kernel : {comet::combine_stream_kernel<16, comet::limb_stream::BW>, comet::combine_stream_kernel<32, comet::limb_stream::BW>,
                          comet::combine_stream_kernel<16, comet::limb_stream::QROWS>, comet::combine_stream_kernel<32, comet::limb_stream::QROWS>})
+        room(kernel, comet::limb_stream::SMEM_BYTES);
+    for (auto* kernel : {comet::combine_stream_kernel<16, comet::limb_stream::BW, true>, comet::combine_stream_kernel<32, comet::limb_stream::BW, true>,
+                         comet::combine_stream_kernel<16, comet::limb_stream::QROWS, true>, comet::combine_stream_kernel<32, comet::limb_stream::QROWS, true>})
         room(kernel, comet::limb_stream::SMEM_BYTES);
     room(comet::combine_limb_kernel, comet::limb::SMEM_BYTES);
     carve(comet::combine_limb_kernel);
@@ -2045,6 +2084,19 @@ bool linear_streams(int64_t T, int64_t K, int64_t N) {
     return T <= comet::limb_stream::BT || (T <= STREAM_TOKENS && 2 * K * N >= STREAM_WORDS);
 }
 
+// Whether a layer of a few rows goes through linear_rows_kernel.  A token's multiply-adds on the ALUs cost it time beside the loads from
+// the second row on, and every chunk of the contraction index a staging of the rows; what it saves is two launches and the streaming
+// kernel's latency.  This kernel and the streaming kernel with its two passes, us: one row, 64 x 64 5.5 and 9.2, 768 x 768 11.3 and 14.7,
+// 1000 x 1364 16.4 and 23.2, 2048 x 2048 41.0 and 41.6, 4096 x 4096 140.6 and 139.3, 4096 x 11008 359 and 356; two rows, 512 x 512 8.5
+// and 12.6, 1024 x 768 18.1 and 18.8, 1536 x 768 20.8 and 19.5, 2048 x 128 14.0 and 12.6; four rows, 256 x 96 6.8 and 10.2, 512 x 256 10.6
+// either way, 512 x 512 12.6 either way, 768 x 512 15.4 and 13.3.  Nothing is gained on deeper layers (one row, 11008 x 4096 365 and
+// 354, 11008 x 64 30 and 17), nor where a feature does not fill a warp and there are many (24 x 50000 48 and 24).
+bool linear_in_rows(int64_t T, int64_t K, int64_t N) {
+    if (K < 64 && N > 8192) return false;
+    if (T <= 2) return T == 1 ? K <= 4096 : K <= 1024 && K * N <= 1 << 20;
+    return T <= comet::rows::MAX_ROWS && K <= 512 && K * N <= 1 << 17;
+}
+
 // A context of one product: what the launching functions of the path read of one, its planes in the caller's workspace.  Returns
 // the bytes of that.
 constexpr size_t LINEAR_ALIGN = 256;
@@ -2057,9 +2109,12 @@ size_t linear_context(comet_ctx* c, int sm_count, int T, int K, int N, uint8_t* 
     c->cfg.block = N;                    // one active block of all features: a gather that moves nothing
     c->n_active = N;
     c->ids_held = true;
+    if (linear_in_rows(T, K, N)) return 0;
     if (linear_streams(T, K, N)) {
-        c->stream_sync_words = ~(size_t)0;         // (none: Z <- C is a launch of its own)
-        return 0;
+        c->stream_sync_words = ~(size_t)0;         // (none: Z <- C is a launch of its own, or is not needed)
+        c->stream_parts.bytes = (size_t)2 * stream_parts(sm_count, T, N, K).parts * T * N * sizeof(u64);
+        c->stream_parts.at = c->stream_parts.bytes ? workspace : nullptr;
+        return c->stream_parts.bytes;
     }
     const bool residue = K <= comet::residue::MAX_DEPTH && residues_pay(sm_count, T, N, K);
     size_t at = 0;
@@ -2077,19 +2132,6 @@ size_t linear_context(comet_ctx* c, int sm_count, int T, int K, int N, uint8_t* 
         c->residues.at = take(c->residues.bytes);
     }
     return at;
-}
-
-// Whether a layer of a few rows goes through linear_rows_kernel.  A token's multiply-adds on the ALUs cost it time beside the loads from
-// the second row on, and every chunk of the contraction index a staging of the rows; what it saves is two launches and the streaming
-// kernel's latency.  This kernel and the streaming kernel with its two passes, us: one row, 64 x 64 5.5 and 9.2, 768 x 768 11.3 and 14.7,
-// 1000 x 1364 16.4 and 23.2, 2048 x 2048 41.0 and 41.6, 4096 x 4096 140.6 and 139.3, 4096 x 11008 359 and 356; two rows, 512 x 512 8.5
-// and 12.6, 1024 x 768 18.1 and 18.8, 1536 x 768 20.8 and 19.5, 2048 x 128 14.0 and 12.6; four rows, 256 x 96 6.8 and 10.2, 512 x 256 10.6
-// either way, 512 x 512 12.6 either way, 768 x 512 15.4 and 13.3.  Nothing is gained on deeper layers (one row, 11008 x 4096 365 and
-// 354, 11008 x 64 30 and 17), nor where a feature does not fill a warp and there are many (24 x 50000 48 and 24).
-bool linear_in_rows(int64_t T, int64_t K, int64_t N) {
-    if (K < 64 && N > 8192) return false;
-    if (T <= 2) return T == 1 ? K <= 4096 : K <= 1024 && K * N <= 1 << 20;
-    return T <= comet::rows::MAX_ROWS && K <= 512 && K * N <= 1 << 17;
 }
 
 // One to four rows: a launch for the whole layer.
@@ -2244,7 +2286,13 @@ extern "C" int comet_linear(void* cuda_stream, const comet_linear_args* g) {
     last.row_pairs = N / 2;
     const int grid = ew_grid(c, last.pairs, 256);
     last.stride_pairs = (int)((long long)grid * 256 % last.row_pairs);
-    return launch_pass(comet::linear_epilogue_kernel, dim3(grid), c->stream, last);
+    if (!c->stream_parts.at) return launch_pass(comet::linear_epilogue_kernel, dim3(grid), c->stream, last);
+    last.parts = stream_parts(c->sm_count, T, N, K).parts;
+    for (int p = 0; p < 2; ++p) {
+        last.C[p] = reinterpret_cast<const u64*>(g->C[p]);
+        last.sums[p] = reinterpret_cast<const u64*>(c->stream_parts.at) + p * last.parts * (int64_t)T * N;
+    }
+    return launch_pass(comet::linear_parts_kernel, dim3(ew_grid(c, last.pairs * comet::LINEAR_SHARERS, 256)), c->stream, last);
 }
 
 // ---------------------------------------------------------------------------

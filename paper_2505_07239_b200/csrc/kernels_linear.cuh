@@ -32,10 +32,50 @@ __device__ __forceinline__ u64 linear_square(u64 y, u64 r, u64 q, u64 m, const L
     return linear_trunc(e.k2 * s + e.k1 * y, party, e.f) + (party ? e.k0 : 0ull);
 }
 
-// The pass behind the products whose sums are added into Z: a thread has two words of both parties.
+// What follows the product for two neighbouring words of both parties, z at pair t of the matrix and pair col of its row.
+__device__ __forceinline__ void linear_finish_pair(const LinearEnd& e, ulonglong2 y[2], long long t, int col, u64* const Z[2]) {
+    ulonglong2 r[2], q[2], res[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        if (e.R[0]) {
+            r[p] = __ldcs(reinterpret_cast<const ulonglong2*>(e.R[p]) + t);
+            q[p] = __ldcs(reinterpret_cast<const ulonglong2*>(e.Q[p]) + t);
+        }
+        res[p] = e.residual[0] ? __ldcs(reinterpret_cast<const ulonglong2*>(e.residual[p]) + t) : make_ulonglong2(0ull, 0ull);
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        if (e.bias[0]) {
+            const ulonglong2 b = __ldg(reinterpret_cast<const ulonglong2*>(e.bias[p]) + col);
+            y[p].x += b.x << e.f;
+            y[p].y += b.y << e.f;
+        }
+        y[p].x = linear_trunc(y[p].x, p, e.f);
+        y[p].y = linear_trunc(y[p].y, p, e.f);
+    }
+    if (e.R[0]) {
+        ulonglong2 m = make_ulonglong2(0ull, 0ull);
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const ulonglong2 mine = make_ulonglong2(y[p].x - r[p].x, y[p].y - r[p].y);
+            __stcs(reinterpret_cast<ulonglong2*>(e.M[p]) + t, mine);
+            m.x += mine.x;                                   // the exchange
+            m.y += mine.y;
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            y[p] = make_ulonglong2(linear_square(y[p].x, r[p].x, q[p].x, m.x, e, p), linear_square(y[p].y, r[p].y, q[p].y, m.y, e, p));
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p) reinterpret_cast<ulonglong2*>(Z[p])[t] = make_ulonglong2(y[p].x + res[p].x, y[p].y + res[p].y);
+}
+
+// The pass behind the products whose sums are added into Z: in place.
 struct LinearEpilogueArgs {
     LinearEnd end;
-    u64* Z[2];                   // in place
+    u64* Z[2];
+    const u64* C[2]; const u64* sums[2];     // linear_parts_kernel: [parts][rows][cols]
+    int parts;
     long long pairs;             // of the whole matrix
     int row_pairs, stride_pairs; // pairs of a row; (gridDim.x * blockDim.x) % row_pairs
 };
@@ -43,49 +83,54 @@ __global__ void __launch_bounds__(256)
 linear_epilogue_kernel(const __grid_constant__ LinearEpilogueArgs a) {
     pdl_wait();
     pdl_launch_dependents();
-    const LinearEnd& e = a.end;
     const long long stride = (long long)gridDim.x * blockDim.x;
     long long t = (long long)blockIdx.x * blockDim.x + threadIdx.x;
     int col = (int)(t % a.row_pairs);
     for (; t < a.pairs; t += stride) {
-        ulonglong2 y[2], r[2], q[2], res[2];
+        ulonglong2 y[2];
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            y[p] = reinterpret_cast<const ulonglong2*>(a.Z[p])[t];
-            if (e.R[0]) {
-                r[p] = __ldcs(reinterpret_cast<const ulonglong2*>(e.R[p]) + t);
-                q[p] = __ldcs(reinterpret_cast<const ulonglong2*>(e.Q[p]) + t);
-            }
-            res[p] = e.residual[0] ? __ldcs(reinterpret_cast<const ulonglong2*>(e.residual[p]) + t) : make_ulonglong2(0ull, 0ull);
-        }
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            if (e.bias[0]) {
-                const ulonglong2 b = __ldg(reinterpret_cast<const ulonglong2*>(e.bias[p]) + col);
-                y[p].x += b.x << e.f;
-                y[p].y += b.y << e.f;
-            }
-            y[p].x = linear_trunc(y[p].x, p, e.f);
-            y[p].y = linear_trunc(y[p].y, p, e.f);
-        }
-        if (e.R[0]) {
-            ulonglong2 m = make_ulonglong2(0ull, 0ull);
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                const ulonglong2 mine = make_ulonglong2(y[p].x - r[p].x, y[p].y - r[p].y);
-                __stcs(reinterpret_cast<ulonglong2*>(e.M[p]) + t, mine);
-                m.x += mine.x;                               // the exchange
-                m.y += mine.y;
-            }
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-                y[p] = make_ulonglong2(linear_square(y[p].x, r[p].x, q[p].x, m.x, e, p), linear_square(y[p].y, r[p].y, q[p].y, m.y, e, p));
-        }
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-            reinterpret_cast<ulonglong2*>(a.Z[p])[t] = make_ulonglong2(y[p].x + res[p].x, y[p].y + res[p].y);
+        for (int p = 0; p < 2; ++p) y[p] = reinterpret_cast<const ulonglong2*>(a.Z[p])[t];
+        linear_finish_pair(a.end, y, t, col, a.Z);
         col += a.stride_pairs;
         if (col >= a.row_pairs) col -= a.row_pairs;
+    }
+}
+
+// The pass behind a product whose sums lie in parts: a pair's parts are dealt to LINEAR_SHARERS lanes, because there are few pairs.  (A
+// thread a pair: 20 tokens, 768 x 768, 24 parts, 21.5 us a layer.)
+constexpr int LINEAR_SHARERS = 8;
+__global__ void __launch_bounds__(256)
+linear_parts_kernel(const __grid_constant__ LinearEpilogueArgs a) {
+    pdl_wait();
+    pdl_launch_dependents();
+    constexpr int PAIRS = 32 / LINEAR_SHARERS;               // of a warp
+    const int lane = threadIdx.x & 31, share = lane / PAIRS;
+    const long long warps = (long long)gridDim.x * (blockDim.x / 32), all = (a.pairs + PAIRS - 1) / PAIRS;
+    for (long long w = (long long)blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5); w < all; w += warps) {
+        const long long t = w * PAIRS + lane % PAIRS;
+        const bool live = t < a.pairs;
+        ulonglong2 y[2] = {make_ulonglong2(0ull, 0ull), make_ulonglong2(0ull, 0ull)};
+        if (live) {
+            if (share == 0)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) y[p] = __ldcs(reinterpret_cast<const ulonglong2*>(a.C[p]) + t);
+#pragma unroll 4
+            for (int k = share; k < a.parts; k += LINEAR_SHARERS)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const ulonglong2 v = __ldcs(reinterpret_cast<const ulonglong2*>(a.sums[p]) + k * a.pairs + t);
+                    y[p].x += v.x;
+                    y[p].y += v.y;
+                }
+        }
+#pragma unroll
+        for (int o = PAIRS; o < 32; o *= 2)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                y[p].x += __shfl_xor_sync(0xffffffffu, y[p].x, o);
+                y[p].y += __shfl_xor_sync(0xffffffffu, y[p].y, o);
+            }
+        if (live && share == 0) linear_finish_pair(a.end, y, t, (int)(t % a.row_pairs), a.Z);
     }
 }
 

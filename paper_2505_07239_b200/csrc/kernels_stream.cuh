@@ -100,6 +100,7 @@ struct StreamArgs {
     int last_cost;           // of a step of the last, possibly ragged, feature tile
     unsigned own_cost;       // of Z <- C for a tile, before its first step
     unsigned cta_cost, cta_extra;   // total cost = gridDim.x * cta_cost + cta_extra, cta_extra < gridDim.x; 0: a step per CTA
+    int parts, part_steps;   // with PARTS instead of the four: CTAs per tile, steps of each but the last
     const uint8_t* tmask;    // per-token mask [M, tmask_ld] over the active blocks of the contraction index, or null:
     int tmask_ld;            // where it is zero, neither X nor A_i has an entry
     const int32_t* row_label;   // component label per token (negative: the row is not opened), or null
@@ -202,7 +203,13 @@ __device__ __forceinline__ bool stream_tile_ready(const uint32_t* flag, uint32_t
 // before the wait for the kernel before this one, Z <- C goes through registers, and three warps a party drain.  From that wait
 // to the end, 16 tokens x 256 deep x 96: 7.8 -> 6.5 us.  A layer of 256 x 96, 32 tokens: 29.9 -> 21.9 us; 16 tokens: 22.3 to 22.9 -> 19.6 to
 // 21.9, which is what the host's calls take; of 448 x 320, 32 tokens: 31.2 -> 28.8.
-template <int COLS, int FEATURES>
+// PARTS: every tile is cut into parts of its own, and a part's sums are stored, [part][M][N] a party, for the pass behind the product to
+// add up: nothing has to be in Z before, so a call without `sync` words is a launch shorter.  (a.Z and a.C are not used.)
+__device__ __forceinline__ void stream_store_part(const CUtensorMap* map, uint32_t src, int x, int y, int part) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(part) : "memory");
+}
+template <int COLS, int FEATURES, bool PARTS = false>
 __global__ void __launch_bounds__(limb_stream::THREADS, 1)
 combine_stream_kernel(const __grid_constant__ StreamArgs a, const __grid_constant__ LimbMaps maps,
                       const __grid_constant__ BlockIds held) {
@@ -256,7 +263,9 @@ combine_stream_kernel(const __grid_constant__ StreamArgs a, const __grid_constan
     // A ticket beyond the launch means that the words are not what the launches before it left: nothing is touched then.
     const bool valid = ticket < gridDim.x;
     if (!valid && threadIdx.x == 0) abort_flag = 1;
-    const unsigned cta = valid ? ticket : 0u, u_begin = stream_cut(a, cta), u_end = valid ? stream_cut(a, cta + 1) : u_begin;
+    const unsigned cta = valid ? ticket : 0u, part = PARTS ? cta % (unsigned)a.parts : 0u;
+    const unsigned u_begin = PARTS ? cta / (unsigned)a.parts * a.kb + part * a.part_steps : stream_cut(a, cta);
+    const unsigned u_end = !valid ? u_begin : PARTS ? u_begin + min(a.part_steps, a.kb - (int)part * a.part_steps) : stream_cut(a, cta + 1);
     constexpr bool SMALL = FEATURES < BW;
     const bool raw_warp = warp >= RAW_WARP0 && warp < RAW_WARP0 + 2;
     // the list of blocks may be the work of the kernel before this one
@@ -284,7 +293,8 @@ combine_stream_kernel(const __grid_constant__ StreamArgs a, const __grid_constan
         ptx::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0 && col0 < a.N) {
-            ptx::tensor_reduce_add(&maps.z[party], ptx::smem_u32(stage), col0, row0 + t0);
+            if (PARTS) stream_store_part(&maps.z[party], ptx::smem_u32(stage), col0, row0 + t0, (int)part);
+            else ptx::tensor_reduce_add(&maps.z[party], ptx::smem_u32(stage), col0, row0 + t0);
             ptx::bulk_commit_group();
         }
     };

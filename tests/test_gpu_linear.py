@@ -325,7 +325,7 @@ def test_refusals_on_a_device(cb):
     a.workspace_bytes = need
     assert lib.comet_linear(None, ctypes.byref(a)) == 0
     torch.cuda.synchronize()
-    assert cb.linear_workspace(32, K, N) == 0 and cb.static_status() == 0
+    assert cb.linear_workspace(1, K, N) == 0 and cb.static_status() == 0
 
 
 def test_a_wait_that_ran_out_is_reported(cb):
