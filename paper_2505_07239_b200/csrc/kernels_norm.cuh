@@ -13,9 +13,19 @@
 // One pass: a thread has both parties' words of its elements, which is the exchange, and a row's words stay in registers from
 // the first load to the last store.
 //
-// What bounds it: memory.  With gain 8 words per element and party, five in (x, U, U v, and the gain's A and C), three out
-// (two messages and the result), 128 bytes an element.  The root is a chain of 3 (steps - 1) dependent products between a row's
-// first loads and its last stores, so what is needed behind it is asked for before it begins.
+// What bounds it: memory, and the time that a row's registers and shared memory are held.  With gain 8 words per element and party,
+// five in (x, U, U v, and the gain's A and C), three out (two messages and the result), 128 bytes an element; beaver_mul_kernel moves
+// the same mix at 0.95 of the copy rate.  The root is a chain of 3 (steps - 1) dependent products between a row's first loads and
+// its last stores, 0.17 us a step, so what is needed behind it is asked for before it begins: UV, A and C wait in shared
+// memory, x's opening and U in registers.
+// Measured, ten steps, gain and rotation: 512 tokens x 64 heads x 128 109 us, 582 MB, 5.3 TB/s, 0.82 of the copy rate (two steps: 94 us,
+// 0.88); 32 tokens 12.6 us, one token 7.5 us, of which the chain 1.6; rows of 4096 words without rotation, 203 of them, 27 us, 0.60 (two
+// waves of clusters, and the second is not full).
+// What it took, 512 tokens x 64 heads: every warp with its row's chain to itself 135 us (2050 instructions a row, 1400 now), one warp for
+// all rows of a CTA 115, a row's own words asked for before the elements 109.  CTAs of four rows: of two or eight 115.  Five CTAs an SM at
+// 96 registers: four at 128 125, six at 80 (16 bytes spilled) 111; with 100 bytes spilled 129.  Left out in scratch builds: the chain
+// 103, the row's own words 105, the predicates of ragged rows 107.  No difference: another warp of the CTA for the chain, CTAs of the
+// first wave begun 1.5 us apart.
 #pragma once
 #include <cstdint>
 #include <cuda_runtime.h>

@@ -9,6 +9,9 @@
 // residual follow in the same launch.  The streaming kernel (kernels_stream.cuh) takes three launches for the same, and 9 us from its
 // first load to its last sum however small the layer.
 //
+// Measured: one row, 4096 x 4096 139 us, 0.88 of the copy rate; 768 x 768 11.3 us, of which 2.5 are the launch, 4.3 the bytes.  From the
+// second row on the multiply-adds show (4096 x 4096: 145 us, four rows 197): comet_api.cu has the rule, with both sides' times.
+//
 // A CTA (one per SM) takes blocks of features.  Its warps split the contraction index in `slices` parts (8, fewer where the rows are
 // short) and the features in 16 / slices.  A lane copies 16 bytes of W_0, W_1, B_0 and B_1 at a time to its own places in shared
 // memory, five such steps ahead, 160 KiB under way per SM, across chunks and blocks.  (Three steps ahead in registers, two CTAs of

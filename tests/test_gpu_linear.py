@@ -288,6 +288,25 @@ def test_agrees_with_the_calls_that_it_replaces(cb):
         ctx.close()
 
 
+@pytest.mark.parametrize("T", [1, 8])
+def test_words_beyond_32_bits(cb, T):
+    """More than 2^31 weights.  Both parties' shares and masks of W are the same words of one buffer, 16 words apart."""
+    K, N = 4096, 528000
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GB of device memory")
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    draw = lambda *s: torch.randint(-2**63, 2**63 - 1, s, generator=gen, device="cuda", dtype=torch.int64)
+    room = draw(N * K + 48)
+    W0, W1, B0, B1 = (room[k:k + N * K].view(N, K) for k in (0, 16, 32, 48))
+    X, A, C = ([draw(T, K), draw(T, K)], [draw(T, K), draw(T, K)], [draw(T, N), draw(T, N)])
+    E, F, M, Y = cb.linear(X, A, [W0, W1], [B0, B1], C, 16)
+    cols = [0, 1, 127, N // 2, (1 << 31) // K - 1, (1 << 31) // K, (1 << 31) // K + 1, N - 2, N - 1]
+    ref = layers.linear([host(v) for v in X], [host(v) for v in A], cut([W0, W1], 0, cols), cut([B0, B1], 0, cols), cut(C, 1, cols), 16)
+    for i in (0, 1):
+        assert np.array_equal(cut(Y, 1, cols)[i], ref["Y"][i])
+        assert np.array_equal(cut(F, 0, cols)[i], ref["F"][i])
+
+
 def test_refusals_on_a_device(cb):
     lib = cb.library()
     t = lambda *s: [torch.zeros(s, dtype=torch.int64, device="cuda") for _ in (0, 1)]

@@ -157,6 +157,22 @@ def test_memory_around_the_results_stays(cb):
                 assert np.array_equal(got[32:-32].reshape(ref[name][i].shape), ref[name][i]), name
 
 
+def test_tokens_far_apart(cb):
+    """Tokens more than 2^31 words apart in X."""
+    T, H, D, far = 3, 2, 64, (1 << 30) + 6                # 2 far words: the last token
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB of device memory")
+    case, _, _ = norm_case(4, T, H, D, 16, 3, D, q_heads=1)
+    g = on_gpu(case, cb)
+    room = torch.zeros(2 * far + 4 * H * D, dtype=torch.int64, device="cuda")
+    g["X"] = [torch.as_strided(room, (T, H, D), (far, D, 1), i * 2 * H * D) for i in (0, 1)]
+    for i in (0, 1):
+        g["X"][i].copy_(dev(case["X"][i]))
+    compare(cb.norm_rotate(**g), layers.norm_rotate(**case))
+    bare = dict(g, norm=None, gain=None)
+    compare(cb.norm_rotate(**bare), layers.norm_rotate(**dict(case, norm=None, gain=None)))
+
+
 def test_streams_and_replays(cb):
     cases = [norm_case(40 + k, *s)[0] for k, s in enumerate(((5, 4, 64, 16, 6, 64), (3, 1, 2048, 16, 6, 0), (70, 6, 128, 13, 5, 128)))]
     gpu = [on_gpu(c, cb) for c in cases]
