@@ -526,21 +526,19 @@ cudaError_t tensor_kernel_attributes() {
     return err;
 }
 
-// The same for the kernels of comet_norm_rotate: room for the longest row words, three CTAs an SM with those of ten steps.
+// The same for the kernels of comet_norm_rotate: room for the longest row words.
 cudaError_t norm_kernel_attributes() {
     namespace nm = comet::norm;
     cudaError_t err = cudaSuccess;
-    auto room = [&](auto* kernel, int rows) {
-        if (err == cudaSuccess)
-            err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       nm::PLACE_BYTES * nm::CLUSTER_THREADS + rows * nm::row_bytes(nm::MAX_STEPS));
+    auto room = [&](auto* kernel, int bytes) {
+        if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (err == cudaSuccess)
             err = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, (int)cudaSharedmemCarveoutMaxShared);
     };
-    for (auto* kernel : {comet::norm_group_kernel<8, true>, comet::norm_group_kernel<8, false>}) room(kernel, nm::GROUP_THREADS / 8);
-    for (auto* kernel : {comet::norm_group_kernel<16, true>, comet::norm_group_kernel<16, false>}) room(kernel, nm::GROUP_THREADS / 16);
-    for (auto* kernel : {comet::norm_group_kernel<32, true>, comet::norm_group_kernel<32, false>}) room(kernel, nm::GROUP_THREADS / 32);
-    for (auto* kernel : {comet::norm_cluster_kernel<true>, comet::norm_cluster_kernel<false>}) room(kernel, 1);
+    for (auto* kernel : {comet::norm_tile_kernel<true>, comet::norm_tile_kernel<false>})
+        room(kernel, nm::PLACE_BYTES * nm::TILE_THREADS + nm::TILE_ROWS * nm::row_bytes(nm::MAX_STEPS) + 2 * nm::TILE_DIM * (int)sizeof(u64));
+    for (auto* kernel : {comet::norm_cluster_kernel<true>, comet::norm_cluster_kernel<false>})
+        room(kernel, nm::PLACE_BYTES * nm::CLUSTER_THREADS + nm::row_bytes(nm::MAX_STEPS));
     return err;
 }
 
@@ -2300,29 +2298,23 @@ extern "C" int comet_linear(void* cuda_stream, const comet_linear_args* g) {
 // ---------------------------------------------------------------------------
 namespace {
 
-// A thread takes four words of a row.  Up to 128 words: a warp for a row, or for two or four; beyond: a cluster of CTAs of at
-// most 256 threads.
-void (*norm_kernel(int dim, bool vec))(comet::NormArgs) {
-    const int quads = ceil_div(dim, 4);
-    if (dim > comet::norm::GROUP_DIM) return vec ? comet::norm_cluster_kernel<true> : comet::norm_cluster_kernel<false>;
-    if (quads <= 8) return vec ? comet::norm_group_kernel<8, true> : comet::norm_group_kernel<8, false>;
-    if (quads <= 16) return vec ? comet::norm_group_kernel<16, true> : comet::norm_group_kernel<16, false>;
-    return vec ? comet::norm_group_kernel<32, true> : comet::norm_group_kernel<32, false>;
-}
-
-int launch_norm(const comet::NormArgs& a, bool vec, cudaStream_t stream) {
+// A thread takes four words of a row.  Up to 512 words: tiles of whole rows; beyond: a cluster of CTAs of at most 256 threads per row.
+int launch_norm(comet::NormArgs& a, bool aligned, cudaStream_t stream) {
     namespace nm = comet::norm;
-    const int quads = ceil_div(a.dim, 4);
-    const size_t row_bytes = nm::row_bytes(a.steps);
+    const int quads = ceil_div(a.dim, 4), row_bytes = nm::row_bytes(a.steps);
+    const bool tiled = a.dim <= nm::TILE_DIM;
+    // in a tile a pair that is apart is one thread's only if it is half a row of a multiple of four words apart
+    a.exchange = tiled && a.half && !a.interleaved && a.half != 2 * quads;
+    const bool vec = aligned && (tiled ? a.exchange || a.interleaved || a.half % 2 == 0 : a.half % 2 == 0);
     int cluster = 1;
-    while (ceil_div(quads, cluster) > nm::CLUSTER_THREADS) cluster *= 2;
+    while (!tiled && ceil_div(quads, cluster) > nm::CLUSTER_THREADS) cluster *= 2;
     cudaLaunchConfig_t lc;
     std::memset(&lc, 0, sizeof(lc));
-    if (a.dim <= nm::GROUP_DIM) {
-        const int rows = nm::GROUP_THREADS / (quads <= 8 ? 8 : quads <= 16 ? 16 : 32);
+    if (tiled) {
+        const int rows = nm::tile_rows(quads);
         lc.gridDim = dim3(ceil_div(a.rows, rows));
-        lc.blockDim = dim3(nm::GROUP_THREADS);
-        lc.dynamicSmemBytes = nm::PLACE_BYTES * nm::GROUP_THREADS + rows * row_bytes;
+        lc.blockDim = dim3(ceil_div(rows * quads, 32) * 32);
+        lc.dynamicSmemBytes = nm::PLACE_BYTES * lc.blockDim.x + rows * (row_bytes + (a.exchange ? 2 * a.dim * (int)sizeof(u64) : 0));
     } else {
         lc.gridDim = dim3((unsigned)a.rows * cluster);
         lc.blockDim = dim3(ceil_div(ceil_div(quads, cluster), 32) * 32);
@@ -2337,7 +2329,9 @@ int launch_norm(const comet::NormArgs& a, bool vec, cudaStream_t stream) {
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     lc.attrs = attr;
     lc.numAttrs = cluster > 1 ? 2 : 1;
-    const cudaError_t err = cudaLaunchKernelEx(&lc, norm_kernel(a.dim, vec), a);
+    auto* const kernel = tiled ? (vec ? comet::norm_tile_kernel<true> : comet::norm_tile_kernel<false>)
+                               : (vec ? comet::norm_cluster_kernel<true> : comet::norm_cluster_kernel<false>);
+    const cudaError_t err = cudaLaunchKernelEx(&lc, kernel, a);
     if (err != cudaSuccess) cudaGetLastError();
     return err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
 }
@@ -2367,7 +2361,7 @@ extern "C" int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args
     if (turned && (g->rot_dim < 0 || g->rot_dim % 2 || g->rot_dim > g->dim || g->table_rows < 1)) return COMET_ERR_SHAPE;
     if (normed && (g->steps < 2 || g->steps > nm::MAX_STEPS)) return COMET_ERR_SHAPE;
     if (normed && (g->guess < 1 || g->guess >> 32)) return COMET_ERR_SHAPE;
-    bool vec = g->rot_dim % 4 == 0 && (g->x_stride % 2 == 0 || g->tokens == 1);
+    bool aligned = g->x_stride % 2 == 0 || g->tokens == 1;
     {
         const int64_t x_words = (int64_t)(g->tokens - 1) * g->x_stride + row;
         const int64_t gains = g->q_heads > 0 && g->q_heads < g->heads ? 2 : 1;
@@ -2391,7 +2385,7 @@ extern "C" int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args
         for (int k = 0; k < count; ++k) {
             const bool narrow = k == 10 || k == count - 1, alone = k == 8 || k == 9 || k == count - 3 || k == count - 2;
             if (span[k].begin % (narrow ? sizeof(int32_t) : sizeof(u64))) return COMET_ERR_INVALID_ARG;
-            if (!narrow && !alone) vec = vec && span[k].begin % 16 == 0;       // (a row's own words are read one by one)
+            if (!narrow && !alone) aligned = aligned && span[k].begin % 16 == 0;       // (a row's own words are read one by one)
         }
     }
     comet::NormArgs a;
@@ -2443,10 +2437,10 @@ extern "C" int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args
             cudaGetLastError();
             return COMET_ERR_CUDA;
         }
-        return launch_norm(a, vec, stream);
+        return launch_norm(a, aligned, stream);
     }
     const unsigned quads = (unsigned)ceil_div(a.dim, 4);
-    return launch_pass(vec ? comet::rotate_kernel<true> : comet::rotate_kernel<false>, dim3(shuffle_grid(rows * quads)), stream, a, quads);
+    return launch_pass(aligned && a.half % 2 == 0 ? comet::rotate_kernel<true> : comet::rotate_kernel<false>, dim3(shuffle_grid(rows * quads)), stream, a, quads);
 }
 
 // ---------------------------------------------------------------------------

@@ -18,14 +18,16 @@
 // the same mix at 0.95 of the copy rate.  The root is a chain of 3 (steps - 1) dependent products between a row's first loads and
 // its last stores, 0.17 us a step, so what is needed behind it is asked for before it begins: UV, A and C wait in shared
 // memory, x's opening and U in registers.
-// Measured, ten steps, gain and rotation: 512 tokens x 64 heads x 128 109 us, 582 MB, 5.3 TB/s, 0.82 of the copy rate (two steps: 94 us,
-// 0.88); 32 tokens 12.6 us, one token 7.5 us, of which the chain 1.6; rows of 4096 words without rotation, 203 of them, 27 us, 0.60 (two
-// waves of clusters, and the second is not full).
+// Measured, ten steps, gain and rotation: 512 tokens x 64 heads x 128 108 us, 582 MB, 5.4 TB/s, 0.82 of the copy rate (two steps: 94 us,
+// 0.88), x 64 66 us (0.73), x 256 200 us (0.86); 32 tokens x 64 heads x 128 13 us, one token 7.5 us, of which the chain 1.6; rows of 4096
+// words without rotation, 203 of them, 27 us, 0.60 (two waves of clusters, and the second is not full).
 // What it took, 512 tokens x 64 heads: every warp with its row's chain to itself 135 us (2050 instructions a row, 1400 now), one warp for
 // all rows of a CTA 115, a row's own words asked for before the elements 109.  CTAs of four rows: of two or eight 115.  Five CTAs an SM at
 // 96 registers: four at 128 125, six at 80 (16 bytes spilled) 111; with 100 bytes spilled 129.  Left out in scratch builds: the chain
 // 103, the row's own words 105, the predicates of ragged rows 107.  No difference: another warp of the CTA for the chain, CTAs of the
-// first wave begun 1.5 us apart.
+// first wave begun 1.5 us apart.  Threads dealt to a tile's words whatever the rows' length, instead of whole lanes or warps to a row:
+// x 160 189 -> 138 us, x 254, all rotated, 312 -> 229, x 126 147 -> 121 (the latter two in accesses of 16 bytes, too, their pairs
+// through shared memory).
 #pragma once
 #include <cstdint>
 #include <cuda_runtime.h>
@@ -38,13 +40,16 @@ typedef unsigned long long u64;
 
 namespace norm {
 constexpr int MAX_STEPS = 24, MAX_DIM = 8192;
-constexpr int GROUP_THREADS = 128;                   // of a CTA that has several rows
+constexpr int TILE_THREADS = 128;                    // at most, of a CTA that has whole rows of up to TILE_DIM words
+constexpr int TILE_DIM = 4 * TILE_THREADS, TILE_ROWS = 16;
 constexpr int CLUSTER_THREADS = 256;                 // at most, of a CTA of a cluster that has one
 constexpr int GROUP_DIM = 128;                       // longest row of one warp: four words a lane
 constexpr int PLACE_BYTES = 6 * 2 * 16;              // of shared memory that a thread's four words of UV, A and C of both parties take
 __host__ __device__ constexpr int words(int steps) { return 6 * steps - 3; }       // a row's own, from the dealer
 __host__ __device__ constexpr int openings(int steps) { return 3 * steps - 1; }    // a row's own, in its message
 constexpr int row_bytes(int steps) { return 2 * (words(steps) + openings(steps)) * 8; }    // of shared memory, both parties' of both
+// Rows of a tile: a thread has four words, a lane pair of one warp a row's root.
+__host__ __device__ constexpr int tile_rows(int quads) { return TILE_THREADS / quads < TILE_ROWS ? TILE_THREADS / quads : TILE_ROWS; }
 }  // namespace norm
 
 struct NormArgs {
@@ -61,6 +66,7 @@ struct NormArgs {
     int rows, heads, q_heads, dim;       // rows = tokens * heads; q_heads 0: one gain for all heads
     int half, interleaved, table_rows;   // half = pairs that are rotated, 0: none
     int f, steps, divisor_bits;          // divisor_bits: its logarithm, or -1
+    int exchange;                        // tiles: a pair's members are different threads', see norm_tile_kernel
 };
 
 // v >> bits for 1 <= bits <= 32: two instructions, where a shift by any count takes twice as many.
@@ -270,7 +276,7 @@ struct NormQuad {
     template <typename F>
     __device__ __forceinline__ void open(const NormArgs& a, int row, int token, int head, int quad, ulonglong2* place, int place_stride,
                                          u64 sq[2], F&& beside) {
-        p = norm_place<VEC>(quad, a.dim, a.half, a.interleaved);
+        p = norm_place<VEC>(quad, a.dim, a.half, a.interleaved | a.exchange);
         at = (size_t)row * a.dim;
         mine = place;
         stride = place_stride;
@@ -308,7 +314,8 @@ struct NormQuad {
 
     // root: the opened y - v; v0, n1: party 0's share of v and party 1's, negated.  `tells`: this row writes the message of its
     // gain.  An access at a time: the registers of both at once would not fit.
-    __device__ __forceinline__ void finish(const NormArgs& a, int token, int head, bool tells, u64 root, u64 v0, u64 n1) {
+    // Leaves the words in U, party 1's negated; `rotate` makes the results of them.
+    __device__ __forceinline__ void finish(const NormArgs& a, int head, bool tells, u64 root, u64 v0, u64 n1) {
         const size_t g_at = a.q_heads > 0 && head >= a.q_heads ? a.dim : 0;
         norm_fetch_wait();
 #pragma unroll
@@ -353,16 +360,41 @@ struct NormQuad {
 #pragma unroll
             for (int j = 0; j < 2; ++j) x0[j] = norm_shift(t[j] + d[j] * b[j] + e[j] * A[0][j], a.f);
         }
+    }
+    __device__ __forceinline__ void rotate(const NormArgs& a, int token) {
         u64 c[2], s[2];
-        if (a.half) norm_angles<VEC>(a, token, p, c, s);
+        if (a.half) {
+            norm_angles<VEC>(a, token, p, c, s);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (a.half) norm_rotate_words(U[i], p, c, s, a.f);
-            if (i)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) U[1][k] = 0ull - U[1][k];
-            norm_store<VEC>(a.Z[i] + at, p, U[i]);
+            for (int i = 0; i < 2; ++i) norm_rotate_words(U[i], p, c, s, a.f);
         }
+        store(a);
+    }
+    __device__ __forceinline__ void store(const NormArgs& a) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) U[1][k] = 0ull - U[1][k];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) norm_store<VEC>(a.Z[i] + at, p, U[i]);
+    }
+    // The same where a pair's members may be any two threads' of a row, whose words lie in shared memory.
+    __device__ __forceinline__ void rotate_from(const NormArgs& a, int token, const u64* row0, const u64* row1) {
+        if (p.has[0] && p.at[0] < 2 * a.half) {
+            const int at_table = __ldg(a.positions + token);
+            const bool inside = at_table >= 0 && at_table < a.table_rows;
+            if (!inside && a.bad_index) *a.bad_index = 1;
+            const size_t o = (size_t)(inside ? at_table : 0) * a.half;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int j = p.at[k];
+                if (!p.has[k >> 1] || j >= 2 * a.half) continue;
+                const bool second = j >= a.half;
+                const int pair = second ? j - a.half : j, other = second ? pair : j + a.half;
+                const u64 c = inside ? __ldg(a.cos + o + pair) : 0ull, t = inside ? __ldg(a.sin + o + pair) : 0ull, s = second ? t : 0ull - t;
+                U[0][k] = norm_shift(U[0][k] * c + row0[other] * s, a.f);
+                U[1][k] = norm_shift(U[1][k] * c + row1[other] * s, a.f);
+            }
+        }
+        store(a);
     }
 };
 
@@ -370,12 +402,11 @@ struct NormQuad {
 __device__ __forceinline__ bool norm_tells(const NormArgs& a, int token, int head) {
     return token == 0 && (head == 0 || head == a.q_heads);
 }
-// The sum over GROUP lanes of both parties' sq, in every lane: even lanes add up party 0's, odd lanes party 1's.
-template <int GROUP>
+// The sum over a warp's lanes of both parties' sq: even lanes add up party 0's, odd lanes party 1's.
 __device__ __forceinline__ u64 norm_lane_sum(const u64 sq[2], int party) {
     u64 sum = (party ? sq[1] : sq[0]) + __shfl_xor_sync(0xffffffffu, party ? sq[0] : sq[1], 1);
 #pragma unroll
-    for (int o = 2; o < GROUP; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    for (int o = 2; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     return sum;
 }
 
@@ -410,48 +441,69 @@ struct NormWords {
     }
 };
 
-// Rows of up to GROUP_DIM words: GROUP lanes each, four words a lane; one warp works out the roots of all of the CTA's rows, a lane
-// a row.
-template <int GROUP, bool VEC>
-__global__ void __launch_bounds__(norm::GROUP_THREADS, 5)
-norm_group_kernel(const __grid_constant__ NormArgs a) {
-    constexpr int ROWS = norm::GROUP_THREADS / GROUP;
+// Rows of up to TILE_DIM words: a tile of as many as its threads cover, a thread per four words whatever the rows' length; one warp
+// works out all of the tile's roots, a pair of lanes a row.  Accesses lie side by side in a row, so the members of a rotated pair are one
+// thread's if they are neighbours, or if all of a row of a multiple of four words is rotated, halves against each other; else (`exchange`)
+// the rows go through shared memory once more.
+template <bool VEC>
+__global__ void __launch_bounds__(norm::TILE_THREADS, 5)
+norm_tile_kernel(const __grid_constant__ NormArgs a) {
     extern __shared__ __align__(16) uint8_t norm_smem[];
-    __shared__ u64 sums[ROWS][2], root[ROWS];
-    ulonglong2* const places = reinterpret_cast<ulonglong2*>(norm_smem);
-    u64* const words = reinterpret_cast<u64*>(norm_smem + norm::PLACE_BYTES * norm::GROUP_THREADS);      // [party][row][count]
-    const int sub = threadIdx.x / GROUP, lane = threadIdx.x % GROUP, party = threadIdx.x & 1;
+    __shared__ u64 sums[norm::TILE_THREADS][2], root[norm::TILE_ROWS];
+    const int quads = (a.dim + 3) / 4, tile = norm::tile_rows(quads);
     const int count = norm::words(a.steps), sent = norm::openings(a.steps);
-    u64* const opened = words + 2 * ROWS * count;                                                         // [party][row][sent]
-    const int first = blockIdx.x * ROWS, rows = min(ROWS, a.rows - first);
+    ulonglong2* const places = reinterpret_cast<ulonglong2*>(norm_smem);
+    u64* const words = reinterpret_cast<u64*>(norm_smem + norm::PLACE_BYTES * blockDim.x);                // [party][row][count]
+    u64* const opened = words + 2 * tile * count;                                                         // [party][row][sent]
+    u64* const rowed = opened + 2 * tile * sent;                                                          // exchange: [party][row][dim]
+    const int first = blockIdx.x * tile, rows = min(tile, a.rows - first);
+    const int sub = threadIdx.x / quads, quad = threadIdx.x - sub * quads;
     const bool live = sub < rows;
-    const int row = first + (live ? sub : 0);                // groups past the last row have none of its words and write nothing
+    const int row = first + (live ? sub : 0);                // threads past the last row have none of its words and write nothing
     const int token = row / a.heads, head = row - token * a.heads;
     pdl_wait();
     pdl_launch_dependents();
-    NormWords<ROWS <= 4 ? 2 : ROWS / 2> early;
-    early.load(a, first, rows * count, norm::GROUP_THREADS);
+    NormWords<3> early;
+    early.load(a, first, rows * count, blockDim.x);
     NormQuad<VEC> q;
     u64 sq[2];
-    q.open(a, row, token, head, live ? lane : a.dim, places + threadIdx.x, norm::GROUP_THREADS, sq,
-           [&] { early.store(a, first, rows * count, norm::GROUP_THREADS, words, words + ROWS * count); });
-    const u64 sum = norm_lane_sum<GROUP>(sq, party);
-    if (lane < 2) sums[sub][party] = party ? 0ull - sum : sum;
+    q.open(a, row, token, head, live ? quad : a.dim, places + threadIdx.x, blockDim.x, sq,
+           [&] { early.store(a, first, rows * count, blockDim.x, words, words + tile * count); });
+    sums[threadIdx.x][0] = sq[0];
+    sums[threadIdx.x][1] = 0ull - sq[1];
     __syncthreads();
     if (threadIdx.x < 32) {
-        const int r = min((int)threadIdx.x >> 1, ROWS - 1);
-        const bool mine = (int)threadIdx.x < 2 * rows;
-        const u64 opened_root = norm_root(a, sums[r][party], words + (party * ROWS + r) * count, opened + (party * ROWS + r) * sent, mine, party);
+        // lanes 2r and 2r + 1 work for row r; the lanes beyond help with the sums
+        const int width = 2 << (32 - __clz(tile - 1));       // lanes that the rows take, a power of two (tile 1: 2)
+        const int lane = threadIdx.x, of = lane & (width - 1), party = lane & 1, r = min(of >> 1, tile - 1);
+        u64 sum = 0ull;
+        for (int k = lane / width; k < quads; k += 32 / width) sum += sums[r * quads + k][party];
+        for (int o = width; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const bool mine = lane < 2 * rows;
+        const u64 opened_root = norm_root(a, sum, words + (party * tile + r) * count, opened + (party * tile + r) * sent, mine, party);
         if (mine) root[r] = opened_root;
     }
     __syncthreads();
-    if (!live) return;
     for (int i = 0; i < 2; ++i)
-        for (int k = lane; k < sent; k += GROUP) {
-            const u64 t = opened[(i * ROWS + sub) * sent + k];
-            __stcs(a.S[i] + (size_t)row * sent + k, i ? 0ull - t : t);
+        for (int k = threadIdx.x; k < rows * sent; k += blockDim.x) {
+            const u64 t = opened[i * tile * sent + k];
+            __stcs(a.S[i] + (size_t)first * sent + k, i ? 0ull - t : t);
         }
-    q.finish(a, token, head, norm_tells(a, token, head), root[sub], words[(sub + 1) * count - 1], words[(ROWS + sub + 1) * count - 1]);
+    if (live) {
+        q.finish(a, head, norm_tells(a, token, head), root[sub], words[(sub + 1) * count - 1], words[(tile + sub + 1) * count - 1]);
+        if (!a.exchange) q.rotate(a, token);
+    }
+    if (!a.exchange) return;
+    u64 *const row0 = rowed + sub * a.dim, *const row1 = row0 + tile * a.dim;
+    if (live)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (q.p.has[k >> 1]) {
+                row0[q.p.at[k]] = q.U[0][k];
+                row1[q.p.at[k]] = q.U[1][k];
+            }
+    __syncthreads();
+    if (live) q.rotate_from(a, token, row0, row1);
 }
 
 // Longer rows: a cluster of CTAs per row, a thread per four words.
@@ -477,7 +529,7 @@ norm_cluster_kernel(const __grid_constant__ NormArgs a) {
     u64 sq[2];
     q.open(a, row, token, head, (int)(rank * blockDim.x + threadIdx.x), places + threadIdx.x, blockDim.x, sq,
            [&] { early.store(a, row, count, blockDim.x, words, words + count); });
-    u64 sum = norm_lane_sum<32>(sq, party);
+    u64 sum = norm_lane_sum(sq, party);
     if (lane < 2) partial[warp][party] = sum;
     __syncthreads();
     if (warp == 0) {
@@ -513,7 +565,8 @@ norm_cluster_kernel(const __grid_constant__ NormArgs a) {
                 const u64 t = opened[i * sent + k];
                 __stcs(a.S[i] + (size_t)row * sent + k, i ? 0ull - t : t);
             }
-    q.finish(a, token, head, norm_tells(a, token, head), root, words[count - 1], words[2 * count - 1]);
+    q.finish(a, head, norm_tells(a, token, head), root, words[count - 1], words[2 * count - 1]);
+    q.rotate(a, token);
     __syncwarp();
     if (cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
