@@ -630,8 +630,8 @@ int comet_beaver_matmul_static(void* cuda_stream, const uint64_t* const X[2], co
                                const uint64_t* const Y[2], const uint64_t* const B[2], const uint64_t* const C[2],
                                uint64_t* const Z[2], int32_t T, int32_t K, int32_t N);
 
-/* Waits for `cuda_stream` and reports whether a comet_beaver_matmul_static call on
- * the current device gave up on a bounded wait since this was last asked:
+/* Waits for `cuda_stream` and reports whether a comet_beaver_matmul_static or comet_linear call
+ * on the current device gave up on a bounded wait since this was last asked:
  * COMET_OK, COMET_ERR_TIMEOUT (the results since then are not to be trusted) or
  * COMET_ERR_CUDA.  The report is given once.  Allocates nothing. */
 int comet_static_status(void* cuda_stream);
