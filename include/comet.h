@@ -542,7 +542,8 @@ int comet_linear_workspace(int32_t tokens, int32_t inner, int32_t cols, int64_t*
  * Stateless; DEVICE pointers on the current device, owned by the caller, 8-byte aligned (16-byte accesses are used where
  * x_stride is even and every pointer 16-byte aligned, and, for a rotation alone or a dim above 512, rot_dim a multiple of
  * 4); what is written must not overlap any other argument.
- * One kernel on `cuda_stream`; the call does not wait, allocates nothing, and may be captured.
+ * One kernel on `cuda_stream`; the call does not wait, allocates nothing, and may be captured (the first call on a device
+ * makes settings once; make it outside stream capture).
  * Errors: INVALID_ARG (null or unaligned pointer, overlap, nothing to do, a gain without a norm), SHAPE (dim odd or outside
  * [2, 8192], tokens or heads < 1 or more than 2^27 rows, x_stride < heads * dim or > 2^32, q_heads outside [0, heads], rot_dim odd
  * or outside [0, dim], table_rows < 1, steps outside {0, 2..24}, guess outside [1, 2^32), frac_bits outside [1, 31]), CUDA. */

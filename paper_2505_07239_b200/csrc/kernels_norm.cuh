@@ -43,7 +43,6 @@ constexpr int MAX_STEPS = 24, MAX_DIM = 8192;
 constexpr int TILE_THREADS = 128;                    // at most, of a CTA that has whole rows of up to TILE_DIM words
 constexpr int TILE_DIM = 4 * TILE_THREADS, TILE_ROWS = 16;
 constexpr int CLUSTER_THREADS = 256;                 // at most, of a CTA of a cluster that has one
-constexpr int GROUP_DIM = 128;                       // longest row of one warp: four words a lane
 constexpr int PLACE_BYTES = 6 * 2 * 16;              // of shared memory that a thread's four words of UV, A and C of both parties take
 __host__ __device__ constexpr int words(int steps) { return 6 * steps - 3; }       // a row's own, from the dealer
 __host__ __device__ constexpr int openings(int steps) { return 3 * steps - 1; }    // a row's own, in its message

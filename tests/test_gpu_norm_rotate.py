@@ -86,6 +86,18 @@ def test_steps_and_fixed_point(cb, steps, f):
         compare(cb.norm_rotate(**on_gpu(case, cb)), layers.norm_rotate(**case))
 
 
+@pytest.mark.parametrize("D", [8, 12, 20, 28, 36, 44, 60, 82, 100, 122, 170, 172, 254, 258, 300, 340, 342, 384, 510, 512, 514, 516])
+@pytest.mark.parametrize("rot,interleaved", [("all", False), ("all", True), ("odd", False), ("odd", True), ("even", False)])
+def test_tiles(cb, D, rot, interleaved):
+    """Tiles of whole rows: as many as 128 threads of four words cover, sixteen at most, the last one not full; pairs of one
+    thread's, and pairs through shared memory."""
+    rot = {"all": D, "odd": 2 * (2 * (D // 8) + 1), "even": 4 * max(1, D // 10)}[rot]
+    tile = min(16, 128 // ((D + 3) // 4)) if D <= 512 else 1
+    for T, H, q in ((1, 1, 1), (1, tile + 1, tile), (5, 7, 3)):
+        case, _, _ = norm_case(D + rot, T, H, D, 16, 3, min(rot, D), interleaved=interleaved, q_heads=q)
+        compare(cb.norm_rotate(**on_gpu(case, cb)), layers.norm_rotate(**case))
+
+
 def test_any_words(cb):
     """Uniform words everywhere, triples that are none, the largest guess and eps: the words are still the formulas'."""
     for D, T, H in ((20, 9, 5), (128, 4, 2), (2052, 2, 1)):
