@@ -21,7 +21,7 @@
 // Measured, ten steps, gain and rotation: 512 tokens x 64 heads x 128 108 us, 582 MB, 5.4 TB/s, 0.82 of the copy rate (two steps: 94 us,
 // 0.88), x 64 66 us (0.73), x 256 200 us (0.86); 32 tokens x 64 heads x 128 13 us, one token 7.5 us, of which the chain 1.6; rows of 4096
 // words without rotation, 203 of them, 27 us, 0.60 (two waves of clusters, and the second is not full).
-// What it took, 512 tokens x 64 heads: every warp with its row's chain to itself 135 us (2050 instructions a row, 1400 now), one warp for
+// What it took, 512 tokens x 64 heads: every warp with its row's chain to itself 135 us (2050 instructions a row, 1460 now), one warp for
 // all rows of a CTA 115, a row's own words asked for before the elements 109.  CTAs of four rows: of two or eight 115.  Five CTAs an SM at
 // 96 registers: four at 128 125, six at 80 (16 bytes spilled) 111; with 100 bytes spilled 129.  Left out in scratch builds: the chain
 // 103, the row's own words 105, the predicates of ragged rows 107.  No difference: another warp of the CTA for the chain, CTAs of the

@@ -232,6 +232,20 @@ def test_calls_on_two_streams_at_once(cb):
             compare(result, ref)
 
 
+@pytest.mark.parametrize("T,K", [(1, 264), (9, 64), (90, 264), (512, 1024)])
+def test_one_tensor_in_several_places(cb, T, K):
+    """What is only read may be given twice: the input as the residual, the product's share as the square's mask, one tensor as both
+    parties' bias, the weights as their own masks (the messages are zero then)."""
+    case = ring_case(70, T, K, K, 16, True, "tame", True)
+    k, _, Q = case["act"]
+    case.update(residual=case["X"], B=case["W"], bias=[case["bias"][0]] * 2, act=(k, case["C"], Q))
+    gpu = on_gpu(case)
+    gpu.update(residual=gpu["X"], B=gpu["W"], bias=[gpu["bias"][0]] * 2, act=(k, gpu["C"], gpu["act"][2]))
+    got = cb.linear(**gpu)
+    compare(got, layers.linear(**case))
+    assert not any(v.any() for v in got[1])
+
+
 @pytest.mark.parametrize("T,K,N", [(1, 768, 300), (9, 64, 36), (90, 264, 132), (512, 1024, 1024)])
 def test_captured_and_replayed(cb, T, K, N):
     case, other = ring_case(3, T, K, N, 13, True, "tame", True), ring_case(4, T, K, N, 13, True, "tame", True)

@@ -49,7 +49,7 @@ def compare(got, ref):
                 assert np.array_equal(host(pair[i]), ref[name][i]), (name, i)
 
 
-# groups of 8, 16 and 32 lanes, one to eight CTAs a row, lengths that fill neither lanes nor pairs of pairs
+# tiles of sixteen rows to one, one to eight CTAs a row, lengths that fill neither threads nor pairs of pairs
 DIMS = [2, 4, 6, 30, 32, 34, 62, 64, 66, 80, 126, 128, 130, 132, 256, 1022, 1024, 1026, 1030, 2048, 2050, 3466, 4096, 4098, 8190, 8192]
 
 
@@ -183,6 +183,41 @@ def test_tokens_far_apart(cb):
     compare(cb.norm_rotate(**g), layers.norm_rotate(**case))
     bare = dict(g, norm=None, gain=None)
     compare(cb.norm_rotate(**bare), layers.norm_rotate(**dict(case, norm=None, gain=None)))
+
+
+@pytest.mark.parametrize("D,rot", [(64, 64), (66, 30), (1024, 0)])
+def test_one_tensor_in_several_places(cb, D, rot):
+    """What is only read may be given twice: the rows as their own masks, both parties' material alike, the tables each other's."""
+    case = norm_case(45, 3, 4, D, 16, 4, rot)[0]
+    X = case["X"]
+    n, g = case["norm"], case["gain"]
+    case = dict(case, norm=dict(n, U=X, UV=[n["UV"][0]] * 2), gain=dict(g, mask=g["weight"], A=X, C=X))
+    if rot:
+        case["rotation"] = dict(case["rotation"], sin=case["rotation"]["cos"])
+    gpu = on_gpu(case, cb)
+    x, n, g = gpu["X"], gpu["norm"], gpu["gain"]
+    gpu.update(norm=n._replace(U=x, UV=[n.UV[0]] * 2), gain=g._replace(mask=g.weight, A=x, C=x))
+    if rot:
+        gpu["rotation"] = gpu["rotation"]._replace(sin=gpu["rotation"].cos)
+    got = cb.norm_rotate(**gpu)
+    compare(got, layers.norm_rotate(**case))
+    assert not any(v.any() for v in got[0].M) and not any(v.any() for v in got[0].G)
+
+
+@pytest.mark.parametrize("normed", [True, False])
+def test_calls_on_two_streams_at_once(cb, normed):
+    """Calls share no memory: two streams at once, rows of tiles and of clusters, give the words of calls one by one."""
+    cases = [norm_case(50 + k, *s)[0] for k, s in enumerate(((70, 6, 128, 13, 5, 128), (9, 3, 66, 16, 6, 30), (40, 1, 2048, 16, 6, 512)))]
+    if not normed:
+        cases = [dict(c, norm=None, gain=None) for c in cases]
+    gpu, refs = [on_gpu(c, cb) for c in cases], [layers.norm_rotate(**c) for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[cb.norm_rotate(**g, stream=streams[(k + j) % 2]) for j, g in enumerate(gpu)] for k in range(4)]
+    torch.cuda.synchronize()
+    for results in got:
+        for result, ref in zip(results, refs):
+            compare(result, ref)
 
 
 def test_streams_and_replays(cb):
