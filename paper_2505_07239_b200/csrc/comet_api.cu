@@ -2299,7 +2299,7 @@ extern "C" int comet_linear(void* cuda_stream, const comet_linear_args* g) {
 namespace {
 
 // A thread takes four words of a row.  Up to 512 words: tiles of whole rows; beyond: a cluster of CTAs of at most 256 threads per row.
-int launch_norm(comet::NormArgs& a, bool aligned, cudaStream_t stream) {
+int launch_norm(comet::NormArgs& a, bool aligned, int sm_count, cudaStream_t stream) {
     namespace nm = comet::norm;
     const int quads = ceil_div(a.dim, 4), row_bytes = nm::row_bytes(a.steps);
     const bool tiled = a.dim <= nm::TILE_DIM;
@@ -2312,10 +2312,12 @@ int launch_norm(comet::NormArgs& a, bool aligned, cudaStream_t stream) {
     std::memset(&lc, 0, sizeof(lc));
     if (tiled) {
         const int rows = nm::tile_rows(quads);
+        a.ahead = nm::TILE_AHEAD * sm_count * rows;
         lc.gridDim = dim3(ceil_div(a.rows, rows));
         lc.blockDim = dim3(ceil_div(rows * quads, 32) * 32);
         lc.dynamicSmemBytes = nm::PLACE_BYTES * lc.blockDim.x + rows * (row_bytes + (a.exchange ? 2 * a.dim * (int)sizeof(u64) : 0));
     } else {
+        a.ahead = nm::CLUSTER_AHEAD * sm_count / cluster;
         lc.gridDim = dim3((unsigned)a.rows * cluster);
         lc.blockDim = dim3(ceil_div(ceil_div(quads, cluster), 32) * 32);
         lc.dynamicSmemBytes = nm::PLACE_BYTES * lc.blockDim.x + row_bytes;
@@ -2437,7 +2439,7 @@ extern "C" int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args
             cudaGetLastError();
             return COMET_ERR_CUDA;
         }
-        return launch_norm(a, aligned, stream);
+        return launch_norm(a, aligned, dev.sm_count, stream);
     }
     const unsigned quads = (unsigned)ceil_div(a.dim, 4);
     return launch_pass(aligned && a.half % 2 == 0 ? comet::rotate_kernel<true> : comet::rotate_kernel<false>, dim3(shuffle_grid(rows * quads)), stream, a, quads);

@@ -17,17 +17,20 @@
 // five in (x, U, U v, and the gain's A and C), three out (two messages and the result), 128 bytes an element; beaver_mul_kernel moves
 // the same mix at 0.95 of the copy rate.  The root is a chain of 3 (steps - 1) dependent products between a row's first loads and
 // its last stores, 0.17 us a step, so what is needed behind it is asked for before it begins: UV, A and C wait in shared
-// memory, x's opening and U in registers.
-// Measured, ten steps, gain and rotation: 512 tokens x 64 heads x 128 108 us, 582 MB, 5.4 TB/s, 0.82 of the copy rate (two steps: 94 us,
-// 0.88), x 64 66 us (0.73), x 256 200 us (0.86); 32 tokens x 64 heads x 128 13 us, one token 7.5 us, of which the chain 1.6; rows of 4096
-// words without rotation, 203 of them, 27 us, 0.60 (two waves of clusters, and the second is not full).
-// What it took, 512 tokens x 64 heads: every warp with its row's chain to itself 135 us (2050 instructions a row, 1460 now), one warp for
+// memory, x's opening and U in registers.  And what a CTA asks for first, x, U and its rows' own words, an earlier CTA has asked the
+// L2 for, three CTAs of the SM ahead: the memory works while chains run, and a row is held for less time.
+// Measured, ten steps, gain and rotation: 512 tokens x 64 heads x 128 99.7 us, 582 MB, 5.8 TB/s, 0.89 of the copy rate (two steps: 91.5 us,
+// 0.90), x 64 60 us (0.81), x 256 178 us (0.97); 32 tokens x 64 heads x 128 13 us, one token 7.5 us, of which the chain 1.6; rows of 4096
+// words without rotation, 203 of them, 27 us, 0.60 (two waves of clusters, and the second is not full), 512 of them 62 us (0.67).
+// What it took, 512 tokens x 64 heads: every warp with its row's chain to itself 135 us (2050 instructions a row, 1500 now), one warp for
 // all rows of a CTA 115, a row's own words asked for before the elements 109.  CTAs of four rows: of two or eight 115.  Five CTAs an SM at
 // 96 registers: four at 128 125, six at 80 (16 bytes spilled) 111; with 100 bytes spilled 129.  Left out in scratch builds: the chain
 // 103, the row's own words 105, the predicates of ragged rows 107.  No difference: another warp of the CTA for the chain, CTAs of the
 // first wave begun 1.5 us apart.  Threads dealt to a tile's words whatever the rows' length, instead of whole lanes or warps to a row:
 // x 160 189 -> 138 us, x 254, all rotated, 312 -> 229, x 126 147 -> 121 (the latter two in accesses of 16 bytes, too, their pairs
-// through shared memory).
+// through shared memory).  The L2 asked ahead (the figures before are without it): 108.5 -> 99.7, x 256 200 -> 178, x 160 133 -> 124,
+// without gain 86.7 -> 75.8, 512 rows of 4096 67 -> 62; the rows' own words alone 103.5, x and U alone 106.5; UV, A and C too 103.8; two and
+// four CTAs ahead 98.5 and 100.4 (x 64 62.1 and 59.4); five with UV, A and C 107, eight 119; four CTAs an SM 104.5, six 102.4.
 #pragma once
 #include <cstdint>
 #include <cuda_runtime.h>
@@ -43,6 +46,8 @@ constexpr int MAX_STEPS = 24, MAX_DIM = 8192;
 constexpr int TILE_THREADS = 128;                    // at most, of a CTA that has whole rows of up to TILE_DIM words
 constexpr int TILE_DIM = 4 * TILE_THREADS, TILE_ROWS = 16;
 constexpr int CLUSTER_THREADS = 256;                 // at most, of a CTA of a cluster that has one
+constexpr int TILE_CTAS = 5, CLUSTER_CTAS = 3;       // on an SM
+constexpr int TILE_AHEAD = 3, CLUSTER_AHEAD = 2;     // how many CTAs of an SM ahead the L2 is asked for rows
 constexpr int PLACE_BYTES = 6 * 2 * 16;              // of shared memory that a thread's four words of UV, A and C of both parties take
 __host__ __device__ constexpr int words(int steps) { return 6 * steps - 3; }       // a row's own, from the dealer
 __host__ __device__ constexpr int openings(int steps) { return 3 * steps - 1; }    // a row's own, in its message
@@ -66,6 +71,7 @@ struct NormArgs {
     int half, interleaved, table_rows;   // half = pairs that are rotated, 0: none
     int f, steps, divisor_bits;          // divisor_bits: its logarithm, or -1
     int exchange;                        // tiles: a pair's members are different threads', see norm_tile_kernel
+    int ahead;                           // rows from a CTA's or cluster's to those that it asks the L2 for
 };
 
 // v >> bits for 1 <= bits <= 32: two instructions, where a shift by any count takes twice as many.
@@ -240,6 +246,11 @@ __device__ __forceinline__ void norm_fetch16(void* dst, const u64* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
 }
 __device__ __forceinline__ void norm_fetch_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// Asks the L2 for words that are read later: 16-byte aligned, an even number of them.
+__device__ __forceinline__ void norm_ask(const u64* words, int count) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(words), "r"(count * 8) : "memory");
+}
 
 // A thread's four words of a row: `open` before the root, `finish` after it.  What `finish` reads is on its way to this thread's
 // places in shared memory meanwhile (nobody else reads them): UV, A and C of both parties.
@@ -445,7 +456,7 @@ struct NormWords {
 // thread's if they are neighbours, or if all of a row of a multiple of four words is rotated, halves against each other; else (`exchange`)
 // the rows go through shared memory once more.
 template <bool VEC>
-__global__ void __launch_bounds__(norm::TILE_THREADS, 5)
+__global__ void __launch_bounds__(norm::TILE_THREADS, norm::TILE_CTAS)
 norm_tile_kernel(const __grid_constant__ NormArgs a) {
     extern __shared__ __align__(16) uint8_t norm_smem[];
     __shared__ u64 sums[norm::TILE_THREADS][2], root[norm::TILE_ROWS];
@@ -466,8 +477,23 @@ norm_tile_kernel(const __grid_constant__ NormArgs a) {
     early.load(a, first, rows * count, blockDim.x);
     NormQuad<VEC> q;
     u64 sq[2];
-    q.open(a, row, token, head, live ? quad : a.dim, places + threadIdx.x, blockDim.x, sq,
-           [&] { early.store(a, first, rows * count, blockDim.x, words, words + tile * count); });
+    q.open(a, row, token, head, live ? quad : a.dim, places + threadIdx.x, blockDim.x, sq, [&] {
+        early.store(a, first, rows * count, blockDim.x, words, words + tile * count);
+        if (VEC && threadIdx.x < 32 && a.ahead < a.rows - first) {       // a lane for a row of a party
+            const int next = first + a.ahead, many = min(tile, a.rows - next), r = threadIdx.x >> 1, i = threadIdx.x & 1;
+            if (r < many) {
+                const int at_token = (next + r) / a.heads;
+                norm_ask(a.X[i] + (size_t)at_token * a.x_stride + (size_t)(next + r - at_token * a.heads) * a.dim, a.dim);
+            }
+            if (r == 0) {
+                const size_t at = (size_t)next * a.dim, own = (size_t)next * count;
+                norm_ask(a.U[i] + at, many * a.dim);
+                const u64* w = a.row_words[i] + own;         // 8-byte aligned: the even words between
+                const int odd = (int)(reinterpret_cast<uintptr_t>(w) >> 3 & 1);
+                norm_ask(w + odd, (many * count - odd) & ~1);
+            }
+        }
+    });
     sums[threadIdx.x][0] = sq[0];
     sums[threadIdx.x][1] = 0ull - sq[1];
     __syncthreads();
@@ -507,7 +533,7 @@ norm_tile_kernel(const __grid_constant__ NormArgs a) {
 
 // Longer rows: a cluster of CTAs per row, a thread per four words.
 template <bool VEC>
-__global__ void __launch_bounds__(norm::CLUSTER_THREADS, 3)
+__global__ void __launch_bounds__(norm::CLUSTER_THREADS, norm::CLUSTER_CTAS)
 norm_cluster_kernel(const __grid_constant__ NormArgs a) {
     extern __shared__ __align__(16) uint8_t norm_smem[];
     __shared__ u64 partial[norm::CLUSTER_THREADS / 32][2], cta_sum[2], root;
@@ -527,7 +553,14 @@ norm_cluster_kernel(const __grid_constant__ NormArgs a) {
     NormQuad<VEC> q;
     u64 sq[2];
     q.open(a, row, token, head, (int)(rank * blockDim.x + threadIdx.x), places + threadIdx.x, blockDim.x, sq,
-           [&] { early.store(a, row, count, blockDim.x, words, words + count); });
+           [&] {
+        early.store(a, row, count, blockDim.x, words, words + count);
+        if (VEC && threadIdx.x < 4 && threadIdx.x % cluster == rank && a.ahead < a.rows - row) {
+            const int next = row + a.ahead, at_token = next / a.heads, i = threadIdx.x & 1;
+            if (threadIdx.x < 2) norm_ask(a.X[i] + (size_t)at_token * a.x_stride + (size_t)(next - at_token * a.heads) * a.dim, a.dim);
+            else norm_ask(a.U[i] + (size_t)next * a.dim, a.dim);
+        }
+    });
     u64 sum = norm_lane_sum(sq, party);
     if (lane < 2) partial[warp][party] = sum;
     __syncthreads();

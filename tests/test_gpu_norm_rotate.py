@@ -98,6 +98,15 @@ def test_tiles(cb, D, rot, interleaved):
         compare(cb.norm_rotate(**on_gpu(case, cb)), layers.norm_rotate(**case))
 
 
+# more rows than the CTAs that run at once and what they ask for ahead, the last tile ragged, tokens apart, an odd number of a row's words
+@pytest.mark.parametrize("T,H,D,rot,pad", [(447, 1, 512, 512, 0), (67, 31, 128, 64, 2), (91, 41, 64, 64, 0), (601, 13, 16, 16, 6), (203, 1, 1030, 0, 4),
+                                           (41, 4, 4096, 1024, 0), (331, 11, 66, 32, 0)])
+def test_many_rows(cb, T, H, D, rot, pad):
+    case = norm_case(12, T, H, D, 16, 3, rot, q_heads=H // 2)[0]
+    for shift in (0, 1):
+        compare(cb.norm_rotate(**on_gpu(case, cb, pad, shift)), layers.norm_rotate(**case))
+
+
 def test_any_words(cb):
     """Uniform words everywhere, triples that are none, the largest guess and eps: the words are still the formulas'."""
     for D, T, H in ((20, 9, 5), (128, 4, 2), (2052, 2, 1)):
