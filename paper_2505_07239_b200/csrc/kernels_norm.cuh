@@ -21,7 +21,7 @@
 // L2 for, three CTAs of the SM ahead: the memory works while chains run, and a row is held for less time.
 // Measured, ten steps, gain and rotation: 512 tokens x 64 heads x 128 99.7 us, 582 MB, 5.8 TB/s, 0.89 of the copy rate (two steps: 91.5 us,
 // 0.90), x 64 60 us (0.81), x 256 178 us (0.97); 32 tokens x 64 heads x 128 13 us, one token 7.5 us, of which the chain 1.6; rows of 4096
-// words without rotation, 203 of them, 27 us, 0.60 (two waves of clusters, and the second is not full), 512 of them 62 us (0.67).
+// words without rotation, 203 of them, 26 us, 0.63 (two waves of clusters, and the second is not full), 512 of them 62 us (0.67), one 7.9 us.
 // What it took, 512 tokens x 64 heads: every warp with its row's chain to itself 135 us (2050 instructions a row, 1500 now), one warp for
 // all rows of a CTA 115, a row's own words asked for before the elements 109.  CTAs of four rows: of two or eight 115.  Five CTAs an SM at
 // 96 registers: four at 128 125, six at 80 (16 bytes spilled) 111; with 100 bytes spilled 129.  Left out in scratch builds: the chain
@@ -45,9 +45,10 @@ namespace norm {
 constexpr int MAX_STEPS = 24, MAX_DIM = 8192;
 constexpr int TILE_THREADS = 128;                    // at most, of a CTA that has whole rows of up to TILE_DIM words
 constexpr int TILE_DIM = 4 * TILE_THREADS, TILE_ROWS = 16;
-constexpr int CLUSTER_THREADS = 256;                 // at most, of a CTA of a cluster that has one
+constexpr int CLUSTER_THREADS = 256, MAX_CLUSTER = 8;   // at most, of a CTA of a cluster that has one; its CTAs
 constexpr int TILE_CTAS = 5, CLUSTER_CTAS = 3;       // on an SM
 constexpr int TILE_AHEAD = 3, CLUSTER_AHEAD = 2;     // how many CTAs of an SM ahead the L2 is asked for rows
+static_assert(4 * MAX_CLUSTER * CLUSTER_THREADS >= MAX_DIM, "a row fits a cluster");
 constexpr int PLACE_BYTES = 6 * 2 * 16;              // of shared memory that a thread's four words of UV, A and C of both parties take
 __host__ __device__ constexpr int words(int steps) { return 6 * steps - 3; }       // a row's own, from the dealer
 __host__ __device__ constexpr int openings(int steps) { return 3 * steps - 1; }    // a row's own, in its message
@@ -531,12 +532,14 @@ norm_tile_kernel(const __grid_constant__ NormArgs a) {
     if (live) q.rotate_from(a, token, row0, row1);
 }
 
-// Longer rows: a cluster of CTAs per row, a thread per four words.
+// Longer rows: a cluster of CTAs per row, a thread per four words.  Every warp's sums are written to every CTA, one barrier of the cluster
+// behind them, and every CTA works out the root for itself.  (Sums per CTA, read from each other's behind a barrier: one row of 4096 words
+// 8.45 us instead of 7.9, of 8192 8.7 instead of 8.2, 203 rows alike, 512 of 4096 60.7 instead of 61.9.)
 template <bool VEC>
 __global__ void __launch_bounds__(norm::CLUSTER_THREADS, norm::CLUSTER_CTAS)
 norm_cluster_kernel(const __grid_constant__ NormArgs a) {
     extern __shared__ __align__(16) uint8_t norm_smem[];
-    __shared__ u64 partial[norm::CLUSTER_THREADS / 32][2], cta_sum[2], root;
+    __shared__ u64 partial[norm::MAX_CLUSTER * norm::CLUSTER_THREADS / 32][2], root;        // every warp's of the row
     ulonglong2* const places = reinterpret_cast<ulonglong2*>(norm_smem);
     u64* const words = reinterpret_cast<u64*>(norm_smem + norm::PLACE_BYTES * blockDim.x);               // [party][count]
     uint32_t rank, cluster;
@@ -546,14 +549,15 @@ norm_cluster_kernel(const __grid_constant__ NormArgs a) {
     const int count = norm::words(a.steps), sent = norm::openings(a.steps);
     u64* const opened = words + 2 * count;                                                               // [party][sent]
     const int row = (int)(blockIdx.x / cluster), token = row / a.heads, head = row - token * a.heads;
+    // (a CTA's shared memory is written to by the others when it has begun)
+    if (cluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     pdl_wait();
     pdl_launch_dependents();
     NormWords<1> early;
     early.load(a, row, count, blockDim.x);
     NormQuad<VEC> q;
     u64 sq[2];
-    q.open(a, row, token, head, (int)(rank * blockDim.x + threadIdx.x), places + threadIdx.x, blockDim.x, sq,
-           [&] {
+    q.open(a, row, token, head, (int)(rank * blockDim.x + threadIdx.x), places + threadIdx.x, blockDim.x, sq, [&] {
         early.store(a, row, count, blockDim.x, words, words + count);
         if (VEC && threadIdx.x < 4 && threadIdx.x % cluster == rank && a.ahead < a.rows - row) {
             const int next = row + a.ahead, at_token = next / a.heads, i = threadIdx.x & 1;
@@ -562,31 +566,25 @@ norm_cluster_kernel(const __grid_constant__ NormArgs a) {
         }
     });
     u64 sum = norm_lane_sum(sq, party);
-    if (lane < 2) partial[warp][party] = sum;
-    __syncthreads();
-    if (warp == 0) {
-        sum = 0ull;
-        for (int k = 0; k < warps; ++k) sum += partial[k][party];
-        if (lane < 2) cta_sum[party] = sum;
-        __syncwarp();
-    }
     if (cluster > 1) {
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-        if (warp == 0) {
-            sum = 0ull;
-            for (uint32_t k = 0; k < cluster; ++k) {
-                uint32_t there;
-                u64 v;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(&cta_sum[party])), "r"(k));
-                asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(there) : "memory");
-                sum += v;
-            }
+        // a warp's sums go to every CTA of the cluster, a lane each
+        __syncwarp();
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (lane < 2 * cluster) {
+            uint32_t there;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there)
+                         : "r"((uint32_t)__cvta_generic_to_shared(&partial[rank * warps + warp][party])), "r"(lane >> 1));
+            asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(there), "l"(sum) : "memory");
         }
         __syncwarp();
-        // a CTA ends when the others have read its sum
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else {
+        if (lane < 2) partial[warp][party] = sum;
+        __syncthreads();
     }
     if (warp == 0) {
+        sum = 0ull;
+        for (int k = 0; k < (int)cluster * warps; ++k) sum += partial[k][party];
         const u64 opened_root = norm_root(a, party ? 0ull - sum : sum, words + party * count, opened + party * sent, lane < 2, party);
         if (lane == 0) root = opened_root;
     }
@@ -599,8 +597,6 @@ norm_cluster_kernel(const __grid_constant__ NormArgs a) {
             }
     q.finish(a, head, norm_tells(a, token, head), root, words[count - 1], words[2 * count - 1]);
     q.rotate(a, token);
-    __syncwarp();
-    if (cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // Rotation without a norm: a thread per four words of a row, both parties.
