@@ -426,8 +426,9 @@ def linear(X, A, W, B, C, frac_bits: int, bias=None, act=None, residual=None, st
     Every tensor argument is a pair (party 0, party 1) of contiguous CUDA tensors of 64-bit integers: X, A [T, K]; W, B [N, K];
     C [T, N] with the dealer's C = A B^T; bias [N]; residual [T, N].  K is a multiple of 8, N of 4.  `act`: None, or
     ((k0, k1, k2), R, Q) for k2 y^2 + k1 y + k0 with coefficients at scale f and the dealer's Q = R * R, [T, N].
-    Returns (E, F, M, Y): the messages (M is None without an activation) and the result's shares, new tensors.  The operand
-    planes of more than a few rows live in a tensor of linear_workspace(T, K, N) bytes for the length of the call.
+    Returns (E, F, M, Y): the messages (M is None without an activation) and the result's shares, new tensors.  A share of the
+    result has memory of its own; a party's messages may lie together in one piece, none of the other party's words in it.  The
+    operand planes of more than a few rows live in a tensor of linear_workspace(T, K, N) bytes for the length of the call.
     A captured call is replayed on the memory that it was captured with.
     """
     code, E, F, M, Y = _native.linear(stream, X, A, W, B, C, frac_bits, bias, act, residual)
@@ -479,7 +480,8 @@ def norm_rotate(X, frac_bits: int, norm: Optional[Norm] = None, gain: Optional[G
     X: a pair of CUDA tensors of 64-bit integers [T, H, D], D even and at most 8192; a token's heads lie together, tokens may
     lie further apart (a view of a stacked projection's result).  Heads below `q_heads` take the gain's first row, the others
     its second; without `q_heads` there is one row.  A rotation may come alone.
-    Returns (NormMessages, Z): Z a pair of new tensors [T, H, D].
+    Returns (NormMessages, Z): Z a pair of new tensors [T, H, D], each in memory of its own; a party's messages may lie together in
+    one piece, none of the other party's words in it.
     """
     code, M, S, D, G, Z = _native.norm_rotate(stream, X, frac_bits, norm, gain, rotation, q_heads, bad_index_flag)
     if code:

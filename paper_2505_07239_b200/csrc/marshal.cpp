@@ -432,50 +432,55 @@ bool stream_of(PyObject* o, c10::Device device, std::optional<c10::Stream>* out)
     return true;
 }
 
-// What a call makes, new contiguous tensors of ring words on the current stream.  Its messages share one piece of memory and its
-// result another, up to 32 MiB each: ten tensors cost 7 us one by one.  Who keeps a result does not keep the messages with it;
-// larger ones have memory of their own.
+// What a call makes, new contiguous tensors of ring words on the current stream.  A result's share has memory of its own, exactly
+// its words: what is saved, sent or grown with it is that share and nothing else.  A party's messages, all of them meant for the
+// other party, share a piece of up to 32 MiB without gaps, so who keeps one of them keeps the others; larger ones have memory of
+// their own.  One token's heads, ten tensors, a pass: 14.8 us; every tensor in memory of its own 17.6, both parties' together 14.2.
 struct Results {
-    static constexpr size_t SHARED = 32 << 20, ALIGN = 256;
-    enum { MESSAGE, RESULT, KINDS };
+    static constexpr size_t SHARED = 32 << 20;
+    enum { MESSAGE, RESULT };
     struct Item {
         c10::SmallVector<int64_t, 3> shape;
         at::Tensor* to;
         uint64_t** at;
-        size_t bytes;
+        size_t bytes;                                        // of either
         int kind;
     };
     const at::Tensor& like;
-    c10::SmallVector<Item, 12> items;
-    size_t total[KINDS] = {0, 0};
+    c10::SmallVector<Item, 6> items;
+    size_t messages = 0;                                     // bytes of a party's
     explicit Results(const at::Tensor& t) : like(t) {}
-    static size_t padded(size_t bytes) { return (bytes + ALIGN - 1) / ALIGN * ALIGN; }
-    // Two tensors, and where their addresses go.
+    // Two tensors, and where their addresses go.  A message whose words may be odd in number comes last: 16-byte accesses are used
+    // for the others.
     void pair(int kind, at::IntArrayRef shape, at::Tensor t[2], uint64_t* to[2]) {
         size_t bytes = sizeof(uint64_t);
         for (int64_t n : shape) bytes *= (size_t)n;
-        for (int p = 0; p < 2; ++p) items.push_back({c10::SmallVector<int64_t, 3>(shape.begin(), shape.end()), t + p, to + p, bytes, kind});
-        total[kind] += 2 * padded(bytes);
+        items.push_back({c10::SmallVector<int64_t, 3>(shape.begin(), shape.end()), t, to, bytes, kind});
+        if (kind == MESSAGE) messages += bytes;
     }
     void make() {
         c10::Allocator* const allocator = c10::GetAllocator(c10::DeviceType::CUDA);
         const c10::DispatchKeySet keys(c10::DispatchKey::CUDA);
-        std::optional<c10::Storage> storage[KINDS];
-        size_t offset[KINDS] = {0, 0};
-        for (int k = 0; k < KINDS; ++k)
-            if (total[k] && total[k] <= SHARED)
-                storage[k].emplace(c10::Storage::use_byte_size_t(), total[k], allocator->allocate(total[k]), allocator, false);
-        for (Item& i : items) {
-            if (storage[i.kind]) {
-                *i.to = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(*storage[i.kind]), keys, like.dtype());
-                c10::TensorImpl* const impl = i.to->unsafeGetTensorImpl();
-                impl->set_storage_offset((int64_t)(offset[i.kind] / sizeof(uint64_t)));
+        const caffe2::TypeMeta type = like.dtype();
+        auto memory = [&](size_t bytes, bool grows) {
+            return c10::Storage(c10::Storage::use_byte_size_t(), bytes, allocator->allocate(bytes), allocator, grows);
+        };
+        for (int p = 0; p < 2; ++p) {
+            c10::Storage together;
+            size_t offset = 0;
+            if (messages && messages <= SHARED) together = memory(messages, false);
+            for (Item& i : items) {
+                const bool shares = i.kind == MESSAGE && together;
+                at::Tensor& t = i.to[p];
+                t = at::detail::make_tensor<c10::TensorImpl>(shares ? c10::Storage(together) : memory(i.bytes, true), keys, type);
+                c10::TensorImpl* const impl = t.unsafeGetTensorImpl();
+                if (shares) {
+                    impl->set_storage_offset((int64_t)(offset / sizeof(uint64_t)));
+                    offset += i.bytes;
+                }
                 impl->set_sizes_contiguous(i.shape);
-                offset[i.kind] += padded(i.bytes);
-            } else {
-                *i.to = at::detail::empty_generic(i.shape, allocator, keys, like.scalar_type(), std::nullopt);
+                i.at[p] = words(t);
             }
-            *i.at = words(*i.to);
         }
     }
 };
@@ -653,14 +658,12 @@ PyObject* norm_rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const OnStream guard(x.device(), *on);
         at::Tensor M[2], S[2], Dm[2], G[2], Z[2];
         Results results(x);
-        if (steps) {
-            results.pair(Results::MESSAGE, like, M, g.M);
-            results.pair(Results::MESSAGE, {T, H, sent}, S, g.S);
-        }
+        if (steps) results.pair(Results::MESSAGE, like, M, g.M);
         if (g.gain[0]) {
             results.pair(Results::MESSAGE, like, Dm, g.D);
             results.pair(Results::MESSAGE, {gains, D}, G, g.G);
         }
+        if (steps) results.pair(Results::MESSAGE, {T, H, sent}, S, g.S);
         results.pair(Results::RESULT, like, Z, g.Z);
         results.make();
         const int code = unlocked([&] { return comet_norm_rotate(stream, &g); });
