@@ -99,6 +99,7 @@ struct comet_ctx {
     int32_t* h_count;             // pinned and mapped: {count, error flag as the compaction kernel saw it, ticket,
                                   // error word written by a kernel whose bounded wait ran out}
     int32_t* h_count_dev;         // device-side address of h_count
+    int32_t* wait_report;         // where a kernel reports a wait that ran out, beside d_error: device-side address of h_count[3]
     int top_priority;             // the device's highest stream / launch priority (numerically lowest)
     int32_t ticket;               // sequence number of the last compaction launch (echoed in h_count[2])
     bool mask_set;
@@ -459,7 +460,7 @@ int stream_product(comet_ctx* c, const Proj& pr) {
         a.blk_label = c->d_blk_label;
     }
     a.error_flag = c->d_error;
-    a.error_host = c->h_count_dev + 3;
+    a.error_host = c->wait_report;
     cudaError_t err;
     {
         PhaseTimer timer(c, COMET_PHASE_COMBINE, 1);
@@ -667,7 +668,7 @@ int limb_combine(comet_ctx* c, const Proj& pr) {
     a.M = pr.M; a.N = pr.N; a.mt = mt; a.nt = nt; a.kb = kb;
     a.parts = c->grouped ? 0 : limb_parts(c->sm_count, 2 * mt * nt, 2 * kb);
     a.error_flag = c->d_error;
-    a.error_host = c->h_count_dev + 3;
+    a.error_host = c->wait_report;
     a.ldz = pr.N; a.bs = c->cfg.block; a.group_units = 0;
     a.groups = nullptr; a.row_map = nullptr; a.col_map = nullptr;
     a.row_label = nullptr; a.blk_label = nullptr; a.blocks = 1;
@@ -810,7 +811,7 @@ int residue_combine(comet_ctx* c, const Proj& pr, const comet::LinearEnd* end = 
     a.nt = t.nt; a.n_tile = t.n_tile;
     a.k32 = ceil_div(pr.K, 32);
     a.error_flag = c->d_error;
-    a.error_host = c->h_count_dev + 3;
+    a.error_host = c->wait_report;
     uint8_t* const left = c->planes_left.at;
     uint8_t* const right = (pr.down ? c->planes_right_dn : c->planes_right_up).at;
     comet::ResidueMaps maps;
@@ -1086,6 +1087,7 @@ int comet_init(const comet_config* cfg, void* cuda_stream, comet_ctx** out) {
     ok = ok && cudaMemsetAsync(c->d_stream_sync, 0, c->stream_sync_words * sizeof(uint32_t), c->stream) == cudaSuccess;
     ok = ok && cudaHostGetDevicePointer((void**)&c->h_masked_dev, c->h_masked, 0) == cudaSuccess;
     ok = ok && cudaHostGetDevicePointer((void**)&c->h_count_dev, c->h_count, 0) == cudaSuccess;
+    if (ok) c->wait_report = c->h_count_dev + 3;
     if (!ok) {
         cudaGetLastError();
         comet_destroy(c);
@@ -2236,8 +2238,7 @@ extern "C" int comet_linear(void* cuda_stream, const comet_linear_args* g) {
     if (g->workspace_bytes < (int64_t)need) return COMET_ERR_SHAPE;
     c->stream = (cudaStream_t)cuda_stream;
     c->top_priority = dev.top_priority;
-    c->d_error = dev.error;
-    c->h_count_dev = reinterpret_cast<int32_t*>(dev.error) - 3;       // both reports of a wait that ran out go to one word
+    c->d_error = c->wait_report = dev.error;                          // both reports of a wait that ran out go to one word
     for (int p = 0; p < 2; ++p) {
         auto in = [](const uint64_t* q) { return const_cast<u64*>(reinterpret_cast<const u64*>(q)); };   // only ever read
         c->buf[p][COMET_X] = in(g->X[p]);
