@@ -38,6 +38,7 @@ EXPORTS = (
     "comet_linear", "comet_linear_workspace", "comet_norm_rotate",
 )
 STATIC_SCRATCH_WORDS = 1 << 20
+ERR_SHAPE = -2
 ERR_SCRATCH_LIMIT = -7
 ERR_TIMEOUT = -6
 NUM_PHASES = 5
@@ -326,7 +327,7 @@ def beaver_matmul_static(X, A, Y, B, C, Z, stream: Optional[torch.cuda.Stream] =
 
 
 def static_status(stream: Optional[torch.cuda.Stream] = None) -> int:
-    """Waits for the stream; ERR_TIMEOUT if a beaver_matmul_static call on the current device gave up on a bounded
+    """Waits for the stream; ERR_TIMEOUT if a beaver_matmul_static or linear call on the current device gave up on a bounded
     wait since this was last asked (comet_static_status), else 0 = ok."""
     return _lib.comet_static_status(ctypes.c_void_p(stream.cuda_stream if stream is not None else 0))
 
@@ -414,7 +415,8 @@ def add_bias(Z, bias, stream: Optional[torch.cuda.Stream] = None):
 def linear_workspace(tokens: int, inner: int, cols: int) -> int:
     """Bytes that `linear` takes for the length of a call on the current device (comet_linear_workspace)."""
     out = ctypes.c_int64(0)
-    code = _lib.comet_linear_workspace(tokens, inner, cols, ctypes.byref(out))
+    held = all(0 <= n < 1 << 31 for n in (tokens, inner, cols))          # ctypes would cut a larger one to 32 bits
+    code = _lib.comet_linear_workspace(tokens, inner, cols, ctypes.byref(out)) if held else ERR_SHAPE
     if code != OK:
         raise CometError(code, "comet_linear_workspace")
     return out.value
