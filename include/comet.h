@@ -467,17 +467,18 @@ int comet_beaver_mul(void* cuda_stream, const uint64_t* const X[2], const uint64
  * comparison -- on the dealer's pair (R, Q), Q = R * R element by element:
  *     M_i = y_i - R_i                                                       (message),  m = M_0 + M_1
  *     y_i <- trunc_f(k2 trunc_f(Q_i + 2 m R_i + i m^2) + k1 y_i) + i k0
- * then, with a residual, Y_i = y_i + residual_i.  trunc_f is comet_truncate's rule.
+ * then, with a residual, Y_i = y_i + residual_i.  trunc_f is comet_truncate's rule, off by one unit at most but for a wrap of
+ * the shares: one word in 2^64 / |z|, z the number before it at scale 2f, and that word is then off by 2^(64 - f).
  *
  * Stateless; X, A, E are [tokens, inner], W, B, F [cols, inner] (output-feature-major), C, residual, R, Q, M, Y
  * [tokens, cols], bias [cols], each pair the two parties'; DEVICE pointers on the current device, 16-byte aligned,
  * owned by the caller.  bias and residual may be null (both parties' or neither's).  k[0..2] are the coefficients as
  * ring words at scale f.  What is written (E, F, M, Y and the workspace) must not overlap any other argument.
- * The work is enqueued on `cuda_stream` (NULL = default stream) and the call does not wait for it.  One row, and up to
- * four of a small layer, take one launch on the integer ALUs; up to 32 rows, and up to 64 of a layer of 786432 weights or
- * more, the product streams the weights (COMET_KERNEL_STREAM); beyond, it goes through operand planes (COMET_KERNEL_LIMB
- * or COMET_KERNEL_RESIDUE).  `workspace` is 256-byte aligned and has at least the bytes that comet_linear_workspace
- * reports for these sizes on this device (none for some).  A captured call keeps its workspace's address; calls whose
+ * The work is enqueued on `cuda_stream` (NULL = default stream) and the call does not wait for it.  One row up to 4096 deep
+ * (less than 64 deep: of up to 8192 features), and up to four of a small layer, take one launch on the integer ALUs; else up
+ * to 32 rows, and up to 64 of a layer of 786432 weights or more, the product streams the weights (COMET_KERNEL_STREAM); beyond, it
+ * goes through operand planes (COMET_KERNEL_LIMB or COMET_KERNEL_RESIDUE).  `workspace` is 256-byte aligned and has at least the
+ * bytes that comet_linear_workspace reports for these sizes on this device; that call alone says whether there are any.  A captured call keeps its workspace's address; calls whose
  * work may overlap in time need one each.
  * The kernels' waits are bounded: comet_static_status says whether one ran out.  The first call on a device makes
  * settings once; make it outside stream capture.
@@ -528,6 +529,11 @@ int comet_linear_workspace(int32_t tokens, int32_t inner, int32_t cols, int64_t*
  * 0 < guess^2 s < 3 (as real numbers); far below the root y grows by half in every step, and at the end the error is squared, so
  * s in (1/8, 8) with a guess of 0.55 takes some eight steps.  Where it does not converge the words are still the ones that
  * the formulas above give.
+ * A local division is off by one unit at most but for a wrap of the shares, one case in 2^64 / |z|, z the number that is
+ * divided.  Where a row's sum of squares wraps the whole row is lost, and z is large there: dim * mean(x^2) * 2^(2f), so with dim 4096
+ * and f = 16 about one row in 2^20 / mean(x^2), with heads of 128 one in 2^25 / mean(x^2).  The other divisions are of numbers
+ * of the size of their results at scale 2f (f = 16: one in some 2^32); those of a row's own numbers lose the row, those of its
+ * words one word or a pair each.
  *
  * From the dealer, per row: row_words, 6 steps - 3 words: sum U^2; the mask a of s; for each of the steps - 1 rounds of
  * Newton's the mask of y, its square, the mask of p, its product with a, the mask of w, its product with that of y; the

@@ -767,6 +767,10 @@ size_t residue_room(int rows, int cols) {
 // With the 5 % asked for, none of the 19 that go through residues is slower for it; of the 117 others three lose 5 % or more, the
 // wide and shallow ones, whose time per result word through limbs is understated: 512 x 4096 columns x 512 deep 152 and 130 us,
 // 384 x 4096 x 512 123 and 117, 256 x 2048 x 4096 278 and 264.
+// Linear layers, whose epilogue is a pass of its own behind the limbs: of 25 sizes, 96 to 512 rows, none is slower through residues
+// where they are taken, with bias alone or with everything.  Through limbs four lose 5 % or more with bias alone: rows x depth x
+// columns, limbs and residues, 512 x 1024 x 1024 71 and 64, 512 x 512 x 4096 141 and 126, 512 x 512 x 2048 75 and 70, 256 x 2048 x 4096 285 and 264; with
+// everything two of them, 77 and 71, 162 and 154, 85 and 84, 299 and 277.
 bool residues_pay(int sm_count, int M, int N, int K) {
     namespace lb = comet::limb;
     const int64_t operands = (int64_t)(M + N) * K, results = (int64_t)M * N;
@@ -2079,18 +2083,24 @@ bool linear_sizes(int64_t T, int64_t K, int64_t N) {
     return tiles * steps <= 0x7fffffffll / 8;
 }
 
-// The kernel for few rows beats the planes up to 64 rows where a layer has STREAM_WORDS of weights in two products (see there).
+// The kernel for few rows beats the planes up to 64 rows where a layer has STREAM_WORDS of weights in two products (see there).  Linear
+// layers with bias, depth x features, streaming / planes, us: 33 rows, 1024 x 512 20.1 / 20.5, 1024 x 768 24.2 / 24.6, 2048 x 512 30.0 / 30.4, 2048 x 2048
+// 75.8 / 95.9, 4096 x 4096 270 / 363; 48 rows, 1024 x 512 21.5 either way, 1024 x 768 26.6 / 25.3, 2048 x 512 31.4 / 31.1, 1024 x 2048 44.7 / 53.6, 4096 x 4096
+// 272 / 365; 64 rows, 1024 x 512 23.9 / 22.5, 1024 x 768 27.3 / 25.6, 2048 x 512 33.5 / 32.4, 1024 x 2048 46.4 / 54.3, 4096 x 4096 272 / 368; 96 rows, 2048 x 2048
+// 104 / 99.7, 4096 x 4096 393 / 379.  So from 48 rows on the smallest layers beyond the line lose up to 7 % by it.
 bool linear_streams(int64_t T, int64_t K, int64_t N) {
     return T <= comet::limb_stream::BT || (T <= STREAM_TOKENS && 2 * K * N >= STREAM_WORDS);
 }
 
 // Whether a layer of a few rows goes through linear_rows_kernel.  A token's multiply-adds on the ALUs cost it time beside the loads from
-// the second row on, and every chunk of the contraction index a staging of the rows; what it saves is two launches and the streaming
-// kernel's latency.  This kernel and the streaming kernel with its two passes, us: one row, 64 x 64 5.5 and 9.2, 768 x 768 11.3 and 14.7,
-// 1000 x 1364 16.4 and 23.2, 2048 x 2048 41.0 and 41.6, 4096 x 4096 140.6 and 139.3, 4096 x 11008 359 and 356; two rows, 512 x 512 8.5
-// and 12.6, 1024 x 768 18.1 and 18.8, 1536 x 768 20.8 and 19.5, 2048 x 128 14.0 and 12.6; four rows, 256 x 96 6.8 and 10.2, 512 x 256 10.6
-// either way, 512 x 512 12.6 either way, 768 x 512 15.4 and 13.3.  Nothing is gained on deeper layers (one row, 11008 x 4096 365 and
-// 354, 11008 x 64 30 and 17), nor where a feature does not fill a warp and there are many (24 x 50000 48 and 24).
+// the second row on, and every chunk of the contraction index a staging of the rows; what it saves is one launch, or two where the streaming
+// kernel does not leave its sums in parts, and that kernel's latency.  This kernel / the streaming kernel with its pass or passes, us, depth x
+// features: one row, 64 x 64 5.1 / 8.5, 768 x 768 10.9 / 15.0, 1000 x 1364 16.1 / 22.9, 2048 x 2048 40.6 / 41.3, 4096 x 4096 141 / 139, 4096 x 11008 356 / 359, 2048 x 50272
+// 777 / 785; two rows, 512 x 512 8.5 / 12.3, 512 x 2048 14.7 / 17.8, 1024 x 256 11.6 / 13.3, 1024 x 768 18.1 / 18.4; four rows, 256 x 96 6.8 / 8.8, 128 x 1024
+// 7.5 / 10.6, 384 x 256 8.5 / 9.9.  It loses a little next to its borders: one row, 4096 x 64 14.0 / 12.3, 4096 x 128 15.0 / 14.0, but 4096 x 256 18.1 / 18.8; two
+// rows, 1024 x 512 15.7 / 14.7, 1024 x 1024 19.8 / 18.1; four rows, 512 x 256 10.6 / 10.2.  Beyond them: one row, 11008 x 4096 373 / 354, 11008 x 64 31 / 18; two rows,
+// 1536 x 768 20.8 / 18.8, 2048 x 128 14.3 / 12.6; four rows, 512 x 512 12.6 / 12.3, 768 x 512 15.7 / 13.7; where a feature does not fill a warp and there are many,
+// 24 x 50000 47 / 24.
 bool linear_in_rows(int64_t T, int64_t K, int64_t N) {
     if (K < 64 && N > 8192) return false;
     if (T <= 2) return T == 1 ? K <= 4096 : K <= 1024 && K * N <= 1 << 20;

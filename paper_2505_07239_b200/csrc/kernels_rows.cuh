@@ -6,8 +6,8 @@
 // What bounds it: memory, 24 bytes per weight word and party (W_i and B_i in, F_i out); a weight word takes part in four 64-bit
 // multiply-adds per token, which the integer ALUs do beside the loads for a few tokens.  No limb planes, no accumulators in tensor
 // memory and no partial sums in Z: a CTA has its features' sums to itself, so the bias, the truncation, the activation and the
-// residual follow in the same launch.  The streaming kernel (kernels_stream.cuh) takes three launches for the same, and 9 us from its
-// first load to its last sum however small the layer.
+// residual follow in the same launch.  The streaming kernel (kernels_stream.cuh) takes two launches for the same, three where its
+// sums do not lie in parts, and 8.5 us however small the layer.
 //
 // Measured: one row, 4096 x 4096 139 us, 0.88 of the copy rate; 768 x 768 11.3 us, of which 2.5 are the launch, 4.3 the bytes.  From the
 // second row on the multiply-adds show (4096 x 4096: 145 us, four rows 197): comet_api.cu has the rule, with both sides' times.
