@@ -582,6 +582,152 @@ typedef struct {
 int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args* args);
 
 /* ---------------------------------------------------------------------------
+ * Linear attention with a decay for every head, for both parties: attention without a softmax, which additive shares evaluate
+ * without a comparison.  Composed of Section 2.1's "Multiplication" and "Addition"; tr is the local truncation by f bits, w[n] the
+ * public n-th power of a key head's decay at scale f; query head h meets key head h / (q_heads / kv_heads).
+ *
+ * A prompt.  `sequences` sequences of any lengths, zero among them, lie behind one another in the tokens: sequence j is the tokens
+ * from starts[j] to before starts[j + 1].  Each is cut into chunks of `chunk` tokens, the last one shorter; the chunks of all sequences, in
+ * that order, are numbered from 0, and `chunks` is their number.  Of a chunk of L tokens r, s = 0 .. L - 1 that finds the state S [k_dim, v_dim]:
+ *     Eq = q - mq, Ek = k - mk, Ev = v - mv                                    (messages, party by party)
+ *     P[r][s] = tr(w[r - s] tr(q_r . k_s)) for s <= r, Ep = P - mp (message, zero for s > r and s >= L), Es = S - ms (message)
+ *     O_r = tr(sum_{s <= r} P[r][s] v_s + w[r + 1] tr(q_r S))
+ *     d_s = tr(w[L - 1 - s] k_s), Ed = d - md (message);   S <- tr(w[L] S + sum_s d_s v_s^T)
+ * every product by Eq. 1.  From the dealer, beside the masks m*: qk[r][s] = mq_r . mk_s, pv_r = sum_{s <= r} mp[r][s] mv_s, qs_r = mq_r ms,
+ * dv = sum_s md_s mv_s^T.  Words of qk, mp off the triangle are ignored.
+ * Single tokens, one for every sequence of a batch:  S <- tr(w S + k v^T), Es = S - ms (message), o = tr(q S), with the dealer's
+ * kv = mk mv^T and qs = mq ms.  The state of a prompt may be continued token by token and the other way round.
+ * A truncation is off by one unit at most but for a wrap of the shares: one word in 2^64 / |z|, z the number before it at scale 2f.
+ *
+ * Shapes: Q [tokens, q_heads, k_dim], K [tokens, kv_heads, k_dim], V [tokens, kv_heads, v_dim], a token's heads together, tokens
+ * q_stride, k_stride, v_stride words apart; their masks and messages and md, Ed (as K) the same, dense; mp, qk, Ep [tokens, q_heads,
+ * chunk]; pv, qs, O [tokens, q_heads, v_dim]; ms, dv, Es [chunks, kv_heads, k_dim, v_dim]; state, state_out [sequences, kv_heads, k_dim,
+ * v_dim]; decay [kv_heads, chunk + 1] (single tokens: [kv_heads], w[1] alone); starts [sequences + 1].  `state` may be null: zero.
+ * `state_out` may be `state`, word for word; nothing else that is written may overlap another argument.
+ * Rows of tokens that are in no sequence stay as they are in every result.  Where the starts are not ascending or leave the tokens, that
+ * sequence counts as empty; where the chunks are more than `chunks` the surplus ones are not worked out; either way, and where they are
+ * fewer, `bad_starts_flag` (device int32, may be null) is set to 1.  The caller clears the flag.
+ * Stateless; DEVICE pointers on the current device, owned by the caller, 8-byte aligned.  The work is enqueued on `cuda_stream` (NULL =
+ * default stream) and the call does not wait for it.  `workspace` is 256-byte aligned and has at least the bytes that
+ * comet_linear_attention_workspace reports for these sizes; a captured call keeps its address, and calls whose work may overlap in
+ * time need one each.
+ * Errors: INVALID_ARG (null or unaligned pointer, overlap), SHAPE (a size below 1, but for chunks; kv_heads not a divisor of q_heads; k_dim or v_dim
+ * odd or above 256; chunk above 64; tokens, sequences or chunks above 2^20; tokens * q_heads or chunks * q_heads above 2^24; batch *
+ * q_heads above 2^24; a stride below its heads' words or above 2^32; frac_bits outside [1, 31]; workspace too small), CUDA. */
+typedef struct {
+    int32_t tokens, sequences, q_heads, kv_heads, k_dim, v_dim, chunk, chunks;
+    int64_t q_stride, k_stride, v_stride;
+    int32_t frac_bits;
+    const int32_t* starts;
+    const uint64_t* decay;
+    const uint64_t* Q[2];
+    const uint64_t* K[2];
+    const uint64_t* V[2];
+    const uint64_t* mq[2];
+    const uint64_t* mk[2];
+    const uint64_t* mv[2];
+    const uint64_t* md[2];
+    const uint64_t* mp[2];
+    const uint64_t* ms[2];          /* ms, dv, Es: may be null where chunks is 0           */
+    const uint64_t* qk[2];
+    const uint64_t* pv[2];
+    const uint64_t* qs[2];
+    const uint64_t* dv[2];
+    const uint64_t* state[2];       /* may be null                                         */
+    uint64_t* Eq[2];
+    uint64_t* Ek[2];
+    uint64_t* Ev[2];
+    uint64_t* Ed[2];
+    uint64_t* Ep[2];
+    uint64_t* Es[2];
+    uint64_t* O[2];
+    uint64_t* state_out[2];
+    int32_t* bad_starts_flag;
+    void* workspace;
+    int64_t workspace_bytes;
+} comet_linear_attention_args;
+int comet_linear_attention(void* cuda_stream, const comet_linear_attention_args* args);
+/* Bytes of workspace that comet_linear_attention takes for these sizes.  Errors: INVALID_ARG, SHAPE. */
+int comet_linear_attention_workspace(int32_t chunks, int32_t kv_heads, int32_t k_dim, int32_t v_dim, int64_t* bytes_out);
+
+typedef struct {
+    int32_t batch, q_heads, kv_heads, k_dim, v_dim;
+    int64_t q_stride, k_stride, v_stride;
+    int32_t frac_bits;
+    const uint64_t* decay;
+    const uint64_t* Q[2];
+    const uint64_t* K[2];
+    const uint64_t* V[2];
+    const uint64_t* mq[2];
+    const uint64_t* mk[2];
+    const uint64_t* mv[2];
+    const uint64_t* ms[2];
+    const uint64_t* kv[2];
+    const uint64_t* qs[2];
+    const uint64_t* state[2];       /* may be null                                         */
+    uint64_t* Eq[2];
+    uint64_t* Ek[2];
+    uint64_t* Ev[2];
+    uint64_t* Es[2];
+    uint64_t* O[2];
+    uint64_t* state_out[2];
+} comet_linear_attention_step_args;
+int comet_linear_attention_step(void* cuda_stream, const comet_linear_attention_step_args* args);
+
+/* ---------------------------------------------------------------------------
+ * Norm of groups of neighbouring channels, channels last, with gain, bias and quadratic activation, for both parties: of every sample and
+ * group the n = positions * channels / groups words of its positions and channels, at scale f.  positions = 1 is the norm of every head
+ * of a token (behind comet_linear_attention, say), groups = 1 that of a whole row.  Composed as comet_norm_rotate; sums run over the n words:
+ *     d_i = x_i - div_n(sum x_i),  M_i = d_i - U_i (message), m = M_0 + M_1
+ *     sq_i = words[0] + sum 2 m U_i + i sum m^2,  s_i = div_{n 2^f}(sq_i) + i eps,  y ~ 1 / sqrt(s) as in comet_norm_rotate from `guess`
+ *   with a gain, of every channel c:  t_c = tr(y gain_c) by Eq. 1 with VW,  D = t - T, G = gain - gain_mask (messages);  without: t = y, T = v
+ *     z = tr(t_c d + 2^f bias_c) by Eq. 1 with UT
+ *   with `quadratic`, on the dealer's pair (R, Q), Q = R * R:  N_i = z_i - R_i (message), z <- tr(k2 tr(z^2) + k1 z) + k0
+ * From the dealer, per group: words, 6 steps - 3, as comet_norm_rotate's row_words (words[0] = sum U^2, the last one v); UT = U T; T the masks of
+ * the t; VW = v gain_mask.  S: a group's openings, 3 steps - 1, as there.  Newton's convergence and the odds of a wrap are as there,
+ * too: with n words and a mean square of 1 a group is lost once in 2^(64 - 2f) / n.
+ * Shapes: X [samples, positions, channels], positions x_stride words apart; U, UT, M, R, Q, N, Z the same, dense; words, S [samples,
+ * groups, ...]; gain, gain_mask, bias, G [channels]; T, VW, D [samples, channels].
+ * Stateless; DEVICE pointers on the current device, owned by the caller, 8-byte aligned; what is written must not overlap any other
+ * argument.  The work is enqueued on `cuda_stream` and the call does not wait for it.  `workspace` is 256-byte aligned and has at least the
+ * bytes that comet_group_norm_workspace reports for these sizes on this device (often none); a captured call keeps its address, and calls
+ * whose work may overlap in time need one each.  The first call on a device makes settings once; make it outside stream capture.
+ * Errors: INVALID_ARG (null or unaligned pointer, overlap, a gain without its bias, a `quadratic` that is neither 0 nor 1), SHAPE
+ * (a size below 1, channels not a multiple of groups, a group of more than 2^24 words, more than 2^24 groups of all samples, channels above
+ * 2^20, x_stride below channels or above 2^32, steps outside 2..24, guess outside [1, 2^32), frac_bits outside [1, 31], workspace too small), CUDA. */
+typedef struct {
+    int32_t samples, positions, channels, groups;
+    int64_t x_stride;
+    int32_t frac_bits;
+    int32_t steps;
+    uint64_t guess, eps;
+    int32_t quadratic;
+    uint64_t k[3];
+    const uint64_t* X[2];
+    const uint64_t* U[2];
+    const uint64_t* words[2];
+    const uint64_t* UT[2];
+    const uint64_t* gain[2];        /* gain .. bias, D, G: null without a gain              */
+    const uint64_t* gain_mask[2];
+    const uint64_t* T[2];
+    const uint64_t* VW[2];
+    const uint64_t* bias[2];
+    const uint64_t* R[2];           /* R, Q, N: with `quadratic` only                       */
+    const uint64_t* Q[2];
+    uint64_t* M[2];
+    uint64_t* S[2];
+    uint64_t* D[2];
+    uint64_t* G[2];
+    uint64_t* N[2];
+    uint64_t* Z[2];
+    void* workspace;
+    int64_t workspace_bytes;
+} comet_group_norm_args;
+int comet_group_norm(void* cuda_stream, const comet_group_norm_args* args);
+/* Bytes of workspace that comet_group_norm takes for these sizes on the current device.  Errors: INVALID_ARG, SHAPE, CUDA. */
+int comet_group_norm_workspace(int32_t samples, int32_t positions, int32_t channels, int32_t groups, int64_t* bytes_out);
+
+/* ---------------------------------------------------------------------------
  * Allocation-free Pi_MatMul.  (The paper has no counterpart; this exists for
  * deployment reasons only.)
  *

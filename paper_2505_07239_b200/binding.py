@@ -35,7 +35,8 @@ EXPORTS = (
     "comet_beaver_mul", "comet_set_token_mask", "comet_get_components", "comet_kv_plan",
     "comet_add_bias", "comet_bind_shares", "comet_truncate_pair", "comet_synchronize", "comet_inject_timeout",
     "comet_pipe_probe", "comet_device_pointer", "comet_static_status", "comet_static_inject_timeout",
-    "comet_linear", "comet_linear_workspace", "comet_norm_rotate",
+    "comet_linear", "comet_linear_workspace", "comet_norm_rotate", "comet_linear_attention",
+    "comet_linear_attention_workspace", "comet_linear_attention_step", "comet_group_norm", "comet_group_norm_workspace",
 )
 STATIC_SCRATCH_WORDS = 1 << 20
 ERR_SHAPE = -2
@@ -72,6 +73,28 @@ class CometNormRotateArgs(ctypes.Structure):
             "X", "U", "row_words", "UV", "gain", "gain_mask", "A", "C")] + [
         (n, ctypes.c_void_p) for n in ("cos", "sin", "positions")] + [(n, ctypes.c_void_p * 2) for n in ("M", "S", "D", "G", "Z")] + [
         ("bad_index_flag", ctypes.c_void_p)]
+
+
+class CometLinearAttentionArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "sequences", "q_heads", "kv_heads", "k_dim", "v_dim", "chunk", "chunks")] + [
+        (n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride")] + [("frac_bits", ctypes.c_int32)] + [
+        (n, ctypes.c_void_p) for n in ("starts", "decay")] + [(n, ctypes.c_void_p * 2) for n in (
+            "Q", "K", "V", "mq", "mk", "mv", "md", "mp", "ms", "qk", "pv", "qs", "dv", "state", "Eq", "Ek", "Ev", "Ed", "Ep", "Es", "O",
+            "state_out")] + [("bad_starts_flag", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
+
+
+class CometLinearAttentionStepArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "q_heads", "kv_heads", "k_dim", "v_dim")] + [
+        (n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride")] + [("frac_bits", ctypes.c_int32), ("decay", ctypes.c_void_p)] + [
+        (n, ctypes.c_void_p * 2) for n in ("Q", "K", "V", "mq", "mk", "mv", "ms", "kv", "qs", "state", "Eq", "Ek", "Ev", "Es", "O", "state_out")]
+
+
+class CometGroupNormArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("samples", "positions", "channels", "groups")] + [("x_stride", ctypes.c_int64)] + [
+        (n, ctypes.c_int32) for n in ("frac_bits", "steps")] + [(n, ctypes.c_uint64) for n in ("guess", "eps")] + [
+        ("quadratic", ctypes.c_int32), ("k", ctypes.c_uint64 * 3)] + [(n, ctypes.c_void_p * 2) for n in (
+            "X", "U", "words", "UT", "gain", "gain_mask", "T", "VW", "bias", "R", "Q", "M", "S", "D", "G", "N", "Z")] + [
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
 
 
 class CometError(RuntimeError):
@@ -127,6 +150,11 @@ def _load():
     lib.comet_linear.argtypes = [vp, ctypes.POINTER(CometLinearArgs)]
     lib.comet_linear_workspace.argtypes = [i32, i32, i32, ctypes.POINTER(i64)]
     lib.comet_norm_rotate.argtypes = [vp, ctypes.POINTER(CometNormRotateArgs)]
+    lib.comet_linear_attention.argtypes = [vp, ctypes.POINTER(CometLinearAttentionArgs)]
+    lib.comet_linear_attention_workspace.argtypes = [i32, i32, i32, i32, ctypes.POINTER(i64)]
+    lib.comet_linear_attention_step.argtypes = [vp, ctypes.POINTER(CometLinearAttentionStepArgs)]
+    lib.comet_group_norm.argtypes = [vp, ctypes.POINTER(CometGroupNormArgs)]
+    lib.comet_group_norm_workspace.argtypes = [i32, i32, i32, i32, ctypes.POINTER(i64)]
     return lib
 
 
@@ -489,3 +517,122 @@ def norm_rotate(X, frac_bits: int, norm: Optional[Norm] = None, gain: Optional[G
     if code:
         raise CometError(code, "comet_norm_rotate")
     return NormMessages(M, S, D, G), Z
+
+
+class PromptDealer(NamedTuple):
+    """Dealer's material of a prompt (comet_linear_attention), pairs: the masks q [T, Hq, Dk], k [T, Hk, Dk], v [T, Hk, Dv], d (of the decayed
+    keys) [T, Hk, Dk], p (of the weights) [T, Hq, C], s (of the states) [chunks, Hk, Dk, Dv], and the products of masks qk [T, Hq, C], pv, qs
+    [T, Hq, Dv], dv [chunks, Hk, Dk, Dv]."""
+    q: Any
+    k: Any
+    v: Any
+    d: Any
+    p: Any
+    s: Any
+    qk: Any
+    pv: Any
+    qs: Any
+    dv: Any
+
+
+class PromptMessages(NamedTuple):
+    """What a party sends: its shares of q, k, v, of the decayed keys d, the weights p and the states s, minus their masks; pairs."""
+    q: Any
+    k: Any
+    v: Any
+    d: Any
+    p: Any
+    s: Any
+
+
+def linear_attention(Q, K, V, starts, decay, dealer: PromptDealer, frac_bits: int, state=None, stream: Optional[torch.cuda.Stream] = None,
+                     bad_starts_flag=None):
+    """Linear attention with a decay for every head over packed prompts (comet_linear_attention), both parties.
+
+    Q [T, Hq, Dk], K [T, Hk, Dk], V [T, Hk, Dv]: pairs of CUDA tensors of 64-bit integers, a token's heads together, tokens may lie further
+    apart (views of a stacked projection's result); Hk divides Hq; Dk and Dv are even, at most 256.  starts: int32 [sequences + 1] on the
+    GPU, sequence j the tokens from starts[j] to before starts[j + 1].  decay: public powers [Hk, C + 1] at scale f, of exponents 0 to C; C, at most 64,
+    is the length of a chunk.  state: None (zero) or a pair [sequences, Hk, Dk, Dv].
+    Returns (PromptMessages, O, state behind the last tokens): new tensors, each share of a result in memory of its own; a party's messages
+    may lie together in one piece, none of the other party's words in it.  Rows of tokens in no sequence are not written.
+    """
+    code, *m, O, S = _native.linear_attention(stream, Q, K, V, starts, decay, dealer, frac_bits, state, bad_starts_flag)
+    if code:
+        raise CometError(code, "comet_linear_attention")
+    return PromptMessages(*m), O, S
+
+
+class StepDealer(NamedTuple):
+    """Dealer's material of a token for every sequence (comet_linear_attention_step), pairs: the masks q [B, Hq, Dk], k [B, Hk, Dk],
+    v [B, Hk, Dv], s (of the new state) [B, Hk, Dk, Dv], and the products of masks kv [B, Hk, Dk, Dv], qs [B, Hq, Dv]."""
+    q: Any
+    k: Any
+    v: Any
+    s: Any
+    kv: Any
+    qs: Any
+
+
+class StepMessages(NamedTuple):
+    """What a party sends: its shares of q, k, v and the new state s, minus their masks; pairs."""
+    q: Any
+    k: Any
+    v: Any
+    s: Any
+
+
+def linear_attention_step(Q, K, V, decay, state, dealer: StepDealer, frac_bits: int, stream: Optional[torch.cuda.Stream] = None):
+    """One token for every sequence of a batch (comet_linear_attention_step), both parties: S <- decay S + k v^T, o = q S.
+
+    Q [B, Hq, Dk], K [B, Hk, Dk], V [B, Hk, Dv] as for linear_attention, a row per sequence; decay: public, [Hk] at scale f; state: a pair
+    [B, Hk, Dk, Dv], or None for zero.  Returns (StepMessages, O, new state), new tensors as linear_attention's.
+    """
+    code, *m, O, S = _native.linear_attention_step(stream, Q, K, V, decay, state, dealer, frac_bits)
+    if code:
+        raise CometError(code, "comet_linear_attention_step")
+    return StepMessages(*m), O, S
+
+
+class GroupNorm(NamedTuple):
+    """Dealer's material and public numbers of a norm of channel groups (comet_group_norm): pairs U [S, P, C] (masks), words [S, groups,
+    6 steps - 3] (a group's own), UT [S, P, C] (U times the mask of what it meets); Newton's steps, its first guess and eps, both at scale f."""
+    U: Any
+    words: Any
+    UT: Any
+    steps: int
+    guess: int
+    eps: int = 0
+
+
+class GroupGain(NamedTuple):
+    """Shared gain and bias of every channel with the gain's material: pairs weight, mask, bias [C]; T (masks of gain times root), VW (mask of the
+    root times mask of the gain) [S, C]."""
+    weight: Any
+    mask: Any
+    T: Any
+    VW: Any
+    bias: Any
+
+
+class GroupNormMessages(NamedTuple):
+    """What a party sends: M (the words without their mean), S (a group's openings), D and G (the gain's), N (the activation's); pairs, or None
+    where the part is absent."""
+    M: Any
+    S: Any
+    D: Any
+    G: Any
+    N: Any
+
+
+def group_norm(X, groups: int, frac_bits: int, norm: GroupNorm, gain: Optional[GroupGain] = None, act=None,
+               stream: Optional[torch.cuda.Stream] = None):
+    """Norm of groups of neighbouring channels over all positions of a sample, gain, bias and quadratic activation (comet_group_norm).
+
+    X: a pair of CUDA tensors of 64-bit integers [samples, positions, channels], positions may lie further apart; positions = 1 norms
+    groups of a token's channels, heads for instance.  act: None, or ((k0, k1, k2), R, Q) for k2 z^2 + k1 z + k0 with coefficients at scale f
+    and the dealer's Q = R * R.  Returns (GroupNormMessages, Z): new tensors as norm_rotate's.
+    """
+    code, *m, Z = _native.group_norm(stream, X, groups, frac_bits, norm, gain, act)
+    if code:
+        raise CometError(code, "comet_group_norm")
+    return GroupNormMessages(*m), Z

@@ -15,6 +15,8 @@
 
 #include <cuda_runtime.h>
 
+#include "kernels_attention.cuh"
+#include "kernels_group.cuh"
 #include "kernels_limb.cuh"
 #include "kernels_linear.cuh"
 #include "kernels_mul.cuh"
@@ -2454,6 +2456,241 @@ extern "C" int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args
     }
     const unsigned quads = (unsigned)ceil_div(a.dim, 4);
     return launch_pass(aligned && a.half % 2 == 0 ? comet::rotate_kernel<true> : comet::rotate_kernel<false>, dim3(shuffle_grid(rows * quads)), stream, a, quads);
+}
+
+// ---------------------------------------------------------------------------
+// Linear attention with a decay for every head: prompts in chunks, single tokens.  Stateless; the workspace is the caller's.
+// ---------------------------------------------------------------------------
+namespace {
+
+constexpr int64_t ATTN_MAX_SIZE = 1 << 20, ATTN_MAX_ROWS = 1 << 24;
+
+bool attn_heads(int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim) {
+    namespace at = comet::attn;
+    return q_heads >= 1 && kv_heads >= 1 && q_heads <= ATTN_MAX_SIZE && q_heads % kv_heads == 0 && k_dim >= 2 && v_dim >= 2 && k_dim % 2 == 0 &&
+           v_dim % 2 == 0 && k_dim <= at::MAX_DIM && v_dim <= at::MAX_DIM;
+}
+bool attn_stride(int64_t stride, int64_t tokens, int64_t row) { return stride >= 0 && stride <= 1ll << 32 && (tokens == 1 || stride >= row); }
+size_t attn_workspace(int64_t chunks, int64_t kv_heads, int64_t k_dim, int64_t v_dim) { return (size_t)(2 * chunks * kv_heads * k_dim * v_dim) * sizeof(u64); }
+
+// A pair of arguments: where it is, its words, whether it may be absent.
+struct SpanPair {
+    const uint64_t* const* p;
+    int64_t words;
+    bool optional;
+    SpanPair(const uint64_t* const q[2], int64_t n, bool may_miss = false) : p(q), words(n), optional(may_miss) {}
+    SpanPair(uint64_t* const q[2], int64_t n, bool may_miss = false) : p(const_cast<const uint64_t* const*>(q)), words(n), optional(may_miss) {}
+};
+// Whether every pair is there (both parties' or, where that is allowed, neither's; pairs without words need not be) and 8-byte aligned,
+// and gathers the spans, those without words as empty ones.
+bool span_pairs(std::initializer_list<SpanPair> pairs, std::vector<Span>& spans) {
+    for (const SpanPair& s : pairs) {
+        if (s.words > 0 && (s.optional ? pair_halved(s.p) : pair_missing(s.p))) return false;
+        for (int i = 0; i < 2; ++i) {
+            if (reinterpret_cast<uintptr_t>(s.p[i]) % sizeof(u64)) return false;
+            spans.emplace_back(s.words > 0 ? s.p[i] : nullptr, s.words);
+        }
+    }
+    return true;
+}
+void give(const u64* to[2], const uint64_t* const from[2]) {
+    for (int i = 0; i < 2; ++i) to[i] = reinterpret_cast<const u64*>(from[i]);
+}
+void give(u64* to[2], uint64_t* const from[2]) {
+    for (int i = 0; i < 2; ++i) to[i] = reinterpret_cast<u64*>(from[i]);
+}
+
+}  // namespace
+
+extern "C" int comet_linear_attention_workspace(int32_t chunks, int32_t kv_heads, int32_t k_dim, int32_t v_dim, int64_t* bytes_out) {
+    if (!bytes_out) return COMET_ERR_INVALID_ARG;
+    if (chunks < 0 || chunks > ATTN_MAX_SIZE || !attn_heads(kv_heads, kv_heads, k_dim, v_dim) || (int64_t)chunks * kv_heads > ATTN_MAX_ROWS)
+        return COMET_ERR_SHAPE;
+    *bytes_out = (int64_t)attn_workspace(chunks, kv_heads, k_dim, v_dim);
+    return COMET_OK;
+}
+
+extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_attention_args* g) {
+    namespace at = comet::attn;
+    if (!g) return COMET_ERR_INVALID_ARG;
+    if (!attn_heads(g->q_heads, g->kv_heads, g->k_dim, g->v_dim) || g->chunk < 1 || g->chunk > at::MAX_CHUNK) return COMET_ERR_SHAPE;
+    if (g->tokens < 1 || g->sequences < 1 || g->chunks < 0 || g->tokens > ATTN_MAX_SIZE || g->sequences > ATTN_MAX_SIZE || g->chunks > ATTN_MAX_SIZE)
+        return COMET_ERR_SHAPE;
+    const int64_t T = g->tokens, n = g->chunks, Hq = g->q_heads, Hk = g->kv_heads, Dk = g->k_dim, Dv = g->v_dim;
+    if (T * Hq > ATTN_MAX_ROWS || n * Hq > ATTN_MAX_ROWS || g->sequences * Hk > ATTN_MAX_ROWS) return COMET_ERR_SHAPE;
+    if (!attn_stride(g->q_stride, T, Hq * Dk) || !attn_stride(g->k_stride, T, Hk * Dk) || !attn_stride(g->v_stride, T, Hk * Dv)) return COMET_ERR_SHAPE;
+    if (g->frac_bits < 1 || g->frac_bits > 31) return COMET_ERR_SHAPE;
+    if (!g->starts || !g->decay || reinterpret_cast<uintptr_t>(g->starts) % sizeof(int32_t) || reinterpret_cast<uintptr_t>(g->decay) % sizeof(u64) ||
+        reinterpret_cast<uintptr_t>(g->bad_starts_flag) % sizeof(int32_t) || reinterpret_cast<uintptr_t>(g->workspace) % LINEAR_ALIGN || g->workspace_bytes < 0)
+        return COMET_ERR_INVALID_ARG;
+    const int64_t q = T * Hq * Dk, k = T * Hk * Dk, v = T * Hk * Dv, p = T * Hq * g->chunk, o = T * Hq * Dv, s = n * Hk * Dk * Dv;
+    const int64_t st = g->sequences * Hk * Dk * Dv;
+    std::vector<Span> spans;
+    spans.reserve(64);
+    spans.emplace_back(g->bad_starts_flag, 1, sizeof(int32_t));
+    spans.emplace_back(g->workspace, g->workspace_bytes, 1);
+    if (!span_pairs({{g->Eq, q}, {g->Ek, k}, {g->Ev, v}, {g->Ed, k}, {g->Ep, p}, {g->Es, s}, {g->O, o}, {g->state_out, st}}, spans)) return COMET_ERR_INVALID_ARG;
+    const int outputs = (int)spans.size();
+    spans.emplace_back(g->starts, g->sequences + 1, sizeof(int32_t));
+    spans.emplace_back(g->decay, Hk * (g->chunk + 1));
+    if (!span_pairs({{g->Q, (T - 1) * g->q_stride + Hq * Dk}, {g->K, (T - 1) * g->k_stride + Hk * Dk}, {g->V, (T - 1) * g->v_stride + Hk * Dv}, {g->mq, q},
+                     {g->mk, k}, {g->mv, v}, {g->md, k}, {g->mp, p}, {g->ms, s}, {g->qk, p}, {g->pv, o}, {g->qs, o}, {g->dv, s}}, spans))
+        return COMET_ERR_INVALID_ARG;
+    // a state may be replaced in place
+    const bool in_place = g->state[0] && g->state[0] == g->state_out[0] && g->state[1] == g->state_out[1];
+    if (pair_halved(g->state) || (!in_place && !span_pairs({{g->state, st, true}}, spans))) return COMET_ERR_INVALID_ARG;
+    if (outputs_overlap(spans.data(), outputs, (int)spans.size())) return COMET_ERR_INVALID_ARG;
+    const size_t need = attn_workspace(n, Hk, Dk, Dv);
+    if (need && !g->workspace) return COMET_ERR_INVALID_ARG;
+    if (g->workspace_bytes < (int64_t)need) return COMET_ERR_SHAPE;
+    comet::AttnArgs a;
+    std::memset(&a, 0, sizeof(a));
+    give(a.Q, g->Q); give(a.K, g->K); give(a.V, g->V);
+    give(a.mq, g->mq); give(a.mk, g->mk); give(a.mv, g->mv); give(a.md, g->md); give(a.mp, g->mp); give(a.ms, g->ms);
+    give(a.qk, g->qk); give(a.pv, g->pv); give(a.qs, g->qs); give(a.dv, g->dv); give(a.S0, g->state);
+    give(a.Eq, g->Eq); give(a.Ek, g->Ek); give(a.Ev, g->Ev); give(a.Ed, g->Ed); give(a.Ep, g->Ep); give(a.Es, g->Es); give(a.O, g->O);
+    give(a.S1, g->state_out);
+    for (int i = 0; i < 2; ++i) a.kv[i] = static_cast<u64*>(g->workspace) + i * s;
+    a.decay = reinterpret_cast<const u64*>(g->decay);
+    a.starts = g->starts;
+    a.bad_starts = g->bad_starts_flag;
+    a.q_stride = g->q_stride; a.k_stride = g->k_stride; a.v_stride = g->v_stride;
+    a.tokens = g->tokens; a.sequences = g->sequences; a.q_heads = g->q_heads; a.kv_heads = g->kv_heads; a.k_dim = g->k_dim; a.v_dim = g->v_dim;
+    a.C = g->chunk; a.chunks = g->chunks; a.f = g->frac_bits;
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    const int pieces = ceil_div(a.k_dim * a.v_dim, at::THREADS), tiles = ceil_div(a.C, at::TILE);
+    cudaError_t err = cudaSuccess;
+    if (n) err = launch_chained(comet::attn_keys_kernel, dim3((unsigned)(n * Hk)), dim3(at::THREADS), 0, stream, nullptr, a);
+    if (err == cudaSuccess)
+        err = launch_chained(comet::attn_state_kernel, dim3((unsigned)(g->sequences * Hk * pieces), 2), dim3(at::THREADS), 0, stream, nullptr, a, pieces);
+    if (err == cudaSuccess && n)
+        err = launch_chained(comet::attn_rows_kernel, dim3((unsigned)(n * Hq * tiles)), dim3(at::THREADS), 0, stream, nullptr, a, tiles);
+    if (err != cudaSuccess) cudaGetLastError();
+    return err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
+}
+
+extern "C" int comet_linear_attention_step(void* cuda_stream, const comet_linear_attention_step_args* g) {
+    namespace at = comet::attn;
+    if (!g) return COMET_ERR_INVALID_ARG;
+    if (!attn_heads(g->q_heads, g->kv_heads, g->k_dim, g->v_dim) || g->batch < 1 || g->batch > ATTN_MAX_SIZE) return COMET_ERR_SHAPE;
+    const int64_t B = g->batch, Hq = g->q_heads, Hk = g->kv_heads, Dk = g->k_dim, Dv = g->v_dim;
+    if (B * Hq > ATTN_MAX_ROWS || !attn_stride(g->q_stride, B, Hq * Dk) || !attn_stride(g->k_stride, B, Hk * Dk) || !attn_stride(g->v_stride, B, Hk * Dv))
+        return COMET_ERR_SHAPE;
+    if (g->frac_bits < 1 || g->frac_bits > 31) return COMET_ERR_SHAPE;
+    if (!g->decay || reinterpret_cast<uintptr_t>(g->decay) % sizeof(u64)) return COMET_ERR_INVALID_ARG;
+    const int64_t q = B * Hq * Dk, k = B * Hk * Dk, v = B * Hk * Dv, o = B * Hq * Dv, s = B * Hk * Dk * Dv;
+    std::vector<Span> spans;
+    spans.reserve(48);
+    if (!span_pairs({{g->Eq, q}, {g->Ek, k}, {g->Ev, v}, {g->Es, s}, {g->O, o}, {g->state_out, s}}, spans)) return COMET_ERR_INVALID_ARG;
+    const int outputs = (int)spans.size();
+    spans.emplace_back(g->decay, Hk);
+    if (!span_pairs({{g->Q, (B - 1) * g->q_stride + Hq * Dk}, {g->K, (B - 1) * g->k_stride + Hk * Dk}, {g->V, (B - 1) * g->v_stride + Hk * Dv}, {g->mq, q},
+                     {g->mk, k}, {g->mv, v}, {g->ms, s}, {g->kv, s}, {g->qs, o}}, spans))
+        return COMET_ERR_INVALID_ARG;
+    const bool in_place = g->state[0] && g->state[0] == g->state_out[0] && g->state[1] == g->state_out[1];
+    if (pair_halved(g->state) || (!in_place && !span_pairs({{g->state, s, true}}, spans))) return COMET_ERR_INVALID_ARG;
+    if (outputs_overlap(spans.data(), outputs, (int)spans.size())) return COMET_ERR_INVALID_ARG;
+    comet::AttnStepArgs a;
+    std::memset(&a, 0, sizeof(a));
+    give(a.Q, g->Q); give(a.K, g->K); give(a.V, g->V); give(a.mq, g->mq); give(a.mk, g->mk); give(a.mv, g->mv); give(a.ms, g->ms);
+    give(a.kv, g->kv); give(a.qs, g->qs); give(a.S0, g->state); give(a.Eq, g->Eq); give(a.Ek, g->Ek); give(a.Ev, g->Ev); give(a.Es, g->Es);
+    give(a.O, g->O); give(a.S1, g->state_out);
+    a.decay = reinterpret_cast<const u64*>(g->decay);
+    a.q_stride = g->q_stride; a.k_stride = g->k_stride; a.v_stride = g->v_stride;
+    a.q_heads = g->q_heads; a.kv_heads = g->kv_heads; a.k_dim = g->k_dim; a.v_dim = g->v_dim; a.f = g->frac_bits;
+    return launch_pass(comet::attn_step_kernel, dim3((unsigned)(B * Hk)), (cudaStream_t)cuda_stream, a);
+}
+
+// ---------------------------------------------------------------------------
+// Norm of groups of channels with gain, bias and activation.  Stateless; the workspace is the caller's.
+// ---------------------------------------------------------------------------
+namespace {
+
+bool group_sizes(int64_t samples, int64_t positions, int64_t channels, int64_t groups) {
+    if (samples < 1 || positions < 1 || channels < 1 || groups < 1 || channels % groups || channels > 1 << 20) return false;
+    return positions <= 1 << 24 && positions * (channels / groups) <= 1 << 24 && samples * groups <= 1 << 24;
+}
+// Slabs of positions, a CTA each, of some 4096 words of a group.
+void group_slabs(comet::GroupArgs& a) {
+    a.slab = std::max(1, 4096 / a.per);
+    a.slabs = ceil_div(a.positions, a.slab);
+}
+int64_t group_blocks(const comet::GroupArgs& a, int64_t samples) { return samples * a.groups * a.slabs; }
+void group_shape(comet::GroupArgs& a, int positions, int channels, int groups) {
+    a.positions = positions;
+    a.channels = channels;
+    a.groups = groups;
+    a.per = channels / groups;
+    group_slabs(a);
+}
+
+}  // namespace
+
+extern "C" int comet_group_norm_workspace(int32_t samples, int32_t positions, int32_t channels, int32_t groups, int64_t* bytes_out) {
+    if (!bytes_out) return COMET_ERR_INVALID_ARG;
+    if (!group_sizes(samples, positions, channels, groups)) return COMET_ERR_SHAPE;
+    comet::GroupArgs a;
+    std::memset(&a, 0, sizeof(a));
+    group_shape(a, positions, channels, groups);
+    const int64_t blocks = group_blocks(a, samples);
+    if (blocks > 0x7fffffffll) return COMET_ERR_SHAPE;
+    *bytes_out = blocks * 4 * (int64_t)sizeof(u64);
+    return COMET_OK;
+}
+
+extern "C" int comet_group_norm(void* cuda_stream, const comet_group_norm_args* g) {
+    namespace nm = comet::norm;
+    if (!g) return COMET_ERR_INVALID_ARG;
+    if (!group_sizes(g->samples, g->positions, g->channels, g->groups)) return COMET_ERR_SHAPE;
+    if (g->quadratic != 0 && g->quadratic != 1) return COMET_ERR_INVALID_ARG;
+    if (g->x_stride < 0 || g->x_stride > 1ll << 32 || g->x_stride < g->channels) return COMET_ERR_SHAPE;
+    if (g->steps < 2 || g->steps > nm::MAX_STEPS || g->guess < 1 || g->guess >> 32 || g->frac_bits < 1 || g->frac_bits > 31) return COMET_ERR_SHAPE;
+    if (reinterpret_cast<uintptr_t>(g->workspace) % LINEAR_ALIGN || g->workspace_bytes < 0) return COMET_ERR_INVALID_ARG;
+    const bool gained = g->gain[0] || g->gain[1];
+    const int64_t S = g->samples, C = g->channels, rows = S * g->positions, n = rows * C, own = S * g->groups;
+    const int64_t gc = gained ? C : 0, gs = gained ? S * C : 0, act = g->quadratic ? n : 0;
+    std::vector<Span> spans;
+    spans.reserve(48);
+    spans.emplace_back(g->workspace, g->workspace_bytes, 1);
+    if (!span_pairs({{g->M, n}, {g->S, own * nm::openings(g->steps)}, {g->Z, n}, {g->D, gs}, {g->G, gc}, {g->N, act}}, spans)) return COMET_ERR_INVALID_ARG;
+    const int outputs = (int)spans.size();
+    if (!span_pairs({{g->X, (rows - 1) * g->x_stride + C}, {g->U, n}, {g->UT, n}, {g->words, own * nm::words(g->steps)}, {g->gain, gc}, {g->gain_mask, gc},
+                     {g->bias, gc}, {g->T, gs}, {g->VW, gs}, {g->R, act}, {g->Q, act}}, spans))
+        return COMET_ERR_INVALID_ARG;
+    if (outputs_overlap(spans.data(), outputs, (int)spans.size())) return COMET_ERR_INVALID_ARG;
+    comet::GroupArgs a;
+    std::memset(&a, 0, sizeof(a));
+    group_shape(a, g->positions, g->channels, g->groups);
+    const int64_t blocks = group_blocks(a, S), need = blocks * 4 * (int64_t)sizeof(u64);
+    if (blocks > 0x7fffffffll) return COMET_ERR_SHAPE;
+    if (need && !g->workspace) return COMET_ERR_INVALID_ARG;
+    if (g->workspace_bytes < need) return COMET_ERR_SHAPE;
+    give(a.X, g->X); give(a.U, g->U); give(a.words, g->words); give(a.UT, g->UT); give(a.M, g->M); give(a.S, g->S); give(a.Z, g->Z);
+    if (gained) {
+        give(a.gain, g->gain); give(a.gain_mask, g->gain_mask); give(a.T, g->T); give(a.VW, g->VW); give(a.bias, g->bias);
+        give(a.D, g->D); give(a.G, g->G);
+    }
+    if (g->quadratic) {
+        give(a.R, g->R); give(a.Q, g->Q); give(a.N, g->N);
+    }
+    a.sums = static_cast<u64*>(g->workspace);
+    a.k0 = g->k[0]; a.k1 = g->k[1]; a.k2 = g->k[2];
+    a.x_stride = g->x_stride;
+    comet::NormArgs& r = a.root;
+    r.guess = g->guess;
+    r.first = g->guess * g->guess >> g->frac_bits;
+    r.eps = g->eps;
+    r.divisor = (u64)a.positions * a.per << g->frac_bits;
+    r.divisor_bits = -1;
+    for (int b = 0; b < 64; ++b)
+        if (r.divisor == 1ull << b) r.divisor_bits = b;
+    r.f = g->frac_bits;
+    r.steps = g->steps;
+    const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    int rc = launch_pass(comet::group_sum_kernel, dim3((unsigned)blocks), stream, a);
+    if (rc == COMET_OK) rc = launch_pass(comet::group_open_kernel, dim3((unsigned)blocks), stream, a);
+    if (rc == COMET_OK) rc = launch_pass(comet::group_apply_kernel, dim3((unsigned)blocks), stream, a);
+    return rc;
 }
 
 // ---------------------------------------------------------------------------

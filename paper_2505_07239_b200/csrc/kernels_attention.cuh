@@ -1,0 +1,269 @@
+// Linear attention with a decay for every head on additive shares (comet_linear_attention, comet_linear_attention_step): products and
+// public weights only, so that it needs no comparison.  f the fixed point, i the party, tr the local truncation by f bits, w[n] the public
+// n-th power of a key head's decay, P, S, q, k, v, d shared; every value that enters a product is masked and opened once.
+//   a prompt, in chunks; of a chunk of L tokens that finds the state S:
+//     P[r][s] = tr(w[r - s] tr(q_r . k_s)), s <= r;   O_r = tr(sum_{s <= r} P[r][s] v_s + w[r + 1] tr(q_r S))
+//     d_s = tr(w[L - 1 - s] k_s);                     S <- tr(w[L] S + sum_s d_s v_s^T)
+//   single tokens:  S <- tr(w S + k v^T),  o = tr(q S)
+// Three kernels for a prompt, because only the states depend on one another: the products d v^T of all chunks and key heads at once
+// (keys), the states from chunk to chunk, a word a thread (state), then everything else of all chunks and query heads (rows).
+#pragma once
+#include <cstdint>
+#include <cuda_runtime.h>
+
+#include "kernels_limb.cuh"
+#include "pdl.cuh"
+
+namespace comet {
+
+namespace attn {
+constexpr int MAX_CHUNK = 64, MAX_DIM = 256;
+constexpr int THREADS = 256;
+constexpr int TILE = 32;                             // query rows of a CTA
+}  // namespace attn
+
+struct AttnArgs {
+    const u64* Q[2]; const u64* K[2]; const u64* V[2];                   // token t at t * stride, heads behind one another
+    const u64* mq[2]; const u64* mk[2]; const u64* mv[2]; const u64* md[2]; const u64* mp[2]; const u64* ms[2];
+    const u64* qk[2]; const u64* pv[2]; const u64* qs[2]; const u64* dv[2];
+    const u64* S0[2];                                                    // states, or null: zero
+    u64* Eq[2]; u64* Ek[2]; u64* Ev[2]; u64* Ed[2]; u64* Ep[2]; u64* Es[2];
+    u64* O[2];
+    u64* S1[2];
+    u64* kv[2];                                                          // [chunks][kv_heads][k_dim][v_dim]: sum d v^T at scale 2f
+    const u64* decay;                                                    // [kv_heads][C + 1]
+    const int32_t* starts;
+    int32_t* bad_starts;
+    long long q_stride, k_stride, v_stride;
+    int tokens, sequences, q_heads, kv_heads, k_dim, v_dim, C, chunks, f;
+};
+
+__device__ __forceinline__ u64 attn_trunc(u64 v, int party, int bits) {
+    return party ? 0ull - ((0ull - v) >> bits) : v >> bits;
+}
+
+// Tokens of sequence j, which begin at *begin: none where the starts are not ascending or leave the tokens.
+__device__ __forceinline__ int attn_length(const AttnArgs& a, int j, int* begin) {
+    const int b = __ldg(a.starts + j), e = __ldg(a.starts + j + 1);
+    *begin = b;
+    return b >= 0 && b <= e && e <= a.tokens ? e - b : 0;
+}
+
+struct AttnChunk {
+    int seq, first, len;                                                 // len 0: there is no such chunk
+};
+
+// Chunk `want` of all sequences', by all threads of a CTA.
+__device__ __forceinline__ AttnChunk attn_find(const AttnArgs& a, int want) {
+    __shared__ AttnChunk found;
+    __shared__ int sums[attn::THREADS / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) found = {0, 0, 0};
+    for (int j0 = 0, base = 0; j0 < a.sequences && base <= want; j0 += attn::THREADS) {
+        const int j = j0 + tid;
+        int begin = 0, len = 0;
+        if (j < a.sequences) len = attn_length(a, j, &begin);
+        const int n = (len + a.C - 1) / a.C;
+        int up = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, up, o);
+            if (lane >= o) up += t;
+        }
+        __syncthreads();
+        if (lane == 31) sums[warp] = up;
+        __syncthreads();
+        int before = base, total = 0;
+        for (int w = 0; w < attn::THREADS / 32; ++w) {
+            before += w < warp ? sums[w] : 0;
+            total += sums[w];
+        }
+        const int mine = want - (before + up - n);
+        if (mine >= 0 && mine < n) found = {j, begin + mine * a.C, min(a.C, len - mine * a.C)};
+        base += total;
+    }
+    __syncthreads();
+    return found;
+}
+
+// The opening of `rows` x `cols` words: x(i, r, c) the shares, masks and messages `row` words apart from token to token.
+template <typename F>
+__device__ __forceinline__ void attn_open(F&& x, const u64* const mask[2], u64* const msg[2], size_t at, size_t row, int rows, int cols) {
+    for (int t = threadIdx.x; t < rows * cols; t += attn::THREADS) {
+        const int r = t / cols, c = t - r * cols;
+        const size_t o = at + (size_t)r * row + c;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) msg[i][o] = x(i, r, c) - __ldg(mask[i] + o);
+    }
+}
+
+// One operand of a product: word (row, k) at row * row_step + k * k_step of the party's mask and of both messages.
+struct AttnOperand {
+    const u64* mask;
+    const u64* msg[2];
+    size_t row_step, k_step;
+};
+// sum over k of (mask + msg)(mask' + msg') without the product of the masks: the party's share by Eq. 1.
+__device__ __forceinline__ u64 attn_dot(const AttnOperand& l, int row, const AttnOperand& r, int col, int depth, int party) {
+    u64 sum = 0ull;
+    for (int k = 0; k < depth; ++k) {
+        const size_t x = row * l.row_step + k * l.k_step, y = col * r.row_step + k * r.k_step;
+        const u64 F = l.msg[0][x] + l.msg[1][x], E = r.msg[0][y] + r.msg[1][y];
+        sum += E * (l.mask[x] + (party ? F : 0ull)) + r.mask[y] * F;
+    }
+    return sum;
+}
+
+// Messages of k, v and d of one chunk and key head, and its sum of d v^T.
+__global__ void __launch_bounds__(attn::THREADS)
+attn_keys_kernel(const __grid_constant__ AttnArgs a) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int c = blockIdx.x / a.kv_heads, h = blockIdx.x - c * a.kv_heads;
+    const AttnChunk at = attn_find(a, c);
+    if (at.len == 0) return;
+    const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
+    const size_t k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
+    auto key = [&](int i, int r, int j) { return __ldg(a.K[i] + (size_t)(at.first + r) * a.k_stride + (size_t)h * a.k_dim + j); };
+    const u64* w = a.decay + (size_t)h * (a.C + 1);
+    attn_open(key, a.mk, a.Ek, k_at, k_row, at.len, a.k_dim);
+    attn_open([&](int i, int r, int j) { return attn_trunc(key(i, r, j) * __ldg(w + at.len - 1 - r), i, a.f); }, a.md, a.Ed, k_at, k_row, at.len, a.k_dim);
+    attn_open([&](int i, int r, int j) { return __ldg(a.V[i] + (size_t)(at.first + r) * a.v_stride + (size_t)h * a.v_dim + j); }, a.mv, a.Ev,
+              v_at, v_row, at.len, a.v_dim);
+    __syncthreads();
+    const size_t out = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
+    for (int i = 0; i < 2; ++i) {
+        const AttnOperand v = {a.mv[i] + v_at, {a.Ev[0] + v_at, a.Ev[1] + v_at}, 1, v_row}, d = {a.md[i] + k_at, {a.Ed[0] + k_at, a.Ed[1] + k_at}, 1, k_row};
+        for (int t = threadIdx.x; t < a.k_dim * a.v_dim; t += attn::THREADS)
+            a.kv[i][out + t] = a.dv[i][out + t] + attn_dot(v, t % a.v_dim, d, t / a.v_dim, at.len, i);
+    }
+}
+
+// The state from chunk to chunk of a sequence and key head, a word of a party a thread; says whether the starts were in order.
+__global__ void __launch_bounds__(attn::THREADS)
+attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
+    __shared__ int before;
+    pdl_wait();
+    pdl_launch_dependents();
+    const int j = blockIdx.x / (a.kv_heads * pieces), rest = blockIdx.x - j * a.kv_heads * pieces, h = rest / pieces;
+    const int party = blockIdx.y, word = (rest - h * pieces) * attn::THREADS + threadIdx.x, words = a.k_dim * a.v_dim;
+    if (threadIdx.x == 0) before = 0;
+    __syncthreads();
+    const bool checks = blockIdx.x == 0 && party == 0;
+    int sum = 0, begin;
+    bool bad = false;
+    for (int s = threadIdx.x; s < (checks ? a.sequences : j); s += attn::THREADS) {
+        const int len = attn_length(a, s, &begin);
+        if (s < j || checks) sum += (len + a.C - 1) / a.C;
+        bad |= begin < 0 || __ldg(a.starts + s + 1) < begin || __ldg(a.starts + s + 1) > a.tokens;
+    }
+    if (sum) atomicAdd(&before, sum);
+    if (bad && checks && a.bad_starts) *a.bad_starts = 1;
+    __syncthreads();
+    if (checks && threadIdx.x == 0 && before != a.chunks && a.bad_starts) *a.bad_starts = 1;
+    int c = checks ? 0 : before;
+    if (word >= words) return;
+    const size_t at = ((size_t)j * a.kv_heads + h) * words + word;
+    u64 S = a.S0[party] ? a.S0[party][at] : 0ull;
+    const u64* w = a.decay + (size_t)h * (a.C + 1);
+    for (int left = attn_length(a, j, &begin); left > 0 && c < a.chunks; left -= a.C, ++c) {
+        const size_t o = ((size_t)c * a.kv_heads + h) * words + word;
+        a.Es[party][o] = S - __ldg(a.ms[party] + o);
+        S = attn_trunc(__ldg(w + min(left, a.C)) * S + a.kv[party][o], party, a.f);
+    }
+    a.S1[party][at] = S;
+}
+
+// Everything else of TILE rows of a chunk and query head.
+__global__ void __launch_bounds__(attn::THREADS)
+attn_rows_kernel(const __grid_constant__ AttnArgs a, int tiles) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int c = blockIdx.x / (a.q_heads * tiles), rest = blockIdx.x - c * a.q_heads * tiles, hq = rest / tiles, r0 = (rest - hq * tiles) * attn::TILE;
+    const AttnChunk at = attn_find(a, c);
+    if (r0 >= at.len) return;
+    const int h = hq / (a.q_heads / a.kv_heads), rows = min(attn::TILE, at.len - r0), keys = r0 + rows;
+    const size_t q_row = (size_t)a.q_heads * a.k_dim, p_row = (size_t)a.q_heads * a.C, o_row = (size_t)a.q_heads * a.v_dim;
+    const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
+    const size_t first = (size_t)at.first + r0, q_at = first * q_row + (size_t)hq * a.k_dim, p_at = first * p_row + (size_t)hq * a.C;
+    const size_t o_at = first * o_row + (size_t)hq * a.v_dim, k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
+    const size_t s_at = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
+    const u64* w = a.decay + (size_t)h * (a.C + 1);
+    attn_open([&](int i, int r, int j) { return __ldg(a.Q[i] + (first + r) * a.q_stride + (size_t)hq * a.k_dim + j); }, a.mq, a.Eq, q_at, q_row, rows, a.k_dim);
+    __syncthreads();
+    for (int i = 0; i < 2; ++i) {
+        const AttnOperand k = {a.mk[i] + k_at, {a.Ek[0] + k_at, a.Ek[1] + k_at}, k_row, 1}, q = {a.mq[i] + q_at, {a.Eq[0] + q_at, a.Eq[1] + q_at}, q_row, 1};
+        for (int t = threadIdx.x; t < rows * a.C; t += attn::THREADS) {
+            const int r = t / a.C, s = t - r * a.C;
+            const size_t o = p_at + r * p_row + s;
+            u64 msg = 0ull;
+            if (s <= r0 + r) {
+                const u64 z = __ldg(a.qk[i] + o) + attn_dot(k, s, q, r, a.k_dim, i);
+                msg = attn_trunc(attn_trunc(z, i, a.f) * __ldg(w + r0 + r - s), i, a.f) - __ldg(a.mp[i] + o);
+            }
+            a.Ep[i][o] = msg;
+        }
+    }
+    __syncthreads();
+    for (int i = 0; i < 2; ++i) {
+        const AttnOperand q = {a.mq[i] + q_at, {a.Eq[0] + q_at, a.Eq[1] + q_at}, q_row, 1}, S = {a.ms[i] + s_at, {a.Es[0] + s_at, a.Es[1] + s_at}, 1, (size_t)a.v_dim};
+        const AttnOperand p = {a.mp[i] + p_at, {a.Ep[0] + p_at, a.Ep[1] + p_at}, p_row, 1}, v = {a.mv[i] + v_at, {a.Ev[0] + v_at, a.Ev[1] + v_at}, 1, v_row};
+        for (int t = threadIdx.x; t < rows * a.v_dim; t += attn::THREADS) {
+            const int r = t / a.v_dim, j = t - r * a.v_dim;
+            const size_t o = o_at + r * o_row + j;
+            const u64 x = __ldg(a.qs[i] + o) + attn_dot(S, j, q, r, a.k_dim, i);
+            const u64 y = __ldg(a.pv[i] + o) + attn_dot(v, j, p, r, min(r0 + r + 1, keys), i);
+            a.O[i][o] = attn_trunc(y + __ldg(w + r0 + r + 1) * attn_trunc(x, i, a.f), i, a.f);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Single tokens: a CTA has both parties' words of a slice of a state's columns, which it reads and writes once.
+// ---------------------------------------------------------------------------
+struct AttnStepArgs {
+    const u64* Q[2]; const u64* K[2]; const u64* V[2];
+    const u64* mq[2]; const u64* mk[2]; const u64* mv[2]; const u64* ms[2];
+    const u64* kv[2]; const u64* qs[2];
+    const u64* S0[2];
+    u64* Eq[2]; u64* Ek[2]; u64* Ev[2]; u64* Es[2];
+    u64* O[2];
+    u64* S1[2];
+    const u64* decay;                                                    // [kv_heads]
+    long long q_stride, k_stride, v_stride;
+    int q_heads, kv_heads, k_dim, v_dim, f;
+};
+
+__global__ void __launch_bounds__(attn::THREADS)
+attn_step_kernel(const __grid_constant__ AttnStepArgs a) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int b = blockIdx.x / a.kv_heads, h = blockIdx.x - b * a.kv_heads, group = a.q_heads / a.kv_heads;
+    const size_t k_at = (size_t)blockIdx.x * a.k_dim, v_at = (size_t)blockIdx.x * a.v_dim, q_at = k_at * group, o_at = v_at * group;
+    const size_t s_at = k_at * a.v_dim;
+    auto word = [&](const u64* const p[2], int i, long long stride, int j) { return __ldg(p[i] + b * stride + j); };
+    attn_open([&](int i, int, int j) { return word(a.Q, i, a.q_stride, h * group * a.k_dim + j); }, a.mq, a.Eq, q_at, 0, 1, group * a.k_dim);
+    attn_open([&](int i, int, int j) { return word(a.K, i, a.k_stride, h * a.k_dim + j); }, a.mk, a.Ek, k_at, 0, 1, a.k_dim);
+    attn_open([&](int i, int, int j) { return word(a.V, i, a.v_stride, h * a.v_dim + j); }, a.mv, a.Ev, v_at, 0, 1, a.v_dim);
+    __syncthreads();
+    const u64 w = __ldg(a.decay + h);
+    for (int i = 0; i < 2; ++i)
+        for (int t = threadIdx.x; t < a.k_dim * a.v_dim; t += attn::THREADS) {
+            const int r = t / a.v_dim, j = t - r * a.v_dim;
+            const u64 E = a.Ek[0][k_at + r] + a.Ek[1][k_at + r], F = a.Ev[0][v_at + j] + a.Ev[1][v_at + j];
+            const u64 z = __ldg(a.kv[i] + s_at + t) + E * (a.mv[i][v_at + j] + (i ? F : 0ull)) + a.mk[i][k_at + r] * F;
+            const u64 S = attn_trunc(w * (a.S0[i] ? a.S0[i][s_at + t] : 0ull) + z, i, a.f);
+            a.S1[i][s_at + t] = S;
+            a.Es[i][s_at + t] = S - __ldg(a.ms[i] + s_at + t);
+        }
+    __syncthreads();
+    for (int i = 0; i < 2; ++i) {
+        const AttnOperand q = {a.mq[i] + q_at, {a.Eq[0] + q_at, a.Eq[1] + q_at}, (size_t)a.k_dim, 1}, S = {a.ms[i] + s_at, {a.Es[0] + s_at, a.Es[1] + s_at}, 1, (size_t)a.v_dim};
+        for (int t = threadIdx.x; t < group * a.v_dim; t += attn::THREADS) {
+            const int g = t / a.v_dim, j = t - g * a.v_dim;
+            a.O[i][o_at + t] = attn_trunc(__ldg(a.qs[i] + o_at + t) + attn_dot(S, j, q, g, a.k_dim, i), i, a.f);
+        }
+    }
+}
+
+}  // namespace comet

@@ -671,6 +671,237 @@ PyObject* norm_rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// The heads of tokens, [tokens, heads, dim], of both parties: a token's heads together, tokens *stride words apart.  `first` is the
+// tensor whose device counts, or null: this one's.
+bool as_heads(PyObject* o, const at::Tensor* first, Pair& out, const uint64_t* to[2], int64_t* stride) {
+    static PyObject* const index[2] = {PyLong_FromLong(0), PyLong_FromLong(1)};
+    for (int p = 0; p < 2; ++p) {
+        if (!(out.item[p] = PyObject_GetItem(o, index[p])) || !(out.t[p] = as_tensor(out.item[p])) || !ring_words(out[p])) return false;
+        const at::Tensor& t = out[p];
+        if (t.dim() != 3 || t.sizes() != out[0].sizes() || t.device() != (first ? *first : out[0]).device())
+            return refuse(PyExc_AssertionError, "rows, [tokens, heads, dim], of both parties on one device are expected");
+        const int64_t T = t.size(0), H = t.size(1), D = t.size(2);
+        if (p == 0) *stride = T > 1 ? t.stride(0) : H * D;
+        if ((D > 1 && t.stride(2) != 1) || (H > 1 && t.stride(1) != D) || (T > 1 && t.stride(0) != *stride))
+            return refuse(PyExc_AssertionError, "a row's words must lie together, and both parties' rows equally far apart");
+        to[p] = words(t);
+    }
+    return true;
+}
+// A tensor of public words or, with `ints`, of int32.
+bool as_public(PyObject* o, at::IntArrayRef shape, const at::Tensor& like, bool ints, const void** to) {
+    const at::Tensor* t = as_tensor(o);
+    if (!t || (!ints && !ring_words(*t))) return false;
+    if (!t->is_cuda() || (ints && t->scalar_type() != at::kInt) || !t->is_contiguous() || t->sizes() != shape || t->device() != like.device())
+        return refuse(PyExc_AssertionError, "contiguous public tensors of the documented type and shape on the shares' device are expected");
+    *to = t->data_ptr();
+    return true;
+}
+bool as_flag(PyObject* o, const at::Tensor& like, int32_t** to) {
+    if (o == Py_None) return true;
+    const at::Tensor* t = as_tensor(o);
+    if (!t) return false;
+    if (!t->is_cuda() || t->scalar_type() != at::kInt || t->numel() < 1 || t->device() != like.device())
+        return refuse(PyExc_AssertionError, "the flag is an int32 on the tensors' device");
+    *to = static_cast<int32_t*>(t->data_ptr());
+    return true;
+}
+
+// linear_attention(stream, Q, K, V, starts, decay, dealer, frac_bits, state or None, bad_starts_flag or None)
+//   -> (code, Eq, Ek, Ev, Ed, Ep, Es, O, state_out); dealer: (q, k, v, d, p, s, qk, pv, qs, dv)
+PyObject* linear_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        void* stream;
+        int64_t frac;
+        Pair Q, K, V, state, m[10];
+        comet_linear_attention_args g;
+        std::memset(&g, 0, sizeof(g));
+        if (!counted(n, 10) || !as_stream(args[0], &stream) || !as_int(args[7], &frac) || !as_heads(args[1], nullptr, Q, g.Q, &g.q_stride)) return nullptr;
+        const at::Tensor& x = Q[0];
+        if (!as_heads(args[2], &x, K, g.K, &g.k_stride) || !as_heads(args[3], &x, V, g.V, &g.v_stride) || !as_tuple(args[6], 10)) return nullptr;
+        const at::Tensor *starts = as_tensor(args[4]), *decay = starts ? as_tensor(args[5]) : nullptr;
+        if (!decay) return nullptr;
+        const int64_t T = x.size(0), Hq = x.size(1), Dk = x.size(2), Hk = K[0].size(1), Dv = V[0].size(2);
+        const int64_t sequences = starts->dim() == 1 ? starts->size(0) - 1 : -1, C = decay->dim() == 2 ? decay->size(1) - 1 : -1;
+        if (K[0].size(0) != T || K[0].size(2) != Dk || V[0].size(0) != T || V[0].size(1) != Hk || sequences < 1 || C < 1) {
+            refuse(PyExc_AssertionError, "K, V, starts [sequences + 1] and decay [kv_heads, chunk + 1] must have the documented shapes");
+            return nullptr;
+        }
+        const void *at_starts, *at_decay;
+        if (!as_public(args[4], {sequences + 1}, x, true, &at_starts) || !as_public(args[5], {Hk, C + 1}, x, false, &at_decay) ||
+            !as_flag(args[9], x, &g.bad_starts_flag))
+            return nullptr;
+        g.starts = static_cast<const int32_t*>(at_starts);
+        g.decay = static_cast<const uint64_t*>(at_decay);
+        auto dealt = [&](int k) { return PyTuple_GET_ITEM(args[6], k); };
+        if (!as_pair(dealt(5), 8, m[5])) return nullptr;
+        const int64_t chunks = m[5][0].dim() == 4 ? m[5][0].size(0) : -1;
+        const at::IntArrayRef q = x.sizes(), k = K[0].sizes(), v = V[0].sizes();
+        if (!words_of(m[5], {chunks, Hk, Dk, Dv}, x, g.ms) || !as_words(dealt(0), q, x, false, m[0], g.mq) || !as_words(dealt(1), k, x, false, m[1], g.mk) ||
+            !as_words(dealt(2), v, x, false, m[2], g.mv) || !as_words(dealt(3), k, x, false, m[3], g.md) ||
+            !as_words(dealt(4), {T, Hq, C}, x, false, m[4], g.mp) || !as_words(dealt(6), {T, Hq, C}, x, false, m[6], g.qk) ||
+            !as_words(dealt(7), {T, Hq, Dv}, x, false, m[7], g.pv) || !as_words(dealt(8), {T, Hq, Dv}, x, false, m[8], g.qs) ||
+            !as_words(dealt(9), {chunks, Hk, Dk, Dv}, x, false, m[9], g.dv) || !as_words(args[8], {sequences, Hk, Dk, Dv}, x, true, state, g.state))
+            return nullptr;
+        at::Tensor Eq[2], Ek[2], Ev[2], Ed[2], Ep[2], Es[2], O[2], S[2];
+        auto done = [&](int code) { return answer_pairs(code, {Eq, Ek, Ev, Ed, Ep, Es, O, S}); };
+        if (!fits_int32({T, sequences, Hq, Hk, Dk, Dv, C, chunks, frac})) return done(COMET_ERR_SHAPE);
+        g.tokens = (int32_t)T; g.sequences = (int32_t)sequences; g.q_heads = (int32_t)Hq; g.kv_heads = (int32_t)Hk;
+        g.k_dim = (int32_t)Dk; g.v_dim = (int32_t)Dv; g.chunk = (int32_t)C; g.chunks = (int32_t)chunks; g.frac_bits = (int32_t)frac;
+        std::optional<c10::Stream> on;
+        if (!stream_of(args[0], x.device(), &on)) return nullptr;
+        const OnStream guard(x.device(), *on);
+        int code = T >= 1 ? comet_linear_attention_workspace(g.chunks, g.kv_heads, g.k_dim, g.v_dim, &g.workspace_bytes) : COMET_ERR_SHAPE;
+        if (code != COMET_OK) return done(code);
+        Results results(x);
+        results.pair(Results::MESSAGE, q, Eq, g.Eq);
+        results.pair(Results::MESSAGE, k, Ek, g.Ek);
+        results.pair(Results::MESSAGE, v, Ev, g.Ev);
+        results.pair(Results::MESSAGE, k, Ed, g.Ed);
+        results.pair(Results::MESSAGE, {chunks, Hk, Dk, Dv}, Es, g.Es);
+        results.pair(Results::MESSAGE, {T, Hq, C}, Ep, g.Ep);
+        results.pair(Results::RESULT, {T, Hq, Dv}, O, g.O);
+        results.pair(Results::RESULT, {sequences, Hk, Dk, Dv}, S, g.state_out);
+        results.make();
+        c10::DataPtr workspace;
+        if (g.workspace_bytes) {
+            workspace = c10::GetAllocator(c10::DeviceType::CUDA)->allocate((size_t)g.workspace_bytes);
+            g.workspace = workspace.get();
+        }
+        return done(unlocked([&] { return comet_linear_attention(stream, &g); }));
+    });
+}
+
+// linear_attention_step(stream, Q, K, V, decay, state or None, dealer, frac_bits) -> (code, Eq, Ek, Ev, Es, O, state_out);
+//   dealer: (q, k, v, s, kv, qs)
+PyObject* linear_attention_step(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        void* stream;
+        int64_t frac;
+        Pair Q, K, V, state, m[6];
+        comet_linear_attention_step_args g;
+        std::memset(&g, 0, sizeof(g));
+        if (!counted(n, 8) || !as_stream(args[0], &stream) || !as_int(args[7], &frac) || !as_heads(args[1], nullptr, Q, g.Q, &g.q_stride)) return nullptr;
+        const at::Tensor& x = Q[0];
+        if (!as_heads(args[2], &x, K, g.K, &g.k_stride) || !as_heads(args[3], &x, V, g.V, &g.v_stride) || !as_tuple(args[6], 6)) return nullptr;
+        const int64_t B = x.size(0), Hq = x.size(1), Dk = x.size(2), Hk = K[0].size(1), Dv = V[0].size(2);
+        if (K[0].size(0) != B || K[0].size(2) != Dk || V[0].size(0) != B || V[0].size(1) != Hk) {
+            refuse(PyExc_AssertionError, "K and V must have the documented shapes");
+            return nullptr;
+        }
+        const void* at_decay;
+        if (!as_public(args[4], {Hk}, x, false, &at_decay)) return nullptr;
+        g.decay = static_cast<const uint64_t*>(at_decay);
+        auto dealt = [&](int k) { return PyTuple_GET_ITEM(args[6], k); };
+        const at::IntArrayRef q = x.sizes(), k = K[0].sizes(), v = V[0].sizes();
+        if (!as_words(dealt(0), q, x, false, m[0], g.mq) || !as_words(dealt(1), k, x, false, m[1], g.mk) || !as_words(dealt(2), v, x, false, m[2], g.mv) ||
+            !as_words(dealt(3), {B, Hk, Dk, Dv}, x, false, m[3], g.ms) || !as_words(dealt(4), {B, Hk, Dk, Dv}, x, false, m[4], g.kv) ||
+            !as_words(dealt(5), {B, Hq, Dv}, x, false, m[5], g.qs) || !as_words(args[5], {B, Hk, Dk, Dv}, x, true, state, g.state))
+            return nullptr;
+        at::Tensor Eq[2], Ek[2], Ev[2], Es[2], O[2], S[2];
+        auto done = [&](int code) { return answer_pairs(code, {Eq, Ek, Ev, Es, O, S}); };
+        if (!fits_int32({B, Hq, Hk, Dk, Dv, frac}) || B < 1) return done(COMET_ERR_SHAPE);
+        g.batch = (int32_t)B; g.q_heads = (int32_t)Hq; g.kv_heads = (int32_t)Hk; g.k_dim = (int32_t)Dk; g.v_dim = (int32_t)Dv;
+        g.frac_bits = (int32_t)frac;
+        std::optional<c10::Stream> on;
+        if (!stream_of(args[0], x.device(), &on)) return nullptr;
+        const OnStream guard(x.device(), *on);
+        Results results(x);
+        results.pair(Results::MESSAGE, {B, Hk, Dk, Dv}, Es, g.Es);
+        results.pair(Results::MESSAGE, q, Eq, g.Eq);
+        results.pair(Results::MESSAGE, k, Ek, g.Ek);
+        results.pair(Results::MESSAGE, v, Ev, g.Ev);
+        results.pair(Results::RESULT, {B, Hq, Dv}, O, g.O);
+        results.pair(Results::RESULT, {B, Hk, Dk, Dv}, S, g.state_out);
+        results.make();
+        return done(unlocked([&] { return comet_linear_attention_step(stream, &g); }));
+    });
+}
+
+// group_norm(stream, X, groups, frac_bits, norm, gain or None, act or None) -> (code, M, S, D, G, N, Z)
+//   norm: (U, words, UT, steps, guess, eps); gain: (weight, mask, T, VW, bias); act: (coefficients, R, Q)
+PyObject* group_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        static PyObject* const index[2] = {PyLong_FromLong(0), PyLong_FromLong(1)};
+        void* stream;
+        int64_t groups, frac, steps;
+        Pair X, U, own, UT, weight, mask, T, VW, bias, R, Q;
+        comet_group_norm_args g;
+        std::memset(&g, 0, sizeof(g));
+        if (!counted(n, 7) || !as_stream(args[0], &stream) || !as_int(args[2], &groups) || !as_int(args[3], &frac)) return nullptr;
+        for (int p = 0; p < 2; ++p)
+            if (!(X.item[p] = PyObject_GetItem(args[1], index[p])) || !(X.t[p] = as_tensor(X.item[p])) || !ring_words(X[p])) return nullptr;
+        const at::Tensor& x = X[0];
+        if (x.dim() != 3 || X[1].sizes() != x.sizes() || X[1].device() != x.device()) {
+            refuse(PyExc_AssertionError, "words [samples, positions, channels] of both parties are expected");
+            return nullptr;
+        }
+        const int64_t S = x.size(0), P = x.size(1), C = x.size(2);
+        const int64_t stride = P > 1 ? x.stride(1) : S > 1 ? x.stride(0) : C;
+        for (int p = 0; p < 2; ++p) {
+            if ((C > 1 && X[p].stride(2) != 1) || (P > 1 && X[p].stride(1) != stride) || (S > 1 && X[p].stride(0) != P * stride)) {
+                refuse(PyExc_AssertionError, "channels must lie together, and all positions of all samples of both parties equally far apart");
+                return nullptr;
+            }
+            g.X[p] = words(X[p]);
+        }
+        at::Tensor M[2], Sm[2], D[2], G[2], N[2], Z[2];
+        auto done = [&](int code) { return answer_pairs(code, {M, Sm, D, G, N, Z}); };
+        if (!as_tuple(args[4], 6) || !as_int(PyTuple_GET_ITEM(args[4], 3), &steps) || !as_word(PyTuple_GET_ITEM(args[4], 4), &g.guess) ||
+            !as_word(PyTuple_GET_ITEM(args[4], 5), &g.eps))
+            return nullptr;
+        if (steps < 2 || steps > INT32_MAX / 8 || groups < 1) return done(COMET_ERR_SHAPE);
+        const at::IntArrayRef like = x.sizes();
+        if (!as_words(PyTuple_GET_ITEM(args[4], 0), like, x, false, U, g.U) ||
+            !as_words(PyTuple_GET_ITEM(args[4], 1), {S, groups, 6 * steps - 3}, x, false, own, g.words) ||
+            !as_words(PyTuple_GET_ITEM(args[4], 2), like, x, false, UT, g.UT))
+            return nullptr;
+        const bool gained = args[5] != Py_None;
+        if (gained && (!as_tuple(args[5], 5) || !as_words(PyTuple_GET_ITEM(args[5], 0), {C}, x, false, weight, g.gain) ||
+                       !as_words(PyTuple_GET_ITEM(args[5], 1), {C}, x, false, mask, g.gain_mask) ||
+                       !as_words(PyTuple_GET_ITEM(args[5], 2), {S, C}, x, false, T, g.T) ||
+                       !as_words(PyTuple_GET_ITEM(args[5], 3), {S, C}, x, false, VW, g.VW) ||
+                       !as_words(PyTuple_GET_ITEM(args[5], 4), {C}, x, false, bias, g.bias)))
+            return nullptr;
+        if (args[6] != Py_None) {
+            if (!as_tuple(args[6], 3)) return nullptr;
+            PyObject* const k = PyTuple_GET_ITEM(args[6], 0);
+            if (!as_tuple(k, 3) || !as_words(PyTuple_GET_ITEM(args[6], 1), like, x, false, R, g.R) ||
+                !as_words(PyTuple_GET_ITEM(args[6], 2), like, x, false, Q, g.Q))
+                return nullptr;
+            for (int j = 0; j < 3; ++j)
+                if (!as_word(PyTuple_GET_ITEM(k, j), &g.k[j])) return nullptr;
+            g.quadratic = 1;
+        }
+        if (!fits_int32({S, P, C, groups, frac}) || S < 1 || P < 1 || C < 1) return done(COMET_ERR_SHAPE);
+        g.samples = (int32_t)S; g.positions = (int32_t)P; g.channels = (int32_t)C; g.groups = (int32_t)groups;
+        g.x_stride = stride;
+        g.frac_bits = (int32_t)frac;
+        g.steps = (int32_t)steps;
+        std::optional<c10::Stream> on;
+        if (!stream_of(args[0], x.device(), &on)) return nullptr;
+        const OnStream guard(x.device(), *on);
+        const int code = comet_group_norm_workspace(g.samples, g.positions, g.channels, g.groups, &g.workspace_bytes);
+        if (code != COMET_OK) return done(code);
+        Results results(x);
+        results.pair(Results::MESSAGE, like, M, g.M);
+        if (g.quadratic) results.pair(Results::MESSAGE, like, N, g.N);
+        if (gained) {
+            results.pair(Results::MESSAGE, {S, C}, D, g.D);
+            results.pair(Results::MESSAGE, {C}, G, g.G);
+        }
+        results.pair(Results::MESSAGE, {S, groups, 3 * steps - 1}, Sm, g.S);
+        results.pair(Results::RESULT, like, Z, g.Z);
+        results.make();
+        c10::DataPtr workspace;
+        if (g.workspace_bytes) {
+            workspace = c10::GetAllocator(c10::DeviceType::CUDA)->allocate((size_t)g.workspace_bytes);
+            g.workspace = workspace.get();
+        }
+        return done(unlocked([&] { return comet_group_norm(stream, &g); }));
+    });
+}
+
 #define FAST(name, f) {name, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     FAST("bind_shares", bind_shares),
@@ -687,6 +918,9 @@ PyMethodDef methods[] = {
     FAST("beaver_matmul_static", beaver_matmul_static),
     FAST("linear", linear),
     FAST("norm_rotate", norm_rotate),
+    FAST("linear_attention", linear_attention),
+    FAST("linear_attention_step", linear_attention_step),
+    FAST("group_norm", group_norm),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

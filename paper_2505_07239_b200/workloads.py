@@ -499,3 +499,72 @@ def rotation_tables(rows: int, rot_dim: int, frac_bits: int, base: float = 10000
     """Public tables (cos, sin) [rows, rot_dim / 2] at scale f of the angles position * base^(-2j / rot_dim)."""
     angle = np.arange(rows)[:, None] * base ** (-np.arange(rot_dim // 2) / (rot_dim // 2))
     return encode(np.cos(angle), frac_bits), encode(np.sin(angle), frac_bits)
+
+
+# ---------------------------------------------------------------------------
+# linear attention and norms of channel groups: the dealer's material and the public powers
+# ---------------------------------------------------------------------------
+def _shared(seed: int, stream: str, values: dict) -> dict:
+    return {name: (t, *split_shares(t, seed, f"{stream}/{name}/split")) for name, t in values.items()}
+
+
+def dealer_prompt(seed: int, stream: str, starts, q_heads: int, kv_heads: int, k_dim: int, v_dim: int, chunk: int, tokens: Optional[int] = None) -> dict:
+    """Material of linear attention over packed prompts: masks q, k, v, d, p, s and the products of masks qk, pv, qs, dv (comet_linear_attention
+    has their shapes).  Words that no product has are uniform.  Each (value, share 0, share 1)."""
+    def draw(name, *shape):
+        return random_u64(seed, f"{stream}/{name}", int(np.prod(shape))).reshape(shape)
+
+    T = int(starts[-1]) if tokens is None else tokens
+    chunks = [(first, min(chunk, starts[j + 1] - first)) for j in range(len(starts) - 1) for first in range(starts[j], starts[j + 1], chunk)]
+    m = {"q": draw("q", T, q_heads, k_dim), "k": draw("k", T, kv_heads, k_dim), "v": draw("v", T, kv_heads, v_dim), "d": draw("d", T, kv_heads, k_dim),
+         "p": draw("p", T, q_heads, chunk), "s": draw("s", len(chunks), kv_heads, k_dim, v_dim), "qk": draw("qk", T, q_heads, chunk),
+         "pv": draw("pv", T, q_heads, v_dim), "qs": draw("qs", T, q_heads, v_dim), "dv": draw("dv", len(chunks), kv_heads, k_dim, v_dim)}
+    for c, (first, n) in enumerate(chunks):
+        rows = slice(first, first + n)
+        for h in range(q_heads):
+            g = h // (q_heads // kv_heads)
+            m["qk"][rows, h, :n] = m["q"][rows, h] @ m["k"][rows, g].T
+            m["pv"][rows, h] = np.tril(m["p"][rows, h, :n]) @ m["v"][rows, g]
+            m["qs"][rows, h] = m["q"][rows, h] @ m["s"][c, g]
+        for g in range(kv_heads):
+            m["dv"][c, g] = m["d"][rows, g].T @ m["v"][rows, g]
+    return _shared(seed, stream, m)
+
+
+def dealer_step(seed: int, stream: str, batch: int, q_heads: int, kv_heads: int, k_dim: int, v_dim: int) -> dict:
+    """Material of one token for every sequence: masks q, k, v, s and the products of masks kv, qs; each (value, share 0, share 1)."""
+    def draw(name, *shape):
+        return random_u64(seed, f"{stream}/{name}", int(np.prod(shape))).reshape(shape)
+
+    m = {"q": draw("q", batch, q_heads, k_dim), "k": draw("k", batch, kv_heads, k_dim), "v": draw("v", batch, kv_heads, v_dim),
+         "s": draw("s", batch, kv_heads, k_dim, v_dim)}
+    with np.errstate(over="ignore"):
+        m["kv"] = m["k"][..., :, None] * m["v"][..., None, :]
+        m["qs"] = (m["q"][..., :, None] * np.repeat(m["s"], q_heads // kv_heads, 1)).sum(2, dtype=U64)
+    return _shared(seed, stream, m)
+
+
+def dealer_group(seed: int, stream: str, samples: int, positions: int, channels: int, groups: int, steps: int, gained: bool = True) -> dict:
+    """Material of the norms of channel groups: U, words as dealer_norm's, UT; with a gain its mask, T and VW.  Each (value, share 0, share 1)."""
+    def draw(name, *shape):
+        return random_u64(seed, f"{stream}/{name}", int(np.prod(shape))).reshape(shape)
+
+    per = channels // groups
+    own = dealer_norm(seed, stream + "/own", samples, groups, 1, steps)["words"][0].copy()
+    U = draw("U", samples, positions, channels)
+    with np.errstate(over="ignore"):
+        own[..., 0] = (U * U).reshape(samples, positions, groups, per).sum((1, 3), dtype=U64)
+        T = np.repeat(own[..., -1], per, 1)
+        m = {"U": U, "words": own}
+        if gained:
+            m["mask"] = draw("mask", channels)
+            m["VW"] = T * m["mask"]
+            T = m["T"] = draw("T", samples, channels)
+        m["UT"] = U * T[:, None]
+    return _shared(seed, stream, m)
+
+
+def decay_powers(kv_heads: int, chunk: int, frac_bits: int) -> np.ndarray:
+    """Public powers 0 .. chunk of every key head's decay at scale f, [kv_heads, chunk + 1]: half-lives from a few tokens to a few hundred."""
+    rate = 1.0 - 2.0 ** (-3.0 - 5.0 * np.arange(kv_heads) / kv_heads)
+    return encode(rate[:, None] ** np.arange(chunk + 1), frac_bits)
