@@ -545,6 +545,34 @@ cudaError_t norm_kernel_attributes() {
     return err;
 }
 
+cudaError_t attn_kernel_attributes() {
+    namespace at = comet::attn;
+    cudaError_t err = cudaSuccess;
+    auto room = [&](auto* kernel, int bytes) {
+        if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    };
+    for (auto* kernel : {comet::attn_step_kernel<true, 1>, comet::attn_step_kernel<false, 1>}) room(kernel, comet::attn_step_smem(at::MAX_DIM, 1));
+    for (auto* kernel : {comet::attn_step_kernel<true, 4>, comet::attn_step_kernel<false, 4>}) room(kernel, comet::attn_step_smem(at::MAX_DIM, 4));
+    return err;
+}
+
+cudaError_t group_kernel_attributes() {
+    namespace gr = comet::group;
+    namespace nm = comet::norm;
+    cudaError_t err = cudaSuccess;
+    auto room = [&](auto* kernel, int bytes) {
+        if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (err == cudaSuccess)
+            err = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, (int)cudaSharedmemCarveoutMaxShared);
+    };
+    const int words = nm::row_bytes(nm::MAX_STEPS), arrays = gr::arrays(true, true);
+    for (auto* kernel : {comet::group_tile_kernel<1>, comet::group_tile_kernel<2>}) room(kernel, arrays * 64 * gr::TILE_THREADS + gr::TILE_GROUPS * words);
+    for (auto* kernel : {comet::group_cluster_kernel<1>, comet::group_cluster_kernel<2>})
+        room(kernel, arrays * 128 * gr::CLUSTER_THREADS + words + gr::TABLE * (int)sizeof(comet::GroupScale));
+    for (auto* kernel : {comet::group_apply_kernel<1>, comet::group_apply_kernel<2>}) room(kernel, gr::SLAB_GROUPS * words);
+    return err;
+}
+
 cudaError_t rows_kernel_attributes() {
     cudaError_t err = cudaSuccess;
     for (auto* kernel : {comet::linear_rows_kernel<1>, comet::linear_rows_kernel<2>, comet::linear_rows_kernel<4>}) {
@@ -1718,6 +1746,8 @@ cudaError_t static_device(StaticDevice* out) {
         if (err == cudaSuccess) err = tensor_kernel_attributes();
         if (err == cudaSuccess) err = norm_kernel_attributes();
         if (err == cudaSuccess) err = rows_kernel_attributes();
+        if (err == cudaSuccess) err = attn_kernel_attributes();
+        if (err == cudaSuccess) err = group_kernel_attributes();
         if (err == cudaSuccess) err = cudaGetSymbolAddress(&p, g_static_scratch);
         if (err == cudaSuccess) err = cudaGetSymbolAddress(&e, g_static_error);
         if (err != cudaSuccess) return err;
@@ -2598,7 +2628,28 @@ extern "C" int comet_linear_attention_step(void* cuda_stream, const comet_linear
     a.decay = reinterpret_cast<const u64*>(g->decay);
     a.q_stride = g->q_stride; a.k_stride = g->k_stride; a.v_stride = g->v_stride;
     a.q_heads = g->q_heads; a.kv_heads = g->kv_heads; a.k_dim = g->k_dim; a.v_dim = g->v_dim; a.f = g->frac_bits;
-    return launch_pass(comet::attn_step_kernel, dim3((unsigned)(B * Hk)), (cudaStream_t)cuda_stream, a);
+    // Slices of the columns, eight pairs at least (a 128-byte line of every row), until there are four CTAs an SM.
+    StaticDevice dev;                                            // (the kernels' shared memory is settled there)
+    if (static_device(&dev) != cudaSuccess) {
+        cudaGetLastError();
+        return COMET_ERR_CUDA;
+    }
+    const int pairs = a.v_dim / 2;
+    a.slice_pairs = pairs;
+    while (a.slice_pairs > 8 && B * Hk * ceil_div(pairs, a.slice_pairs) < 4 * dev.sm_count) a.slice_pairs = ceil_div(a.slice_pairs, 2);
+    a.slices = ceil_div(pairs, a.slice_pairs);
+    bool vec = true;
+    for (int i = 0; i < 2; ++i)
+        for (const void* p : {(const void*)a.S0[i], (const void*)a.S1[i], (const void*)a.kv[i], (const void*)a.ms[i], (const void*)a.Es[i]}) vec = vec && aligned16(p);
+    const int64_t group = Hq / Hk;
+    auto run = [&](auto* kernel, int heads) {
+        const cudaError_t err = launch_chained(kernel, dim3((unsigned)(B * Hk * a.slices)), dim3(at::THREADS), comet::attn_step_smem(a.k_dim, heads),
+                                               (cudaStream_t)cuda_stream, nullptr, a);
+        if (err != cudaSuccess) cudaGetLastError();
+        return err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
+    };
+    if (group == 1) return vec ? run(comet::attn_step_kernel<true, 1>, 1) : run(comet::attn_step_kernel<false, 1>, 1);
+    return vec ? run(comet::attn_step_kernel<true, 4>, 4) : run(comet::attn_step_kernel<false, 4>, 4);
 }
 
 // ---------------------------------------------------------------------------
@@ -2610,18 +2661,72 @@ bool group_sizes(int64_t samples, int64_t positions, int64_t channels, int64_t g
     if (samples < 1 || positions < 1 || channels < 1 || groups < 1 || channels % groups || channels > 1 << 20) return false;
     return positions <= 1 << 24 && positions * (channels / groups) <= 1 << 24 && samples * groups <= 1 << 24;
 }
-// Slabs of positions, a CTA each, of some 4096 words of a group.
-void group_slabs(comet::GroupArgs& a) {
-    a.slab = std::max(1, 4096 / a.per);
+// How long groups are cut: tiles of whole groups, up to SLAB_GROUPS of them and as many channels as a CTA has threads of `wide` words, or parts of
+// one group; slabs of positions until there are eight CTAs an SM.
+void group_slabs(comet::GroupArgs& a, int samples, int wide, int sm_count) {
+    namespace gr = comet::group;
+    const int most = gr::SLAB_THREADS * wide;
+    a.parts = ceil_div(a.per, most);
+    if (a.parts == 1) {
+        a.tiles = ceil_div(a.groups, std::min(gr::SLAB_GROUPS, most / a.per));
+        a.tile_groups = ceil_div(a.groups, a.tiles);
+        a.tiles = ceil_div(a.groups, a.tile_groups);
+        a.units = a.tile_groups * a.per / wide;
+    } else {
+        a.tiles = a.groups * a.parts;
+        a.tile_groups = 1;
+        a.units = gr::SLAB_THREADS;
+    }
+    a.subs = std::max(1, gr::SLAB_THREADS / a.units);
+    const int64_t columns = (int64_t)samples * a.tiles, want = std::max<int64_t>(1, ((int64_t)sm_count * 8 + columns - 1) / columns);
+    a.slab = (int)std::max<int64_t>(a.subs, (a.positions + want - 1) / want);
+    a.slab = ceil_div(a.slab, a.subs) * a.subs;
     a.slabs = ceil_div(a.positions, a.slab);
 }
-int64_t group_blocks(const comet::GroupArgs& a, int64_t samples) { return samples * a.groups * a.slabs; }
-void group_shape(comet::GroupArgs& a, int positions, int channels, int groups) {
-    a.positions = positions;
-    a.channels = channels;
-    a.groups = groups;
-    a.per = channels / groups;
-    group_slabs(a);
+// A group that fits a cluster is held on the chip from its first load to its last store.
+constexpr int64_t GROUP_HELD = 8ll * comet::group::MAX_CLUSTER * comet::group::CLUSTER_THREADS;
+int64_t group_workspace(int64_t samples, int64_t positions, int64_t channels, int64_t groups) {
+    return positions * (channels / groups) <= GROUP_HELD ? 0 : samples * groups * 4 * (int64_t)sizeof(u64);
+}
+}  // namespace
+
+namespace {
+
+int launch_group(const comet::GroupArgs& a, bool vec, cudaStream_t stream) {
+    namespace gr = comet::group;
+    namespace nm = comet::norm;
+    const bool tiled = a.count <= gr::TILE_WORDS;
+    const int quads = ceil_div(a.count, 4), words = 2 * (nm::words(a.root.steps) + nm::openings(a.root.steps)) * (int)sizeof(u64);
+    const int arrays = gr::arrays(a.R[0] != nullptr, a.positions == 1 && a.gain[0]);
+    int cluster = 1;
+    cudaLaunchConfig_t lc;
+    std::memset(&lc, 0, sizeof(lc));
+    if (tiled) {
+        const int groups = gr::tile_groups(quads);
+        lc.gridDim = dim3((unsigned)ceil_div(a.all, groups));
+        lc.blockDim = dim3(ceil_div(groups * quads, 32) * 32);
+        lc.dynamicSmemBytes = (size_t)arrays * 2 * 4 * 8 * lc.blockDim.x + groups * words;
+    } else {
+        const int eighths = ceil_div(a.count, 8);
+        while (ceil_div(eighths, cluster) > gr::CLUSTER_THREADS) cluster *= 2;
+        lc.gridDim = dim3((unsigned)a.all * cluster);
+        lc.blockDim = dim3(ceil_div(ceil_div(eighths, cluster), 32) * 32);
+        lc.dynamicSmemBytes = (size_t)arrays * 2 * 8 * 8 * lc.blockDim.x + words +
+                              (a.positions > 1 && a.per <= gr::TABLE ? a.per * (int)sizeof(comet::GroupScale) : 0);
+    }
+    lc.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = cluster > 1 ? 2 : 1;
+    auto* const kernel = tiled ? (vec ? comet::group_tile_kernel<2> : comet::group_tile_kernel<1>) : (vec ? comet::group_cluster_kernel<2> : comet::group_cluster_kernel<1>);
+    const cudaError_t err = cudaLaunchKernelEx(&lc, kernel, a);
+    if (err != cudaSuccess) cudaGetLastError();
+    return err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
 }
 
 }  // namespace
@@ -2629,12 +2734,7 @@ void group_shape(comet::GroupArgs& a, int positions, int channels, int groups) {
 extern "C" int comet_group_norm_workspace(int32_t samples, int32_t positions, int32_t channels, int32_t groups, int64_t* bytes_out) {
     if (!bytes_out) return COMET_ERR_INVALID_ARG;
     if (!group_sizes(samples, positions, channels, groups)) return COMET_ERR_SHAPE;
-    comet::GroupArgs a;
-    std::memset(&a, 0, sizeof(a));
-    group_shape(a, positions, channels, groups);
-    const int64_t blocks = group_blocks(a, samples);
-    if (blocks > 0x7fffffffll) return COMET_ERR_SHAPE;
-    *bytes_out = blocks * 4 * (int64_t)sizeof(u64);
+    *bytes_out = group_workspace(samples, positions, channels, groups);
     return COMET_OK;
 }
 
@@ -2660,9 +2760,12 @@ extern "C" int comet_group_norm(void* cuda_stream, const comet_group_norm_args* 
     if (outputs_overlap(spans.data(), outputs, (int)spans.size())) return COMET_ERR_INVALID_ARG;
     comet::GroupArgs a;
     std::memset(&a, 0, sizeof(a));
-    group_shape(a, g->positions, g->channels, g->groups);
-    const int64_t blocks = group_blocks(a, S), need = blocks * 4 * (int64_t)sizeof(u64);
-    if (blocks > 0x7fffffffll) return COMET_ERR_SHAPE;
+    a.positions = g->positions;
+    a.channels = g->channels;
+    a.groups = g->groups;
+    a.per = a.channels / a.groups;
+    a.count = a.positions * a.per;
+    const int64_t need = group_workspace(S, g->positions, C, g->groups);
     if (need && !g->workspace) return COMET_ERR_INVALID_ARG;
     if (g->workspace_bytes < need) return COMET_ERR_SHAPE;
     give(a.X, g->X); give(a.U, g->U); give(a.words, g->words); give(a.UT, g->UT); give(a.M, g->M); give(a.S, g->S); give(a.Z, g->Z);
@@ -2686,11 +2789,31 @@ extern "C" int comet_group_norm(void* cuda_stream, const comet_group_norm_args* 
         if (r.divisor == 1ull << b) r.divisor_bits = b;
     r.f = g->frac_bits;
     r.steps = g->steps;
+    a.all = (int)own;
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
-    int rc = launch_pass(comet::group_sum_kernel, dim3((unsigned)blocks), stream, a);
-    if (rc == COMET_OK) rc = launch_pass(comet::group_open_kernel, dim3((unsigned)blocks), stream, a);
-    if (rc == COMET_OK) rc = launch_pass(comet::group_apply_kernel, dim3((unsigned)blocks), stream, a);
-    return rc;
+    StaticDevice dev;                                            // (the kernels' shared memory is settled there)
+    if (static_device(&dev) != cudaSuccess) {
+        cudaGetLastError();
+        return COMET_ERR_CUDA;
+    }
+    // two words at once where pairs of channels lie on 16-byte boundaries throughout
+    bool vec = a.per % 2 == 0 && a.x_stride % 2 == 0;
+    for (int i = 0; i < 2; ++i)
+        for (const void* p : {(const void*)a.X[i], (const void*)a.U[i], (const void*)a.UT[i], (const void*)a.M[i], (const void*)a.Z[i], (const void*)a.T[i],
+                              (const void*)a.VW[i], (const void*)a.R[i], (const void*)a.Q[i], (const void*)a.N[i]})
+            vec = vec && aligned16(p);
+    if (a.count <= GROUP_HELD) return launch_group(a, vec, stream);
+    group_slabs(a, g->samples, vec ? 2 : 1, dev.sm_count);
+    const int64_t blocks = S * a.tiles * a.slabs;
+    if (blocks > 0x7fffffffll) return COMET_ERR_SHAPE;
+    const dim3 grid((unsigned)blocks), block(ceil_div(a.units * a.subs, 32) * 32);
+    const size_t words = (size_t)a.tile_groups * nm::row_bytes(a.root.steps);
+    cudaError_t err = cudaMemsetAsync(a.sums, 0, (size_t)need, stream);
+    if (err == cudaSuccess) err = launch_chained(vec ? comet::group_sum_kernel<2> : comet::group_sum_kernel<1>, grid, block, 0, stream, nullptr, a);
+    if (err == cudaSuccess) err = launch_chained(vec ? comet::group_open_kernel<2> : comet::group_open_kernel<1>, grid, block, 0, stream, nullptr, a);
+    if (err == cudaSuccess) err = launch_chained(vec ? comet::group_apply_kernel<2> : comet::group_apply_kernel<1>, grid, block, words, stream, nullptr, a);
+    if (err != cudaSuccess) cudaGetLastError();
+    return err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
 }
 
 // ---------------------------------------------------------------------------

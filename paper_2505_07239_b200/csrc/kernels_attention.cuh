@@ -12,6 +12,7 @@
 #include <cuda_runtime.h>
 
 #include "kernels_limb.cuh"
+#include "kernels_norm.cuh"
 #include "pdl.cuh"
 
 namespace comet {
@@ -219,7 +220,10 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a, int tiles) {
 }
 
 // ---------------------------------------------------------------------------
-// Single tokens: a CTA has both parties' words of a slice of a state's columns, which it reads and writes once.
+// Single tokens.  Bound by memory: of every word of a state and party five words, the state, its mask and the product in, the message
+// and the new state out.  A CTA has both parties' words of a slice of a state's columns, a thread one pair of columns in every
+// row_groups-th row, so every word passes once through the thread that exchanges it; q and k lie in shared memory, what they
+// are multiplied with as they are needed.  The sums of o are added up over the row groups at the end.
 // ---------------------------------------------------------------------------
 struct AttnStepArgs {
     const u64* Q[2]; const u64* K[2]; const u64* V[2];
@@ -232,37 +236,151 @@ struct AttnStepArgs {
     const u64* decay;                                                    // [kv_heads]
     long long q_stride, k_stride, v_stride;
     int q_heads, kv_heads, k_dim, v_dim, f;
+    int slices, slice_pairs;                                             // of the columns
 };
 
+// Dynamic shared memory: a row's opened k and both parties' masks (party 1's with the opened value added: V_i of Eq. 1), the same of q for
+// `heads` heads; the sums of o of every thread.
+__host__ __device__ constexpr int attn_step_smem(int k_dim, int heads) {
+    return 3 * (1 + heads) * k_dim * 8 + heads * attn::THREADS * 2 * 16;
+}
+
+template <bool VEC>
+__device__ __forceinline__ ulonglong2 attn_load2(const u64* p) {         // words that nobody else reads
+    if (VEC) return __ldcs(reinterpret_cast<const ulonglong2*>(p));
+    return make_ulonglong2(__ldcs(p), __ldcs(p + 1));
+}
+template <bool VEC>
+__device__ __forceinline__ void attn_store2(u64* p, ulonglong2 v) {
+    if (VEC) {
+        *reinterpret_cast<ulonglong2*>(p) = v;
+    } else {
+        p[0] = v.x;
+        p[1] = v.y;
+    }
+}
+
+// HEADS query heads of a key head's are worked on at a time; those beyond read masks and messages of the state a second time.
+template <bool VEC, int HEADS>
 __global__ void __launch_bounds__(attn::THREADS)
 attn_step_kernel(const __grid_constant__ AttnStepArgs a) {
+    extern __shared__ __align__(16) uint8_t step_smem[];
+    u64* const keys = reinterpret_cast<u64*>(step_smem);                                 // [k_dim][3]
+    u64* const queries = keys + 3 * a.k_dim;                                             // [k_dim][HEADS][3]
+    ulonglong2* const sums = reinterpret_cast<ulonglong2*>(queries + 3 * HEADS * a.k_dim);   // [HEADS][2][THREADS]
+    const int bh = blockIdx.x / a.slices, slice = blockIdx.x - bh * a.slices, b = bh / a.kv_heads, h = bh - b * a.kv_heads;
+    const int group = a.q_heads / a.kv_heads, tid = threadIdx.x, f = a.f;
+    const int row_groups = attn::THREADS / a.slice_pairs, rg = tid / a.slice_pairs, pair = slice * a.slice_pairs + tid - rg * a.slice_pairs;
+    const bool mine = rg < row_groups && pair < a.v_dim / 2;
+    const int col = 2 * (mine ? pair : 0);
+    const size_t k_at = (size_t)bh * a.k_dim, v_at = (size_t)bh * a.v_dim, q_at = k_at * group, o_at = v_at * group, s_at = k_at * a.v_dim + col;
     pdl_wait();
     pdl_launch_dependents();
-    const int b = blockIdx.x / a.kv_heads, h = blockIdx.x - b * a.kv_heads, group = a.q_heads / a.kv_heads;
-    const size_t k_at = (size_t)blockIdx.x * a.k_dim, v_at = (size_t)blockIdx.x * a.v_dim, q_at = k_at * group, o_at = v_at * group;
-    const size_t s_at = k_at * a.v_dim;
-    auto word = [&](const u64* const p[2], int i, long long stride, int j) { return __ldg(p[i] + b * stride + j); };
-    attn_open([&](int i, int, int j) { return word(a.Q, i, a.q_stride, h * group * a.k_dim + j); }, a.mq, a.Eq, q_at, 0, 1, group * a.k_dim);
-    attn_open([&](int i, int, int j) { return word(a.K, i, a.k_stride, h * a.k_dim + j); }, a.mk, a.Ek, k_at, 0, 1, a.k_dim);
-    attn_open([&](int i, int, int j) { return word(a.V, i, a.v_stride, h * a.v_dim + j); }, a.mv, a.Ev, v_at, 0, 1, a.v_dim);
-    __syncthreads();
+    // a row's words: state, product, mask
+    ulonglong2 S[2], kv[2], ms[2];
+    auto load = [&](int r) {
+        const size_t o = s_at + (size_t)r * a.v_dim;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            S[i] = a.S0[i] ? attn_load2<VEC>(a.S0[i] + o) : make_ulonglong2(0ull, 0ull);
+            kv[i] = attn_load2<VEC>(a.kv[i] + o);
+            ms[i] = attn_load2<VEC>(a.ms[i] + o);
+        }
+    };
+    if (mine && rg < a.k_dim) load(rg);
     const u64 w = __ldg(a.decay + h);
-    for (int i = 0; i < 2; ++i)
-        for (int t = threadIdx.x; t < a.k_dim * a.v_dim; t += attn::THREADS) {
-            const int r = t / a.v_dim, j = t - r * a.v_dim;
-            const u64 E = a.Ek[0][k_at + r] + a.Ek[1][k_at + r], F = a.Ev[0][v_at + j] + a.Ev[1][v_at + j];
-            const u64 z = __ldg(a.kv[i] + s_at + t) + E * (a.mv[i][v_at + j] + (i ? F : 0ull)) + a.mk[i][k_at + r] * F;
-            const u64 S = attn_trunc(w * (a.S0[i] ? a.S0[i][s_at + t] : 0ull) + z, i, a.f);
-            a.S1[i][s_at + t] = S;
-            a.Es[i][s_at + t] = S - __ldg(a.ms[i] + s_at + t);
+    ulonglong2 F = make_ulonglong2(0ull, 0ull), mv[2];
+    if (mine) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const u64* const V = a.V[i] + b * a.v_stride + (long long)h * a.v_dim + col;
+            mv[i] = make_ulonglong2(__ldg(a.mv[i] + v_at + col), __ldg(a.mv[i] + v_at + col + 1));
+            const ulonglong2 e = make_ulonglong2(__ldg(V) - mv[i].x, __ldg(V + 1) - mv[i].y);
+            if (rg == 0) attn_store2<false>(a.Ev[i] + v_at + col, e);
+            F.x += e.x;
+            F.y += e.y;
         }
-    __syncthreads();
-    for (int i = 0; i < 2; ++i) {
-        const AttnOperand q = {a.mq[i] + q_at, {a.Eq[0] + q_at, a.Eq[1] + q_at}, (size_t)a.k_dim, 1}, S = {a.ms[i] + s_at, {a.Es[0] + s_at, a.Es[1] + s_at}, 1, (size_t)a.v_dim};
-        for (int t = threadIdx.x; t < group * a.v_dim; t += attn::THREADS) {
-            const int g = t / a.v_dim, j = t - g * a.v_dim;
-            a.O[i][o_at + t] = attn_trunc(__ldg(a.qs[i] + o_at + t) + attn_dot(S, j, q, g, a.k_dim, i), i, a.f);
+    }
+    auto open = [&](u64* to, int step, const u64* const x[2], long long x_at, const u64* const m[2], u64* const msg[2], size_t at) {
+        for (int r = tid; r < a.k_dim; r += attn::THREADS) {
+            u64 mask[2], e[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                mask[i] = __ldg(m[i] + at + r);
+                e[i] = __ldg(x[i] + x_at + r) - mask[i];
+                if (slice == 0) msg[i][at + r] = e[i];
+            }
+            to[r * step] = e[0] + e[1];
+            to[r * step + 1] = mask[0];
+            to[r * step + 2] = mask[1] + e[0] + e[1];
         }
+    };
+    open(keys, 3, a.K, b * a.k_stride + (long long)h * a.k_dim, a.mk, a.Ek, k_at);
+    for (int g0 = 0; g0 < group; g0 += HEADS) {
+#pragma unroll
+        for (int g = 0; g < HEADS; ++g)
+            if (g0 + g < group)
+                open(queries + 3 * g, 3 * HEADS, a.Q, b * a.q_stride + (long long)(h * group + g0 + g) * a.k_dim, a.mq, a.Eq, q_at + (size_t)(g0 + g) * a.k_dim);
+        __syncthreads();
+        u64 o[HEADS][2][2];
+#pragma unroll
+        for (int g = 0; g < HEADS; ++g) o[g][0][0] = o[g][0][1] = o[g][1][0] = o[g][1][1] = 0ull;
+        if (mine)
+            for (int r = rg; r < a.k_dim; r += row_groups) {
+                const size_t at = s_at + (size_t)r * a.v_dim;
+                ulonglong2 mask[2], e[2];
+                if (g0 == 0) {
+                    const u64 E = keys[3 * r];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const u64 A = keys[3 * r + 1 + i];
+                        u64 x = kv[i].x + E * mv[i].x + A * F.x + w * S[i].x, y = kv[i].y + E * mv[i].y + A * F.y + w * S[i].y;
+                        x = i ? 0ull - norm_shift(0ull - x, f) : norm_shift(x, f);
+                        y = i ? 0ull - norm_shift(0ull - y, f) : norm_shift(y, f);
+                        mask[i] = ms[i];
+                        e[i] = make_ulonglong2(x - mask[i].x, y - mask[i].y);
+                        attn_store2<VEC>(a.S1[i] + at, make_ulonglong2(x, y));
+                        attn_store2<VEC>(a.Es[i] + at, e[i]);
+                    }
+                    if (r + row_groups < a.k_dim) load(r + row_groups);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        mask[i] = attn_load2<VEC>(a.ms[i] + at);
+                        e[i] = make_ulonglong2(a.Es[i][at], a.Es[i][at + 1]);      // this thread's own
+                    }
+                }
+                const u64 ex = e[0].x + e[1].x, ey = e[0].y + e[1].y;
+#pragma unroll
+                for (int g = 0; g < HEADS; ++g) {
+                    const u64* const q = queries + 3 * (r * HEADS + g);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        o[g][i][0] += q[0] * mask[i].x + q[1 + i] * ex;
+                        o[g][i][1] += q[0] * mask[i].y + q[1 + i] * ey;
+                    }
+                }
+            }
+#pragma unroll
+        for (int g = 0; g < HEADS; ++g)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) sums[(g * 2 + i) * attn::THREADS + tid] = make_ulonglong2(o[g][i][0], o[g][i][1]);
+        __syncthreads();
+        for (int t = tid; t < HEADS * 2 * a.slice_pairs; t += attn::THREADS) {
+            const int gi = t / a.slice_pairs, p = t - gi * a.slice_pairs, g = gi >> 1, i = gi & 1, c = slice * a.slice_pairs + p;
+            if (g0 + g >= group || c >= a.v_dim / 2) continue;
+            ulonglong2 z = make_ulonglong2(0ull, 0ull);
+            for (int k = 0; k < row_groups; ++k) {
+                const ulonglong2 v = sums[gi * attn::THREADS + k * a.slice_pairs + p];
+                z.x += v.x;
+                z.y += v.y;
+            }
+            const size_t at = o_at + (size_t)(g0 + g) * a.v_dim + 2 * c;
+            z.x += __ldg(a.qs[i] + at);
+            z.y += __ldg(a.qs[i] + at + 1);
+            attn_store2<false>(a.O[i] + at, make_ulonglong2(attn_trunc(z.x, i, f), attn_trunc(z.y, i, f)));
+        }
+        __syncthreads();
     }
 }
 
