@@ -552,6 +552,8 @@ cudaError_t attn_kernel_attributes() {
         if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     };
     for (auto* kernel : {comet::attn_step_kernel<true, 1>, comet::attn_step_kernel<false, 1>}) room(kernel, comet::attn_step_smem(at::MAX_DIM, 1));
+    for (auto* kernel : {comet::attn_keys_kernel<true>, comet::attn_keys_kernel<false>}) room(kernel, at::TILE_SMEM);
+    for (auto* kernel : {comet::attn_rows_kernel<true>, comet::attn_rows_kernel<false>}) room(kernel, at::TILE_SMEM);
     for (auto* kernel : {comet::attn_step_kernel<true, 4>, comet::attn_step_kernel<false, 4>}) room(kernel, comet::attn_step_smem(at::MAX_DIM, 4));
     return err;
 }
@@ -2588,13 +2590,26 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
     a.tokens = g->tokens; a.sequences = g->sequences; a.q_heads = g->q_heads; a.kv_heads = g->kv_heads; a.k_dim = g->k_dim; a.v_dim = g->v_dim;
     a.C = g->chunk; a.chunks = g->chunks; a.f = g->frac_bits;
     const cudaStream_t stream = (cudaStream_t)cuda_stream;
+    StaticDevice dev;
+    if (static_device(&dev) != cudaSuccess) {
+        cudaGetLastError();
+        return COMET_ERR_CUDA;
+    }
+    a.error = dev.error;
+    // two words at once where an operand's rows begin on 16-byte boundaries (their lengths are even)
+    bool vec = true;
+    for (int i = 0; i < 2; ++i)
+        for (const void* p : {(const void*)a.mq[i], (const void*)a.mk[i], (const void*)a.mp[i], (const void*)a.Eq[i], (const void*)a.Ek[i], (const void*)a.Ep[i]})
+            vec = vec && aligned16(p);
     const int pieces = ceil_div(a.k_dim * a.v_dim, at::THREADS), tiles = ceil_div(a.C, at::TILE);
     cudaError_t err = cudaSuccess;
-    if (n) err = launch_chained(comet::attn_keys_kernel, dim3((unsigned)(n * Hk)), dim3(at::THREADS), 0, stream, nullptr, a);
+    if (n) err = launch_chained(vec ? comet::attn_keys_kernel<true> : comet::attn_keys_kernel<false>, dim3((unsigned)(n * Hk)), dim3(at::TILE_THREADS),
+                                at::TILE_SMEM, stream, nullptr, a);
     if (err == cudaSuccess)
         err = launch_chained(comet::attn_state_kernel, dim3((unsigned)(g->sequences * Hk * pieces), 2), dim3(at::THREADS), 0, stream, nullptr, a, pieces);
     if (err == cudaSuccess && n)
-        err = launch_chained(comet::attn_rows_kernel, dim3((unsigned)(n * Hq * tiles)), dim3(at::THREADS), 0, stream, nullptr, a, tiles);
+        err = launch_chained(vec ? comet::attn_rows_kernel<true> : comet::attn_rows_kernel<false>, dim3((unsigned)(n * Hq * tiles)), dim3(at::TILE_THREADS),
+                             at::TILE_SMEM, stream, nullptr, a, tiles);
     if (err != cudaSuccess) cudaGetLastError();
     return err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
 }

@@ -9,6 +9,7 @@
 // (keys), the states from chunk to chunk, a word a thread (state), then everything else of all chunks and query heads (rows).
 #pragma once
 #include <cstdint>
+#include <type_traits>
 #include <cuda_runtime.h>
 
 #include "kernels_limb.cuh"
@@ -20,7 +21,8 @@ namespace comet {
 namespace attn {
 constexpr int MAX_CHUNK = 64, MAX_DIM = 256;
 constexpr int THREADS = 256;
-constexpr int TILE = 32;                             // query rows of a CTA
+constexpr int TILE = 32;                             // columns of a tile of a product
+constexpr int TILE_THREADS = THREADS + 32;           // eight warps that convert, one that issues MMAs
 }  // namespace attn
 
 struct AttnArgs {
@@ -37,6 +39,7 @@ struct AttnArgs {
     int32_t* bad_starts;
     long long q_stride, k_stride, v_stride;
     int tokens, sequences, q_heads, kv_heads, k_dim, v_dim, C, chunks, f;
+    int* error;                                                          // set where a wait ran out
 };
 
 __device__ __forceinline__ u64 attn_trunc(u64 v, int party, int bits) {
@@ -57,10 +60,10 @@ struct AttnChunk {
 // Chunk `want` of all sequences', by all threads of a CTA.
 __device__ __forceinline__ AttnChunk attn_find(const AttnArgs& a, int want) {
     __shared__ AttnChunk found;
-    __shared__ int sums[attn::THREADS / 32];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __shared__ int sums[attn::TILE_THREADS / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     if (tid == 0) found = {0, 0, 0};
-    for (int j0 = 0, base = 0; j0 < a.sequences && base <= want; j0 += attn::THREADS) {
+    for (int j0 = 0, base = 0; j0 < a.sequences && base <= want; j0 += blockDim.x) {
         const int j = j0 + tid;
         int begin = 0, len = 0;
         if (j < a.sequences) len = attn_length(a, j, &begin);
@@ -75,7 +78,7 @@ __device__ __forceinline__ AttnChunk attn_find(const AttnArgs& a, int want) {
         if (lane == 31) sums[warp] = up;
         __syncthreads();
         int before = base, total = 0;
-        for (int w = 0; w < attn::THREADS / 32; ++w) {
+        for (int w = 0; w < warps; ++w) {
             before += w < warp ? sums[w] : 0;
             total += sums[w];
         }
@@ -87,9 +90,10 @@ __device__ __forceinline__ AttnChunk attn_find(const AttnArgs& a, int want) {
     return found;
 }
 
-// The opening of `rows` x `cols` words: x(i, r, c) the shares, masks and messages `row` words apart from token to token.
+// The opening of `rows` x `cols` words by the first THREADS threads: x(i, r, c) the shares, masks and messages `row` words apart from token to token.
 template <typename F>
 __device__ __forceinline__ void attn_open(F&& x, const u64* const mask[2], u64* const msg[2], size_t at, size_t row, int rows, int cols) {
+#pragma unroll 4
     for (int t = threadIdx.x; t < rows * cols; t += attn::THREADS) {
         const int r = t / cols, c = t - r * cols;
         const size_t o = at + (size_t)r * row + c;
@@ -98,46 +102,258 @@ __device__ __forceinline__ void attn_open(F&& x, const u64* const mask[2], u64* 
     }
 }
 
-// One operand of a product: word (row, k) at row * row_step + k * k_step of the party's mask and of both messages.
+// ---------------------------------------------------------------------------
+// Products on the int8 tensor cores.  A CTA works out tiles of 128 x TILE words of Z_i = (triple) + E B_i + V_i F, V_i = A_i + i E (Eq. 1), one party's
+// after the other's, from words in memory: eight warps turn 32 contraction indices of either product at a time into limb planes in shared memory
+// (two slots), a ninth issues the MMAs (kernels_limb.cuh has the decomposition and the layout), and the eight read the sums out of
+// tensor memory.  Left operands, 128 rows, are keys, values or states, right ones, TILE rows, queries, weights or decayed keys; rows past an
+// operand's are whatever lies in shared memory and their sums are never looked at.  Half an SM's tensor and shared memory per CTA, so that one CTA
+// converts, opens or drains while the other's MMAs run.
+// ---------------------------------------------------------------------------
 struct AttnOperand {
-    const u64* mask;
+    const u64* mask;                     // the party's
     const u64* msg[2];
-    size_t row_step, k_step;
+    size_t step;                         // words from row to row; of a DEEP operand, whose rows lie side by side, from index to index
 };
-// sum over k of (mask + msg)(mask' + msg') without the product of the masks: the party's share by Eq. 1.
-__device__ __forceinline__ u64 attn_dot(const AttnOperand& l, int row, const AttnOperand& r, int col, int depth, int party) {
-    u64 sum = 0ull;
-    for (int k = 0; k < depth; ++k) {
-        const size_t x = row * l.row_step + k * l.k_step, y = col * r.row_step + k * r.k_step;
-        const u64 F = l.msg[0][x] + l.msg[1][x], E = r.msg[0][y] + r.msg[1][y];
-        sum += E * (l.mask[x] + (party ? F : 0ull)) + r.mask[y] * F;
+enum AttnWords { MASK, MESSAGES, BOTH };                 // of a plane set: the mask, the opened value, their sum
+
+template <AttnWords WHAT>
+__device__ __forceinline__ u64 attn_word(const AttnOperand& x, size_t at, bool masked) {
+    u64 v = 0ull;
+    if (WHAT != MASK) v = x.msg[0][at] + x.msg[1][at];
+    if (WHAT != MESSAGES && masked) v += x.mask[at];
+    return v;
+}
+// Planes of `rows` rows, indices k0 .. k0 + 31 of `depth`, zero from `depth` on.  causal >= 0: row r has masks up to index causal + r only
+// (its messages are zero beyond).
+template <AttnWords WHAT, bool DEEP, bool VEC>
+__device__ __forceinline__ void attn_planes(uint8_t* planes, int plane_bytes, const AttnOperand& x, int rows, int k0, int depth, int causal) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (DEEP) {
+        // eight rows x four of the eight groups of indices a warp: 64-byte pieces of memory, 128 bytes of a plane
+        const int tasks = (rows + 7) / 8 * 2;
+#pragma unroll 2
+        for (int t = warp; t < tasks; t += attn::THREADS / 32) {
+            const int row = (t >> 1) * 8 + (lane & 7), c = (t & 1) * 4 + (lane >> 3);
+            u64 w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = k0 + 2 * c + (j & 1) + 16 * (j >> 1);
+                w[j] = row < rows && k < depth ? attn_word<WHAT>(x, k * x.step + row, true) : 0ull;
+            }
+            limb_emit4(planes + (row >> 3) * 256 + (c >> 2) * 128 + (row & 7) * 16 + (c & 3) * 4, plane_bytes, w);
+        }
+    } else {
+        // limb_emit4's order; lanes of the upper groups take the row four further, against bank conflicts
+        const int c = lane & 7, sub = 4 * (2 * (warp >> 1) + ((warp & 1) ^ (c >> 2))) + (lane >> 3);
+#pragma unroll 2
+        for (int row = sub; row < rows; row += 32) {
+            u64 w[4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = k0 + 16 * h + 2 * c;
+                const size_t at = row * x.step + k;
+                const int last = causal >= 0 ? causal + row : depth;
+                if (VEC) {
+                    ulonglong2 v = make_ulonglong2(0ull, 0ull);
+                    if (k < depth) {
+                        if (WHAT != MASK) {
+                            const ulonglong2 e = *reinterpret_cast<const ulonglong2*>(x.msg[0] + at), g = *reinterpret_cast<const ulonglong2*>(x.msg[1] + at);
+                            v = make_ulonglong2(e.x + g.x, e.y + g.y);
+                        }
+                        if (WHAT != MESSAGES) {
+                            const ulonglong2 m = __ldg(reinterpret_cast<const ulonglong2*>(x.mask + at));
+                            if (k <= last) v.x += m.x;
+                            if (k + 1 <= last) v.y += m.y;
+                        }
+                    }
+                    w[2 * h] = v.x;
+                    w[2 * h + 1] = v.y;
+                } else {
+                    w[2 * h] = k < depth ? attn_word<WHAT>(x, at, k <= last) : 0ull;
+                    w[2 * h + 1] = k + 1 < depth ? attn_word<WHAT>(x, at + 1, k + 1 <= last) : 0ull;
+                }
+            }
+            limb_emit4(planes + (row >> 3) * 256 + (c >> 2) * 128 + (row & 7) * 16 + (c & 3) * 4, plane_bytes, w);
+        }
     }
-    return sum;
 }
 
+// What a CTA's warps share.
+struct AttnTile {
+    uint64_t full[2], empty[2], acc_full, acc_empty;
+    uint32_t tmem;
+    int abort_flag;
+    uint8_t* planes;                     // two slots
+};
+namespace attn {
+constexpr int LEFT_PLANE = 128 * limb::KC, RIGHT_PLANE = TILE * limb::KC, LEFT_BYTES = limb::PLANES * LEFT_PLANE;
+constexpr int SLOT_BYTES = LEFT_BYTES + limb::PLANES * RIGHT_PLANE, TILE_SMEM = 2 * SLOT_BYTES + 128, ACC_COLS = limb::PLANES * TILE;
+}  // namespace attn
+
+__device__ __forceinline__ void attn_tile_begin(AttnTile& s, uint8_t* raw) {
+    if (threadIdx.x == 0) {
+        for (int k = 0; k < 2; ++k) {
+            ptx::mbar_init(ptx::smem_u32(&s.full[k]), attn::THREADS / 32);
+            ptx::mbar_init(ptx::smem_u32(&s.empty[k]), 1);
+        }
+        ptx::mbar_init(ptx::smem_u32(&s.acc_full), 1);
+        ptx::mbar_init(ptx::smem_u32(&s.acc_empty), attn::THREADS / 32);
+        s.abort_flag = 0;
+        s.planes = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
+        ptx::fence_barrier_init();
+    }
+    if (threadIdx.x >= attn::THREADS) {
+        ptx::tmem_alloc(ptx::smem_u32(&s.tmem), attn::ACC_COLS);
+        ptx::tmem_relinquish();
+    }
+    ptx::fence_before_sync();
+    __syncthreads();
+    ptx::fence_after_sync();
+}
+__device__ __forceinline__ void attn_tile_end(AttnTile& s, int* error) {
+    __syncwarp();
+    ptx::fence_before_sync();
+    __syncthreads();
+    if (threadIdx.x == 0 && s.abort_flag) {
+        *error = 1;
+        __threadfence_system();
+    }
+    if (threadIdx.x >= attn::THREADS) {
+        ptx::fence_after_sync();
+        ptx::tmem_dealloc(s.tmem, attn::ACC_COLS);
+    }
+}
+// The eight converting warps wait for one another.
+__device__ __forceinline__ void attn_meet() { asm volatile("bar.sync 1, %0;" ::"n"(attn::THREADS) : "memory"); }
+
+// Where a warp is in the order of slots and tiles; the converting warps and the issuing one count alike.
+struct AttnTurn {
+    uint32_t stage = 0, tile = 0;
+};
+// The issuing warp's part of a tile: `stages` plane sets, each one product of 32 indices.
+__device__ __forceinline__ void attn_issue(AttnTile& s, AttnTurn& turn, int stages, bool& ok) {
+    if (ptx::elect_one() && ok) {
+        constexpr uint32_t IDESC = (2u << 4) | (128u >> 4 << 24);
+        ok = limb_wait(ptx::smem_u32(&s.acc_empty), (turn.tile & 1u) ^ 1u, &s.abort_flag);
+        ptx::fence_after_sync();
+        for (int t = 0; t < stages && ok; ++t) {
+            const uint32_t n = turn.stage + t, slot = n & 1u;
+            ok = limb_wait(ptx::smem_u32(&s.full[slot]), n >> 1 & 1u, &s.abort_flag);
+            if (!ok) break;
+            ptx::fence_after_sync();
+            const uint32_t left = limb_desc_lo(ptx::smem_u32(s.planes) + slot * attn::SLOT_BYTES), right = left + (attn::LEFT_BYTES >> 4);
+#pragma unroll
+            for (int q = 0; q < limb::PLANES; ++q)
+                ptx::mma_i8(s.tmem + attn::TILE * q, left + (q * attn::LEFT_PLANE >> 4), LIMB_DESC_HI, right, LIMB_DESC_HI,
+                            IDESC | ((uint32_t)(attn::TILE * (limb::PLANES - q)) >> 3 << 17), t > 0 || q > 0 ? 1u : 0u);
+            ptx::mma_commit(ptx::smem_u32(&s.empty[slot]));
+        }
+        if (ok) ptx::mma_commit(ptx::smem_u32(&s.acc_full));
+    }
+    turn.stage += stages;
+    ++turn.tile;
+}
+// The converting warps' part: planes of both products, 32 indices at a time, then the sums: done(row, column, product) for this thread's row, one
+// of four columns after the other.
+template <bool DEEP_LEFT, bool DEEP_RIGHT, bool VEC, typename F>
+__device__ __forceinline__ void attn_product(AttnTile& s, AttnTurn& turn, const AttnOperand& left, int rows, const AttnOperand& right, int cols, int depth,
+                                             int party, int causal, bool right_vec, bool& ok, F&& done) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int k0 = 0; k0 < depth; k0 += limb::KC)
+#pragma unroll
+        for (int second = 0; second < 2; ++second) {
+            const uint32_t n = turn.stage++, slot = n & 1u;
+            ok = ok && limb_wait(ptx::smem_u32(&s.empty[slot]), (n >> 1 & 1u) ^ 1u, &s.abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) continue;
+            uint8_t* const l = s.planes + slot * attn::SLOT_BYTES;
+            uint8_t* const r = l + attn::LEFT_BYTES;
+            auto convert_right = [&](auto what) {
+                constexpr AttnWords WHAT = decltype(what)::value;
+                if (VEC && right_vec) attn_planes<WHAT, DEEP_RIGHT, true>(r, attn::RIGHT_PLANE, right, cols, k0, depth, causal);
+                else attn_planes<WHAT, DEEP_RIGHT, false>(r, attn::RIGHT_PLANE, right, cols, k0, depth, causal);
+            };
+            if (second == 0) {
+                attn_planes<MASK, DEEP_LEFT, VEC>(l, attn::LEFT_PLANE, left, rows, k0, depth, -1);
+                convert_right(std::integral_constant<AttnWords, MESSAGES>{});
+            } else {
+                attn_planes<MESSAGES, DEEP_LEFT, VEC>(l, attn::LEFT_PLANE, left, rows, k0, depth, -1);
+                if (party) convert_right(std::integral_constant<AttnWords, BOTH>{});
+                else convert_right(std::integral_constant<AttnWords, MASK>{});
+            }
+            ptx::fence_proxy_async_smem();                   // the planes are read by the tensor cores
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&s.full[slot]));
+        }
+    ok = ok && limb_wait_warp(ptx::smem_u32(&s.acc_full), turn.tile & 1u, &s.abort_flag);
+    ++turn.tile;
+    if (!ok) return;
+    ptx::fence_after_sync();
+    const int row = (warp & 3) * 32 + lane;
+    const uint32_t acc = s.tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    if ((warp & 3) * 32 < rows) {
+#pragma unroll 1
+        for (int c = (warp >> 2) * (attn::TILE / 2); c < min((warp >> 2) * (attn::TILE / 2) + attn::TILE / 2, cols); c += 4) {
+            uint32_t d[limb::PLANES][4];
+#pragma unroll
+            for (int p = 0; p < limb::PLANES; ++p) ptx::tmem_ld4(acc + attn::TILE * p + c, d[p]);
+            ptx::tmem_wait_ld();
+            if (row < rows)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (c + j < cols) done(row, c + j, limb_recombine(d[0][j], d[1][j], d[2][j], d[3][j], d[4][j], d[5][j], d[6][j], d[7][j]));
+        }
+    }
+    ptx::fence_before_sync();
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&s.acc_empty));
+}
+__device__ __forceinline__ int attn_stages(int depth) { return 2 * ((depth + limb::KC - 1) / limb::KC); }
+
 // Messages of k, v and d of one chunk and key head, and its sum of d v^T.
-__global__ void __launch_bounds__(attn::THREADS)
+template <bool VEC>
+__global__ void __launch_bounds__(attn::TILE_THREADS, 2)
 attn_keys_kernel(const __grid_constant__ AttnArgs a) {
+    extern __shared__ uint8_t attn_smem[];
+    __shared__ AttnTile s;
     pdl_wait();
     pdl_launch_dependents();
     const int c = blockIdx.x / a.kv_heads, h = blockIdx.x - c * a.kv_heads;
     const AttnChunk at = attn_find(a, c);
     if (at.len == 0) return;
-    const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
-    const size_t k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
-    auto key = [&](int i, int r, int j) { return __ldg(a.K[i] + (size_t)(at.first + r) * a.k_stride + (size_t)h * a.k_dim + j); };
-    const u64* w = a.decay + (size_t)h * (a.C + 1);
-    attn_open(key, a.mk, a.Ek, k_at, k_row, at.len, a.k_dim);
-    attn_open([&](int i, int r, int j) { return attn_trunc(key(i, r, j) * __ldg(w + at.len - 1 - r), i, a.f); }, a.md, a.Ed, k_at, k_row, at.len, a.k_dim);
-    attn_open([&](int i, int r, int j) { return __ldg(a.V[i] + (size_t)(at.first + r) * a.v_stride + (size_t)h * a.v_dim + j); }, a.mv, a.Ev,
-              v_at, v_row, at.len, a.v_dim);
-    __syncthreads();
-    const size_t out = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
-    for (int i = 0; i < 2; ++i) {
-        const AttnOperand v = {a.mv[i] + v_at, {a.Ev[0] + v_at, a.Ev[1] + v_at}, 1, v_row}, d = {a.md[i] + k_at, {a.Ed[0] + k_at, a.Ed[1] + k_at}, 1, k_row};
-        for (int t = threadIdx.x; t < a.k_dim * a.v_dim; t += attn::THREADS)
-            a.kv[i][out + t] = a.dv[i][out + t] + attn_dot(v, t % a.v_dim, d, t / a.v_dim, at.len, i);
+    attn_tile_begin(s, attn_smem);
+    AttnTurn turn;
+    bool ok = true;
+    if (threadIdx.x >= attn::THREADS) {
+        for (int i = 0; i < 2; ++i)
+            for (int v0 = 0; v0 < a.v_dim; v0 += 128)
+                for (int k0 = 0; k0 < a.k_dim; k0 += attn::TILE) attn_issue(s, turn, attn_stages(at.len), ok);
+    } else {
+        const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
+        const size_t k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
+        auto key = [&](int i, int r, int j) { return __ldg(a.K[i] + (size_t)(at.first + r) * a.k_stride + (size_t)h * a.k_dim + j); };
+        const u64* w = a.decay + (size_t)h * (a.C + 1);
+        attn_open(key, a.mk, a.Ek, k_at, k_row, at.len, a.k_dim);
+        attn_open([&](int i, int r, int j) { return attn_trunc(key(i, r, j) * __ldg(w + at.len - 1 - r), i, a.f); }, a.md, a.Ed, k_at, k_row, at.len, a.k_dim);
+        attn_open([&](int i, int r, int j) { return __ldg(a.V[i] + (size_t)(at.first + r) * a.v_stride + (size_t)h * a.v_dim + j); }, a.mv, a.Ev,
+                  v_at, v_row, at.len, a.v_dim);
+        attn_meet();
+        const size_t out = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
+        for (int i = 0; i < 2; ++i)
+            for (int v0 = 0; v0 < a.v_dim; v0 += 128) {
+                const AttnOperand v = {a.mv[i] + v_at + v0, {a.Ev[0] + v_at + v0, a.Ev[1] + v_at + v0}, v_row};
+                for (int k0 = 0; k0 < a.k_dim; k0 += attn::TILE) {
+                    const AttnOperand d = {a.md[i] + k_at + k0, {a.Ed[0] + k_at + k0, a.Ed[1] + k_at + k0}, k_row};
+                    attn_product<true, true, VEC>(s, turn, v, min(128, a.v_dim - v0), d, min(attn::TILE, a.k_dim - k0), at.len, i, -1, true, ok,
+                                                  [&](int row, int col, u64 z) {
+                                                      const size_t o = out + (size_t)(k0 + col) * a.v_dim + v0 + row;
+                                                      a.kv[i][o] = __ldcs(a.dv[i] + o) + z;
+                                                  });
+                }
+            }
     }
+    attn_tile_end(s, a.error);
 }
 
 // The state from chunk to chunk of a sequence and key head, a word of a party a thread; says whether the starts were in order.
@@ -176,47 +392,70 @@ attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
 }
 
 // Everything else of TILE rows of a chunk and query head.
-__global__ void __launch_bounds__(attn::THREADS)
+template <bool VEC>
+__global__ void __launch_bounds__(attn::TILE_THREADS, 2)
 attn_rows_kernel(const __grid_constant__ AttnArgs a, int tiles) {
+    extern __shared__ uint8_t attn_smem[];
+    __shared__ AttnTile s;
     pdl_wait();
     pdl_launch_dependents();
     const int c = blockIdx.x / (a.q_heads * tiles), rest = blockIdx.x - c * a.q_heads * tiles, hq = rest / tiles, r0 = (rest - hq * tiles) * attn::TILE;
     const AttnChunk at = attn_find(a, c);
     if (r0 >= at.len) return;
     const int h = hq / (a.q_heads / a.kv_heads), rows = min(attn::TILE, at.len - r0), keys = r0 + rows;
-    const size_t q_row = (size_t)a.q_heads * a.k_dim, p_row = (size_t)a.q_heads * a.C, o_row = (size_t)a.q_heads * a.v_dim;
-    const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
-    const size_t first = (size_t)at.first + r0, q_at = first * q_row + (size_t)hq * a.k_dim, p_at = first * p_row + (size_t)hq * a.C;
-    const size_t o_at = first * o_row + (size_t)hq * a.v_dim, k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
-    const size_t s_at = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
-    const u64* w = a.decay + (size_t)h * (a.C + 1);
-    attn_open([&](int i, int r, int j) { return __ldg(a.Q[i] + (first + r) * a.q_stride + (size_t)hq * a.k_dim + j); }, a.mq, a.Eq, q_at, q_row, rows, a.k_dim);
-    __syncthreads();
-    for (int i = 0; i < 2; ++i) {
-        const AttnOperand k = {a.mk[i] + k_at, {a.Ek[0] + k_at, a.Ek[1] + k_at}, k_row, 1}, q = {a.mq[i] + q_at, {a.Eq[0] + q_at, a.Eq[1] + q_at}, q_row, 1};
-        for (int t = threadIdx.x; t < rows * a.C; t += attn::THREADS) {
-            const int r = t / a.C, s = t - r * a.C;
-            const size_t o = p_at + r * p_row + s;
-            u64 msg = 0ull;
-            if (s <= r0 + r) {
-                const u64 z = __ldg(a.qk[i] + o) + attn_dot(k, s, q, r, a.k_dim, i);
-                msg = attn_trunc(attn_trunc(z, i, a.f) * __ldg(w + r0 + r - s), i, a.f) - __ldg(a.mp[i] + o);
+    attn_tile_begin(s, attn_smem);
+    AttnTurn turn;
+    bool ok = true;
+    if (threadIdx.x >= attn::THREADS) {
+        for (int i = 0; i < 2; ++i) attn_issue(s, turn, attn_stages(a.k_dim), ok);
+        for (int i = 0; i < 2; ++i)
+            for (int v0 = 0; v0 < a.v_dim; v0 += 128) {
+                attn_issue(s, turn, attn_stages(a.k_dim), ok);
+                attn_issue(s, turn, attn_stages(keys), ok);
             }
-            a.Ep[i][o] = msg;
+    } else {
+        const size_t q_row = (size_t)a.q_heads * a.k_dim, p_row = (size_t)a.q_heads * a.C, o_row = (size_t)a.q_heads * a.v_dim;
+        const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
+        const size_t first = (size_t)at.first + r0, q_at = first * q_row + (size_t)hq * a.k_dim, p_at = first * p_row + (size_t)hq * a.C;
+        const size_t o_at = first * o_row + (size_t)hq * a.v_dim, k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
+        const size_t s_at = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
+        const u64* w = a.decay + (size_t)h * (a.C + 1);
+        attn_open([&](int i, int r, int j) { return __ldg(a.Q[i] + (first + r) * a.q_stride + (size_t)hq * a.k_dim + j); }, a.mq, a.Eq, q_at, q_row, rows, a.k_dim);
+        // off the triangle nothing is sent
+        for (int t = threadIdx.x; t < rows * a.C; t += attn::THREADS) {
+            const int r = t / a.C, k = t - r * a.C;
+            if (k > r0 + r) a.Ep[0][p_at + r * p_row + k] = a.Ep[1][p_at + r * p_row + k] = 0ull;
         }
-    }
-    __syncthreads();
-    for (int i = 0; i < 2; ++i) {
-        const AttnOperand q = {a.mq[i] + q_at, {a.Eq[0] + q_at, a.Eq[1] + q_at}, q_row, 1}, S = {a.ms[i] + s_at, {a.Es[0] + s_at, a.Es[1] + s_at}, 1, (size_t)a.v_dim};
-        const AttnOperand p = {a.mp[i] + p_at, {a.Ep[0] + p_at, a.Ep[1] + p_at}, p_row, 1}, v = {a.mv[i] + v_at, {a.Ev[0] + v_at, a.Ev[1] + v_at}, 1, v_row};
-        for (int t = threadIdx.x; t < rows * a.v_dim; t += attn::THREADS) {
-            const int r = t / a.v_dim, j = t - r * a.v_dim;
-            const size_t o = o_at + r * o_row + j;
-            const u64 x = __ldg(a.qs[i] + o) + attn_dot(S, j, q, r, a.k_dim, i);
-            const u64 y = __ldg(a.pv[i] + o) + attn_dot(v, j, p, r, min(r0 + r + 1, keys), i);
-            a.O[i][o] = attn_trunc(y + __ldg(w + r0 + r + 1) * attn_trunc(x, i, a.f), i, a.f);
+        attn_meet();
+        for (int i = 0; i < 2; ++i) {
+            const AttnOperand k = {a.mk[i] + k_at, {a.Ek[0] + k_at, a.Ek[1] + k_at}, k_row}, q = {a.mq[i] + q_at, {a.Eq[0] + q_at, a.Eq[1] + q_at}, q_row};
+            attn_product<false, false, VEC>(s, turn, k, keys, q, rows, a.k_dim, i, -1, true, ok, [&](int key, int r, u64 z) {
+                if (key > r0 + r) return;
+                const size_t o = p_at + r * p_row + key;
+                z += __ldg(a.qk[i] + o);
+                a.Ep[i][o] = attn_trunc(attn_trunc(z, i, a.f) * __ldg(w + r0 + r - key), i, a.f) - __ldg(a.mp[i] + o);
+            });
         }
+        attn_meet();
+        for (int i = 0; i < 2; ++i)
+            for (int v0 = 0; v0 < a.v_dim; v0 += 128) {
+                const int wide = min(128, a.v_dim - v0);
+                const AttnOperand q = {a.mq[i] + q_at, {a.Eq[0] + q_at, a.Eq[1] + q_at}, q_row}, p = {a.mp[i] + p_at, {a.Ep[0] + p_at, a.Ep[1] + p_at}, p_row};
+                const AttnOperand S = {a.ms[i] + s_at + v0, {a.Es[0] + s_at + v0, a.Es[1] + s_at + v0}, (size_t)a.v_dim};
+                const AttnOperand v = {a.mv[i] + v_at + v0, {a.Ev[0] + v_at + v0, a.Ev[1] + v_at + v0}, v_row};
+                // what the near part is added to waits in the result's place, where the same thread finds it again
+                attn_product<true, false, VEC>(s, turn, S, wide, q, rows, a.k_dim, i, -1, true, ok, [&](int row, int r, u64 z) {
+                    const size_t o = o_at + r * o_row + v0 + row;
+                    z += __ldg(a.qs[i] + o);
+                    a.O[i][o] = __ldg(a.pv[i] + o) + __ldg(w + r0 + r + 1) * attn_trunc(z, i, a.f);
+                });
+                attn_product<true, false, VEC>(s, turn, v, wide, p, rows, keys, i, r0, a.C % 2 == 0, ok, [&](int row, int r, u64 z) {
+                    const size_t o = o_at + r * o_row + v0 + row;
+                    a.O[i][o] = attn_trunc(a.O[i][o] + z, i, a.f);
+                });
+            }
     }
+    attn_tile_end(s, a.error);
 }
 
 // ---------------------------------------------------------------------------
