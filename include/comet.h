@@ -648,7 +648,8 @@ typedef struct {
 } comet_linear_attention_args;
 int comet_linear_attention(void* cuda_stream, const comet_linear_attention_args* args);
 /* Bytes of workspace that comet_linear_attention takes for these sizes.  Errors: INVALID_ARG, SHAPE. */
-int comet_linear_attention_workspace(int32_t chunks, int32_t kv_heads, int32_t k_dim, int32_t v_dim, int64_t* bytes_out);
+int comet_linear_attention_workspace(int32_t tokens, int32_t chunks, int32_t q_heads, int32_t kv_heads, int32_t k_dim, int32_t v_dim, int32_t chunk,
+                                     int64_t* bytes_out);
 
 typedef struct {
     int32_t batch, q_heads, kv_heads, k_dim, v_dim;

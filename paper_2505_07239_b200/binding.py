@@ -151,7 +151,7 @@ def _load():
     lib.comet_linear_workspace.argtypes = [i32, i32, i32, ctypes.POINTER(i64)]
     lib.comet_norm_rotate.argtypes = [vp, ctypes.POINTER(CometNormRotateArgs)]
     lib.comet_linear_attention.argtypes = [vp, ctypes.POINTER(CometLinearAttentionArgs)]
-    lib.comet_linear_attention_workspace.argtypes = [i32, i32, i32, i32, ctypes.POINTER(i64)]
+    lib.comet_linear_attention_workspace.argtypes = [i32] * 7 + [ctypes.POINTER(i64)]
     lib.comet_linear_attention_step.argtypes = [vp, ctypes.POINTER(CometLinearAttentionStepArgs)]
     lib.comet_group_norm.argtypes = [vp, ctypes.POINTER(CometGroupNormArgs)]
     lib.comet_group_norm_workspace.argtypes = [i32, i32, i32, i32, ctypes.POINTER(i64)]

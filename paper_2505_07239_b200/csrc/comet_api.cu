@@ -2503,7 +2503,19 @@ bool attn_heads(int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim)
            v_dim % 2 == 0 && k_dim <= at::MAX_DIM && v_dim <= at::MAX_DIM;
 }
 bool attn_stride(int64_t stride, int64_t tokens, int64_t row) { return stride >= 0 && stride <= 1ll << 32 && (tokens == 1 || stride >= row); }
-size_t attn_workspace(int64_t chunks, int64_t kv_heads, int64_t k_dim, int64_t v_dim) { return (size_t)(2 * chunks * kv_heads * k_dim * v_dim) * sizeof(u64); }
+// The workspace in words: the products d v^T of both parties; the opened states, queries, keys, decayed keys, values and weights.  All are even.
+struct AttnRoom {
+    int64_t kv, q, k, v, p;
+    AttnRoom(int64_t tokens, int64_t chunks, int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim, int64_t chunk)
+        : kv(chunks * kv_heads * k_dim * v_dim), q(tokens * q_heads * k_dim), k(tokens * kv_heads * k_dim), v(tokens * kv_heads * v_dim),
+          p(tokens * q_heads * chunk) {}
+    size_t bytes() const { return kv ? (size_t)(3 * kv + q + 2 * k + v + p) * sizeof(u64) : 0; }
+};
+
+bool attn_sizes(int64_t tokens, int64_t chunks, int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim, int64_t chunk) {
+    return attn_heads(q_heads, kv_heads, k_dim, v_dim) && chunk >= 1 && chunk <= comet::attn::MAX_CHUNK && tokens >= 1 && tokens <= ATTN_MAX_SIZE &&
+           chunks >= 0 && chunks <= ATTN_MAX_SIZE && tokens * q_heads <= ATTN_MAX_ROWS && chunks * q_heads <= ATTN_MAX_ROWS;
+}
 
 // A pair of arguments: where it is, its words, whether it may be absent.
 struct SpanPair {
@@ -2534,22 +2546,21 @@ void give(u64* to[2], uint64_t* const from[2]) {
 
 }  // namespace
 
-extern "C" int comet_linear_attention_workspace(int32_t chunks, int32_t kv_heads, int32_t k_dim, int32_t v_dim, int64_t* bytes_out) {
+extern "C" int comet_linear_attention_workspace(int32_t tokens, int32_t chunks, int32_t q_heads, int32_t kv_heads, int32_t k_dim, int32_t v_dim,
+                                                int32_t chunk, int64_t* bytes_out) {
     if (!bytes_out) return COMET_ERR_INVALID_ARG;
-    if (chunks < 0 || chunks > ATTN_MAX_SIZE || !attn_heads(kv_heads, kv_heads, k_dim, v_dim) || (int64_t)chunks * kv_heads > ATTN_MAX_ROWS)
-        return COMET_ERR_SHAPE;
-    *bytes_out = (int64_t)attn_workspace(chunks, kv_heads, k_dim, v_dim);
+    if (!attn_sizes(tokens, chunks, q_heads, kv_heads, k_dim, v_dim, chunk)) return COMET_ERR_SHAPE;
+    *bytes_out = (int64_t)AttnRoom(tokens, chunks, q_heads, kv_heads, k_dim, v_dim, chunk).bytes();
     return COMET_OK;
 }
 
 extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_attention_args* g) {
     namespace at = comet::attn;
     if (!g) return COMET_ERR_INVALID_ARG;
-    if (!attn_heads(g->q_heads, g->kv_heads, g->k_dim, g->v_dim) || g->chunk < 1 || g->chunk > at::MAX_CHUNK) return COMET_ERR_SHAPE;
-    if (g->tokens < 1 || g->sequences < 1 || g->chunks < 0 || g->tokens > ATTN_MAX_SIZE || g->sequences > ATTN_MAX_SIZE || g->chunks > ATTN_MAX_SIZE)
-        return COMET_ERR_SHAPE;
+    if (!attn_sizes(g->tokens, g->chunks, g->q_heads, g->kv_heads, g->k_dim, g->v_dim, g->chunk)) return COMET_ERR_SHAPE;
+    if (g->sequences < 1 || g->sequences > ATTN_MAX_SIZE) return COMET_ERR_SHAPE;
     const int64_t T = g->tokens, n = g->chunks, Hq = g->q_heads, Hk = g->kv_heads, Dk = g->k_dim, Dv = g->v_dim;
-    if (T * Hq > ATTN_MAX_ROWS || n * Hq > ATTN_MAX_ROWS || g->sequences * Hk > ATTN_MAX_ROWS) return COMET_ERR_SHAPE;
+    if (g->sequences * Hk > ATTN_MAX_ROWS) return COMET_ERR_SHAPE;
     if (!attn_stride(g->q_stride, T, Hq * Dk) || !attn_stride(g->k_stride, T, Hk * Dk) || !attn_stride(g->v_stride, T, Hk * Dv)) return COMET_ERR_SHAPE;
     if (g->frac_bits < 1 || g->frac_bits > 31) return COMET_ERR_SHAPE;
     if (!g->starts || !g->decay || reinterpret_cast<uintptr_t>(g->starts) % sizeof(int32_t) || reinterpret_cast<uintptr_t>(g->decay) % sizeof(u64) ||
@@ -2572,7 +2583,8 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
     const bool in_place = g->state[0] && g->state[0] == g->state_out[0] && g->state[1] == g->state_out[1];
     if (pair_halved(g->state) || (!in_place && !span_pairs({{g->state, st, true}}, spans))) return COMET_ERR_INVALID_ARG;
     if (outputs_overlap(spans.data(), outputs, (int)spans.size())) return COMET_ERR_INVALID_ARG;
-    const size_t need = attn_workspace(n, Hk, Dk, Dv);
+    const AttnRoom room(T, n, Hq, Hk, Dk, Dv, g->chunk);
+    const size_t need = room.bytes();
     if (need && !g->workspace) return COMET_ERR_INVALID_ARG;
     if (g->workspace_bytes < (int64_t)need) return COMET_ERR_SHAPE;
     comet::AttnArgs a;
@@ -2582,7 +2594,14 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
     give(a.qk, g->qk); give(a.pv, g->pv); give(a.qs, g->qs); give(a.dv, g->dv); give(a.S0, g->state);
     give(a.Eq, g->Eq); give(a.Ek, g->Ek); give(a.Ev, g->Ev); give(a.Ed, g->Ed); give(a.Ep, g->Ep); give(a.Es, g->Es); give(a.O, g->O);
     give(a.S1, g->state_out);
-    for (int i = 0; i < 2; ++i) a.kv[i] = static_cast<u64*>(g->workspace) + i * s;
+    u64* piece = static_cast<u64*>(g->workspace);
+    auto take = [&](int64_t words) {
+        u64* const p = piece;
+        piece += words;
+        return p;
+    };
+    a.kv[0] = take(room.kv); a.kv[1] = take(room.kv); a.s = take(room.kv); a.q = take(room.q); a.k = take(room.k); a.d = take(room.k);
+    a.v = take(room.v); a.p = take(room.p);
     a.decay = reinterpret_cast<const u64*>(g->decay);
     a.starts = g->starts;
     a.bad_starts = g->bad_starts_flag;
@@ -2596,20 +2615,24 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
         return COMET_ERR_CUDA;
     }
     a.error = dev.error;
-    // two words at once where an operand's rows begin on 16-byte boundaries (their lengths are even)
+    // two words at once where all rows begin on 16-byte boundaries (their lengths are even)
+    auto even = [](const u64* const p[2], int64_t stride) { return aligned16(p[0]) && aligned16(p[1]) && stride % 2 == 0; };
+    a.in_vec = even(a.Q, T > 1 ? a.q_stride : 0) && even(a.K, T > 1 ? a.k_stride : 0) && even(a.V, T > 1 ? a.v_stride : 0);
     bool vec = true;
     for (int i = 0; i < 2; ++i)
-        for (const void* p : {(const void*)a.mq[i], (const void*)a.mk[i], (const void*)a.mp[i], (const void*)a.Eq[i], (const void*)a.Ek[i], (const void*)a.Ep[i]})
+        for (const u64* p : {a.mq[i], a.mk[i], a.mv[i], a.md[i], a.mp[i], a.ms[i], a.S0[i], (const u64*)a.Eq[i], (const u64*)a.Ek[i], (const u64*)a.Ev[i],
+                             (const u64*)a.Ed[i], (const u64*)a.Es[i], (const u64*)a.S1[i]})
             vec = vec && aligned16(p);
-    const int pieces = ceil_div(a.k_dim * a.v_dim, at::THREADS), tiles = ceil_div(a.C, at::TILE);
+    const int pieces = ceil_div(a.k_dim * a.v_dim, 2 * at::THREADS);
     cudaError_t err = cudaSuccess;
     if (n) err = launch_chained(vec ? comet::attn_keys_kernel<true> : comet::attn_keys_kernel<false>, dim3((unsigned)(n * Hk)), dim3(at::TILE_THREADS),
                                 at::TILE_SMEM, stream, nullptr, a);
     if (err == cudaSuccess)
-        err = launch_chained(comet::attn_state_kernel, dim3((unsigned)(g->sequences * Hk * pieces), 2), dim3(at::THREADS), 0, stream, nullptr, a, pieces);
+        err = launch_chained(vec ? comet::attn_state_kernel<true> : comet::attn_state_kernel<false>, dim3((unsigned)(g->sequences * Hk * pieces)),
+                             dim3(at::THREADS), 0, stream, nullptr, a, pieces);
     if (err == cudaSuccess && n)
-        err = launch_chained(vec ? comet::attn_rows_kernel<true> : comet::attn_rows_kernel<false>, dim3((unsigned)(n * Hq * tiles)), dim3(at::TILE_THREADS),
-                             at::TILE_SMEM, stream, nullptr, a, tiles);
+        err = launch_chained(vec ? comet::attn_rows_kernel<true> : comet::attn_rows_kernel<false>, dim3((unsigned)(n * Hq)), dim3(at::TILE_THREADS), at::TILE_SMEM,
+                             stream, nullptr, a);
     if (err != cudaSuccess) cudaGetLastError();
     return err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
 }

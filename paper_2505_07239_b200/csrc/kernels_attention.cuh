@@ -20,9 +20,13 @@ namespace comet {
 
 namespace attn {
 constexpr int MAX_CHUNK = 64, MAX_DIM = 256;
-constexpr int THREADS = 256;
-constexpr int TILE = 32;                             // columns of a tile of a product
-constexpr int TILE_THREADS = THREADS + 32;           // eight warps that convert, one that issues MMAs
+constexpr int THREADS = 256;                         // of the kernels without products
+constexpr int ROWS = 128, TILE = 64;                 // of a tile of a product: rows, columns
+constexpr int CONVERTERS = 16, DRAINERS = 8, WORKERS = 32 * (CONVERTERS + DRAINERS), ISSUER = CONVERTERS + DRAINERS;
+constexpr int TILE_THREADS = WORKERS + 32;
+constexpr int SLOTS = 4;                             // of planes: one of the two products of 32 indices each
+constexpr int LEFT_PLANE = ROWS * limb::KC, RIGHT_PLANE = TILE * limb::KC, LEFT_BYTES = limb::PLANES * LEFT_PLANE;
+constexpr int SLOT_BYTES = LEFT_BYTES + limb::PLANES * RIGHT_PLANE, TILE_SMEM = SLOTS * SLOT_BYTES + 128, ACC_COLS = limb::PLANES * TILE;
 }  // namespace attn
 
 struct AttnArgs {
@@ -34,17 +38,15 @@ struct AttnArgs {
     u64* O[2];
     u64* S1[2];
     u64* kv[2];                                                          // [chunks][kv_heads][k_dim][v_dim]: sum d v^T at scale 2f
+    u64* q; u64* k; u64* v; u64* d; u64* p; u64* s;                      // opened values, as their messages lie
     const u64* decay;                                                    // [kv_heads][C + 1]
     const int32_t* starts;
     int32_t* bad_starts;
     long long q_stride, k_stride, v_stride;
     int tokens, sequences, q_heads, kv_heads, k_dim, v_dim, C, chunks, f;
+    int in_vec;                                                          // 16-byte accesses of Q, K and V
     int* error;                                                          // set where a wait ran out
 };
-
-__device__ __forceinline__ u64 attn_trunc(u64 v, int party, int bits) {
-    return party ? 0ull - ((0ull - v) >> bits) : v >> bits;
-}
 
 // Tokens of sequence j, which begin at *begin: none where the starts are not ascending or leave the tokens.
 __device__ __forceinline__ int attn_length(const AttnArgs& a, int j, int* begin) {
@@ -90,120 +92,127 @@ __device__ __forceinline__ AttnChunk attn_find(const AttnArgs& a, int want) {
     return found;
 }
 
-// The opening of `rows` x `cols` words by the first THREADS threads: x(i, r, c) the shares, masks and messages `row` words apart from token to token.
-template <typename F>
-__device__ __forceinline__ void attn_open(F&& x, const u64* const mask[2], u64* const msg[2], size_t at, size_t row, int rows, int cols) {
-#pragma unroll 4
-    for (int t = threadIdx.x; t < rows * cols; t += attn::THREADS) {
-        const int r = t / cols, c = t - r * cols;
-        const size_t o = at + (size_t)r * row + c;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) msg[i][o] = x(i, r, c) - __ldg(mask[i] + o);
+template <bool VEC>
+__device__ __forceinline__ ulonglong2 attn_load2(const u64* p) {         // words that nobody else reads
+    if (VEC) return __ldcs(reinterpret_cast<const ulonglong2*>(p));
+    return make_ulonglong2(__ldcs(p), __ldcs(p + 1));
+}
+template <bool VEC>
+__device__ __forceinline__ void attn_store2(u64* p, ulonglong2 v) {
+    if (VEC) {
+        *reinterpret_cast<ulonglong2*>(p) = v;
+    } else {
+        p[0] = v.x;
+        p[1] = v.y;
     }
 }
 
+__device__ __forceinline__ ulonglong2 attn_input2(const u64* p, int vec) { return vec ? attn_load2<true>(p) : attn_load2<false>(p); }
+__device__ __forceinline__ ulonglong2 attn_sub(ulonglong2 x, ulonglong2 y) { return make_ulonglong2(x.x - y.x, x.y - y.y); }
+__device__ __forceinline__ ulonglong2 attn_add(ulonglong2 x, ulonglong2 y) { return make_ulonglong2(x.x + y.x, x.y + y.y); }
+__device__ __forceinline__ u64 attn_rescale(u64 v, int party, int f) { return party ? 0ull - norm_shift(0ull - v, f) : norm_shift(v, f); }
+
 // ---------------------------------------------------------------------------
-// Products on the int8 tensor cores.  A CTA works out tiles of 128 x TILE words of Z_i = (triple) + E B_i + V_i F, V_i = A_i + i E (Eq. 1), one party's
-// after the other's, from words in memory: eight warps turn 32 contraction indices of either product at a time into limb planes in shared memory
-// (two slots), a ninth issues the MMAs (kernels_limb.cuh has the decomposition and the layout), and the eight read the sums out of
-// tensor memory.  Left operands, 128 rows, are keys, values or states, right ones, TILE rows, queries, weights or decayed keys; rows past an
-// operand's are whatever lies in shared memory and their sums are never looked at.  Half an SM's tensor and shared memory per CTA, so that one CTA
-// converts, opens or drains while the other's MMAs run.
+// Products on the int8 tensor cores.  A CTA works out tiles of ROWS x TILE words of Z_i = (triple) + E B_i + V_i F, V_i = A_i + i E (Eq. 1), one
+// party's after the other's, from words in memory, masks and opened values: sixteen warps turn 32 contraction indices of either product at
+// a time into limb planes in shared memory (kernels_limb.cuh has the decomposition and the layout), a warp issues the MMAs, eight warps read the
+// sums out of tensor memory.  Left operands are keys, values or states, right ones queries, weights or decayed keys; rows past an operand's are
+// whatever lies in shared memory, and their sums are never looked at.
 // ---------------------------------------------------------------------------
 struct AttnOperand {
     const u64* mask;                     // the party's
-    const u64* msg[2];
+    const u64* open;                     // the opened value
     size_t step;                         // words from row to row; of a DEEP operand, whose rows lie side by side, from index to index
 };
-enum AttnWords { MASK, MESSAGES, BOTH };                 // of a plane set: the mask, the opened value, their sum
+enum AttnWords { MASK, OPEN, BOTH };     // of a plane set: the mask, the opened value, their sum
 
-template <AttnWords WHAT>
-__device__ __forceinline__ u64 attn_word(const AttnOperand& x, size_t at, bool masked) {
-    u64 v = 0ull;
-    if (WHAT != MASK) v = x.msg[0][at] + x.msg[1][at];
-    if (WHAT != MESSAGES && masked) v += x.mask[at];
-    return v;
-}
-// Planes of `rows` rows, indices k0 .. k0 + 31 of `depth`, zero from `depth` on.  causal >= 0: row r has masks up to index causal + r only
-// (its messages are zero beyond).
-template <AttnWords WHAT, bool DEEP, bool VEC>
-__device__ __forceinline__ void attn_planes(uint8_t* planes, int plane_bytes, const AttnOperand& x, int rows, int k0, int depth, int causal) {
+// A thread's words of the planes of `rows` rows, indices k0 .. k0 + 31 of `depth` (zero from there on), and where they go: four of one row.  TASKS
+// covers ROWS rows of a DEEP operand (2), TILE rows of either kind (1).
+template <int TASKS>
+struct AttnCell {
+    u64 w[TASKS][4];
+    int to[TASKS];                       // in a plane, -1: nothing
+};
+// causal >= 0: row r has masks up to index causal + r only (its opened values are zero beyond).
+template <AttnWords WHAT, bool DEEP, bool VEC, int TASKS>
+__device__ __forceinline__ void attn_read(AttnCell<TASKS>& c, const AttnOperand& x, int rows, int k0, int depth, int causal) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (DEEP) {
-        // eight rows x four of the eight groups of indices a warp: 64-byte pieces of memory, 128 bytes of a plane
-        const int tasks = (rows + 7) / 8 * 2;
-#pragma unroll 2
-        for (int t = warp; t < tasks; t += attn::THREADS / 32) {
-            const int row = (t >> 1) * 8 + (lane & 7), c = (t & 1) * 4 + (lane >> 3);
-            u64 w[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = k0 + 2 * c + (j & 1) + 16 * (j >> 1);
-                w[j] = row < rows && k < depth ? attn_word<WHAT>(x, k * x.step + row, true) : 0ull;
-            }
-            limb_emit4(planes + (row >> 3) * 256 + (c >> 2) * 128 + (row & 7) * 16 + (c & 3) * 4, plane_bytes, w);
+    for (int t = 0; t < TASKS; ++t) {
+        int row, g;                      // limb_emit4's order: indices 2g, 2g + 1, 16 + 2g, 17 + 2g
+        if (DEEP) {
+            // eight rows x four groups of indices a warp: 64-byte pieces of memory, 128 bytes of a plane
+            const int task = warp + t * attn::CONVERTERS;
+            row = (task >> 1) * 8 + (lane & 7);
+            g = (task & 1) * 4 + (lane >> 3);
+        } else {
+            // lanes of the upper groups take the row four further, against bank conflicts
+            g = lane & 7;
+            row = 4 * (2 * (warp >> 1) + ((warp & 1) ^ (g >> 2))) + (lane >> 3);
         }
-    } else {
-        // limb_emit4's order; lanes of the upper groups take the row four further, against bank conflicts
-        const int c = lane & 7, sub = 4 * (2 * (warp >> 1) + ((warp & 1) ^ (c >> 2))) + (lane >> 3);
-#pragma unroll 2
-        for (int row = sub; row < rows; row += 32) {
-            u64 w[4];
+        c.to[t] = row < rows ? (row >> 3) * 256 + (g >> 2) * 128 + (row & 7) * 16 + (g & 3) * 4 : -1;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int k = k0 + 16 * h + 2 * c;
-                const size_t at = row * x.step + k;
-                const int last = causal >= 0 ? causal + row : depth;
-                if (VEC) {
-                    ulonglong2 v = make_ulonglong2(0ull, 0ull);
+        for (int h = 0; h < 2; ++h) {
+            const int k = k0 + 16 * h + 2 * g, last = causal >= 0 ? causal + row : depth;
+            u64 v[2] = {0ull, 0ull};
+            if (row < rows) {
+                if (!DEEP && VEC) {
                     if (k < depth) {
+                        const size_t at = row * x.step + k;
                         if (WHAT != MASK) {
-                            const ulonglong2 e = *reinterpret_cast<const ulonglong2*>(x.msg[0] + at), g = *reinterpret_cast<const ulonglong2*>(x.msg[1] + at);
-                            v = make_ulonglong2(e.x + g.x, e.y + g.y);
+                            const ulonglong2 e = *reinterpret_cast<const ulonglong2*>(x.open + at);
+                            v[0] = e.x;
+                            v[1] = e.y;
                         }
-                        if (WHAT != MESSAGES) {
+                        if (WHAT != OPEN) {
                             const ulonglong2 m = __ldg(reinterpret_cast<const ulonglong2*>(x.mask + at));
-                            if (k <= last) v.x += m.x;
-                            if (k + 1 <= last) v.y += m.y;
+                            if (k <= last) v[0] += m.x;
+                            if (k + 1 <= last) v[1] += m.y;
                         }
                     }
-                    w[2 * h] = v.x;
-                    w[2 * h + 1] = v.y;
                 } else {
-                    w[2 * h] = k < depth ? attn_word<WHAT>(x, at, k <= last) : 0ull;
-                    w[2 * h + 1] = k + 1 < depth ? attn_word<WHAT>(x, at + 1, k + 1 <= last) : 0ull;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        if (k + j < depth) {
+                            const size_t at = DEEP ? (k + j) * x.step + row : row * x.step + k + j;
+                            if (WHAT != MASK) v[j] = x.open[at];
+                            if (WHAT != OPEN && k + j <= last) v[j] += __ldg(x.mask + at);
+                        }
                 }
             }
-            limb_emit4(planes + (row >> 3) * 256 + (c >> 2) * 128 + (row & 7) * 16 + (c & 3) * 4, plane_bytes, w);
+            c.w[t][2 * h] = v[0];
+            c.w[t][2 * h + 1] = v[1];
         }
     }
+}
+template <int TASKS>
+__device__ __forceinline__ void attn_emit(uint8_t* planes, int plane_bytes, const AttnCell<TASKS>& c) {
+#pragma unroll
+    for (int t = 0; t < TASKS; ++t)
+        if (c.to[t] >= 0) limb_emit4(planes + c.to[t], plane_bytes, c.w[t]);
 }
 
 // What a CTA's warps share.
 struct AttnTile {
-    uint64_t full[2], empty[2], acc_full, acc_empty;
+    uint64_t full[attn::SLOTS], empty[attn::SLOTS], acc_full, acc_empty, weights;
     uint32_t tmem;
     int abort_flag;
-    uint8_t* planes;                     // two slots
+    uint8_t* planes;
 };
-namespace attn {
-constexpr int LEFT_PLANE = 128 * limb::KC, RIGHT_PLANE = TILE * limb::KC, LEFT_BYTES = limb::PLANES * LEFT_PLANE;
-constexpr int SLOT_BYTES = LEFT_BYTES + limb::PLANES * RIGHT_PLANE, TILE_SMEM = 2 * SLOT_BYTES + 128, ACC_COLS = limb::PLANES * TILE;
-}  // namespace attn
-
 __device__ __forceinline__ void attn_tile_begin(AttnTile& s, uint8_t* raw) {
     if (threadIdx.x == 0) {
-        for (int k = 0; k < 2; ++k) {
-            ptx::mbar_init(ptx::smem_u32(&s.full[k]), attn::THREADS / 32);
+        for (int k = 0; k < attn::SLOTS; ++k) {
+            ptx::mbar_init(ptx::smem_u32(&s.full[k]), attn::CONVERTERS);
             ptx::mbar_init(ptx::smem_u32(&s.empty[k]), 1);
         }
         ptx::mbar_init(ptx::smem_u32(&s.acc_full), 1);
-        ptx::mbar_init(ptx::smem_u32(&s.acc_empty), attn::THREADS / 32);
+        ptx::mbar_init(ptx::smem_u32(&s.acc_empty), attn::DRAINERS);
+        ptx::mbar_init(ptx::smem_u32(&s.weights), attn::DRAINERS);
         s.abort_flag = 0;
         s.planes = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
         ptx::fence_barrier_init();
     }
-    if (threadIdx.x >= attn::THREADS) {
+    if (threadIdx.x >> 5 == attn::ISSUER) {
         ptx::tmem_alloc(ptx::smem_u32(&s.tmem), attn::ACC_COLS);
         ptx::tmem_relinquish();
     }
@@ -219,82 +228,99 @@ __device__ __forceinline__ void attn_tile_end(AttnTile& s, int* error) {
         *error = 1;
         __threadfence_system();
     }
-    if (threadIdx.x >= attn::THREADS) {
+    if (threadIdx.x >> 5 == attn::ISSUER) {
         ptx::fence_after_sync();
         ptx::tmem_dealloc(s.tmem, attn::ACC_COLS);
     }
 }
-// The eight converting warps wait for one another.
-__device__ __forceinline__ void attn_meet() { asm volatile("bar.sync 1, %0;" ::"n"(attn::THREADS) : "memory"); }
+// All warps but the issuer wait for one another.
+__device__ __forceinline__ void attn_meet() { asm volatile("bar.sync 1, %0;" ::"n"(attn::WORKERS) : "memory"); }
 
-// Where a warp is in the order of slots and tiles; the converting warps and the issuing one count alike.
+// Where a warp is in the order of slots and tiles; all count alike.
 struct AttnTurn {
     uint32_t stage = 0, tile = 0;
+    bool ok = true;
 };
-// The issuing warp's part of a tile: `stages` plane sets, each one product of 32 indices.
-__device__ __forceinline__ void attn_issue(AttnTile& s, AttnTurn& turn, int stages, bool& ok) {
-    if (ptx::elect_one() && ok) {
-        constexpr uint32_t IDESC = (2u << 4) | (128u >> 4 << 24);
-        ok = limb_wait(ptx::smem_u32(&s.acc_empty), (turn.tile & 1u) ^ 1u, &s.abort_flag);
+__device__ __forceinline__ int attn_blocks(int depth) { return (depth + limb::KC - 1) / limb::KC; }
+
+// The issuing warp's part of a tile.
+__device__ __forceinline__ void attn_issue(AttnTile& s, AttnTurn& turn, int depth) {
+    const int stages = 2 * attn_blocks(depth);
+    if (ptx::elect_one() && turn.ok) {
+        constexpr uint32_t IDESC = (2u << 4) | ((uint32_t)(attn::ROWS >> 4) << 24);
+        bool ok = limb_wait(ptx::smem_u32(&s.acc_empty), (turn.tile & 1u) ^ 1u, &s.abort_flag);
         ptx::fence_after_sync();
         for (int t = 0; t < stages && ok; ++t) {
-            const uint32_t n = turn.stage + t, slot = n & 1u;
-            ok = limb_wait(ptx::smem_u32(&s.full[slot]), n >> 1 & 1u, &s.abort_flag);
+            const uint32_t n = turn.stage + t, slot = n % attn::SLOTS;
+            ok = limb_wait(ptx::smem_u32(&s.full[slot]), n / attn::SLOTS & 1u, &s.abort_flag);
             if (!ok) break;
             ptx::fence_after_sync();
             const uint32_t left = limb_desc_lo(ptx::smem_u32(s.planes) + slot * attn::SLOT_BYTES), right = left + (attn::LEFT_BYTES >> 4);
+            const uint32_t acc = t > 0 ? 1u : 0u;
 #pragma unroll
-            for (int q = 0; q < limb::PLANES; ++q)
-                ptx::mma_i8(s.tmem + attn::TILE * q, left + (q * attn::LEFT_PLANE >> 4), LIMB_DESC_HI, right, LIMB_DESC_HI,
-                            IDESC | ((uint32_t)(attn::TILE * (limb::PLANES - q)) >> 3 << 17), t > 0 || q > 0 ? 1u : 0u);
+            for (int i = 0; i < limb::PLANES; ++i) {
+                // wide and narrow instructions alternate, plane 0, which overwrites all sums, first
+                const int p = i & 1 ? limb::PLANES - 1 - (i >> 1) : i >> 1, n_total = attn::TILE * (limb::PLANES - p);
+                const uint32_t at = left + (p * attn::LEFT_PLANE >> 4), acc_p = p == 0 ? acc : 1u;
+                if (n_total > 256) {
+                    ptx::mma_i8_keep_a(s.tmem + attn::TILE * p, at, LIMB_DESC_HI, right, LIMB_DESC_HI, IDESC | (256u >> 3 << 17), acc_p);
+                    ptx::mma_i8_reuse_a(s.tmem + attn::TILE * p + 256, at, LIMB_DESC_HI, right + (256 * limb::KC >> 4), LIMB_DESC_HI,
+                                        IDESC | ((uint32_t)(n_total - 256) >> 3 << 17), acc_p);
+                } else {
+                    ptx::mma_i8(s.tmem + attn::TILE * p, at, LIMB_DESC_HI, right, LIMB_DESC_HI, IDESC | ((uint32_t)n_total >> 3 << 17), acc_p);
+                }
+            }
             ptx::mma_commit(ptx::smem_u32(&s.empty[slot]));
         }
         if (ok) ptx::mma_commit(ptx::smem_u32(&s.acc_full));
+        turn.ok = ok;
     }
     turn.stage += stages;
     ++turn.tile;
 }
-// The converting warps' part: planes of both products, 32 indices at a time, then the sums: done(row, column, product) for this thread's row, one
-// of four columns after the other.
-template <bool DEEP_LEFT, bool DEEP_RIGHT, bool VEC, typename F>
-__device__ __forceinline__ void attn_product(AttnTile& s, AttnTurn& turn, const AttnOperand& left, int rows, const AttnOperand& right, int cols, int depth,
-                                             int party, int causal, bool right_vec, bool& ok, F&& done) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int k0 = 0; k0 < depth; k0 += limb::KC)
-#pragma unroll
-        for (int second = 0; second < 2; ++second) {
-            const uint32_t n = turn.stage++, slot = n & 1u;
-            ok = ok && limb_wait(ptx::smem_u32(&s.empty[slot]), (n >> 1 & 1u) ^ 1u, &s.abort_flag);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) continue;
-            uint8_t* const l = s.planes + slot * attn::SLOT_BYTES;
-            uint8_t* const r = l + attn::LEFT_BYTES;
-            auto convert_right = [&](auto what) {
-                constexpr AttnWords WHAT = decltype(what)::value;
-                if (VEC && right_vec) attn_planes<WHAT, DEEP_RIGHT, true>(r, attn::RIGHT_PLANE, right, cols, k0, depth, causal);
-                else attn_planes<WHAT, DEEP_RIGHT, false>(r, attn::RIGHT_PLANE, right, cols, k0, depth, causal);
-            };
-            if (second == 0) {
-                attn_planes<MASK, DEEP_LEFT, VEC>(l, attn::LEFT_PLANE, left, rows, k0, depth, -1);
-                convert_right(std::integral_constant<AttnWords, MESSAGES>{});
-            } else {
-                attn_planes<MESSAGES, DEEP_LEFT, VEC>(l, attn::LEFT_PLANE, left, rows, k0, depth, -1);
-                if (party) convert_right(std::integral_constant<AttnWords, BOTH>{});
-                else convert_right(std::integral_constant<AttnWords, MASK>{});
-            }
-            ptx::fence_proxy_async_smem();                   // the planes are read by the tensor cores
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&s.full[slot]));
-        }
-    ok = ok && limb_wait_warp(ptx::smem_u32(&s.acc_full), turn.tile & 1u, &s.abort_flag);
+// The converting warps' part: planes of both products, 32 indices at a time.  A stage's words are asked for before the wait for its slot.
+template <bool DEEP_LEFT, bool DEEP_RIGHT, bool VEC>
+__device__ __forceinline__ void attn_convert(AttnTile& s, AttnTurn& turn, const AttnOperand& left, int rows, const AttnOperand& right, int cols, int depth,
+                                             int party, int causal) {
+    const int lane = threadIdx.x & 31;
+    auto put = [&](const auto& l, const auto& r) {
+        const uint32_t n = turn.stage++, slot = n % attn::SLOTS;
+        turn.ok = turn.ok && limb_wait(ptx::smem_u32(&s.empty[slot]), (n / attn::SLOTS & 1u) ^ 1u, &s.abort_flag);
+        turn.ok = __all_sync(0xffffffffu, turn.ok);
+        if (!turn.ok) return;
+        uint8_t* const at = s.planes + slot * attn::SLOT_BYTES;
+        attn_emit(at, attn::LEFT_PLANE, l);
+        attn_emit(at + attn::LEFT_BYTES, attn::RIGHT_PLANE, r);
+        ptx::fence_proxy_async_smem();                       // the planes are read by the tensor cores
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&s.full[slot]));
+    };
+    constexpr int TASKS = DEEP_LEFT ? 2 : 1;
+    for (int k0 = 0; k0 < depth; k0 += limb::KC) {
+        AttnCell<TASKS> l;
+        AttnCell<1> r;
+        attn_read<MASK, DEEP_LEFT, VEC>(l, left, rows, k0, depth, -1);
+        attn_read<OPEN, DEEP_RIGHT, VEC>(r, right, cols, k0, depth, causal);
+        put(l, r);
+        attn_read<OPEN, DEEP_LEFT, VEC>(l, left, rows, k0, depth, -1);
+        if (party) attn_read<BOTH, DEEP_RIGHT, VEC>(r, right, cols, k0, depth, causal);
+        else attn_read<MASK, DEEP_RIGHT, VEC>(r, right, cols, k0, depth, causal);
+        put(l, r);
+    }
+}
+// The draining warps' part: the sums, done(row, column, sum) for this thread's row, a quarter of the columns' halves after the other.
+template <typename F>
+__device__ __forceinline__ void attn_drain(AttnTile& s, AttnTurn& turn, int rows, int cols, F&& done) {
+    const int warp = (threadIdx.x >> 5) - attn::CONVERTERS, lane = threadIdx.x & 31, quarter = warp & 3;
+    turn.ok = turn.ok && limb_wait_warp(ptx::smem_u32(&s.acc_full), turn.tile & 1u, &s.abort_flag);
     ++turn.tile;
-    if (!ok) return;
+    if (!turn.ok) return;
     ptx::fence_after_sync();
-    const int row = (warp & 3) * 32 + lane;
-    const uint32_t acc = s.tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    if ((warp & 3) * 32 < rows) {
+    const int row = quarter * 32 + lane, c0 = (warp >> 2) * (attn::TILE / 2), c1 = min(c0 + attn::TILE / 2, cols);
+    const uint32_t acc = s.tmem + ((uint32_t)(quarter * 32) << 16);
+    if (quarter * 32 < rows) {
 #pragma unroll 1
-        for (int c = (warp >> 2) * (attn::TILE / 2); c < min((warp >> 2) * (attn::TILE / 2) + attn::TILE / 2, cols); c += 4) {
+        for (int c = c0; c < c1; c += 4) {
             uint32_t d[limb::PLANES][4];
 #pragma unroll
             for (int p = 0; p < limb::PLANES; ++p) ptx::tmem_ld4(acc + attn::TILE * p + c, d[p]);
@@ -302,159 +328,231 @@ __device__ __forceinline__ void attn_product(AttnTile& s, AttnTurn& turn, const 
             if (row < rows)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (c + j < cols) done(row, c + j, limb_recombine(d[0][j], d[1][j], d[2][j], d[3][j], d[4][j], d[5][j], d[6][j], d[7][j]));
+                    if (c + j < c1) done(row, c + j, limb_recombine(d[0][j], d[1][j], d[2][j], d[3][j], d[4][j], d[5][j], d[6][j], d[7][j]));
         }
     }
     ptx::fence_before_sync();
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&s.acc_empty));
 }
-__device__ __forceinline__ int attn_stages(int depth) { return 2 * ((depth + limb::KC - 1) / limb::KC); }
 
 // Messages of k, v and d of one chunk and key head, and its sum of d v^T.
 template <bool VEC>
-__global__ void __launch_bounds__(attn::TILE_THREADS, 2)
+__global__ void __launch_bounds__(attn::TILE_THREADS, 1)
 attn_keys_kernel(const __grid_constant__ AttnArgs a) {
     extern __shared__ uint8_t attn_smem[];
     __shared__ AttnTile s;
     pdl_wait();
     pdl_launch_dependents();
-    const int c = blockIdx.x / a.kv_heads, h = blockIdx.x - c * a.kv_heads;
+    const int c = blockIdx.x / a.kv_heads, h = blockIdx.x - c * a.kv_heads, warp = threadIdx.x >> 5;
     const AttnChunk at = attn_find(a, c);
     if (at.len == 0) return;
     attn_tile_begin(s, attn_smem);
     AttnTurn turn;
-    bool ok = true;
-    if (threadIdx.x >= attn::THREADS) {
-        for (int i = 0; i < 2; ++i)
-            for (int v0 = 0; v0 < a.v_dim; v0 += 128)
-                for (int k0 = 0; k0 < a.k_dim; k0 += attn::TILE) attn_issue(s, turn, attn_stages(at.len), ok);
-    } else {
-        const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
-        const size_t k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
-        auto key = [&](int i, int r, int j) { return __ldg(a.K[i] + (size_t)(at.first + r) * a.k_stride + (size_t)h * a.k_dim + j); };
-        const u64* w = a.decay + (size_t)h * (a.C + 1);
-        attn_open(key, a.mk, a.Ek, k_at, k_row, at.len, a.k_dim);
-        attn_open([&](int i, int r, int j) { return attn_trunc(key(i, r, j) * __ldg(w + at.len - 1 - r), i, a.f); }, a.md, a.Ed, k_at, k_row, at.len, a.k_dim);
-        attn_open([&](int i, int r, int j) { return __ldg(a.V[i] + (size_t)(at.first + r) * a.v_stride + (size_t)h * a.v_dim + j); }, a.mv, a.Ev,
-                  v_at, v_row, at.len, a.v_dim);
+    const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
+    const size_t k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
+    if (warp != attn::ISSUER) {
+        const u64* const w = a.decay + (size_t)h * (a.C + 1) + at.len - 1;
+#pragma unroll 2
+        for (int t = threadIdx.x; t < at.len * (a.k_dim / 2); t += attn::WORKERS) {
+            const int r = t / (a.k_dim / 2), j = 2 * (t - r * (a.k_dim / 2));
+            const size_t o = k_at + r * k_row + j, x_at = (size_t)(at.first + r) * a.k_stride + (size_t)h * a.k_dim + j;
+            const u64 weight = __ldg(w - r);
+            ulonglong2 k = make_ulonglong2(0ull, 0ull), d = k;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const ulonglong2 x = attn_input2(a.K[i] + x_at, a.in_vec), e = attn_sub(x, attn_load2<VEC>(a.mk[i] + o));
+                const ulonglong2 y = make_ulonglong2(attn_rescale(x.x * weight, i, a.f), attn_rescale(x.y * weight, i, a.f)), g = attn_sub(y, attn_load2<VEC>(a.md[i] + o));
+                attn_store2<VEC>(a.Ek[i] + o, e);
+                attn_store2<VEC>(a.Ed[i] + o, g);
+                k = attn_add(k, e);                          // the exchange
+                d = attn_add(d, g);
+            }
+            attn_store2<VEC>(a.k + o, k);
+            attn_store2<VEC>(a.d + o, d);
+        }
+#pragma unroll 2
+        for (int t = threadIdx.x; t < at.len * (a.v_dim / 2); t += attn::WORKERS) {
+            const int r = t / (a.v_dim / 2), j = 2 * (t - r * (a.v_dim / 2));
+            const size_t o = v_at + r * v_row + j, x_at = (size_t)(at.first + r) * a.v_stride + (size_t)h * a.v_dim + j;
+            ulonglong2 v = make_ulonglong2(0ull, 0ull);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const ulonglong2 e = attn_sub(attn_input2(a.V[i] + x_at, a.in_vec), attn_load2<VEC>(a.mv[i] + o));
+                attn_store2<VEC>(a.Ev[i] + o, e);
+                v = attn_add(v, e);
+            }
+            attn_store2<VEC>(a.v + o, v);
+        }
         attn_meet();
-        const size_t out = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
-        for (int i = 0; i < 2; ++i)
-            for (int v0 = 0; v0 < a.v_dim; v0 += 128) {
-                const AttnOperand v = {a.mv[i] + v_at + v0, {a.Ev[0] + v_at + v0, a.Ev[1] + v_at + v0}, v_row};
-                for (int k0 = 0; k0 < a.k_dim; k0 += attn::TILE) {
-                    const AttnOperand d = {a.md[i] + k_at + k0, {a.Ed[0] + k_at + k0, a.Ed[1] + k_at + k0}, k_row};
-                    attn_product<true, true, VEC>(s, turn, v, min(128, a.v_dim - v0), d, min(attn::TILE, a.k_dim - k0), at.len, i, -1, true, ok,
-                                                  [&](int row, int col, u64 z) {
-                                                      const size_t o = out + (size_t)(k0 + col) * a.v_dim + v0 + row;
-                                                      a.kv[i][o] = __ldcs(a.dv[i] + o) + z;
-                                                  });
+    }
+    const size_t out = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
+    for (int i = 0; i < 2; ++i)
+        for (int v0 = 0; v0 < a.v_dim; v0 += attn::ROWS)
+            for (int k0 = 0; k0 < a.k_dim; k0 += attn::TILE) {
+                const int rows = min(attn::ROWS, a.v_dim - v0), cols = min(attn::TILE, a.k_dim - k0);
+                if (warp == attn::ISSUER) {
+                    attn_issue(s, turn, at.len);
+                } else if (warp < attn::CONVERTERS) {
+                    const AttnOperand v = {a.mv[i] + v_at + v0, a.v + v_at + v0, v_row}, d = {a.md[i] + k_at + k0, a.d + k_at + k0, k_row};
+                    attn_convert<true, true, VEC>(s, turn, v, rows, d, cols, at.len, i, -1);
+                } else {
+                    attn_drain(s, turn, rows, cols, [&](int row, int col, u64 z) {
+                        const size_t o = out + (size_t)(k0 + col) * a.v_dim + v0 + row;
+                        a.kv[i][o] = __ldcs(a.dv[i] + o) + z;
+                    });
                 }
             }
-    }
     attn_tile_end(s, a.error);
 }
 
-// The state from chunk to chunk of a sequence and key head, a word of a party a thread; says whether the starts were in order.
+// The state from chunk to chunk of a sequence and key head, two words of both parties a thread; says whether the starts were in order.
+template <bool VEC>
 __global__ void __launch_bounds__(attn::THREADS)
 attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
     __shared__ int before;
     pdl_wait();
     pdl_launch_dependents();
     const int j = blockIdx.x / (a.kv_heads * pieces), rest = blockIdx.x - j * a.kv_heads * pieces, h = rest / pieces;
-    const int party = blockIdx.y, word = (rest - h * pieces) * attn::THREADS + threadIdx.x, words = a.k_dim * a.v_dim;
+    const int word = 2 * ((rest - h * pieces) * attn::THREADS + threadIdx.x), words = a.k_dim * a.v_dim;
     if (threadIdx.x == 0) before = 0;
     __syncthreads();
-    const bool checks = blockIdx.x == 0 && party == 0;
+    const bool checks = blockIdx.x == 0;
     int sum = 0, begin;
     bool bad = false;
     for (int s = threadIdx.x; s < (checks ? a.sequences : j); s += attn::THREADS) {
-        const int len = attn_length(a, s, &begin);
-        if (s < j || checks) sum += (len + a.C - 1) / a.C;
-        bad |= begin < 0 || __ldg(a.starts + s + 1) < begin || __ldg(a.starts + s + 1) > a.tokens;
+        sum += (attn_length(a, s, &begin) + a.C - 1) / a.C;
+        const int end = __ldg(a.starts + s + 1);
+        bad |= begin < 0 || end < begin || end > a.tokens;
     }
     if (sum) atomicAdd(&before, sum);
     if (bad && checks && a.bad_starts) *a.bad_starts = 1;
     __syncthreads();
     if (checks && threadIdx.x == 0 && before != a.chunks && a.bad_starts) *a.bad_starts = 1;
-    int c = checks ? 0 : before;
     if (word >= words) return;
-    const size_t at = ((size_t)j * a.kv_heads + h) * words + word;
-    u64 S = a.S0[party] ? a.S0[party][at] : 0ull;
-    const u64* w = a.decay + (size_t)h * (a.C + 1);
-    for (int left = attn_length(a, j, &begin); left > 0 && c < a.chunks; left -= a.C, ++c) {
-        const size_t o = ((size_t)c * a.kv_heads + h) * words + word;
-        a.Es[party][o] = S - __ldg(a.ms[party] + o);
-        S = attn_trunc(__ldg(w + min(left, a.C)) * S + a.kv[party][o], party, a.f);
+    const size_t at = ((size_t)j * a.kv_heads + h) * words + word, step = (size_t)a.kv_heads * words;
+    const u64* const w = a.decay + (size_t)h * (a.C + 1);
+    int c = checks ? 0 : before, left = attn_length(a, j, &begin);
+    const int end = min(a.chunks, c + (left + a.C - 1) / a.C);
+    ulonglong2 S[2], kv[2], ms[2];
+    size_t o = ((size_t)c * a.kv_heads + h) * words + word;
+    auto load = [&] {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            kv[i] = attn_load2<VEC>(a.kv[i] + o);
+            ms[i] = attn_load2<VEC>(a.ms[i] + o);
+        }
+    };
+    if (c < end) load();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) S[i] = a.S0[i] ? attn_load2<VEC>(a.S0[i] + at) : make_ulonglong2(0ull, 0ull);
+    for (; c < end; ++c, left -= a.C) {
+        const u64 weight = __ldg(w + min(left, a.C));
+        ulonglong2 e[2];
+        const size_t here = o;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            e[i] = attn_sub(S[i], ms[i]);
+            S[i] = make_ulonglong2(attn_rescale(weight * S[i].x + kv[i].x, i, a.f), attn_rescale(weight * S[i].y + kv[i].y, i, a.f));
+        }
+        o += step;
+        if (c + 1 < end) load();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) attn_store2<VEC>(a.Es[i] + here, e[i]);
+        attn_store2<VEC>(a.s + here, attn_add(e[0], e[1]));              // the exchange
     }
-    a.S1[party][at] = S;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) attn_store2<VEC>(a.S1[i] + at, S[i]);
 }
 
-// Everything else of TILE rows of a chunk and query head.
+// Everything else of a chunk and query head.
 template <bool VEC>
-__global__ void __launch_bounds__(attn::TILE_THREADS, 2)
-attn_rows_kernel(const __grid_constant__ AttnArgs a, int tiles) {
+__global__ void __launch_bounds__(attn::TILE_THREADS, 1)
+attn_rows_kernel(const __grid_constant__ AttnArgs a) {
     extern __shared__ uint8_t attn_smem[];
     __shared__ AttnTile s;
     pdl_wait();
     pdl_launch_dependents();
-    const int c = blockIdx.x / (a.q_heads * tiles), rest = blockIdx.x - c * a.q_heads * tiles, hq = rest / tiles, r0 = (rest - hq * tiles) * attn::TILE;
+    const int c = blockIdx.x / a.q_heads, hq = blockIdx.x - c * a.q_heads, h = hq / (a.q_heads / a.kv_heads), warp = threadIdx.x >> 5;
     const AttnChunk at = attn_find(a, c);
-    if (r0 >= at.len) return;
-    const int h = hq / (a.q_heads / a.kv_heads), rows = min(attn::TILE, at.len - r0), keys = r0 + rows;
+    if (at.len == 0) return;
     attn_tile_begin(s, attn_smem);
     AttnTurn turn;
-    bool ok = true;
-    if (threadIdx.x >= attn::THREADS) {
-        for (int i = 0; i < 2; ++i) attn_issue(s, turn, attn_stages(a.k_dim), ok);
-        for (int i = 0; i < 2; ++i)
-            for (int v0 = 0; v0 < a.v_dim; v0 += 128) {
-                attn_issue(s, turn, attn_stages(a.k_dim), ok);
-                attn_issue(s, turn, attn_stages(keys), ok);
+    const int rows = at.len;
+    const size_t q_row = (size_t)a.q_heads * a.k_dim, p_row = (size_t)a.q_heads * a.C, o_row = (size_t)a.q_heads * a.v_dim;
+    const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
+    const size_t q_at = at.first * q_row + (size_t)hq * a.k_dim, p_at = at.first * p_row + (size_t)hq * a.C, o_at = at.first * o_row + (size_t)hq * a.v_dim;
+    const size_t k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
+    const size_t s_at = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
+    const u64* const w = a.decay + (size_t)h * (a.C + 1);
+    if (warp != attn::ISSUER) {
+#pragma unroll 2
+        for (int t = threadIdx.x; t < rows * (a.k_dim / 2); t += attn::WORKERS) {
+            const int r = t / (a.k_dim / 2), j = 2 * (t - r * (a.k_dim / 2));
+            const size_t o = q_at + r * q_row + j, x_at = (size_t)(at.first + r) * a.q_stride + (size_t)hq * a.k_dim + j;
+            ulonglong2 q = make_ulonglong2(0ull, 0ull);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const ulonglong2 e = attn_sub(attn_input2(a.Q[i] + x_at, a.in_vec), attn_load2<VEC>(a.mq[i] + o));
+                attn_store2<VEC>(a.Eq[i] + o, e);
+                q = attn_add(q, e);                          // the exchange
             }
-    } else {
-        const size_t q_row = (size_t)a.q_heads * a.k_dim, p_row = (size_t)a.q_heads * a.C, o_row = (size_t)a.q_heads * a.v_dim;
-        const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
-        const size_t first = (size_t)at.first + r0, q_at = first * q_row + (size_t)hq * a.k_dim, p_at = first * p_row + (size_t)hq * a.C;
-        const size_t o_at = first * o_row + (size_t)hq * a.v_dim, k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
-        const size_t s_at = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
-        const u64* w = a.decay + (size_t)h * (a.C + 1);
-        attn_open([&](int i, int r, int j) { return __ldg(a.Q[i] + (first + r) * a.q_stride + (size_t)hq * a.k_dim + j); }, a.mq, a.Eq, q_at, q_row, rows, a.k_dim);
+            attn_store2<VEC>(a.q + o, q);
+        }
         // off the triangle nothing is sent
-        for (int t = threadIdx.x; t < rows * a.C; t += attn::THREADS) {
+        for (int t = threadIdx.x; t < rows * a.C; t += attn::WORKERS) {
             const int r = t / a.C, k = t - r * a.C;
-            if (k > r0 + r) a.Ep[0][p_at + r * p_row + k] = a.Ep[1][p_at + r * p_row + k] = 0ull;
+            if (k > r) a.Ep[0][p_at + r * p_row + k] = a.Ep[1][p_at + r * p_row + k] = a.p[p_at + r * p_row + k] = 0ull;
         }
         attn_meet();
-        for (int i = 0; i < 2; ++i) {
-            const AttnOperand k = {a.mk[i] + k_at, {a.Ek[0] + k_at, a.Ek[1] + k_at}, k_row}, q = {a.mq[i] + q_at, {a.Eq[0] + q_at, a.Eq[1] + q_at}, q_row};
-            attn_product<false, false, VEC>(s, turn, k, keys, q, rows, a.k_dim, i, -1, true, ok, [&](int key, int r, u64 z) {
-                if (key > r0 + r) return;
+    }
+    for (int i = 0; i < 2; ++i) {
+        const AttnOperand k = {a.mk[i] + k_at, a.k + k_at, k_row}, q = {a.mq[i] + q_at, a.q + q_at, q_row};
+        if (warp == attn::ISSUER) {
+            attn_issue(s, turn, a.k_dim);
+        } else if (warp < attn::CONVERTERS) {
+            attn_convert<false, false, VEC>(s, turn, k, rows, q, rows, a.k_dim, i, -1);
+        } else {
+            attn_drain(s, turn, rows, rows, [&](int key, int r, u64 z) {
+                if (key > r) return;
                 const size_t o = p_at + r * p_row + key;
                 z += __ldg(a.qk[i] + o);
-                a.Ep[i][o] = attn_trunc(attn_trunc(z, i, a.f) * __ldg(w + r0 + r - key), i, a.f) - __ldg(a.mp[i] + o);
+                const u64 e = attn_rescale(attn_rescale(z, i, a.f) * __ldg(w + r - key), i, a.f) - __ldg(a.mp[i] + o);
+                a.Ep[i][o] = e;
+                a.p[o] = i ? a.p[o] + e : e;                 // the exchange; this thread's own
             });
         }
-        attn_meet();
-        for (int i = 0; i < 2; ++i)
-            for (int v0 = 0; v0 < a.v_dim; v0 += 128) {
-                const int wide = min(128, a.v_dim - v0);
-                const AttnOperand q = {a.mq[i] + q_at, {a.Eq[0] + q_at, a.Eq[1] + q_at}, q_row}, p = {a.mp[i] + p_at, {a.Ep[0] + p_at, a.Ep[1] + p_at}, p_row};
-                const AttnOperand S = {a.ms[i] + s_at + v0, {a.Es[0] + s_at + v0, a.Es[1] + s_at + v0}, (size_t)a.v_dim};
-                const AttnOperand v = {a.mv[i] + v_at + v0, {a.Ev[0] + v_at + v0, a.Ev[1] + v_at + v0}, v_row};
+    }
+    if (warp >= attn::CONVERTERS && warp < attn::ISSUER) {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(ptx::smem_u32(&s.weights));
+    }
+    for (int i = 0; i < 2; ++i)
+        for (int v0 = 0; v0 < a.v_dim; v0 += attn::ROWS) {
+            const int wide = min(attn::ROWS, a.v_dim - v0);
+            if (warp == attn::ISSUER) {
+                attn_issue(s, turn, a.k_dim);
+                attn_issue(s, turn, rows);
+            } else if (warp < attn::CONVERTERS) {
+                const AttnOperand q = {a.mq[i] + q_at, a.q + q_at, q_row}, p = {a.mp[i] + p_at, a.p + p_at, p_row};
+                const AttnOperand S = {a.ms[i] + s_at + v0, a.s + s_at + v0, (size_t)a.v_dim}, v = {a.mv[i] + v_at + v0, a.v + v_at + v0, v_row};
+                attn_convert<true, false, VEC>(s, turn, S, wide, q, rows, a.k_dim, i, -1);
+                if (i == 0 && v0 == 0) turn.ok = turn.ok && limb_wait_warp(ptx::smem_u32(&s.weights), 0, &s.abort_flag);
+                if (a.C % 2 == 0) attn_convert<true, false, VEC>(s, turn, v, wide, p, rows, rows, i, 0);
+                else attn_convert<true, false, false>(s, turn, v, wide, p, rows, rows, i, 0);
+            } else {
                 // what the near part is added to waits in the result's place, where the same thread finds it again
-                attn_product<true, false, VEC>(s, turn, S, wide, q, rows, a.k_dim, i, -1, true, ok, [&](int row, int r, u64 z) {
+                attn_drain(s, turn, wide, rows, [&](int row, int r, u64 z) {
                     const size_t o = o_at + r * o_row + v0 + row;
                     z += __ldg(a.qs[i] + o);
-                    a.O[i][o] = __ldg(a.pv[i] + o) + __ldg(w + r0 + r + 1) * attn_trunc(z, i, a.f);
+                    a.O[i][o] = __ldg(a.pv[i] + o) + __ldg(w + r + 1) * attn_rescale(z, i, a.f);
                 });
-                attn_product<true, false, VEC>(s, turn, v, wide, p, rows, keys, i, r0, a.C % 2 == 0, ok, [&](int row, int r, u64 z) {
+                attn_drain(s, turn, wide, rows, [&](int row, int r, u64 z) {
                     const size_t o = o_at + r * o_row + v0 + row;
-                    a.O[i][o] = attn_trunc(a.O[i][o] + z, i, a.f);
+                    a.O[i][o] = attn_rescale(a.O[i][o] + z, i, a.f);
                 });
             }
-    }
+        }
     attn_tile_end(s, a.error);
 }
 
@@ -482,21 +580,6 @@ struct AttnStepArgs {
 // `heads` heads; the sums of o of every thread.
 __host__ __device__ constexpr int attn_step_smem(int k_dim, int heads) {
     return 3 * (1 + heads) * k_dim * 8 + heads * attn::THREADS * 2 * 16;
-}
-
-template <bool VEC>
-__device__ __forceinline__ ulonglong2 attn_load2(const u64* p) {         // words that nobody else reads
-    if (VEC) return __ldcs(reinterpret_cast<const ulonglong2*>(p));
-    return make_ulonglong2(__ldcs(p), __ldcs(p + 1));
-}
-template <bool VEC>
-__device__ __forceinline__ void attn_store2(u64* p, ulonglong2 v) {
-    if (VEC) {
-        *reinterpret_cast<ulonglong2*>(p) = v;
-    } else {
-        p[0] = v.x;
-        p[1] = v.y;
-    }
 }
 
 // HEADS query heads of a key head's are worked on at a time; those beyond read masks and messages of the state a second time.
@@ -573,9 +656,8 @@ attn_step_kernel(const __grid_constant__ AttnStepArgs a) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const u64 A = keys[3 * r + 1 + i];
-                        u64 x = kv[i].x + E * mv[i].x + A * F.x + w * S[i].x, y = kv[i].y + E * mv[i].y + A * F.y + w * S[i].y;
-                        x = i ? 0ull - norm_shift(0ull - x, f) : norm_shift(x, f);
-                        y = i ? 0ull - norm_shift(0ull - y, f) : norm_shift(y, f);
+                        const u64 x = attn_rescale(kv[i].x + E * mv[i].x + A * F.x + w * S[i].x, i, f);
+                        const u64 y = attn_rescale(kv[i].y + E * mv[i].y + A * F.y + w * S[i].y, i, f);
                         mask[i] = ms[i];
                         e[i] = make_ulonglong2(x - mask[i].x, y - mask[i].y);
                         attn_store2<VEC>(a.S1[i] + at, make_ulonglong2(x, y));
@@ -617,7 +699,7 @@ attn_step_kernel(const __grid_constant__ AttnStepArgs a) {
             const size_t at = o_at + (size_t)(g0 + g) * a.v_dim + 2 * c;
             z.x += __ldg(a.qs[i] + at);
             z.y += __ldg(a.qs[i] + at + 1);
-            attn_store2<false>(a.O[i] + at, make_ulonglong2(attn_trunc(z.x, i, f), attn_trunc(z.y, i, f)));
+            attn_store2<false>(a.O[i] + at, make_ulonglong2(attn_rescale(z.x, i, f), attn_rescale(z.y, i, f)));
         }
         __syncthreads();
     }

@@ -751,7 +751,7 @@ PyObject* linear_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
         std::optional<c10::Stream> on;
         if (!stream_of(args[0], x.device(), &on)) return nullptr;
         const OnStream guard(x.device(), *on);
-        int code = T >= 1 ? comet_linear_attention_workspace(g.chunks, g.kv_heads, g.k_dim, g.v_dim, &g.workspace_bytes) : COMET_ERR_SHAPE;
+        int code = T >= 1 ? comet_linear_attention_workspace(g.tokens, g.chunks, g.q_heads, g.kv_heads, g.k_dim, g.v_dim, g.chunk, &g.workspace_bytes) : COMET_ERR_SHAPE;
         if (code != COMET_OK) return done(code);
         Results results(x);
         results.pair(Results::MESSAGE, q, Eq, g.Eq);

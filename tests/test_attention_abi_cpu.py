@@ -18,8 +18,10 @@ def prompt_args(cb, T=9, S=3, Hq=4, Hk=2, Dk=6, Dv=4, C=4, chunks=5):
         setattr(a, name, at.pair(sizes[like.get(name, name)]))
     a.starts, a.bad_starts_flag = at.pair(S + 1)
     a.decay, _ = at.pair(Hk * (C + 1))
-    a.workspace, _ = at.pair(2 * chunks * Hk * Dk * Dv)
-    a.workspace_bytes = 16 * chunks * Hk * Dk * Dv
+    need = ctypes.c_int64()
+    assert cb.library().comet_linear_attention_workspace(T, chunks, Hq, Hk, Dk, Dv, C, ctypes.byref(need)) == 0
+    a.workspace, _ = at.pair(need.value // 8)
+    a.workspace_bytes = need.value
     return a
 
 
@@ -91,10 +93,11 @@ def test_prompt_refusals(cb):  # noqa: F811
                dict(q_stride=(1 << 32) + 1), dict(frac_bits=0), dict(frac_bits=32), dict(tokens=(1 << 20) + 1), dict(sequences=(1 << 20) + 1),
                dict(chunks=(1 << 20) + 1), dict(tokens=1 << 20, q_heads=18), dict(chunks=1 << 20, q_heads=18), dict(workspace_bytes=64)):
         assert call(**kw) == -2, kw
-    assert lib.comet_linear_attention_workspace(4, 2, 6, 4, None) == -1
+    assert lib.comet_linear_attention_workspace(9, 4, 4, 2, 6, 4, 8, None) == -1
     out = ctypes.c_int64()
-    assert lib.comet_linear_attention_workspace(4, 2, 7, 4, ctypes.byref(out)) == -2
-    assert lib.comet_linear_attention_workspace(0, 2, 6, 4, ctypes.byref(out)) == 0 and out.value == 0
+    assert lib.comet_linear_attention_workspace(9, 4, 4, 2, 7, 4, 8, ctypes.byref(out)) == -2
+    assert lib.comet_linear_attention_workspace(9, 4, 4, 2, 6, 4, 65, ctypes.byref(out)) == -2
+    assert lib.comet_linear_attention_workspace(9, 0, 4, 2, 6, 4, 8, ctypes.byref(out)) == 0 and out.value == 0
 
 
 STEP_IN = ("Q", "K", "V", "mq", "mk", "mv", "ms", "kv", "qs")

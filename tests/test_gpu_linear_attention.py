@@ -188,7 +188,7 @@ def run_raw(cb, case, fill=None):
     flag = torch.zeros(1, dtype=torch.int32, device="cuda")
     a.bad_starts_flag = flag.data_ptr()
     need = ctypes.c_int64()
-    assert cb.library().comet_linear_attention_workspace(n, Hk, Dk, Dv, ctypes.byref(need)) == 0
+    assert cb.library().comet_linear_attention_workspace(T, n, Hq, Hk, Dk, Dv, C, ctypes.byref(need)) == 0
     room = torch.zeros(need.value // 8 + 32, dtype=torch.int64, device="cuda")
     a.workspace, a.workspace_bytes = room.data_ptr(), need.value
     stream = torch.cuda.current_stream().cuda_stream
