@@ -611,8 +611,8 @@ int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args* args);
  * default stream) and the call does not wait for it.  `workspace` is 256-byte aligned and has at least the bytes that
  * comet_linear_attention_workspace reports for these sizes; a captured call keeps its address, and calls whose work may overlap in
  * time need one each.
- * Errors: INVALID_ARG (null or unaligned pointer, overlap), SHAPE (a size below 1, but for chunks; kv_heads not a divisor of q_heads; k_dim or v_dim
- * odd or above 256; chunk above 64; tokens, sequences or chunks above 2^20; tokens * q_heads or chunks * q_heads above 2^24; batch *
+ * Errors: INVALID_ARG (null or unaligned pointer, overlap), SHAPE (a size below 1, but for chunks; kv_heads not a divisor of q_heads; q_heads above
+ * 4096; k_dim or v_dim odd or above 256; chunk above 64; tokens, sequences or chunks above 2^20; tokens * q_heads or chunks * q_heads above 2^24; batch *
  * q_heads above 2^24; a stride below its heads' words or above 2^32; frac_bits outside [1, 31]; workspace too small), CUDA. */
 typedef struct {
     int32_t tokens, sequences, q_heads, kv_heads, k_dim, v_dim, chunk, chunks;

@@ -2495,21 +2495,22 @@ extern "C" int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args
 // ---------------------------------------------------------------------------
 namespace {
 
-constexpr int64_t ATTN_MAX_SIZE = 1 << 20, ATTN_MAX_ROWS = 1 << 24;
+constexpr int64_t ATTN_MAX_SIZE = 1 << 20, ATTN_MAX_ROWS = 1 << 24, ATTN_MAX_HEADS = 1 << 12;    // (a chunk of a tensor spans less than 2^29 words)
 
 bool attn_heads(int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim) {
     namespace at = comet::attn;
-    return q_heads >= 1 && kv_heads >= 1 && q_heads <= ATTN_MAX_SIZE && q_heads % kv_heads == 0 && k_dim >= 2 && v_dim >= 2 && k_dim % 2 == 0 &&
+    return q_heads >= 1 && kv_heads >= 1 && q_heads <= ATTN_MAX_HEADS && q_heads % kv_heads == 0 && k_dim >= 2 && v_dim >= 2 && k_dim % 2 == 0 &&
            v_dim % 2 == 0 && k_dim <= at::MAX_DIM && v_dim <= at::MAX_DIM;
 }
 bool attn_stride(int64_t stride, int64_t tokens, int64_t row) { return stride >= 0 && stride <= 1ll << 32 && (tokens == 1 || stride >= row); }
-// The workspace in words: the products d v^T of both parties; the opened states, queries, keys, decayed keys, values and weights.  All are even.
+// The workspace in words: the products d v^T of both parties; the opened states, queries, keys, decayed keys and values, which
+// are even, and the opened weights and their masks.
 struct AttnRoom {
     int64_t kv, q, k, v, p;
     AttnRoom(int64_t tokens, int64_t chunks, int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim, int64_t chunk)
         : kv(chunks * kv_heads * k_dim * v_dim), q(tokens * q_heads * k_dim), k(tokens * kv_heads * k_dim), v(tokens * kv_heads * v_dim),
-          p(tokens * q_heads * chunk) {}
-    size_t bytes() const { return kv ? (size_t)(3 * kv + q + 2 * k + v + p) * sizeof(u64) : 0; }
+          p(tokens * q_heads * (chunk + chunk % 2)) {}
+    size_t bytes() const { return kv ? (size_t)(3 * kv + q + 2 * k + v + 3 * p) * sizeof(u64) : 0; }
 };
 
 bool attn_sizes(int64_t tokens, int64_t chunks, int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim, int64_t chunk) {
@@ -2601,7 +2602,7 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
         return p;
     };
     a.kv[0] = take(room.kv); a.kv[1] = take(room.kv); a.s = take(room.kv); a.q = take(room.q); a.k = take(room.k); a.d = take(room.k);
-    a.v = take(room.v); a.p = take(room.p);
+    a.v = take(room.v); a.p = take(room.p); a.pm[0] = take(room.p); a.pm[1] = take(room.p);
     a.decay = reinterpret_cast<const u64*>(g->decay);
     a.starts = g->starts;
     a.bad_starts = g->bad_starts_flag;

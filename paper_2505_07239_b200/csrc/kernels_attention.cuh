@@ -38,7 +38,8 @@ struct AttnArgs {
     u64* O[2];
     u64* S1[2];
     u64* kv[2];                                                          // [chunks][kv_heads][k_dim][v_dim]: sum d v^T at scale 2f
-    u64* q; u64* k; u64* v; u64* d; u64* p; u64* s;                      // opened values, as their messages lie
+    u64* q; u64* k; u64* v; u64* d; u64* s;                              // opened values, as their messages lie
+    u64* p; u64* pm[2];                                                  // opened weights and their masks, zero off the triangle
     const u64* decay;                                                    // [kv_heads][C + 1]
     const int32_t* starts;
     int32_t* bad_starts;
@@ -122,75 +123,76 @@ __device__ __forceinline__ u64 attn_rescale(u64 v, int party, int f) { return pa
 struct AttnOperand {
     const u64* mask;                     // the party's
     const u64* open;                     // the opened value
-    size_t step;                         // words from row to row; of a DEEP operand, whose rows lie side by side, from index to index
+    uint32_t step;                       // words from row to row; of a DEEP operand, whose rows lie side by side, from index to index
 };
 enum AttnWords { MASK, OPEN, BOTH };     // of a plane set: the mask, the opened value, their sum
 
-// A thread's words of the planes of `rows` rows, indices k0 .. k0 + 31 of `depth` (zero from there on), and where they go: four of one row.  TASKS
-// covers ROWS rows of a DEEP operand (2), TILE rows of either kind (1).
-template <int TASKS>
-struct AttnCell {
-    u64 w[TASKS][4];
-    int to[TASKS];                       // in a plane, -1: nothing
-};
-// causal >= 0: row r has masks up to index causal + r only (its opened values are zero beyond).
-template <AttnWords WHAT, bool DEEP, bool VEC, int TASKS>
-__device__ __forceinline__ void attn_read(AttnCell<TASKS>& c, const AttnOperand& x, int rows, int k0, int depth, int causal) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-#pragma unroll
-    for (int t = 0; t < TASKS; ++t) {
-        int row, g;                      // limb_emit4's order: indices 2g, 2g + 1, 16 + 2g, 17 + 2g
+// A thread's cells of the planes of `rows` rows: four words of a row, indices 2g, 2g + 1, 16 + 2g, 17 + 2g of every 32 (limb_emit4's order).  A DEEP
+// operand of up to ROWS rows has TASKS = 2 of them, TILE rows apart, else there is one.  Places are counted in 32 bits: an operand spans less than
+// 2^29 words (comet_linear_attention sees to that).
+template <bool DEEP, int TASKS>
+struct AttnCells {
+    uint32_t at;                                 // of the first word, from the operand's on
+    int to, row, g;                              // to: in a plane
+
+    __device__ __forceinline__ AttnCells(const AttnOperand& x) {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
         if (DEEP) {
             // eight rows x four groups of indices a warp: 64-byte pieces of memory, 128 bytes of a plane
-            const int task = warp + t * attn::CONVERTERS;
-            row = (task >> 1) * 8 + (lane & 7);
-            g = (task & 1) * 4 + (lane >> 3);
+            row = (warp >> 1) * 8 + (lane & 7);
+            g = (warp & 1) * 4 + (lane >> 3);
         } else {
             // lanes of the upper groups take the row four further, against bank conflicts
             g = lane & 7;
             row = 4 * (2 * (warp >> 1) + ((warp & 1) ^ (g >> 2))) + (lane >> 3);
         }
-        c.to[t] = row < rows ? (row >> 3) * 256 + (g >> 2) * 128 + (row & 7) * 16 + (g & 3) * 4 : -1;
+        to = (row >> 3) * 256 + (g >> 2) * 128 + (row & 7) * 16 + (g & 3) * 4;
+        at = DEEP ? 2 * g * x.step + row : row * x.step + 2 * g;
+    }
+    // Of the 32 indices from k0 on; those from `depth` on are zero.
+    template <AttnWords WHAT, bool VEC>
+    __device__ __forceinline__ void read(const AttnOperand& x, u64 (&w)[TASKS][4], int rows, int k0, int depth) const {
+        const uint32_t from = at + (DEEP ? k0 * x.step : k0);
+        const int left = depth - k0 - 2 * g;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int k = k0 + 16 * h + 2 * g, last = causal >= 0 ? causal + row : depth;
-            u64 v[2] = {0ull, 0ull};
-            if (row < rows) {
-                if (!DEEP && VEC) {
-                    if (k < depth) {
-                        const size_t at = row * x.step + k;
+        for (int t = 0; t < TASKS; ++t) {
+            const bool live = row + t * attn::TILE < rows;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u64 v[2] = {0ull, 0ull};
+                if (!DEEP && VEC) {              // (rows are even in length, zero behind an odd depth)
+                    if (live && 16 * h < left) {
                         if (WHAT != MASK) {
-                            const ulonglong2 e = *reinterpret_cast<const ulonglong2*>(x.open + at);
+                            const ulonglong2 e = *reinterpret_cast<const ulonglong2*>(x.open + (from + 16 * h));
                             v[0] = e.x;
                             v[1] = e.y;
                         }
                         if (WHAT != OPEN) {
-                            const ulonglong2 m = __ldg(reinterpret_cast<const ulonglong2*>(x.mask + at));
-                            if (k <= last) v[0] += m.x;
-                            if (k + 1 <= last) v[1] += m.y;
+                            const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(x.mask + (from + 16 * h));
+                            v[0] += m.x;
+                            v[1] += m.y;
                         }
                     }
                 } else {
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
-                        if (k + j < depth) {
-                            const size_t at = DEEP ? (k + j) * x.step + row : row * x.step + k + j;
-                            if (WHAT != MASK) v[j] = x.open[at];
-                            if (WHAT != OPEN && k + j <= last) v[j] += __ldg(x.mask + at);
+                        if (live && 16 * h + j < left) {
+                            const uint32_t o = from + (DEEP ? x.step : 1u) * (16 * h + j) + t * attn::TILE;
+                            if (WHAT != MASK) v[j] = x.open[o];
+                            if (WHAT != OPEN) v[j] += x.mask[o];
                         }
                 }
+                w[t][2 * h] = v[0];
+                w[t][2 * h + 1] = v[1];
             }
-            c.w[t][2 * h] = v[0];
-            c.w[t][2 * h + 1] = v[1];
         }
     }
-}
-template <int TASKS>
-__device__ __forceinline__ void attn_emit(uint8_t* planes, int plane_bytes, const AttnCell<TASKS>& c) {
+    __device__ __forceinline__ void emit(uint8_t* planes, int plane_bytes, const u64 (&w)[TASKS][4], int rows) const {
 #pragma unroll
-    for (int t = 0; t < TASKS; ++t)
-        if (c.to[t] >= 0) limb_emit4(planes + c.to[t], plane_bytes, c.w[t]);
-}
+        for (int t = 0; t < TASKS; ++t)
+            if (row + t * attn::TILE < rows) limb_emit4(planes + to + t * (attn::TILE / 8 * 256), plane_bytes, w[t]);
+    }
+};
 
 // What a CTA's warps share.
 struct AttnTile {
@@ -212,6 +214,7 @@ __device__ __forceinline__ void attn_tile_begin(AttnTile& s, uint8_t* raw) {
         s.planes = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
         ptx::fence_barrier_init();
     }
+    __syncwarp();
     if (threadIdx.x >> 5 == attn::ISSUER) {
         ptx::tmem_alloc(ptx::smem_u32(&s.tmem), attn::ACC_COLS);
         ptx::tmem_relinquish();
@@ -233,8 +236,12 @@ __device__ __forceinline__ void attn_tile_end(AttnTile& s, int* error) {
         ptx::tmem_dealloc(s.tmem, attn::ACC_COLS);
     }
 }
-// All warps but the issuer wait for one another.
-__device__ __forceinline__ void attn_meet() { asm volatile("bar.sync 1, %0;" ::"n"(attn::WORKERS) : "memory"); }
+// All warps but the issuer wait for one another.  (A warp comes to a barrier, and to a read of tensor memory, as a whole: both are
+// undefined for lanes on their own, and what stands before may have parted them.)
+__device__ __forceinline__ void attn_meet() {
+    __syncwarp();
+    asm volatile("bar.sync 1, %0;" ::"n"(attn::WORKERS) : "memory");
+}
 
 // Where a warp is in the order of slots and tiles; all count alike.
 struct AttnTurn {
@@ -246,6 +253,7 @@ __device__ __forceinline__ int attn_blocks(int depth) { return (depth + limb::KC
 // The issuing warp's part of a tile.
 __device__ __forceinline__ void attn_issue(AttnTile& s, AttnTurn& turn, int depth) {
     const int stages = 2 * attn_blocks(depth);
+    __syncwarp();
     if (ptx::elect_one() && turn.ok) {
         constexpr uint32_t IDESC = (2u << 4) | ((uint32_t)(attn::ROWS >> 4) << 24);
         bool ok = limb_wait(ptx::smem_u32(&s.acc_empty), (turn.tile & 1u) ^ 1u, &s.abort_flag);
@@ -281,59 +289,122 @@ __device__ __forceinline__ void attn_issue(AttnTile& s, AttnTurn& turn, int dept
 // The converting warps' part: planes of both products, 32 indices at a time.  A stage's words are asked for before the wait for its slot.
 template <bool DEEP_LEFT, bool DEEP_RIGHT, bool VEC>
 __device__ __forceinline__ void attn_convert(AttnTile& s, AttnTurn& turn, const AttnOperand& left, int rows, const AttnOperand& right, int cols, int depth,
-                                             int party, int causal) {
-    const int lane = threadIdx.x & 31;
-    auto put = [&](const auto& l, const auto& r) {
-        const uint32_t n = turn.stage++, slot = n % attn::SLOTS;
-        turn.ok = turn.ok && limb_wait(ptx::smem_u32(&s.empty[slot]), (n / attn::SLOTS & 1u) ^ 1u, &s.abort_flag);
-        turn.ok = __all_sync(0xffffffffu, turn.ok);
-        if (!turn.ok) return;
-        uint8_t* const at = s.planes + slot * attn::SLOT_BYTES;
-        attn_emit(at, attn::LEFT_PLANE, l);
-        attn_emit(at + attn::LEFT_BYTES, attn::RIGHT_PLANE, r);
-        ptx::fence_proxy_async_smem();                       // the planes are read by the tensor cores
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&s.full[slot]));
-    };
+                                             int party) {
     constexpr int TASKS = DEEP_LEFT ? 2 : 1;
-    for (int k0 = 0; k0 < depth; k0 += limb::KC) {
-        AttnCell<TASKS> l;
-        AttnCell<1> r;
-        attn_read<MASK, DEEP_LEFT, VEC>(l, left, rows, k0, depth, -1);
-        attn_read<OPEN, DEEP_RIGHT, VEC>(r, right, cols, k0, depth, causal);
-        put(l, r);
-        attn_read<OPEN, DEEP_LEFT, VEC>(l, left, rows, k0, depth, -1);
-        if (party) attn_read<BOTH, DEEP_RIGHT, VEC>(r, right, cols, k0, depth, causal);
-        else attn_read<MASK, DEEP_RIGHT, VEC>(r, right, cols, k0, depth, causal);
-        put(l, r);
-    }
+    const int lane = threadIdx.x & 31;
+    const AttnCells<DEEP_LEFT, TASKS> l(left);
+    const AttnCells<DEEP_RIGHT, 1> r(right);
+#pragma unroll 1
+    for (int k0 = 0; k0 < depth; k0 += limb::KC)
+#pragma unroll
+        for (int second = 0; second < 2; ++second) {
+            u64 lw[TASKS][4], rw[1][4];
+            if (second == 0) {
+                l.template read<MASK, VEC>(left, lw, rows, k0, depth);
+                r.template read<OPEN, VEC>(right, rw, cols, k0, depth);
+            } else {
+                l.template read<OPEN, VEC>(left, lw, rows, k0, depth);
+                if (party) r.template read<BOTH, VEC>(right, rw, cols, k0, depth);
+                else r.template read<MASK, VEC>(right, rw, cols, k0, depth);
+            }
+            const uint32_t n = turn.stage++, slot = n % attn::SLOTS;
+            turn.ok = turn.ok && limb_wait(ptx::smem_u32(&s.empty[slot]), (n / attn::SLOTS & 1u) ^ 1u, &s.abort_flag);
+            turn.ok = __all_sync(0xffffffffu, turn.ok);
+            if (!turn.ok) continue;
+            uint8_t* const at = s.planes + slot * attn::SLOT_BYTES;
+            l.emit(at, attn::LEFT_PLANE, lw, rows);
+            r.emit(at + attn::LEFT_BYTES, attn::RIGHT_PLANE, rw, cols);
+            ptx::fence_proxy_async_smem();                   // the planes are read by the tensor cores
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&s.full[slot]));
+        }
 }
-// The draining warps' part: the sums, done(row, column, sum) for this thread's row, a quarter of the columns' halves after the other.
-template <typename F>
-__device__ __forceinline__ void attn_drain(AttnTile& s, AttnTurn& turn, int rows, int cols, F&& done) {
+// Four columns of the eight accumulators, loads and wait in one statement: until the wait is over the hardware may write the registers at any
+// time, so nothing may be moved out of them or put into their place before it.
+__device__ __forceinline__ void attn_sums(uint32_t at, uint32_t (&d)[limb::PLANES][4]) {
+    constexpr int N = attn::TILE;
+    __syncwarp();
+    asm volatile(
+        "{\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%32];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%4, %5, %6, %7}, [%33];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%8, %9, %10, %11}, [%34];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%12, %13, %14, %15}, [%35];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%16, %17, %18, %19}, [%36];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%20, %21, %22, %23}, [%37];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%24, %25, %26, %27}, [%38];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%28, %29, %30, %31}, [%39];\n\t"
+        "tcgen05.wait::ld.sync.aligned;\n\t}"
+        : "=&r"(d[0][0]), "=&r"(d[0][1]), "=&r"(d[0][2]), "=&r"(d[0][3]), "=&r"(d[1][0]), "=&r"(d[1][1]), "=&r"(d[1][2]), "=&r"(d[1][3]),
+          "=&r"(d[2][0]), "=&r"(d[2][1]), "=&r"(d[2][2]), "=&r"(d[2][3]), "=&r"(d[3][0]), "=&r"(d[3][1]), "=&r"(d[3][2]), "=&r"(d[3][3]),
+          "=&r"(d[4][0]), "=&r"(d[4][1]), "=&r"(d[4][2]), "=&r"(d[4][3]), "=&r"(d[5][0]), "=&r"(d[5][1]), "=&r"(d[5][2]), "=&r"(d[5][3]),
+          "=&r"(d[6][0]), "=&r"(d[6][1]), "=&r"(d[6][2]), "=&r"(d[6][3]), "=&r"(d[7][0]), "=&r"(d[7][1]), "=&r"(d[7][2]), "=&r"(d[7][3])
+        : "r"(at), "r"(at + N), "r"(at + 2 * N), "r"(at + 3 * N), "r"(at + 4 * N), "r"(at + 5 * N), "r"(at + 6 * N), "r"(at + 7 * N)
+        : "memory");
+}
+// The draining warps' part: the sums of this thread's row, four columns after four: done(row, column, sum, words), with the words that
+// ask(row, column, words) has asked for four columns ahead, the first before the wait for the sums.
+template <int WORDS, typename A, typename F>
+__device__ __forceinline__ void attn_drain(AttnTile& s, AttnTurn& turn, int rows, int cols, A&& ask, F&& done) {
     const int warp = (threadIdx.x >> 5) - attn::CONVERTERS, lane = threadIdx.x & 31, quarter = warp & 3;
+    const int row = quarter * 32 + lane, c0 = (warp >> 2) * (attn::TILE / 2), c1 = min(c0 + attn::TILE / 2, cols);
+    u64 words[4][WORDS];
+    auto fetch = [&](int c) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int k = 0; k < WORDS; ++k) words[j][k] = 0ull;
+            if (row < rows && c + j < c1) ask(row, c + j, words[j]);
+        }
+    };
+    fetch(c0);
+    __syncwarp();
     turn.ok = turn.ok && limb_wait_warp(ptx::smem_u32(&s.acc_full), turn.tile & 1u, &s.abort_flag);
     ++turn.tile;
     if (!turn.ok) return;
     ptx::fence_after_sync();
-    const int row = quarter * 32 + lane, c0 = (warp >> 2) * (attn::TILE / 2), c1 = min(c0 + attn::TILE / 2, cols);
     const uint32_t acc = s.tmem + ((uint32_t)(quarter * 32) << 16);
     if (quarter * 32 < rows) {
 #pragma unroll 1
         for (int c = c0; c < c1; c += 4) {
             uint32_t d[limb::PLANES][4];
+            u64 z[4], here[4][WORDS];
+            attn_sums(acc + c, d);
 #pragma unroll
-            for (int p = 0; p < limb::PLANES; ++p) ptx::tmem_ld4(acc + attn::TILE * p + c, d[p]);
-            ptx::tmem_wait_ld();
+            for (int j = 0; j < 4; ++j) {
+                z[j] = limb_recombine(d[0][j], d[1][j], d[2][j], d[3][j], d[4][j], d[5][j], d[6][j], d[7][j]);
+#pragma unroll
+                for (int k = 0; k < WORDS; ++k) here[j][k] = words[j][k];
+            }
+            if (c + 4 < c1) fetch(c + 4);
             if (row < rows)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (c + j < c1) done(row, c + j, limb_recombine(d[0][j], d[1][j], d[2][j], d[3][j], d[4][j], d[5][j], d[6][j], d[7][j]));
+                    if (c + j < c1) done(row, c + j, z[j], here[j]);
         }
     }
     ptx::fence_before_sync();
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&s.acc_empty));
+}
+
+// The pairs of words of `rows` rows of `cols`, two at a time a thread of the WORKERS: load(n, row, column) for both, then finish(n, row, column).
+template <typename L, typename F>
+__device__ __forceinline__ void attn_pairs(int rows, int cols, L&& load, F&& finish) {
+    const int half = cols / 2, all = rows * half;
+    for (int t = threadIdx.x; t < all; t += 2 * attn::WORKERS) {
+        int r[2], j[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int u = t + n * attn::WORKERS;
+            r[n] = u < all ? u / half : -1;
+            j[n] = 2 * (u - r[n] * half);
+            if (r[n] >= 0) load(n, r[n], j[n]);
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+            if (r[n] >= 0) finish(n, r[n], j[n]);
+    }
 }
 
 // Messages of k, v and d of one chunk and key head, and its sum of d v^T.
@@ -353,56 +424,73 @@ attn_keys_kernel(const __grid_constant__ AttnArgs a) {
     const size_t k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
     if (warp != attn::ISSUER) {
         const u64* const w = a.decay + (size_t)h * (a.C + 1) + at.len - 1;
-#pragma unroll 2
-        for (int t = threadIdx.x; t < at.len * (a.k_dim / 2); t += attn::WORKERS) {
-            const int r = t / (a.k_dim / 2), j = 2 * (t - r * (a.k_dim / 2));
+        ulonglong2 x[2][2], mk[2][2], md[2][2];
+        attn_pairs(at.len, a.k_dim, [&](int n, int r, int j) {
             const size_t o = k_at + r * k_row + j, x_at = (size_t)(at.first + r) * a.k_stride + (size_t)h * a.k_dim + j;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                x[n][i] = attn_input2(a.K[i] + x_at, a.in_vec);
+                mk[n][i] = attn_load2<VEC>(a.mk[i] + o);
+                md[n][i] = attn_load2<VEC>(a.md[i] + o);
+            }
+        }, [&](int n, int r, int j) {
+            const size_t o = k_at + r * k_row + j;
             const u64 weight = __ldg(w - r);
-            ulonglong2 k = make_ulonglong2(0ull, 0ull), d = k;
+            ulonglong2 e[2], g[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const ulonglong2 x = attn_input2(a.K[i] + x_at, a.in_vec), e = attn_sub(x, attn_load2<VEC>(a.mk[i] + o));
-                const ulonglong2 y = make_ulonglong2(attn_rescale(x.x * weight, i, a.f), attn_rescale(x.y * weight, i, a.f)), g = attn_sub(y, attn_load2<VEC>(a.md[i] + o));
-                attn_store2<VEC>(a.Ek[i] + o, e);
-                attn_store2<VEC>(a.Ed[i] + o, g);
-                k = attn_add(k, e);                          // the exchange
-                d = attn_add(d, g);
+                e[i] = attn_sub(x[n][i], mk[n][i]);
+                g[i] = attn_sub(make_ulonglong2(attn_rescale(x[n][i].x * weight, i, a.f), attn_rescale(x[n][i].y * weight, i, a.f)), md[n][i]);
+                attn_store2<VEC>(a.Ek[i] + o, e[i]);
+                attn_store2<VEC>(a.Ed[i] + o, g[i]);
             }
-            attn_store2<VEC>(a.k + o, k);
-            attn_store2<VEC>(a.d + o, d);
-        }
-#pragma unroll 2
-        for (int t = threadIdx.x; t < at.len * (a.v_dim / 2); t += attn::WORKERS) {
-            const int r = t / (a.v_dim / 2), j = 2 * (t - r * (a.v_dim / 2));
+            attn_store2<VEC>(a.k + o, attn_add(e[0], e[1]));         // the exchange
+            attn_store2<VEC>(a.d + o, attn_add(g[0], g[1]));
+        });
+        attn_pairs(at.len, a.v_dim, [&](int n, int r, int j) {
             const size_t o = v_at + r * v_row + j, x_at = (size_t)(at.first + r) * a.v_stride + (size_t)h * a.v_dim + j;
-            ulonglong2 v = make_ulonglong2(0ull, 0ull);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const ulonglong2 e = attn_sub(attn_input2(a.V[i] + x_at, a.in_vec), attn_load2<VEC>(a.mv[i] + o));
-                attn_store2<VEC>(a.Ev[i] + o, e);
-                v = attn_add(v, e);
+                x[n][i] = attn_input2(a.V[i] + x_at, a.in_vec);
+                mk[n][i] = attn_load2<VEC>(a.mv[i] + o);
             }
-            attn_store2<VEC>(a.v + o, v);
-        }
+        }, [&](int n, int r, int j) {
+            const size_t o = v_at + r * v_row + j;
+            ulonglong2 e[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                e[i] = attn_sub(x[n][i], mk[n][i]);
+                attn_store2<VEC>(a.Ev[i] + o, e[i]);
+            }
+            attn_store2<VEC>(a.v + o, attn_add(e[0], e[1]));
+        });
         attn_meet();
     }
-    const size_t out = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
-    for (int i = 0; i < 2; ++i)
-        for (int v0 = 0; v0 < a.v_dim; v0 += attn::ROWS)
-            for (int k0 = 0; k0 < a.k_dim; k0 += attn::TILE) {
-                const int rows = min(attn::ROWS, a.v_dim - v0), cols = min(attn::TILE, a.k_dim - k0);
-                if (warp == attn::ISSUER) {
-                    attn_issue(s, turn, at.len);
-                } else if (warp < attn::CONVERTERS) {
-                    const AttnOperand v = {a.mv[i] + v_at + v0, a.v + v_at + v0, v_row}, d = {a.md[i] + k_at + k0, a.d + k_at + k0, k_row};
-                    attn_convert<true, true, VEC>(s, turn, v, rows, d, cols, at.len, i, -1);
-                } else {
-                    attn_drain(s, turn, rows, cols, [&](int row, int col, u64 z) {
-                        const size_t o = out + (size_t)(k0 + col) * a.v_dim + v0 + row;
-                        a.kv[i][o] = __ldcs(a.dv[i] + o) + z;
-                    });
-                }
-            }
+    // the tiles of either party, the same order for every role
+    auto tiles = [&](auto&& tile) {
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i)
+#pragma unroll 1
+            for (int v0 = 0; v0 < a.v_dim; v0 += attn::ROWS)
+#pragma unroll 1
+                for (int k0 = 0; k0 < a.k_dim; k0 += attn::TILE) tile(i, v0, k0, min(attn::ROWS, a.v_dim - v0), min(attn::TILE, a.k_dim - k0));
+    };
+    if (warp == attn::ISSUER) {
+        tiles([&](int, int, int, int, int) { attn_issue(s, turn, at.len); });
+    } else if (warp < attn::CONVERTERS) {
+        tiles([&](int i, int v0, int k0, int rows, int cols) {
+            const AttnOperand v = {a.mv[i] + v_at + v0, a.v + v_at + v0, (uint32_t)v_row}, d = {a.md[i] + k_at + k0, a.d + k_at + k0, (uint32_t)k_row};
+            attn_convert<true, true, VEC>(s, turn, v, rows, d, cols, at.len, i);
+        });
+    } else {
+        const size_t out = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
+        tiles([&](int i, int v0, int k0, int rows, int cols) {
+            const u64* const dv = a.dv[i] + out + (size_t)k0 * a.v_dim + v0;
+            u64* const kv = a.kv[i] + out + (size_t)k0 * a.v_dim + v0;
+            attn_drain<1>(s, turn, rows, cols, [&](int row, int col, u64* words) { words[0] = __ldcs(dv + col * a.v_dim + row); },
+                          [&](int row, int col, u64 z, const u64* words) { kv[col * a.v_dim + row] = words[0] + z; });
+        });
+    }
     attn_tile_end(s, a.error);
 }
 
@@ -484,75 +572,109 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a) {
     const size_t q_at = at.first * q_row + (size_t)hq * a.k_dim, p_at = at.first * p_row + (size_t)hq * a.C, o_at = at.first * o_row + (size_t)hq * a.v_dim;
     const size_t k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
     const size_t s_at = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
+    const int wide_C = a.C + (a.C & 1);                      // of the opened weights' rows, which begin on 16-byte boundaries
+    const uint32_t w_row = a.q_heads * wide_C;
+    const size_t w_at = (size_t)at.first * w_row + hq * wide_C;
     const u64* const w = a.decay + (size_t)h * (a.C + 1);
     if (warp != attn::ISSUER) {
-#pragma unroll 2
-        for (int t = threadIdx.x; t < rows * (a.k_dim / 2); t += attn::WORKERS) {
-            const int r = t / (a.k_dim / 2), j = 2 * (t - r * (a.k_dim / 2));
+        ulonglong2 x[2][2], m[2][2];
+        attn_pairs(rows, a.k_dim, [&](int n, int r, int j) {
             const size_t o = q_at + r * q_row + j, x_at = (size_t)(at.first + r) * a.q_stride + (size_t)hq * a.k_dim + j;
-            ulonglong2 q = make_ulonglong2(0ull, 0ull);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const ulonglong2 e = attn_sub(attn_input2(a.Q[i] + x_at, a.in_vec), attn_load2<VEC>(a.mq[i] + o));
-                attn_store2<VEC>(a.Eq[i] + o, e);
-                q = attn_add(q, e);                          // the exchange
+                x[n][i] = attn_input2(a.Q[i] + x_at, a.in_vec);
+                m[n][i] = attn_load2<VEC>(a.mq[i] + o);
             }
-            attn_store2<VEC>(a.q + o, q);
-        }
+        }, [&](int n, int r, int j) {
+            const size_t o = q_at + r * q_row + j;
+            ulonglong2 e[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                e[i] = attn_sub(x[n][i], m[n][i]);
+                attn_store2<VEC>(a.Eq[i] + o, e[i]);
+            }
+            attn_store2<VEC>(a.q + o, attn_add(e[0], e[1]));         // the exchange
+        });
         // off the triangle nothing is sent
-        for (int t = threadIdx.x; t < rows * a.C; t += attn::WORKERS) {
-            const int r = t / a.C, k = t - r * a.C;
-            if (k > r) a.Ep[0][p_at + r * p_row + k] = a.Ep[1][p_at + r * p_row + k] = a.p[p_at + r * p_row + k] = 0ull;
+        for (int t = threadIdx.x; t < rows * wide_C; t += attn::WORKERS) {
+            const int r = t / wide_C, k = t - r * wide_C;
+            if (k <= r) continue;
+            const size_t o = w_at + (size_t)r * w_row + k;
+            a.p[o] = a.pm[0][o] = a.pm[1][o] = 0ull;
+            if (k < a.C) a.Ep[0][p_at + r * p_row + k] = a.Ep[1][p_at + r * p_row + k] = 0ull;
         }
         attn_meet();
     }
-    for (int i = 0; i < 2; ++i) {
-        const AttnOperand k = {a.mk[i] + k_at, a.k + k_at, k_row}, q = {a.mq[i] + q_at, a.q + q_at, q_row};
-        if (warp == attn::ISSUER) {
+    if (warp == attn::ISSUER) {
+        attn_issue(s, turn, a.k_dim);
+        attn_issue(s, turn, a.k_dim);
+#pragma unroll 1
+        for (int t = 0; t < 2 * ((a.v_dim + attn::ROWS - 1) / attn::ROWS); ++t) {
             attn_issue(s, turn, a.k_dim);
-        } else if (warp < attn::CONVERTERS) {
-            attn_convert<false, false, VEC>(s, turn, k, rows, q, rows, a.k_dim, i, -1);
-        } else {
-            attn_drain(s, turn, rows, rows, [&](int key, int r, u64 z) {
+            attn_issue(s, turn, rows);
+        }
+    } else if (warp < attn::CONVERTERS) {
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i) {
+            const AttnOperand k = {a.mk[i] + k_at, a.k + k_at, (uint32_t)k_row}, q = {a.mq[i] + q_at, a.q + q_at, (uint32_t)q_row};
+            attn_convert<false, false, VEC>(s, turn, k, rows, q, rows, a.k_dim, i);
+        }
+        // far part and near part in turn
+        const int tiles = (a.v_dim + attn::ROWS - 1) / attn::ROWS;
+#pragma unroll 1
+        for (int n = 0; n < 4 * tiles; ++n) {
+            const bool near = n & 1;
+            const int i = n >= 2 * tiles, v0 = (n / 2 - i * tiles) * attn::ROWS;
+            if (n == 1) turn.ok = turn.ok && limb_wait_warp(ptx::smem_u32(&s.weights), 0, &s.abort_flag);
+            AttnOperand left, right;
+            left.mask = (near ? a.mv[i] + v_at : a.ms[i] + s_at) + v0;
+            left.open = (near ? a.v + v_at : a.s + s_at) + v0;
+            left.step = near ? (uint32_t)v_row : (uint32_t)a.v_dim;
+            right.mask = near ? a.pm[i] + w_at : a.mq[i] + q_at;
+            right.open = near ? a.p + w_at : a.q + q_at;
+            right.step = near ? w_row : (uint32_t)q_row;
+            attn_convert<true, false, VEC>(s, turn, left, min(attn::ROWS, a.v_dim - v0), right, rows, near ? rows : a.k_dim, i);
+        }
+    } else {
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i) {
+            const u64 *const qk = a.qk[i] + p_at, *const mp = a.mp[i] + p_at;
+            u64 *const Ep = a.Ep[i] + p_at, *const p = a.p + w_at, *const pm = a.pm[i] + w_at;
+            attn_drain<3>(s, turn, rows, rows, [&](int key, int r, u64* words) {
                 if (key > r) return;
-                const size_t o = p_at + r * p_row + key;
-                z += __ldg(a.qk[i] + o);
-                const u64 e = attn_rescale(attn_rescale(z, i, a.f) * __ldg(w + r - key), i, a.f) - __ldg(a.mp[i] + o);
-                a.Ep[i][o] = e;
-                a.p[o] = i ? a.p[o] + e : e;                 // the exchange; this thread's own
+                const size_t o = r * p_row + key;
+                words[0] = __ldcs(qk + o);
+                words[1] = __ldg(mp + o);
+                words[2] = i ? p[r * w_row + key] : 0ull;    // this thread's own
+            }, [&](int key, int r, u64 z, const u64* words) {
+                if (key > r) return;
+                const size_t o = r * p_row + key;
+                const u64 e = attn_rescale(attn_rescale(z + words[0], i, a.f) * __ldg(w + r - key), i, a.f) - words[1];
+                Ep[o] = e;
+                pm[r * w_row + key] = words[1];
+                p[r * w_row + key] = words[2] + e;           // the exchange
             });
         }
-    }
-    if (warp >= attn::CONVERTERS && warp < attn::ISSUER) {
         __syncwarp();
         if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(ptx::smem_u32(&s.weights));
-    }
-    for (int i = 0; i < 2; ++i)
-        for (int v0 = 0; v0 < a.v_dim; v0 += attn::ROWS) {
-            const int wide = min(attn::ROWS, a.v_dim - v0);
-            if (warp == attn::ISSUER) {
-                attn_issue(s, turn, a.k_dim);
-                attn_issue(s, turn, rows);
-            } else if (warp < attn::CONVERTERS) {
-                const AttnOperand q = {a.mq[i] + q_at, a.q + q_at, q_row}, p = {a.mp[i] + p_at, a.p + p_at, p_row};
-                const AttnOperand S = {a.ms[i] + s_at + v0, a.s + s_at + v0, (size_t)a.v_dim}, v = {a.mv[i] + v_at + v0, a.v + v_at + v0, v_row};
-                attn_convert<true, false, VEC>(s, turn, S, wide, q, rows, a.k_dim, i, -1);
-                if (i == 0 && v0 == 0) turn.ok = turn.ok && limb_wait_warp(ptx::smem_u32(&s.weights), 0, &s.abort_flag);
-                if (a.C % 2 == 0) attn_convert<true, false, VEC>(s, turn, v, wide, p, rows, rows, i, 0);
-                else attn_convert<true, false, false>(s, turn, v, wide, p, rows, rows, i, 0);
-            } else {
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i)
+#pragma unroll 1
+            for (int v0 = 0; v0 < a.v_dim; v0 += attn::ROWS) {
                 // what the near part is added to waits in the result's place, where the same thread finds it again
-                attn_drain(s, turn, wide, rows, [&](int row, int r, u64 z) {
-                    const size_t o = o_at + r * o_row + v0 + row;
-                    z += __ldg(a.qs[i] + o);
-                    a.O[i][o] = __ldg(a.pv[i] + o) + __ldg(w + r + 1) * attn_rescale(z, i, a.f);
+                const int wide = min(attn::ROWS, a.v_dim - v0);
+                u64* const O = a.O[i] + o_at + v0;
+                const u64 *const qs = a.qs[i] + o_at + v0, *const pv = a.pv[i] + o_at + v0;
+                attn_drain<2>(s, turn, wide, rows, [&](int row, int r, u64* words) {
+                    words[0] = __ldcs(qs + r * o_row + row);
+                    words[1] = __ldcs(pv + r * o_row + row);
+                }, [&](int row, int r, u64 z, const u64* words) {
+                    O[r * o_row + row] = words[1] + __ldg(w + r + 1) * attn_rescale(z + words[0], i, a.f);
                 });
-                attn_drain(s, turn, wide, rows, [&](int row, int r, u64 z) {
-                    const size_t o = o_at + r * o_row + v0 + row;
-                    a.O[i][o] = attn_rescale(a.O[i][o] + z, i, a.f);
-                });
+                attn_drain<1>(s, turn, wide, rows, [&](int row, int r, u64* words) { words[0] = O[r * o_row + row]; },
+                              [&](int row, int r, u64 z, const u64* words) { O[r * o_row + row] = attn_rescale(words[0] + z, i, a.f); });
             }
-        }
+    }
     attn_tile_end(s, a.error);
 }
 

@@ -88,7 +88,7 @@ def test_prompt_refusals(cb):  # noqa: F811
         assert call(**{name: (1, good.workspace)}) == -1 and call(**{name: (1, good.decay)}) == -1 and call(**{name: (0, good.starts)}) == -1
     assert call(state_out=(0, good.state[0])) == -1          # in place for one party alone
     assert call(state_out=(0, good.state[0] + 8)) == -1
-    for kw in (dict(tokens=0), dict(sequences=0), dict(chunks=-1), dict(q_heads=0), dict(kv_heads=0), dict(kv_heads=3), dict(k_dim=5), dict(k_dim=0),
+    for kw in (dict(tokens=0), dict(sequences=0), dict(chunks=-1), dict(q_heads=0), dict(q_heads=4098), dict(kv_heads=0), dict(kv_heads=3), dict(k_dim=5), dict(k_dim=0),
                dict(k_dim=258), dict(v_dim=3), dict(v_dim=258), dict(chunk=0), dict(chunk=65), dict(q_stride=23), dict(k_stride=11), dict(v_stride=-8),
                dict(q_stride=(1 << 32) + 1), dict(frac_bits=0), dict(frac_bits=32), dict(tokens=(1 << 20) + 1), dict(sequences=(1 << 20) + 1),
                dict(chunks=(1 << 20) + 1), dict(tokens=1 << 20, q_heads=18), dict(chunks=1 << 20, q_heads=18), dict(workspace_bytes=64)):
