@@ -22,11 +22,15 @@ namespace attn {
 constexpr int MAX_CHUNK = 64, MAX_DIM = 256;
 constexpr int THREADS = 256;                         // of the kernels without products
 constexpr int ROWS = 128, TILE = 64;                 // of a tile of a product: rows, columns
-constexpr int CONVERTERS = 16, DRAINERS = 8, WORKERS = 32 * (CONVERTERS + DRAINERS), ISSUER = CONVERTERS + DRAINERS;
+constexpr int GROUP = 8;                             // warps that convert one of the two products
+constexpr int CONVERTERS = 2 * GROUP, DRAINERS = 8, WORKERS = 32 * (CONVERTERS + DRAINERS), ISSUER = CONVERTERS + DRAINERS;
 constexpr int TILE_THREADS = WORKERS + 32;
-constexpr int SLOTS = 4;                             // of planes: one of the two products of 32 indices each
+constexpr int SLOTS = 3;                             // of planes: one of the two products of 32 indices each
 constexpr int LEFT_PLANE = ROWS * limb::KC, RIGHT_PLANE = TILE * limb::KC, LEFT_BYTES = limb::PLANES * LEFT_PLANE;
-constexpr int SLOT_BYTES = LEFT_BYTES + limb::PLANES * RIGHT_PLANE, TILE_SMEM = SLOTS * SLOT_BYTES + 128, ACC_COLS = limb::PLANES * TILE;
+constexpr int SLOT_BYTES = LEFT_BYTES + limb::PLANES * RIGHT_PLANE, ACC_COLS = limb::PLANES * TILE;
+constexpr int CELL_ROWS = 32;                        // rows that a group covers at a time
+constexpr int AHEAD = 3, BATCH = 4;                  // a draining thread's dealer's words: batches of columns under way, columns of one
+constexpr int RING_BYTES = AHEAD * BATCH * 2 * 32 * DRAINERS * 8, TILE_SMEM = SLOTS * SLOT_BYTES + RING_BYTES + 128;
 }  // namespace attn
 
 struct AttnArgs {
@@ -115,10 +119,10 @@ __device__ __forceinline__ u64 attn_rescale(u64 v, int party, int f) { return pa
 
 // ---------------------------------------------------------------------------
 // Products on the int8 tensor cores.  A CTA works out tiles of ROWS x TILE words of Z_i = (triple) + E B_i + V_i F, V_i = A_i + i E (Eq. 1), one
-// party's after the other's, from words in memory, masks and opened values: sixteen warps turn 32 contraction indices of either product at
-// a time into limb planes in shared memory (kernels_limb.cuh has the decomposition and the layout), a warp issues the MMAs, eight warps read the
-// sums out of tensor memory.  Left operands are keys, values or states, right ones queries, weights or decayed keys; rows past an operand's are
-// whatever lies in shared memory, and their sums are never looked at.
+// party's after the other's, from words in memory, masks and opened values: two groups of eight warps turn 32 contraction indices of one product each
+// into limb planes in shared memory (kernels_limb.cuh has the decomposition and the layout), a warp issues the MMAs, eight warps read the sums out
+// of tensor memory.  Left operands are keys, values or states, right ones queries, weights or decayed keys; rows past an operand's are whatever lies
+// in shared memory, and their sums are never looked at.
 // ---------------------------------------------------------------------------
 struct AttnOperand {
     const u64* mask;                     // the party's
@@ -127,16 +131,15 @@ struct AttnOperand {
 };
 enum AttnWords { MASK, OPEN, BOTH };     // of a plane set: the mask, the opened value, their sum
 
-// A thread's cells of the planes of `rows` rows: four words of a row, indices 2g, 2g + 1, 16 + 2g, 17 + 2g of every 32 (limb_emit4's order).  A DEEP
-// operand of up to ROWS rows has TASKS = 2 of them, TILE rows apart, else there is one.  Places are counted in 32 bits: an operand spans less than
-// 2^29 words (comet_linear_attention sees to that).
+// A thread's cells of the planes of `rows` rows: four words of a row, indices 2g, 2g + 1, 16 + 2g, 17 + 2g of every 32 (limb_emit4's order), TASKS of
+// them, CELL_ROWS rows apart.  Places are counted in 32 bits: an operand spans less than 2^29 words (comet_linear_attention sees to that).
 template <bool DEEP, int TASKS>
 struct AttnCells {
     uint32_t at;                                 // of the first word, from the operand's on
     int to, row, g;                              // to: in a plane
 
     __device__ __forceinline__ AttnCells(const AttnOperand& x) {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        const int warp = (threadIdx.x >> 5) % attn::GROUP, lane = threadIdx.x & 31;
         if (DEEP) {
             // eight rows x four groups of indices a warp: 64-byte pieces of memory, 128 bytes of a plane
             row = (warp >> 1) * 8 + (lane & 7);
@@ -156,19 +159,20 @@ struct AttnCells {
         const int left = depth - k0 - 2 * g;
 #pragma unroll
         for (int t = 0; t < TASKS; ++t) {
-            const bool live = row + t * attn::TILE < rows;
+            const bool live = row + t * attn::CELL_ROWS < rows;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 u64 v[2] = {0ull, 0ull};
                 if (!DEEP && VEC) {              // (rows are even in length, zero behind an odd depth)
                     if (live && 16 * h < left) {
+                        const uint32_t o = from + 16 * h + t * attn::CELL_ROWS * x.step;
                         if (WHAT != MASK) {
-                            const ulonglong2 e = *reinterpret_cast<const ulonglong2*>(x.open + (from + 16 * h));
+                            const ulonglong2 e = *reinterpret_cast<const ulonglong2*>(x.open + o);
                             v[0] = e.x;
                             v[1] = e.y;
                         }
                         if (WHAT != OPEN) {
-                            const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(x.mask + (from + 16 * h));
+                            const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(x.mask + o);
                             v[0] += m.x;
                             v[1] += m.y;
                         }
@@ -177,7 +181,7 @@ struct AttnCells {
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
                         if (live && 16 * h + j < left) {
-                            const uint32_t o = from + (DEEP ? x.step : 1u) * (16 * h + j) + t * attn::TILE;
+                            const uint32_t o = from + (DEEP ? x.step : 1u) * (16 * h + j) + t * attn::CELL_ROWS * (DEEP ? 1u : x.step);
                             if (WHAT != MASK) v[j] = x.open[o];
                             if (WHAT != OPEN) v[j] += x.mask[o];
                         }
@@ -190,7 +194,7 @@ struct AttnCells {
     __device__ __forceinline__ void emit(uint8_t* planes, int plane_bytes, const u64 (&w)[TASKS][4], int rows) const {
 #pragma unroll
         for (int t = 0; t < TASKS; ++t)
-            if (row + t * attn::TILE < rows) limb_emit4(planes + to + t * (attn::TILE / 8 * 256), plane_bytes, w[t]);
+            if (row + t * attn::CELL_ROWS < rows) limb_emit4(planes + to + t * (attn::CELL_ROWS / 8 * 256), plane_bytes, w[t]);
     }
 };
 
@@ -204,7 +208,7 @@ struct AttnTile {
 __device__ __forceinline__ void attn_tile_begin(AttnTile& s, uint8_t* raw) {
     if (threadIdx.x == 0) {
         for (int k = 0; k < attn::SLOTS; ++k) {
-            ptx::mbar_init(ptx::smem_u32(&s.full[k]), attn::CONVERTERS);
+            ptx::mbar_init(ptx::smem_u32(&s.full[k]), attn::GROUP);
             ptx::mbar_init(ptx::smem_u32(&s.empty[k]), 1);
         }
         ptx::mbar_init(ptx::smem_u32(&s.acc_full), 1);
@@ -223,24 +227,34 @@ __device__ __forceinline__ void attn_tile_begin(AttnTile& s, uint8_t* raw) {
     __syncthreads();
     ptx::fence_after_sync();
 }
-__device__ __forceinline__ void attn_tile_end(AttnTile& s, int* error) {
-    __syncwarp();
-    ptx::fence_before_sync();
-    __syncthreads();
-    if (threadIdx.x == 0 && s.abort_flag) {
-        *error = 1;
-        __threadfence_system();
-    }
-    if (threadIdx.x >> 5 == attn::ISSUER) {
-        ptx::fence_after_sync();
-        ptx::tmem_dealloc(s.tmem, attn::ACC_COLS);
-    }
-}
 // All warps but the issuer wait for one another.  (A warp comes to a barrier, and to a read of tensor memory, as a whole: both are
 // undefined for lanes on their own, and what stands before may have parted them.)
 __device__ __forceinline__ void attn_meet() {
     __syncwarp();
     asm volatile("bar.sync 1, %0;" ::"n"(attn::WORKERS) : "memory");
+}
+
+// Bounded wait, written out where it stands: false, and the CTA's abort flag raised, if the barrier did not flip in time or another warp has given up.
+// Not a call: loads and asynchronous copies are under way when a warp comes to wait here.
+__device__ __forceinline__ bool attn_wait(uint64_t& bar, uint32_t parity, AttnTile& s) {
+    const uint32_t at = ptx::smem_u32(&bar);
+    bool ok = ptx::mbar_try_wait(at, parity);
+    if (!ok) {
+        const long long t0 = clock64();
+        volatile int* const abort_flag = &s.abort_flag;
+        do {
+            ok = ptx::mbar_try_wait(at, parity);
+            if (!ok && (*abort_flag || clock64() - t0 > limb::WAIT_CYCLES)) {
+                *abort_flag = 1;
+                break;
+            }
+        } while (!ok);
+    }
+    return ok;
+}
+// The same for a whole warp.
+__device__ __forceinline__ bool attn_wait_warp(uint64_t& bar, uint32_t parity, AttnTile& s) {
+    return __all_sync(0xffffffffu, attn_wait(bar, parity, s));
 }
 
 // Where a warp is in the order of slots and tiles; all count alike.
@@ -250,17 +264,41 @@ struct AttnTurn {
 };
 __device__ __forceinline__ int attn_blocks(int depth) { return (depth + limb::KC - 1) / limb::KC; }
 
+// The end of a CTA.  What the tensor core still owes is waited for first: the last stages' slots, which nobody uses again, are reported free through
+// shared memory, and a report that comes when the CTA is gone is an access to an address that does not exist.  (It happened, where the last sums were
+// drained fast enough.)
+__device__ __forceinline__ void attn_tile_end(AttnTile& s, const AttnTurn& turn, int* error) {
+    __syncwarp();
+    if (threadIdx.x >> 5 == attn::ISSUER && turn.ok)
+        for (uint32_t k = 1; k <= attn::SLOTS && k <= turn.stage; ++k) {
+            const uint32_t n = turn.stage - k;
+            attn_wait(s.empty[n % attn::SLOTS], n / attn::SLOTS & 1u, s);
+        }
+    __syncwarp();
+    ptx::fence_before_sync();
+    __syncthreads();
+    if (threadIdx.x == 0 && s.abort_flag) {
+        *error = 1;
+        __threadfence_system();
+    }
+    __syncwarp();
+    if (threadIdx.x >> 5 == attn::ISSUER) {
+        ptx::fence_after_sync();
+        ptx::tmem_dealloc(s.tmem, attn::ACC_COLS);
+    }
+}
+
 // The issuing warp's part of a tile.
 __device__ __forceinline__ void attn_issue(AttnTile& s, AttnTurn& turn, int depth) {
     const int stages = 2 * attn_blocks(depth);
     __syncwarp();
     if (ptx::elect_one() && turn.ok) {
         constexpr uint32_t IDESC = (2u << 4) | ((uint32_t)(attn::ROWS >> 4) << 24);
-        bool ok = limb_wait(ptx::smem_u32(&s.acc_empty), (turn.tile & 1u) ^ 1u, &s.abort_flag);
+        bool ok = attn_wait(s.acc_empty, (turn.tile & 1u) ^ 1u, s);
         ptx::fence_after_sync();
         for (int t = 0; t < stages && ok; ++t) {
             const uint32_t n = turn.stage + t, slot = n % attn::SLOTS;
-            ok = limb_wait(ptx::smem_u32(&s.full[slot]), n / attn::SLOTS & 1u, &s.abort_flag);
+            ok = attn_wait(s.full[slot], n / attn::SLOTS & 1u, s);
             if (!ok) break;
             ptx::fence_after_sync();
             const uint32_t left = limb_desc_lo(ptx::smem_u32(s.planes) + slot * attn::SLOT_BYTES), right = left + (attn::LEFT_BYTES >> 4);
@@ -286,38 +324,37 @@ __device__ __forceinline__ void attn_issue(AttnTile& s, AttnTurn& turn, int dept
     turn.stage += stages;
     ++turn.tile;
 }
-// The converting warps' part: planes of both products, 32 indices at a time.  A stage's words are asked for before the wait for its slot.
+// The converting warps' part: planes of both products, 32 indices at a time, E B_i by the first group, V_i F by the second.  A stage's words are asked
+// for before the wait for its slot, and while one group waits for its words the other puts its own away.
 template <bool DEEP_LEFT, bool DEEP_RIGHT, bool VEC>
 __device__ __forceinline__ void attn_convert(AttnTile& s, AttnTurn& turn, const AttnOperand& left, int rows, const AttnOperand& right, int cols, int depth,
                                              int party) {
-    constexpr int TASKS = DEEP_LEFT ? 2 : 1;
-    const int lane = threadIdx.x & 31;
-    const AttnCells<DEEP_LEFT, TASKS> l(left);
-    const AttnCells<DEEP_RIGHT, 1> r(right);
+    constexpr int LEFT = DEEP_LEFT ? 4 : 2, RIGHT = 2;       // up to ROWS rows of a deep left operand, MAX_CHUNK of another; TILE rows of a right one
+    const int lane = threadIdx.x & 31, second = threadIdx.x / (32 * attn::GROUP);
+    const AttnCells<DEEP_LEFT, LEFT> l(left);
+    const AttnCells<DEEP_RIGHT, RIGHT> r(right);
 #pragma unroll 1
-    for (int k0 = 0; k0 < depth; k0 += limb::KC)
-#pragma unroll
-        for (int second = 0; second < 2; ++second) {
-            u64 lw[TASKS][4], rw[1][4];
-            if (second == 0) {
-                l.template read<MASK, VEC>(left, lw, rows, k0, depth);
-                r.template read<OPEN, VEC>(right, rw, cols, k0, depth);
-            } else {
-                l.template read<OPEN, VEC>(left, lw, rows, k0, depth);
-                if (party) r.template read<BOTH, VEC>(right, rw, cols, k0, depth);
-                else r.template read<MASK, VEC>(right, rw, cols, k0, depth);
-            }
-            const uint32_t n = turn.stage++, slot = n % attn::SLOTS;
-            turn.ok = turn.ok && limb_wait(ptx::smem_u32(&s.empty[slot]), (n / attn::SLOTS & 1u) ^ 1u, &s.abort_flag);
-            turn.ok = __all_sync(0xffffffffu, turn.ok);
-            if (!turn.ok) continue;
-            uint8_t* const at = s.planes + slot * attn::SLOT_BYTES;
-            l.emit(at, attn::LEFT_PLANE, lw, rows);
-            r.emit(at + attn::LEFT_BYTES, attn::RIGHT_PLANE, rw, cols);
-            ptx::fence_proxy_async_smem();                   // the planes are read by the tensor cores
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&s.full[slot]));
+    for (int k0 = 0; k0 < depth; k0 += limb::KC) {
+        u64 lw[LEFT][4], rw[RIGHT][4];
+        if (second == 0) {
+            l.template read<MASK, VEC>(left, lw, rows, k0, depth);
+            r.template read<OPEN, VEC>(right, rw, cols, k0, depth);
+        } else {
+            l.template read<OPEN, VEC>(left, lw, rows, k0, depth);
+            if (party) r.template read<BOTH, VEC>(right, rw, cols, k0, depth);
+            else r.template read<MASK, VEC>(right, rw, cols, k0, depth);
         }
+        const uint32_t n = turn.stage + second, slot = n % attn::SLOTS;
+        turn.stage += 2;
+        turn.ok = turn.ok && attn_wait_warp(s.empty[slot], (n / attn::SLOTS & 1u) ^ 1u, s);
+        if (!turn.ok) continue;
+        uint8_t* const at = s.planes + slot * attn::SLOT_BYTES;
+        l.emit(at, attn::LEFT_PLANE, lw, rows);
+        r.emit(at + attn::LEFT_BYTES, attn::RIGHT_PLANE, rw, cols);
+        ptx::fence_proxy_async_smem();                       // the planes are read by the tensor cores
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&s.full[slot]));
+    }
 }
 // Four columns of the eight accumulators, loads and wait in one statement: until the wait is over the hardware may write the registers at any
 // time, so nothing may be moved out of them or put into their place before it.
@@ -342,51 +379,73 @@ __device__ __forceinline__ void attn_sums(uint32_t at, uint32_t (&d)[limb::PLANE
         : "r"(at), "r"(at + N), "r"(at + 2 * N), "r"(at + 3 * N), "r"(at + 4 * N), "r"(at + 5 * N), "r"(at + 6 * N), "r"(at + 7 * N)
         : "memory");
 }
-// The draining warps' part: the sums of this thread's row, four columns after four: done(row, column, sum, words), with the words that
-// ask(row, column, words) has asked for four columns ahead, the first before the wait for the sums.
-template <int WORDS, typename A, typename F>
-__device__ __forceinline__ void attn_drain(AttnTile& s, AttnTurn& turn, int rows, int cols, A&& ask, F&& done) {
-    const int warp = (threadIdx.x >> 5) - attn::CONVERTERS, lane = threadIdx.x & 31, quarter = warp & 3;
-    const int row = quarter * 32 + lane, c0 = (warp >> 2) * (attn::TILE / 2), c1 = min(c0 + attn::TILE / 2, cols);
-    u64 words[4][WORDS];
+// The draining warps' part: the sums of this thread's row, a batch of columns after the other: done(row, column, sum, words, own).  The dealer's
+// words, at(k, row, column) the place of the k-th, come into the thread's own places of shared memory AHEAD batches before they are needed, the
+// first before the wait for the sums; a word that the thread itself has written, own(row, column), one batch before.
+template <int WORDS, typename P, typename O, typename F>
+__device__ __forceinline__ void attn_drain(AttnTile& s, AttnTurn& turn, int rows, int cols, P&& at, O&& own, F&& done) {
+    using namespace attn;
+    const int thread = threadIdx.x - 32 * CONVERTERS, quarter = (thread >> 5) & 3, row = thread & (ROWS - 1);
+    const int c0 = thread / ROWS * (TILE / 2), c1 = min(cols, c0 + TILE / 2);                // a half of the columns
+    u64* const ring = reinterpret_cast<u64*>(s.planes + SLOTS * SLOT_BYTES) + thread;       // [AHEAD][BATCH][2][threads]
+    constexpr int NEXT = 32 * DRAINERS;
     auto fetch = [&](int c) {
+        u64* const to = ring + (c / BATCH % AHEAD) * (BATCH * 2 * NEXT);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < BATCH; ++j)
+            if (row < rows && c + j < c1)
 #pragma unroll
-            for (int k = 0; k < WORDS; ++k) words[j][k] = 0ull;
-            if (row < rows && c + j < c1) ask(row, c + j, words[j]);
-        }
+                for (int k = 0; k < WORDS; ++k) {
+                    const u64* const from = at(k, row, c + j);
+                    if (from) norm_fetch8(to + (2 * j + k) * NEXT, from);
+                }
+        limb_copy_commit();
     };
-    fetch(c0);
+    u64 mine[BATCH];
+    auto owned = [&](int c) {
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) mine[j] = row < rows && c + j < c1 ? own(row, c + j) : 0ull;
+    };
+    if (WORDS)
+#pragma unroll
+        for (int b = 0; b < AHEAD; ++b) fetch(c0 + b * BATCH);
+    owned(c0);
     __syncwarp();
-    turn.ok = turn.ok && limb_wait_warp(ptx::smem_u32(&s.acc_full), turn.tile & 1u, &s.abort_flag);
+    turn.ok = turn.ok && attn_wait_warp(s.acc_full, turn.tile & 1u, s);
     ++turn.tile;
-    if (!turn.ok) return;
-    ptx::fence_after_sync();
-    const uint32_t acc = s.tmem + ((uint32_t)(quarter * 32) << 16);
-    if (quarter * 32 < rows) {
+    if (turn.ok) {
+        ptx::fence_after_sync();
+        const uint32_t acc = s.tmem + ((uint32_t)(quarter * 32) << 16);
+        if (quarter * 32 < rows) {
 #pragma unroll 1
-        for (int c = c0; c < c1; c += 4) {
-            uint32_t d[limb::PLANES][4];
-            u64 z[4], here[4][WORDS];
-            attn_sums(acc + c, d);
+            for (int c = c0; c < c1; c += BATCH) {
+                uint32_t d[limb::PLANES][4];
+                attn_sums(acc + c, d);
+                if (WORDS) limb_copy_wait<AHEAD - 1>();
+                u64 here[BATCH], z[BATCH], words[BATCH][WORDS ? WORDS : 1];
+                const u64* const from = ring + (c / BATCH % AHEAD) * (BATCH * 2 * NEXT);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                z[j] = limb_recombine(d[0][j], d[1][j], d[2][j], d[3][j], d[4][j], d[5][j], d[6][j], d[7][j]);
+                for (int j = 0; j < BATCH; ++j) {
+                    z[j] = limb_recombine(d[0][j], d[1][j], d[2][j], d[3][j], d[4][j], d[5][j], d[6][j], d[7][j]);
+                    here[j] = mine[j];
 #pragma unroll
-                for (int k = 0; k < WORDS; ++k) here[j][k] = words[j][k];
+                    for (int k = 0; k < WORDS; ++k) words[j][k] = from[(2 * j + k) * NEXT];
+                }
+                owned(c + BATCH);
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j)
+                    if (row < rows && c + j < c1) done(row, c + j, z[j], words[j], here[j]);
+                if (WORDS) fetch(c + AHEAD * BATCH);             // (the words have been read)
             }
-            if (c + 4 < c1) fetch(c + 4);
-            if (row < rows)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (c + j < c1) done(row, c + j, z[j], here[j]);
         }
+        ptx::fence_before_sync();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(ptx::smem_u32(&s.acc_empty));
     }
-    ptx::fence_before_sync();
-    __syncwarp();
-    if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&s.acc_empty));
+    if (WORDS) limb_copy_wait<0>();
 }
+
+__device__ __forceinline__ u64 attn_nothing(int, int) { return 0ull; }
 
 // The pairs of words of `rows` rows of `cols`, two at a time a thread of the WORKERS: load(n, row, column) for both, then finish(n, row, column).
 template <typename L, typename F>
@@ -487,11 +546,11 @@ attn_keys_kernel(const __grid_constant__ AttnArgs a) {
         tiles([&](int i, int v0, int k0, int rows, int cols) {
             const u64* const dv = a.dv[i] + out + (size_t)k0 * a.v_dim + v0;
             u64* const kv = a.kv[i] + out + (size_t)k0 * a.v_dim + v0;
-            attn_drain<1>(s, turn, rows, cols, [&](int row, int col, u64* words) { words[0] = __ldcs(dv + col * a.v_dim + row); },
-                          [&](int row, int col, u64 z, const u64* words) { kv[col * a.v_dim + row] = words[0] + z; });
+            attn_drain<1>(s, turn, rows, cols, [&](int, int row, int col) { return dv + col * a.v_dim + row; }, attn_nothing,
+                          [&](int row, int col, u64 z, const u64* words, u64) { kv[col * a.v_dim + row] = words[0] + z; });
         });
     }
-    attn_tile_end(s, a.error);
+    attn_tile_end(s, turn, a.error);
 }
 
 // The state from chunk to chunk of a sequence and key head, two words of both parties a thread; says whether the starts were in order.
@@ -566,20 +625,20 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a) {
     if (at.len == 0) return;
     attn_tile_begin(s, attn_smem);
     AttnTurn turn;
-    const int rows = at.len;
+    const int rows = at.len, first = at.first;
     const size_t q_row = (size_t)a.q_heads * a.k_dim, p_row = (size_t)a.q_heads * a.C, o_row = (size_t)a.q_heads * a.v_dim;
     const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
-    const size_t q_at = at.first * q_row + (size_t)hq * a.k_dim, p_at = at.first * p_row + (size_t)hq * a.C, o_at = at.first * o_row + (size_t)hq * a.v_dim;
+    const size_t q_at = first * q_row + (size_t)hq * a.k_dim, p_at = first * p_row + (size_t)hq * a.C, o_at = first * o_row + (size_t)hq * a.v_dim;
     const size_t k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
     const size_t s_at = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
     const int wide_C = a.C + (a.C & 1);                      // of the opened weights' rows, which begin on 16-byte boundaries
     const uint32_t w_row = a.q_heads * wide_C;
-    const size_t w_at = (size_t)at.first * w_row + hq * wide_C;
+    const size_t w_at = (size_t)first * w_row + hq * wide_C;
     const u64* const w = a.decay + (size_t)h * (a.C + 1);
     if (warp != attn::ISSUER) {
         ulonglong2 x[2][2], m[2][2];
         attn_pairs(rows, a.k_dim, [&](int n, int r, int j) {
-            const size_t o = q_at + r * q_row + j, x_at = (size_t)(at.first + r) * a.q_stride + (size_t)hq * a.k_dim + j;
+            const size_t o = q_at + r * q_row + j, x_at = (size_t)(first + r) * a.q_stride + (size_t)hq * a.k_dim + j;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 x[n][i] = attn_input2(a.Q[i] + x_at, a.in_vec);
@@ -625,7 +684,7 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a) {
         for (int n = 0; n < 4 * tiles; ++n) {
             const bool near = n & 1;
             const int i = n >= 2 * tiles, v0 = (n / 2 - i * tiles) * attn::ROWS;
-            if (n == 1) turn.ok = turn.ok && limb_wait_warp(ptx::smem_u32(&s.weights), 0, &s.abort_flag);
+            if (n == 1) turn.ok = turn.ok && attn_wait_warp(s.weights, 0, s);
             AttnOperand left, right;
             left.mask = (near ? a.mv[i] + v_at : a.ms[i] + s_at) + v0;
             left.open = (near ? a.v + v_at : a.s + s_at) + v0;
@@ -640,19 +699,13 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a) {
         for (int i = 0; i < 2; ++i) {
             const u64 *const qk = a.qk[i] + p_at, *const mp = a.mp[i] + p_at;
             u64 *const Ep = a.Ep[i] + p_at, *const p = a.p + w_at, *const pm = a.pm[i] + w_at;
-            attn_drain<3>(s, turn, rows, rows, [&](int key, int r, u64* words) {
+            attn_drain<2>(s, turn, rows, rows, [&](int k, int key, int r) { return key > r ? nullptr : (k ? mp : qk) + (r * p_row + key); },
+                          [&](int key, int r) { return i && key <= r ? p[r * w_row + key] : 0ull; }, [&](int key, int r, u64 z, const u64* words, u64 own) {
                 if (key > r) return;
-                const size_t o = r * p_row + key;
-                words[0] = __ldcs(qk + o);
-                words[1] = __ldg(mp + o);
-                words[2] = i ? p[r * w_row + key] : 0ull;    // this thread's own
-            }, [&](int key, int r, u64 z, const u64* words) {
-                if (key > r) return;
-                const size_t o = r * p_row + key;
                 const u64 e = attn_rescale(attn_rescale(z + words[0], i, a.f) * __ldg(w + r - key), i, a.f) - words[1];
-                Ep[o] = e;
+                Ep[r * p_row + key] = e;
                 pm[r * w_row + key] = words[1];
-                p[r * w_row + key] = words[2] + e;           // the exchange
+                p[r * w_row + key] = own + e;                // the exchange
             });
         }
         __syncwarp();
@@ -665,17 +718,15 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a) {
                 const int wide = min(attn::ROWS, a.v_dim - v0);
                 u64* const O = a.O[i] + o_at + v0;
                 const u64 *const qs = a.qs[i] + o_at + v0, *const pv = a.pv[i] + o_at + v0;
-                attn_drain<2>(s, turn, wide, rows, [&](int row, int r, u64* words) {
-                    words[0] = __ldcs(qs + r * o_row + row);
-                    words[1] = __ldcs(pv + r * o_row + row);
-                }, [&](int row, int r, u64 z, const u64* words) {
+                attn_drain<2>(s, turn, wide, rows, [&](int k, int row, int r) { return (k ? pv : qs) + (r * o_row + row); }, attn_nothing,
+                              [&](int row, int r, u64 z, const u64* words, u64) {
                     O[r * o_row + row] = words[1] + __ldg(w + r + 1) * attn_rescale(z + words[0], i, a.f);
                 });
-                attn_drain<1>(s, turn, wide, rows, [&](int row, int r, u64* words) { words[0] = O[r * o_row + row]; },
-                              [&](int row, int r, u64 z, const u64* words) { O[r * o_row + row] = attn_rescale(words[0] + z, i, a.f); });
+                attn_drain<0>(s, turn, wide, rows, [&](int, int, int) { return (const u64*)nullptr; }, [&](int row, int r) { return O[r * o_row + row]; },
+                              [&](int row, int r, u64 z, const u64*, u64 own) { O[r * o_row + row] = attn_rescale(own + z, i, a.f); });
             }
     }
-    attn_tile_end(s, a.error);
+    attn_tile_end(s, turn, a.error);
 }
 
 // ---------------------------------------------------------------------------

@@ -316,6 +316,18 @@ def test_two_calls_at_once(cb):  # noqa: F811
             compare(r, ref)
 
 
+@pytest.mark.parametrize("starts,Dk,Dv", [([0, 70, 75], 2, 128), ([0, 16], 16, 24), ([0, 1], 2, 2), ([0, 3, 40], 64, 4)])
+def test_short_work_again_and_again(cb, starts, Dk, Dv):  # noqa: F811
+    """CTAs that are over as soon as their last sums are: what they left to the tensor core has to be over before them."""
+    case = ring_prompt(30, starts, 4, 2, Dk, Dv, 64, 16)
+    c, ref = OnGpu(cb)(case), attention.linear_attention(**case)
+    got = [cb.linear_attention(**c) for _ in range(200)]
+    torch.cuda.synchronize()
+    for g in got[::20]:
+        compare(g, ref)
+    assert cb.static_status() == 0
+
+
 def test_refusals_in_python(cb):  # noqa: F811
     case = OnGpu(cb)(ring_prompt(1, [0, 9], 2, 1, 8, 6, 4, 16))
     with pytest.raises(AssertionError):
