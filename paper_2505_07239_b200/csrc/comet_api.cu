@@ -552,7 +552,7 @@ cudaError_t attn_kernel_attributes() {
         if (err == cudaSuccess) err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     };
     for (auto* kernel : {comet::attn_step_kernel<true, 1>, comet::attn_step_kernel<false, 1>}) room(kernel, comet::attn_step_smem(at::MAX_DIM, 1));
-    for (auto* kernel : {comet::attn_keys_kernel<true>, comet::attn_keys_kernel<false>}) room(kernel, at::TILE_SMEM);
+    for (auto* kernel : {comet::attn_products_kernel<true>, comet::attn_products_kernel<false>}) room(kernel, at::TILE_SMEM);
     for (auto* kernel : {comet::attn_rows_kernel<true>, comet::attn_rows_kernel<false>}) room(kernel, at::TILE_SMEM);
     for (auto* kernel : {comet::attn_step_kernel<true, 4>, comet::attn_step_kernel<false, 4>}) room(kernel, comet::attn_step_smem(at::MAX_DIM, 4));
     return err;
@@ -2503,14 +2503,14 @@ bool attn_heads(int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim)
            v_dim % 2 == 0 && k_dim <= at::MAX_DIM && v_dim <= at::MAX_DIM;
 }
 bool attn_stride(int64_t stride, int64_t tokens, int64_t row) { return stride >= 0 && stride <= 1ll << 32 && (tokens == 1 || stride >= row); }
-// The workspace in words: the products d v^T of both parties; the opened states, queries, keys, decayed keys and values, which
-// are even, and the opened weights and their masks.
+// The workspace in words: the products d v^T of both parties; the opened states, queries, keys, decayed keys and values, all of them
+// even, V_1 of queries and decayed keys; the opened weights, their masks and V_1.
 struct AttnRoom {
     int64_t kv, q, k, v, p;
     AttnRoom(int64_t tokens, int64_t chunks, int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim, int64_t chunk)
         : kv(chunks * kv_heads * k_dim * v_dim), q(tokens * q_heads * k_dim), k(tokens * kv_heads * k_dim), v(tokens * kv_heads * v_dim),
           p(tokens * q_heads * (chunk + chunk % 2)) {}
-    size_t bytes() const { return kv ? (size_t)(3 * kv + q + 2 * k + v + 3 * p) * sizeof(u64) : 0; }
+    size_t bytes() const { return kv ? (size_t)(3 * kv + 2 * q + 3 * k + v + 3 * p) * sizeof(u64) : 0; }
 };
 
 bool attn_sizes(int64_t tokens, int64_t chunks, int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim, int64_t chunk) {
@@ -2602,7 +2602,7 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
         return p;
     };
     a.kv[0] = take(room.kv); a.kv[1] = take(room.kv); a.s = take(room.kv); a.q = take(room.q); a.k = take(room.k); a.d = take(room.k);
-    a.v = take(room.v); a.p = take(room.p); a.pm[0] = take(room.p); a.pm[1] = take(room.p);
+    a.v = take(room.v); a.q1 = take(room.q); a.d1 = take(room.k); a.p = take(room.p); a.pm[0] = take(room.p); a.pm[1] = take(room.p);
     a.decay = reinterpret_cast<const u64*>(g->decay);
     a.starts = g->starts;
     a.bad_starts = g->bad_starts_flag;
@@ -2622,18 +2622,23 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
     bool vec = true;
     for (int i = 0; i < 2; ++i)
         for (const u64* p : {a.mq[i], a.mk[i], a.mv[i], a.md[i], a.mp[i], a.ms[i], a.S0[i], (const u64*)a.Eq[i], (const u64*)a.Ek[i], (const u64*)a.Ev[i],
-                             (const u64*)a.Ed[i], (const u64*)a.Es[i], (const u64*)a.S1[i]})
+                             (const u64*)a.Ed[i], (const u64*)a.Ep[i], (const u64*)a.Es[i], (const u64*)a.S1[i], (const u64*)a.O[i], a.qk[i], a.pv[i], a.qs[i], a.dv[i]})
             vec = vec && aligned16(p);
     const int pieces = ceil_div(a.k_dim * a.v_dim, 2 * at::THREADS);
     cudaError_t err = cudaSuccess;
-    if (n) err = launch_chained(vec ? comet::attn_keys_kernel<true> : comet::attn_keys_kernel<false>, dim3((unsigned)(n * Hk)), dim3(at::TILE_THREADS),
-                                at::TILE_SMEM, stream, nullptr, a);
+    const int slabs = ceil_div(a.C, at::SLAB), k_tiles = ceil_div(a.k_dim, at::ROWS), v_tiles = ceil_div(a.v_dim, at::COLS), s_tiles = ceil_div(a.C, at::COLS);
+    const int keys_ctas = (int)(n * Hk) * k_tiles * v_tiles;
+    if (n) err = launch_chained(vec ? comet::attn_open_kernel<true> : comet::attn_open_kernel<false>, dim3((unsigned)(n * slabs), (unsigned)(Hk + Hq)),
+                                dim3(at::THREADS), 0, stream, nullptr, a, slabs);
+    if (err == cudaSuccess && n)
+        err = launch_chained(vec ? comet::attn_products_kernel<true> : comet::attn_products_kernel<false>, dim3((unsigned)(keys_ctas + n * Hq * s_tiles)),
+                             dim3(at::THREADS), at::TILE_SMEM, stream, nullptr, a, keys_ctas, k_tiles, v_tiles, s_tiles);
     if (err == cudaSuccess)
         err = launch_chained(vec ? comet::attn_state_kernel<true> : comet::attn_state_kernel<false>, dim3((unsigned)(g->sequences * Hk * pieces)),
                              dim3(at::THREADS), 0, stream, nullptr, a, pieces);
     if (err == cudaSuccess && n)
-        err = launch_chained(vec ? comet::attn_rows_kernel<true> : comet::attn_rows_kernel<false>, dim3((unsigned)(n * Hq)), dim3(at::TILE_THREADS), at::TILE_SMEM,
-                             stream, nullptr, a);
+        err = launch_chained(vec ? comet::attn_rows_kernel<true> : comet::attn_rows_kernel<false>, dim3((unsigned)(n * Hq * v_tiles * 2)), dim3(at::THREADS),
+                             at::TILE_SMEM, stream, nullptr, a, v_tiles);
     if (err != cudaSuccess) cudaGetLastError();
     return err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
 }

@@ -5,8 +5,8 @@
 //     P[r][s] = tr(w[r - s] tr(q_r . k_s)), s <= r;   O_r = tr(sum_{s <= r} P[r][s] v_s + w[r + 1] tr(q_r S))
 //     d_s = tr(w[L - 1 - s] k_s);                     S <- tr(w[L] S + sum_s d_s v_s^T)
 //   single tokens:  S <- tr(w S + k v^T),  o = tr(q S)
-// Three kernels for a prompt, because only the states depend on one another: the products d v^T of all chunks and key heads at once
-// (keys), the states from chunk to chunk, a word a thread (state), then everything else of all chunks and query heads (rows).
+// Four kernels for a prompt: all values that need no product are opened (open); the products d v^T of all chunks and key heads and the weights P
+// of all chunks and query heads (products); the states from chunk to chunk, a word a thread (state); the rows of O (rows).
 #pragma once
 #include <cstdint>
 #include <type_traits>
@@ -20,17 +20,14 @@ namespace comet {
 
 namespace attn {
 constexpr int MAX_CHUNK = 64, MAX_DIM = 256;
-constexpr int THREADS = 256;                         // of the kernels without products
-constexpr int ROWS = 128, TILE = 64;                 // of a tile of a product: rows, columns
-constexpr int GROUP = 8;                             // warps that convert one of the two products
-constexpr int CONVERTERS = 2 * GROUP, DRAINERS = 8, WORKERS = 32 * (CONVERTERS + DRAINERS), ISSUER = CONVERTERS + DRAINERS;
-constexpr int TILE_THREADS = WORKERS + 32;
-constexpr int SLOTS = 3;                             // of planes: one of the two products of 32 indices each
-constexpr int LEFT_PLANE = ROWS * limb::KC, RIGHT_PLANE = TILE * limb::KC, LEFT_BYTES = limb::PLANES * LEFT_PLANE;
-constexpr int SLOT_BYTES = LEFT_BYTES + limb::PLANES * RIGHT_PLANE, ACC_COLS = limb::PLANES * TILE;
-constexpr int CELL_ROWS = 32;                        // rows that a group covers at a time
-constexpr int AHEAD = 3, BATCH = 4;                  // a draining thread's dealer's words: batches of columns under way, columns of one
-constexpr int RING_BYTES = AHEAD * BATCH * 2 * 32 * DRAINERS * 8, TILE_SMEM = SLOTS * SLOT_BYTES + RING_BYTES + 128;
+constexpr int THREADS = 256;
+constexpr int ROWS = 64, COLS = 32, DEPTH = 32;      // of a tile of a product; contraction indices of a step
+constexpr int WARP = 16;                             // rows and columns of a warp's part
+constexpr int LEFT_BYTES = ROWS * DEPTH * 8, STEP_BYTES = LEFT_BYTES + COLS * DEPTH * 8;
+constexpr int STEPS = 4;                             // in shared memory
+constexpr int KEPT = 8;                              // words that a thread keeps from one product to the next
+constexpr int TILE_SMEM = STEPS * STEP_BYTES + KEPT * THREADS * 8;
+constexpr int SLAB = 16;                             // rows of a chunk that a CTA opens
 }  // namespace attn
 
 struct AttnArgs {
@@ -43,7 +40,8 @@ struct AttnArgs {
     u64* S1[2];
     u64* kv[2];                                                          // [chunks][kv_heads][k_dim][v_dim]: sum d v^T at scale 2f
     u64* q; u64* k; u64* v; u64* d; u64* s;                              // opened values, as their messages lie
-    u64* p; u64* pm[2];                                                  // opened weights and their masks, zero off the triangle
+    u64* q1; u64* d1;                                                    // V_1 of Eq. 1: party 1's mask and the opened value
+    u64* p; u64* pm[2];                                                  // opened weights, party 0's mask, V_1; zero off the triangle
     const u64* decay;                                                    // [kv_heads][C + 1]
     const int32_t* starts;
     int32_t* bad_starts;
@@ -55,7 +53,7 @@ struct AttnArgs {
 
 // Tokens of sequence j, which begin at *begin: none where the starts are not ascending or leave the tokens.
 __device__ __forceinline__ int attn_length(const AttnArgs& a, int j, int* begin) {
-    const int b = __ldg(a.starts + j), e = __ldg(a.starts + j + 1);
+    const int b = a.starts[j], e = a.starts[j + 1];
     *begin = b;
     return b >= 0 && b <= e && e <= a.tokens ? e - b : 0;
 }
@@ -67,7 +65,7 @@ struct AttnChunk {
 // Chunk `want` of all sequences', by all threads of a CTA.
 __device__ __forceinline__ AttnChunk attn_find(const AttnArgs& a, int want) {
     __shared__ AttnChunk found;
-    __shared__ int sums[attn::TILE_THREADS / 32];
+    __shared__ int sums[attn::THREADS / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     if (tid == 0) found = {0, 0, 0};
     for (int j0 = 0, base = 0; j0 < a.sequences && base <= want; j0 += blockDim.x) {
@@ -98,9 +96,23 @@ __device__ __forceinline__ AttnChunk attn_find(const AttnArgs& a, int want) {
 }
 
 template <bool VEC>
-__device__ __forceinline__ ulonglong2 attn_load2(const u64* p) {         // words that nobody else reads
+__device__ __forceinline__ ulonglong2 attn_load2(const u64* p) {         // words that nobody reads again
     if (VEC) return __ldcs(reinterpret_cast<const ulonglong2*>(p));
     return make_ulonglong2(__ldcs(p), __ldcs(p + 1));
+}
+template <bool VEC>
+__device__ __forceinline__ ulonglong2 attn_keep2(const u64* p) {         // words that the same kernel reads again
+    if (VEC) return *reinterpret_cast<const ulonglong2*>(p);
+    return make_ulonglong2(p[0], p[1]);
+}
+template <bool VEC>
+__device__ __forceinline__ void attn_send2(u64* p, ulonglong2 v) {       // a message or result: nobody here reads it
+    if (VEC) {
+        __stcs(reinterpret_cast<ulonglong2*>(p), v);
+    } else {
+        __stcs(p, v.x);
+        __stcs(p + 1, v.y);
+    }
 }
 template <bool VEC>
 __device__ __forceinline__ void attn_store2(u64* p, ulonglong2 v) {
@@ -118,344 +130,150 @@ __device__ __forceinline__ ulonglong2 attn_add(ulonglong2 x, ulonglong2 y) { ret
 __device__ __forceinline__ u64 attn_rescale(u64 v, int party, int f) { return party ? 0ull - norm_shift(0ull - v, f) : norm_shift(v, f); }
 
 // ---------------------------------------------------------------------------
-// Products on the int8 tensor cores.  A CTA works out tiles of ROWS x TILE words of Z_i = (triple) + E B_i + V_i F, V_i = A_i + i E (Eq. 1), one
-// party's after the other's, from words in memory, masks and opened values: two groups of eight warps turn 32 contraction indices of one product each
-// into limb planes in shared memory (kernels_limb.cuh has the decomposition and the layout), a warp issues the MMAs, eight warps read the sums out
-// of tensor memory.  Left operands are keys, values or states, right ones queries, weights or decayed keys; rows past an operand's are whatever lies
-// in shared memory, and their sums are never looked at.
+// Products.  A CTA works out tiles of ROWS x COLS words of Z_i = (triple) + E B_i + V_i F, V_i = A_i + i E (Eq. 1), on the int8 tensor cores: a word is
+// eight bytes, x = sum_p x_p 2^(8p), and of the 64 products of bytes the 36 with p + q <= 7 matter mod 2^64, summed up by p + q in eight 32-bit
+// accumulators (kernels_limb.cuh has why 32 bits are enough).
+//
+// The words come to shared memory by asynchronous copies, STEPS steps of 32 indices of one product ahead; a warp cuts the words of its 16 rows and 16
+// columns into bytes in registers, 72 instructions of 16 x 8 x 32 a step.  Which byte of an operand's registers is which contraction index does not
+// matter as long as both operands agree: lane t of four has the indices 8j + 2t, 8j + 2t + 1, j < 4, words that lie side by side.
 // ---------------------------------------------------------------------------
-struct AttnOperand {
-    const u64* mask;                     // the party's
-    const u64* open;                     // the opened value
-    uint32_t step;                       // words from row to row; of a DEEP operand, whose rows lie side by side, from index to index
-};
-enum AttnWords { MASK, OPEN, BOTH };     // of a plane set: the mask, the opened value, their sum
-
-// A thread's cells of the planes of `rows` rows: four words of a row, indices 2g, 2g + 1, 16 + 2g, 17 + 2g of every 32 (limb_emit4's order), TASKS of
-// them, CELL_ROWS rows apart.  Places are counted in 32 bits: an operand spans less than 2^29 words (comet_linear_attention sees to that).
-template <bool DEEP, int TASKS>
-struct AttnCells {
-    uint32_t at;                                 // of the first word, from the operand's on
-    int to, row, g;                              // to: in a plane
-
-    __device__ __forceinline__ AttnCells(const AttnOperand& x) {
-        const int warp = (threadIdx.x >> 5) % attn::GROUP, lane = threadIdx.x & 31;
-        if (DEEP) {
-            // eight rows x four groups of indices a warp: 64-byte pieces of memory, 128 bytes of a plane
-            row = (warp >> 1) * 8 + (lane & 7);
-            g = (warp & 1) * 4 + (lane >> 3);
-        } else {
-            // lanes of the upper groups take the row four further, against bank conflicts
-            g = lane & 7;
-            row = 4 * (2 * (warp >> 1) + ((warp & 1) ^ (g >> 2))) + (lane >> 3);
-        }
-        to = (row >> 3) * 256 + (g >> 2) * 128 + (row & 7) * 16 + (g & 3) * 4;
-        at = DEEP ? 2 * g * x.step + row : row * x.step + 2 * g;
+template <bool VEC>
+__device__ __forceinline__ void attn_copy2(uint32_t to, const u64* from, int words) {        // those behind the words are zero
+    if (VEC) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(8 * words) : "memory");
+    } else {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(from), "r"(words > 0 ? 8 : 0) : "memory");
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to + 8), "l"(words > 1 ? from + 1 : from), "r"(words > 1 ? 8 : 0) : "memory");
     }
-    // Of the 32 indices from k0 on; those from `depth` on are zero.
-    template <AttnWords WHAT, bool VEC>
-    __device__ __forceinline__ void read(const AttnOperand& x, u64 (&w)[TASKS][4], int rows, int k0, int depth) const {
-        const uint32_t from = at + (DEEP ? k0 * x.step : k0);
-        const int left = depth - k0 - 2 * g;
+}
+
+// An operand's part of a step, N rows or columns.  Its words lie `step` words from row to row; of a DEEP operand, whose rows lie side by side, from
+// index to index.  In shared memory pieces change places so that the reads below meet no bank twice: of a row, whose 256 bytes eight lanes read in
+// turns of 64, those halves of 128 bytes that its number says; of an index of a deep operand, of which sixteen lanes read four words of four
+// indices, the pieces of 32 bytes.
+template <bool DEEP, int N>
+struct AttnSide {
+    static_assert(N % 16 == 0, "whole passes");
+    __device__ __forceinline__ static uint32_t place(int row, int piece) {           // of a pair of words
+        return DEEP ? row * (N * 8) + (((piece >> 1) ^ ((row >> 1) & 3)) << 5) + ((piece & 1) << 4)
+                    : row * 256 + (((piece >> 2) ^ (row & 1)) << 6) + ((piece & 3) << 4);
+    }
+    // `size` of the N rows are the operand's, `depth` of the 32 indices
+    template <bool VEC>
+    __device__ __forceinline__ static void copy(uint32_t to, const u64* x, uint32_t step, int size, int depth) {
+        constexpr int PIECES = DEEP ? N / 2 : 16, LINES = DEEP ? attn::DEPTH : N, PASS = attn::THREADS / PIECES;
+        const int piece = threadIdx.x % PIECES, first = threadIdx.x / PIECES;
+        const int lines = DEEP ? depth : size, words = max(0, min(2, (DEEP ? size : depth) - 2 * piece));
 #pragma unroll
-        for (int t = 0; t < TASKS; ++t) {
-            const bool live = row + t * attn::CELL_ROWS < rows;
+        for (int l = first; l < LINES; l += PASS) {
+            const int n = l < lines ? words : 0;
+            attn_copy2<VEC>(to + place(l, piece), n ? x + (l * step + 2 * piece) : x, n);
+        }
+    }
+    // The eight words of row `row` of lane t of four, cut into bytes: planes[p][h] byte p of the words 4h .. 4h + 3.
+    __device__ __forceinline__ static void bytes(const uint8_t* from, int row, int t, uint32_t (&planes)[limb::PLANES][2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            u64 w[4];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (DEEP) {
+                    const uint8_t* const at = from + (16 * h + 8 * j + 2 * t) * (N * 8) + (((row >> 2) ^ t) << 5) + ((row & 3) << 3);
+                    w[2 * j] = *reinterpret_cast<const u64*>(at);
+                    w[2 * j + 1] = *reinterpret_cast<const u64*>(at + N * 8);
+                } else {
+                    const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(from + row * 256 + (((2 * h + j) ^ (row & 1)) << 6) + (t << 4));
+                    w[2 * j] = v.x;
+                    w[2 * j + 1] = v.y;
+                }
+            }
+            limb_transpose4((uint32_t)w[0], (uint32_t)w[1], (uint32_t)w[2], (uint32_t)w[3], planes[0][h], planes[1][h], planes[2][h], planes[3][h]);
+            limb_transpose4((uint32_t)(w[0] >> 32), (uint32_t)(w[1] >> 32), (uint32_t)(w[2] >> 32), (uint32_t)(w[3] >> 32), planes[4][h], planes[5][h],
+                            planes[6][h], planes[7][h]);
+        }
+    }
+};
+
+// A warp's sums: [half of the columns][p + q][register of the instruction].
+struct AttnSums {
+    uint32_t d[2][limb::PLANES][4];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int p = 0; p < limb::PLANES; ++p)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[n][p][j] = 0u;
+    }
+    // Pairs of words of a row: f(which of the thread's four pairs, row, column, pair)
+    template <typename F>
+    __device__ __forceinline__ void each(F&& f) const {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = (warp >> 1) * attn::WARP + (lane >> 2), col = (warp & 1) * attn::WARP + 2 * (lane & 3);
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                u64 v[2] = {0ull, 0ull};
-                if (!DEEP && VEC) {              // (rows are even in length, zero behind an odd depth)
-                    if (live && 16 * h < left) {
-                        const uint32_t o = from + 16 * h + t * attn::CELL_ROWS * x.step;
-                        if (WHAT != MASK) {
-                            const ulonglong2 e = *reinterpret_cast<const ulonglong2*>(x.open + o);
-                            v[0] = e.x;
-                            v[1] = e.y;
-                        }
-                        if (WHAT != OPEN) {
-                            const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(x.mask + o);
-                            v[0] += m.x;
-                            v[1] += m.y;
-                        }
-                    }
-                } else {
+                u64 z[2];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        if (live && 16 * h + j < left) {
-                            const uint32_t o = from + (DEEP ? x.step : 1u) * (16 * h + j) + t * attn::CELL_ROWS * (DEEP ? 1u : x.step);
-                            if (WHAT != MASK) v[j] = x.open[o];
-                            if (WHAT != OPEN) v[j] += x.mask[o];
-                        }
+                for (int j = 0; j < 2; ++j) {
+                    const int e = 2 * h + j;
+                    z[j] = limb_recombine(d[n][0][e], d[n][1][e], d[n][2][e], d[n][3][e], d[n][4][e], d[n][5][e], d[n][6][e], d[n][7][e]);
                 }
-                w[t][2 * h] = v[0];
-                w[t][2 * h + 1] = v[1];
+                f(2 * n + h, row + 8 * h, col + 8 * n, make_ulonglong2(z[0], z[1]));
             }
-        }
     }
-    __device__ __forceinline__ void emit(uint8_t* planes, int plane_bytes, const u64 (&w)[TASKS][4], int rows) const {
+};
+__device__ __forceinline__ void attn_mma(uint32_t (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.u8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <bool DEEP_LEFT, bool DEEP_RIGHT>
+__device__ __forceinline__ void attn_multiply(const uint8_t* step, AttnSums& sums) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, row = (warp >> 1) * attn::WARP + g, col = (warp & 1) * attn::WARP + g;
+    uint32_t a[2][limb::PLANES][2];
 #pragma unroll
-        for (int t = 0; t < TASKS; ++t)
-            if (row + t * attn::CELL_ROWS < rows) limb_emit4(planes + to + t * (attn::CELL_ROWS / 8 * 256), plane_bytes, w[t]);
-    }
-};
-
-// What a CTA's warps share.
-struct AttnTile {
-    uint64_t full[attn::SLOTS], empty[attn::SLOTS], acc_full, acc_empty, weights;
-    uint32_t tmem;
-    int abort_flag;
-    uint8_t* planes;
-};
-__device__ __forceinline__ void attn_tile_begin(AttnTile& s, uint8_t* raw) {
-    if (threadIdx.x == 0) {
-        for (int k = 0; k < attn::SLOTS; ++k) {
-            ptx::mbar_init(ptx::smem_u32(&s.full[k]), attn::GROUP);
-            ptx::mbar_init(ptx::smem_u32(&s.empty[k]), 1);
-        }
-        ptx::mbar_init(ptx::smem_u32(&s.acc_full), 1);
-        ptx::mbar_init(ptx::smem_u32(&s.acc_empty), attn::DRAINERS);
-        ptx::mbar_init(ptx::smem_u32(&s.weights), attn::DRAINERS);
-        s.abort_flag = 0;
-        s.planes = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~(uintptr_t)127);
-        ptx::fence_barrier_init();
-    }
-    __syncwarp();
-    if (threadIdx.x >> 5 == attn::ISSUER) {
-        ptx::tmem_alloc(ptx::smem_u32(&s.tmem), attn::ACC_COLS);
-        ptx::tmem_relinquish();
-    }
-    ptx::fence_before_sync();
-    __syncthreads();
-    ptx::fence_after_sync();
-}
-// All warps but the issuer wait for one another.  (A warp comes to a barrier, and to a read of tensor memory, as a whole: both are
-// undefined for lanes on their own, and what stands before may have parted them.)
-__device__ __forceinline__ void attn_meet() {
-    __syncwarp();
-    asm volatile("bar.sync 1, %0;" ::"n"(attn::WORKERS) : "memory");
-}
-
-// Bounded wait, written out where it stands: false, and the CTA's abort flag raised, if the barrier did not flip in time or another warp has given up.
-// Not a call: loads and asynchronous copies are under way when a warp comes to wait here.
-__device__ __forceinline__ bool attn_wait(uint64_t& bar, uint32_t parity, AttnTile& s) {
-    const uint32_t at = ptx::smem_u32(&bar);
-    bool ok = ptx::mbar_try_wait(at, parity);
-    if (!ok) {
-        const long long t0 = clock64();
-        volatile int* const abort_flag = &s.abort_flag;
-        do {
-            ok = ptx::mbar_try_wait(at, parity);
-            if (!ok && (*abort_flag || clock64() - t0 > limb::WAIT_CYCLES)) {
-                *abort_flag = 1;
-                break;
-            }
-        } while (!ok);
-    }
-    return ok;
-}
-// The same for a whole warp.
-__device__ __forceinline__ bool attn_wait_warp(uint64_t& bar, uint32_t parity, AttnTile& s) {
-    return __all_sync(0xffffffffu, attn_wait(bar, parity, s));
-}
-
-// Where a warp is in the order of slots and tiles; all count alike.
-struct AttnTurn {
-    uint32_t stage = 0, tile = 0;
-    bool ok = true;
-};
-__device__ __forceinline__ int attn_blocks(int depth) { return (depth + limb::KC - 1) / limb::KC; }
-
-// The end of a CTA.  What the tensor core still owes is waited for first: the last stages' slots, which nobody uses again, are reported free through
-// shared memory, and a report that comes when the CTA is gone is an access to an address that does not exist.  (It happened, where the last sums were
-// drained fast enough.)
-__device__ __forceinline__ void attn_tile_end(AttnTile& s, const AttnTurn& turn, int* error) {
-    __syncwarp();
-    if (threadIdx.x >> 5 == attn::ISSUER && turn.ok)
-        for (uint32_t k = 1; k <= attn::SLOTS && k <= turn.stage; ++k) {
-            const uint32_t n = turn.stage - k;
-            attn_wait(s.empty[n % attn::SLOTS], n / attn::SLOTS & 1u, s);
-        }
-    __syncwarp();
-    ptx::fence_before_sync();
-    __syncthreads();
-    if (threadIdx.x == 0 && s.abort_flag) {
-        *error = 1;
-        __threadfence_system();
-    }
-    __syncwarp();
-    if (threadIdx.x >> 5 == attn::ISSUER) {
-        ptx::fence_after_sync();
-        ptx::tmem_dealloc(s.tmem, attn::ACC_COLS);
-    }
-}
-
-// The issuing warp's part of a tile.
-__device__ __forceinline__ void attn_issue(AttnTile& s, AttnTurn& turn, int depth) {
-    const int stages = 2 * attn_blocks(depth);
-    __syncwarp();
-    if (ptx::elect_one() && turn.ok) {
-        constexpr uint32_t IDESC = (2u << 4) | ((uint32_t)(attn::ROWS >> 4) << 24);
-        bool ok = attn_wait(s.acc_empty, (turn.tile & 1u) ^ 1u, s);
-        ptx::fence_after_sync();
-        for (int t = 0; t < stages && ok; ++t) {
-            const uint32_t n = turn.stage + t, slot = n % attn::SLOTS;
-            ok = attn_wait(s.full[slot], n / attn::SLOTS & 1u, s);
-            if (!ok) break;
-            ptx::fence_after_sync();
-            const uint32_t left = limb_desc_lo(ptx::smem_u32(s.planes) + slot * attn::SLOT_BYTES), right = left + (attn::LEFT_BYTES >> 4);
-            const uint32_t acc = t > 0 ? 1u : 0u;
+    for (int h = 0; h < 2; ++h) AttnSide<DEEP_LEFT, attn::ROWS>::bytes(step, row + 8 * h, t, a[h]);
 #pragma unroll
-            for (int i = 0; i < limb::PLANES; ++i) {
-                // wide and narrow instructions alternate, plane 0, which overwrites all sums, first
-                const int p = i & 1 ? limb::PLANES - 1 - (i >> 1) : i >> 1, n_total = attn::TILE * (limb::PLANES - p);
-                const uint32_t at = left + (p * attn::LEFT_PLANE >> 4), acc_p = p == 0 ? acc : 1u;
-                if (n_total > 256) {
-                    ptx::mma_i8_keep_a(s.tmem + attn::TILE * p, at, LIMB_DESC_HI, right, LIMB_DESC_HI, IDESC | (256u >> 3 << 17), acc_p);
-                    ptx::mma_i8_reuse_a(s.tmem + attn::TILE * p + 256, at, LIMB_DESC_HI, right + (256 * limb::KC >> 4), LIMB_DESC_HI,
-                                        IDESC | ((uint32_t)(n_total - 256) >> 3 << 17), acc_p);
-                } else {
-                    ptx::mma_i8(s.tmem + attn::TILE * p, at, LIMB_DESC_HI, right, LIMB_DESC_HI, IDESC | ((uint32_t)n_total >> 3 << 17), acc_p);
-                }
-            }
-            ptx::mma_commit(ptx::smem_u32(&s.empty[slot]));
-        }
-        if (ok) ptx::mma_commit(ptx::smem_u32(&s.acc_full));
-        turn.ok = ok;
+    for (int n = 0; n < 2; ++n) {
+        uint32_t b[limb::PLANES][2];
+        AttnSide<DEEP_RIGHT, attn::COLS>::bytes(step + attn::LEFT_BYTES, col + 8 * n, t, b);
+#pragma unroll
+        for (int p = 0; p < limb::PLANES; ++p)
+#pragma unroll
+            for (int q = 0; p + q < limb::PLANES; ++q) attn_mma(sums.d[n][p + q], a[0][p][0], a[1][p][0], a[0][p][1], a[1][p][1], b[q][0], b[q][1]);
     }
-    turn.stage += stages;
-    ++turn.tile;
 }
-// The converting warps' part: planes of both products, 32 indices at a time, E B_i by the first group, V_i F by the second.  A stage's words are asked
-// for before the wait for its slot, and while one group waits for its words the other puts its own away.
-template <bool DEEP_LEFT, bool DEEP_RIGHT, bool VEC>
-__device__ __forceinline__ void attn_convert(AttnTile& s, AttnTurn& turn, const AttnOperand& left, int rows, const AttnOperand& right, int cols, int depth,
-                                             int party) {
-    constexpr int LEFT = DEEP_LEFT ? 4 : 2, RIGHT = 2;       // up to ROWS rows of a deep left operand, MAX_CHUNK of another; TILE rows of a right one
-    const int lane = threadIdx.x & 31, second = threadIdx.x / (32 * attn::GROUP);
-    const AttnCells<DEEP_LEFT, LEFT> l(left);
-    const AttnCells<DEEP_RIGHT, RIGHT> r(right);
+// Steps 0 .. steps - 1 of a CTA: copy(step, where) asks for a step's words, work(step, where) uses them.
+template <typename C, typename W>
+__device__ __forceinline__ void attn_steps(uint8_t* smem, int steps, C&& copy, W&& work) {
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem);
+#pragma unroll
+    for (int n = 0; n < attn::STEPS - 1; ++n) {
+        if (n < steps) copy(n, base + n * attn::STEP_BYTES);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
 #pragma unroll 1
-    for (int k0 = 0; k0 < depth; k0 += limb::KC) {
-        u64 lw[LEFT][4], rw[RIGHT][4];
-        if (second == 0) {
-            l.template read<MASK, VEC>(left, lw, rows, k0, depth);
-            r.template read<OPEN, VEC>(right, rw, cols, k0, depth);
-        } else {
-            l.template read<OPEN, VEC>(left, lw, rows, k0, depth);
-            if (party) r.template read<BOTH, VEC>(right, rw, cols, k0, depth);
-            else r.template read<MASK, VEC>(right, rw, cols, k0, depth);
-        }
-        const uint32_t n = turn.stage + second, slot = n % attn::SLOTS;
-        turn.stage += 2;
-        turn.ok = turn.ok && attn_wait_warp(s.empty[slot], (n / attn::SLOTS & 1u) ^ 1u, s);
-        if (!turn.ok) continue;
-        uint8_t* const at = s.planes + slot * attn::SLOT_BYTES;
-        l.emit(at, attn::LEFT_PLANE, lw, rows);
-        r.emit(at + attn::LEFT_BYTES, attn::RIGHT_PLANE, rw, cols);
-        ptx::fence_proxy_async_smem();                       // the planes are read by the tensor cores
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&s.full[slot]));
+    for (int n = 0; n < steps; ++n) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(attn::STEPS - 2) : "memory");
+        __syncthreads();                                     // the step is there, and the one before has been used by all
+        const int ahead = n + attn::STEPS - 1;
+        if (ahead < steps) copy(ahead, base + ahead % attn::STEPS * attn::STEP_BYTES);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        work(n, smem + n % attn::STEPS * attn::STEP_BYTES);
     }
 }
-// Four columns of the eight accumulators, loads and wait in one statement: until the wait is over the hardware may write the registers at any
-// time, so nothing may be moved out of them or put into their place before it.
-__device__ __forceinline__ void attn_sums(uint32_t at, uint32_t (&d)[limb::PLANES][4]) {
-    constexpr int N = attn::TILE;
-    __syncwarp();
-    asm volatile(
-        "{\n\t"
-        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%32];\n\t"
-        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%4, %5, %6, %7}, [%33];\n\t"
-        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%8, %9, %10, %11}, [%34];\n\t"
-        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%12, %13, %14, %15}, [%35];\n\t"
-        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%16, %17, %18, %19}, [%36];\n\t"
-        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%20, %21, %22, %23}, [%37];\n\t"
-        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%24, %25, %26, %27}, [%38];\n\t"
-        "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%28, %29, %30, %31}, [%39];\n\t"
-        "tcgen05.wait::ld.sync.aligned;\n\t}"
-        : "=&r"(d[0][0]), "=&r"(d[0][1]), "=&r"(d[0][2]), "=&r"(d[0][3]), "=&r"(d[1][0]), "=&r"(d[1][1]), "=&r"(d[1][2]), "=&r"(d[1][3]),
-          "=&r"(d[2][0]), "=&r"(d[2][1]), "=&r"(d[2][2]), "=&r"(d[2][3]), "=&r"(d[3][0]), "=&r"(d[3][1]), "=&r"(d[3][2]), "=&r"(d[3][3]),
-          "=&r"(d[4][0]), "=&r"(d[4][1]), "=&r"(d[4][2]), "=&r"(d[4][3]), "=&r"(d[5][0]), "=&r"(d[5][1]), "=&r"(d[5][2]), "=&r"(d[5][3]),
-          "=&r"(d[6][0]), "=&r"(d[6][1]), "=&r"(d[6][2]), "=&r"(d[6][3]), "=&r"(d[7][0]), "=&r"(d[7][1]), "=&r"(d[7][2]), "=&r"(d[7][3])
-        : "r"(at), "r"(at + N), "r"(at + 2 * N), "r"(at + 3 * N), "r"(at + 4 * N), "r"(at + 5 * N), "r"(at + 6 * N), "r"(at + 7 * N)
-        : "memory");
-}
-// The draining warps' part: the sums of this thread's row, a batch of columns after the other: done(row, column, sum, words, own).  The dealer's
-// words, at(k, row, column) the place of the k-th, come into the thread's own places of shared memory AHEAD batches before they are needed, the
-// first before the wait for the sums; a word that the thread itself has written, own(row, column), one batch before.
-template <int WORDS, typename P, typename O, typename F>
-__device__ __forceinline__ void attn_drain(AttnTile& s, AttnTurn& turn, int rows, int cols, P&& at, O&& own, F&& done) {
-    using namespace attn;
-    const int thread = threadIdx.x - 32 * CONVERTERS, quarter = (thread >> 5) & 3, row = thread & (ROWS - 1);
-    const int c0 = thread / ROWS * (TILE / 2), c1 = min(cols, c0 + TILE / 2);                // a half of the columns
-    u64* const ring = reinterpret_cast<u64*>(s.planes + SLOTS * SLOT_BYTES) + thread;       // [AHEAD][BATCH][2][threads]
-    constexpr int NEXT = 32 * DRAINERS;
-    auto fetch = [&](int c) {
-        u64* const to = ring + (c / BATCH % AHEAD) * (BATCH * 2 * NEXT);
-#pragma unroll
-        for (int j = 0; j < BATCH; ++j)
-            if (row < rows && c + j < c1)
-#pragma unroll
-                for (int k = 0; k < WORDS; ++k) {
-                    const u64* const from = at(k, row, c + j);
-                    if (from) norm_fetch8(to + (2 * j + k) * NEXT, from);
-                }
-        limb_copy_commit();
-    };
-    u64 mine[BATCH];
-    auto owned = [&](int c) {
-#pragma unroll
-        for (int j = 0; j < BATCH; ++j) mine[j] = row < rows && c + j < c1 ? own(row, c + j) : 0ull;
-    };
-    if (WORDS)
-#pragma unroll
-        for (int b = 0; b < AHEAD; ++b) fetch(c0 + b * BATCH);
-    owned(c0);
-    __syncwarp();
-    turn.ok = turn.ok && attn_wait_warp(s.acc_full, turn.tile & 1u, s);
-    ++turn.tile;
-    if (turn.ok) {
-        ptx::fence_after_sync();
-        const uint32_t acc = s.tmem + ((uint32_t)(quarter * 32) << 16);
-        if (quarter * 32 < rows) {
-#pragma unroll 1
-            for (int c = c0; c < c1; c += BATCH) {
-                uint32_t d[limb::PLANES][4];
-                attn_sums(acc + c, d);
-                if (WORDS) limb_copy_wait<AHEAD - 1>();
-                u64 here[BATCH], z[BATCH], words[BATCH][WORDS ? WORDS : 1];
-                const u64* const from = ring + (c / BATCH % AHEAD) * (BATCH * 2 * NEXT);
-#pragma unroll
-                for (int j = 0; j < BATCH; ++j) {
-                    z[j] = limb_recombine(d[0][j], d[1][j], d[2][j], d[3][j], d[4][j], d[5][j], d[6][j], d[7][j]);
-                    here[j] = mine[j];
-#pragma unroll
-                    for (int k = 0; k < WORDS; ++k) words[j][k] = from[(2 * j + k) * NEXT];
-                }
-                owned(c + BATCH);
-#pragma unroll
-                for (int j = 0; j < BATCH; ++j)
-                    if (row < rows && c + j < c1) done(row, c + j, z[j], words[j], here[j]);
-                if (WORDS) fetch(c + AHEAD * BATCH);             // (the words have been read)
-            }
-        }
-        ptx::fence_before_sync();
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(ptx::smem_u32(&s.acc_empty));
-    }
-    if (WORDS) limb_copy_wait<0>();
-}
+__device__ __forceinline__ int attn_blocks(int depth) { return (depth + attn::DEPTH - 1) / attn::DEPTH; }
 
-__device__ __forceinline__ u64 attn_nothing(int, int) { return 0ull; }
-
-// The pairs of words of `rows` rows of `cols`, two at a time a thread of the WORKERS: load(n, row, column) for both, then finish(n, row, column).
+// The pairs of words of `rows` rows of `cols`, two at a time a thread: load(n, row, column) for both, then finish(n, row, column).
 template <typename L, typename F>
 __device__ __forceinline__ void attn_pairs(int rows, int cols, L&& load, F&& finish) {
     const int half = cols / 2, all = rows * half;
-    for (int t = threadIdx.x; t < all; t += 2 * attn::WORKERS) {
+    for (int t = threadIdx.x; t < all; t += 2 * attn::THREADS) {
         int r[2], j[2];
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
-            const int u = t + n * attn::WORKERS;
+            const int u = t + n * attn::THREADS;
             r[n] = u < all ? u / half : -1;
             j[n] = 2 * (u - r[n] * half);
             if (r[n] >= 0) load(n, r[n], j[n]);
@@ -466,26 +284,24 @@ __device__ __forceinline__ void attn_pairs(int rows, int cols, L&& load, F&& fin
     }
 }
 
-// Messages of k, v and d of one chunk and key head, and its sum of d v^T.
+// Messages of q, or of k, v and d, of a head and SLAB rows of a chunk, and the opened values; zeros where no weight is sent.  Bound by memory.
 template <bool VEC>
-__global__ void __launch_bounds__(attn::TILE_THREADS, 1)
-attn_keys_kernel(const __grid_constant__ AttnArgs a) {
-    extern __shared__ uint8_t attn_smem[];
-    __shared__ AttnTile s;
+__global__ void __launch_bounds__(attn::THREADS, 2)
+attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
     pdl_wait();
     pdl_launch_dependents();
-    const int c = blockIdx.x / a.kv_heads, h = blockIdx.x - c * a.kv_heads, warp = threadIdx.x >> 5;
+    const int c = blockIdx.x / slabs, r0 = (blockIdx.x - c * slabs) * attn::SLAB;
     const AttnChunk at = attn_find(a, c);
-    if (at.len == 0) return;
-    attn_tile_begin(s, attn_smem);
-    AttnTurn turn;
-    const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
-    const size_t k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
-    if (warp != attn::ISSUER) {
-        const u64* const w = a.decay + (size_t)h * (a.C + 1) + at.len - 1;
+    const int rows = min(attn::SLAB, at.len - r0), first = at.first + r0;
+    if (rows <= 0) return;
+    if ((int)blockIdx.y < a.kv_heads) {
+        const int h = blockIdx.y;
+        const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
+        const size_t k_at = first * k_row + (size_t)h * a.k_dim, v_at = first * v_row + (size_t)h * a.v_dim;
+        const u64* const w = a.decay + (size_t)h * (a.C + 1) + at.len - 1 - r0;
         ulonglong2 x[2][2], mk[2][2], md[2][2];
-        attn_pairs(at.len, a.k_dim, [&](int n, int r, int j) {
-            const size_t o = k_at + r * k_row + j, x_at = (size_t)(at.first + r) * a.k_stride + (size_t)h * a.k_dim + j;
+        attn_pairs(rows, a.k_dim, [&](int n, int r, int j) {
+            const size_t o = k_at + r * k_row + j, x_at = (size_t)(first + r) * a.k_stride + (size_t)h * a.k_dim + j;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 x[n][i] = attn_input2(a.K[i] + x_at, a.in_vec);
@@ -500,14 +316,16 @@ attn_keys_kernel(const __grid_constant__ AttnArgs a) {
             for (int i = 0; i < 2; ++i) {
                 e[i] = attn_sub(x[n][i], mk[n][i]);
                 g[i] = attn_sub(make_ulonglong2(attn_rescale(x[n][i].x * weight, i, a.f), attn_rescale(x[n][i].y * weight, i, a.f)), md[n][i]);
-                attn_store2<VEC>(a.Ek[i] + o, e[i]);
-                attn_store2<VEC>(a.Ed[i] + o, g[i]);
+                attn_send2<VEC>(a.Ek[i] + o, e[i]);
+                attn_send2<VEC>(a.Ed[i] + o, g[i]);
             }
-            attn_store2<VEC>(a.k + o, attn_add(e[0], e[1]));         // the exchange
-            attn_store2<VEC>(a.d + o, attn_add(g[0], g[1]));
+            const ulonglong2 d = attn_add(g[0], g[1]);               // the exchange
+            attn_store2<VEC>(a.k + o, attn_add(e[0], e[1]));
+            attn_store2<VEC>(a.d + o, d);
+            attn_store2<VEC>(a.d1 + o, attn_add(md[n][1], d));
         });
-        attn_pairs(at.len, a.v_dim, [&](int n, int r, int j) {
-            const size_t o = v_at + r * v_row + j, x_at = (size_t)(at.first + r) * a.v_stride + (size_t)h * a.v_dim + j;
+        attn_pairs(rows, a.v_dim, [&](int n, int r, int j) {
+            const size_t o = v_at + r * v_row + j, x_at = (size_t)(first + r) * a.v_stride + (size_t)h * a.v_dim + j;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 x[n][i] = attn_input2(a.V[i] + x_at, a.in_vec);
@@ -519,38 +337,152 @@ attn_keys_kernel(const __grid_constant__ AttnArgs a) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 e[i] = attn_sub(x[n][i], mk[n][i]);
-                attn_store2<VEC>(a.Ev[i] + o, e[i]);
+                attn_send2<VEC>(a.Ev[i] + o, e[i]);
             }
-            attn_store2<VEC>(a.v + o, attn_add(e[0], e[1]));
-        });
-        attn_meet();
-    }
-    // the tiles of either party, the same order for every role
-    auto tiles = [&](auto&& tile) {
-#pragma unroll 1
-        for (int i = 0; i < 2; ++i)
-#pragma unroll 1
-            for (int v0 = 0; v0 < a.v_dim; v0 += attn::ROWS)
-#pragma unroll 1
-                for (int k0 = 0; k0 < a.k_dim; k0 += attn::TILE) tile(i, v0, k0, min(attn::ROWS, a.v_dim - v0), min(attn::TILE, a.k_dim - k0));
-    };
-    if (warp == attn::ISSUER) {
-        tiles([&](int, int, int, int, int) { attn_issue(s, turn, at.len); });
-    } else if (warp < attn::CONVERTERS) {
-        tiles([&](int i, int v0, int k0, int rows, int cols) {
-            const AttnOperand v = {a.mv[i] + v_at + v0, a.v + v_at + v0, (uint32_t)v_row}, d = {a.md[i] + k_at + k0, a.d + k_at + k0, (uint32_t)k_row};
-            attn_convert<true, true, VEC>(s, turn, v, rows, d, cols, at.len, i);
+            attn_store2<VEC>(a.v + o, attn_add(e[0], e[1]));         // the exchange
         });
     } else {
-        const size_t out = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
-        tiles([&](int i, int v0, int k0, int rows, int cols) {
-            const u64* const dv = a.dv[i] + out + (size_t)k0 * a.v_dim + v0;
-            u64* const kv = a.kv[i] + out + (size_t)k0 * a.v_dim + v0;
-            attn_drain<1>(s, turn, rows, cols, [&](int, int row, int col) { return dv + col * a.v_dim + row; }, attn_nothing,
-                          [&](int row, int col, u64 z, const u64* words, u64) { kv[col * a.v_dim + row] = words[0] + z; });
+        const int h = blockIdx.y - a.kv_heads, wide_C = a.C + (a.C & 1);
+        const size_t q_row = (size_t)a.q_heads * a.k_dim, p_row = (size_t)a.q_heads * a.C, w_row = (size_t)a.q_heads * wide_C;
+        const size_t q_at = first * q_row + (size_t)h * a.k_dim, p_at = first * p_row + (size_t)h * a.C, w_at = first * w_row + (size_t)h * wide_C;
+        ulonglong2 x[2][2], m[2][2];
+        attn_pairs(rows, a.k_dim, [&](int n, int r, int j) {
+            const size_t o = q_at + r * q_row + j, x_at = (size_t)(first + r) * a.q_stride + (size_t)h * a.k_dim + j;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                x[n][i] = attn_input2(a.Q[i] + x_at, a.in_vec);
+                m[n][i] = attn_load2<VEC>(a.mq[i] + o);
+            }
+        }, [&](int n, int r, int j) {
+            const size_t o = q_at + r * q_row + j;
+            ulonglong2 e[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                e[i] = attn_sub(x[n][i], m[n][i]);
+                attn_send2<VEC>(a.Eq[i] + o, e[i]);
+            }
+            const ulonglong2 q = attn_add(e[0], e[1]);               // the exchange
+            attn_store2<VEC>(a.q + o, q);
+            attn_store2<VEC>(a.q1 + o, attn_add(m[n][1], q));
         });
+        // off the triangle nothing is sent
+        for (int t = threadIdx.x; t < rows * wide_C; t += attn::THREADS) {
+            const int r = t / wide_C, k = t - r * wide_C;
+            if (k <= r0 + r) continue;
+            const size_t o = w_at + r * w_row + k;
+            a.p[o] = a.pm[0][o] = a.pm[1][o] = 0ull;
+            if (k < a.C) a.Ep[0][p_at + r * p_row + k] = a.Ep[1][p_at + r * p_row + k] = 0ull;
+        }
     }
-    attn_tile_end(s, turn, a.error);
+}
+
+// A tile of the sum of d v^T of a chunk and key head, [k_dim][v_dim], of one party after the other.
+template <bool VEC>
+__device__ __forceinline__ void attn_keys(const AttnArgs& a, uint8_t* smem, const AttnChunk& at, int c, int h, int k0, int v0) {
+    const uint32_t k_row = (uint32_t)a.kv_heads * a.k_dim, v_row = (uint32_t)a.kv_heads * a.v_dim;
+    const size_t k_at = (size_t)at.first * k_row + (size_t)h * a.k_dim + k0, v_at = (size_t)at.first * v_row + (size_t)h * a.v_dim + v0;
+    const size_t out = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim + (size_t)k0 * a.v_dim + v0;
+    const int rows = min(attn::ROWS, a.k_dim - k0), cols = min(attn::COLS, a.v_dim - v0), half = 2 * attn_blocks(at.len);
+    AttnSums sums;
+    sums.clear();
+    attn_steps(smem, 2 * half, [&](int n, uint32_t to) {
+        const int i = n >= half, k = (n - i * half) / 2 * attn::DEPTH;
+        const bool first = n % 2 == 0;                       // V_i F, then E B_i
+        const u64* const d = (first ? i ? a.d1 : a.md[0] : a.d) + k_at;
+        const u64* const v = (first ? a.v : i ? a.mv[1] : a.mv[0]) + v_at;
+        AttnSide<true, attn::ROWS>::copy<VEC>(to, d + (size_t)k * k_row, k_row, rows, at.len - k);
+        AttnSide<true, attn::COLS>::copy<VEC>(to + attn::LEFT_BYTES, v + (size_t)k * v_row, v_row, cols, at.len - k);
+    }, [&](int n, const uint8_t* step) {
+        attn_multiply<true, true>(step, sums);
+        if ((n + 1) % half) return;
+        const u64* const dv = (n < half ? a.dv[0] : a.dv[1]) + out;
+        u64* const kv = (n < half ? a.kv[0] : a.kv[1]) + out;
+        sums.each([&](int, int row, int col, ulonglong2 z) {
+            if (row >= rows || col >= cols) return;
+            const int o = row * a.v_dim + col;
+            attn_store2<VEC>(kv + o, attn_add(z, attn_load2<VEC>(dv + o)));
+        });
+        sums.clear();
+    });
+}
+// A tile of the weights of a chunk and query head: P of all rows and the keys from s0 on.
+template <bool VEC>
+__device__ __forceinline__ void attn_weights(const AttnArgs& a, uint8_t* smem, const AttnChunk& at, int hq, int s0) {
+    const int h = hq / (a.q_heads / a.kv_heads), rows = at.len, keys = min(attn::COLS, rows - s0), half = 2 * attn_blocks(a.k_dim);
+    const int wide_C = a.C + (a.C & 1);                      // of the opened weights' rows, which begin on 16-byte boundaries
+    const uint32_t q_row = (uint32_t)a.q_heads * a.k_dim, k_row = (uint32_t)a.kv_heads * a.k_dim, p_row = (uint32_t)a.q_heads * a.C;
+    const uint32_t w_row = (uint32_t)a.q_heads * wide_C;
+    const size_t q_at = (size_t)at.first * q_row + (size_t)hq * a.k_dim, k_at = (size_t)(at.first + s0) * k_row + (size_t)h * a.k_dim;
+    const size_t p_at = (size_t)at.first * p_row + (size_t)hq * a.C, w_at = (size_t)at.first * w_row + (size_t)hq * wide_C;
+    const u64* const w = a.decay + (size_t)h * (a.C + 1);
+    const bool pairs = VEC && a.C % 2 == 0;
+    ulonglong2* const kept = reinterpret_cast<ulonglong2*>(smem + attn::STEPS * attn::STEP_BYTES) + threadIdx.x;
+    const int warp = threadIdx.x >> 5;
+    // off the triangle, or behind the rows: nothing to work out
+    const bool idle = s0 + (warp & 1) * attn::WARP > (warp >> 1) * attn::WARP + attn::WARP - 1 || (warp >> 1) * attn::WARP >= rows;
+    AttnSums sums;
+    sums.clear();
+    attn_steps(smem, 2 * half, [&](int n, uint32_t to) {
+        const int i = n >= half, k = (n - i * half) / 2 * attn::DEPTH;
+        const bool first = n % 2 == 0;
+        const u64* const q = (first ? i ? a.q1 : a.mq[0] : a.q) + q_at + k;
+        const u64* const x = (first ? a.k : i ? a.mk[1] : a.mk[0]) + k_at + k;
+        AttnSide<false, attn::ROWS>::copy<VEC>(to, q, q_row, rows, a.k_dim - k);
+        AttnSide<false, attn::COLS>::copy<VEC>(to + attn::LEFT_BYTES, x, k_row, keys, a.k_dim - k);
+    }, [&](int n, const uint8_t* step) {
+        if (idle) return;
+        attn_multiply<false, false>(step, sums);
+        if ((n + 1) % half) return;
+        const bool second = n >= half;
+        const u64* const qk = (second ? a.qk[1] : a.qk[0]) + p_at;
+        const u64* const mp = (second ? a.mp[1] : a.mp[0]) + p_at;
+        u64* const Ep = (second ? a.Ep[1] : a.Ep[0]) + p_at;
+        u64* const pm = (second ? a.pm[1] : a.pm[0]) + w_at;
+        // (the second word of a pair may lie off the triangle, where everything is zero, and behind an odd row's end)
+        sums.each([&](int e, int r, int col, ulonglong2 z) {
+            const int key = s0 + col;
+            if (key > r || r >= rows) return;
+            const bool both = key < r;
+            const uint32_t o = r * p_row + key, to = r * w_row + key;
+            auto load = [&](const u64* x) { return pairs ? attn_load2<true>(x + o) : make_ulonglong2(__ldcs(x + o), both ? __ldcs(x + o + 1) : 0ull); };
+            const ulonglong2 x = load(qk);
+            ulonglong2 m = load(mp);
+            if (!both) m.y = 0ull;
+            const u64 one = attn_rescale(attn_rescale(z.x + x.x, second, a.f) * __ldg(w + r - key), second, a.f) - m.x;
+            u64 two = 0ull;
+            if (both) two = attn_rescale(attn_rescale(z.y + x.y, second, a.f) * __ldg(w + r - key - 1), second, a.f) - m.y;
+            if (pairs) attn_send2<true>(Ep + o, make_ulonglong2(one, two));
+            else {
+                Ep[o] = one;
+                if (both) Ep[o + 1] = two;
+            }
+            if (!second) {
+                kept[e * attn::THREADS] = make_ulonglong2(one, two);
+            } else {
+                const ulonglong2 open = attn_add(kept[e * attn::THREADS], make_ulonglong2(one, two));    // the exchange
+                *reinterpret_cast<ulonglong2*>(a.p + w_at + to) = open;
+                m = attn_add(m, open);
+            }
+            *reinterpret_cast<ulonglong2*>(pm + to) = m;
+        });
+        sums.clear();
+    });
+}
+template <bool VEC>
+__global__ void __launch_bounds__(attn::THREADS, 2)
+attn_products_kernel(const __grid_constant__ AttnArgs a, int keys_ctas, int k_tiles, int v_tiles, int s_tiles) {
+    extern __shared__ __align__(128) uint8_t attn_smem[];
+    pdl_wait();
+    pdl_launch_dependents();
+    if ((int)blockIdx.x < keys_ctas) {
+        const int tiles = k_tiles * v_tiles, ch = blockIdx.x / tiles, tile = blockIdx.x - ch * tiles, c = ch / a.kv_heads, kt = tile / v_tiles;
+        const AttnChunk at = attn_find(a, c);
+        if (at.len) attn_keys<VEC>(a, attn_smem, at, c, ch - c * a.kv_heads, kt * attn::ROWS, (tile - kt * v_tiles) * attn::COLS);
+    } else {
+        const int b = blockIdx.x - keys_ctas, ch = b / s_tiles, s0 = (b - ch * s_tiles) * attn::COLS, c = ch / a.q_heads;
+        const AttnChunk at = attn_find(a, c);
+        if (s0 < at.len) attn_weights<VEC>(a, attn_smem, at, ch - c * a.q_heads, s0);
+    }
 }
 
 // The state from chunk to chunk of a sequence and key head, two words of both parties a thread; says whether the starts were in order.
@@ -587,7 +519,7 @@ attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             kv[i] = attn_load2<VEC>(a.kv[i] + o);
-            ms[i] = attn_load2<VEC>(a.ms[i] + o);
+            ms[i] = attn_keep2<VEC>(a.ms[i] + o);
         }
     };
     if (c < end) load();
@@ -605,128 +537,76 @@ attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
         o += step;
         if (c + 1 < end) load();
 #pragma unroll
-        for (int i = 0; i < 2; ++i) attn_store2<VEC>(a.Es[i] + here, e[i]);
+        for (int i = 0; i < 2; ++i) attn_send2<VEC>(a.Es[i] + here, e[i]);
         attn_store2<VEC>(a.s + here, attn_add(e[0], e[1]));              // the exchange
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) attn_store2<VEC>(a.S1[i] + at, S[i]);
 }
 
-// Everything else of a chunk and query head.
+// A tile of the rows of O of a chunk, query head and party: the far part w[r + 1] tr(q S), then the near part P v.
 template <bool VEC>
-__global__ void __launch_bounds__(attn::TILE_THREADS, 1)
-attn_rows_kernel(const __grid_constant__ AttnArgs a) {
-    extern __shared__ uint8_t attn_smem[];
-    __shared__ AttnTile s;
+__global__ void __launch_bounds__(attn::THREADS, 2)
+attn_rows_kernel(const __grid_constant__ AttnArgs a, int v_tiles) {
+    extern __shared__ __align__(128) uint8_t attn_smem[];
     pdl_wait();
     pdl_launch_dependents();
-    const int c = blockIdx.x / a.q_heads, hq = blockIdx.x - c * a.q_heads, h = hq / (a.q_heads / a.kv_heads), warp = threadIdx.x >> 5;
+    const int tile = blockIdx.x / 2, ch = tile / v_tiles, c = ch / a.q_heads, hq = ch - c * a.q_heads, h = hq / (a.q_heads / a.kv_heads);
+    const int v0 = (tile - ch * v_tiles) * attn::COLS;
+    const bool second = blockIdx.x % 2;                      // party
     const AttnChunk at = attn_find(a, c);
     if (at.len == 0) return;
-    attn_tile_begin(s, attn_smem);
-    AttnTurn turn;
-    const int rows = at.len, first = at.first;
-    const size_t q_row = (size_t)a.q_heads * a.k_dim, p_row = (size_t)a.q_heads * a.C, o_row = (size_t)a.q_heads * a.v_dim;
-    const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
-    const size_t q_at = first * q_row + (size_t)hq * a.k_dim, p_at = first * p_row + (size_t)hq * a.C, o_at = first * o_row + (size_t)hq * a.v_dim;
-    const size_t k_at = at.first * k_row + (size_t)h * a.k_dim, v_at = at.first * v_row + (size_t)h * a.v_dim;
-    const size_t s_at = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim;
-    const int wide_C = a.C + (a.C & 1);                      // of the opened weights' rows, which begin on 16-byte boundaries
-    const uint32_t w_row = a.q_heads * wide_C;
-    const size_t w_at = (size_t)first * w_row + hq * wide_C;
-    const u64* const w = a.decay + (size_t)h * (a.C + 1);
-    if (warp != attn::ISSUER) {
-        ulonglong2 x[2][2], m[2][2];
-        attn_pairs(rows, a.k_dim, [&](int n, int r, int j) {
-            const size_t o = q_at + r * q_row + j, x_at = (size_t)(first + r) * a.q_stride + (size_t)hq * a.k_dim + j;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                x[n][i] = attn_input2(a.Q[i] + x_at, a.in_vec);
-                m[n][i] = attn_load2<VEC>(a.mq[i] + o);
-            }
-        }, [&](int n, int r, int j) {
-            const size_t o = q_at + r * q_row + j;
-            ulonglong2 e[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                e[i] = attn_sub(x[n][i], m[n][i]);
-                attn_store2<VEC>(a.Eq[i] + o, e[i]);
-            }
-            attn_store2<VEC>(a.q + o, attn_add(e[0], e[1]));         // the exchange
-        });
-        // off the triangle nothing is sent
-        for (int t = threadIdx.x; t < rows * wide_C; t += attn::WORKERS) {
-            const int r = t / wide_C, k = t - r * wide_C;
-            if (k <= r) continue;
-            const size_t o = w_at + (size_t)r * w_row + k;
-            a.p[o] = a.pm[0][o] = a.pm[1][o] = 0ull;
-            if (k < a.C) a.Ep[0][p_at + r * p_row + k] = a.Ep[1][p_at + r * p_row + k] = 0ull;
+    const int rows = at.len, cols = min(attn::COLS, a.v_dim - v0), far = 2 * attn_blocks(a.k_dim), near = 2 * attn_blocks(rows), wide_C = a.C + (a.C & 1);
+    const uint32_t q_row = (uint32_t)a.q_heads * a.k_dim, v_row = (uint32_t)a.kv_heads * a.v_dim, o_row = (uint32_t)a.q_heads * a.v_dim;
+    const uint32_t w_row = (uint32_t)a.q_heads * wide_C;
+    const size_t q_at = (size_t)at.first * q_row + (size_t)hq * a.k_dim, v_at = (size_t)at.first * v_row + (size_t)h * a.v_dim + v0;
+    const size_t s_at = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim + v0;
+    const size_t w_at = (size_t)at.first * w_row + (size_t)hq * wide_C, o_at = (size_t)at.first * o_row + (size_t)hq * a.v_dim + v0;
+    ulonglong2* const kept = reinterpret_cast<ulonglong2*>(attn_smem + attn::STEPS * attn::STEP_BYTES) + threadIdx.x;
+    const int warp_row = (threadIdx.x >> 6) * attn::WARP;
+    AttnSums sums;
+    sums.clear();
+    attn_steps(attn_smem, far + near, [&](int n, uint32_t to) {
+        const bool first = n % 2 == 0;
+        if (n < far) {
+            const int k = n / 2 * attn::DEPTH;
+            const u64* const q = (first ? second ? a.q1 : a.mq[0] : a.q) + q_at + k;
+            const u64* const S = (first ? a.s : second ? a.ms[1] : a.ms[0]) + s_at + (size_t)k * a.v_dim;
+            AttnSide<false, attn::ROWS>::copy<VEC>(to, q, q_row, rows, a.k_dim - k);
+            AttnSide<true, attn::COLS>::copy<VEC>(to + attn::LEFT_BYTES, S, a.v_dim, cols, a.k_dim - k);
+        } else {
+            const int k = (n - far) / 2 * attn::DEPTH;
+            const u64* const p = (first ? second ? a.pm[1] : a.pm[0] : a.p) + w_at + k;
+            const u64* const v = (first ? a.v : second ? a.mv[1] : a.mv[0]) + v_at + (size_t)k * v_row;
+            // (the opened weights' rows are longer than an odd number of keys by a word, zero)
+            AttnSide<false, attn::ROWS>::copy<VEC>(to, p, w_row, rows, rows - k);
+            AttnSide<true, attn::COLS>::copy<VEC>(to + attn::LEFT_BYTES, v, v_row, cols, rows - k);
         }
-        attn_meet();
-    }
-    if (warp == attn::ISSUER) {
-        attn_issue(s, turn, a.k_dim);
-        attn_issue(s, turn, a.k_dim);
-#pragma unroll 1
-        for (int t = 0; t < 2 * ((a.v_dim + attn::ROWS - 1) / attn::ROWS); ++t) {
-            attn_issue(s, turn, a.k_dim);
-            attn_issue(s, turn, rows);
-        }
-    } else if (warp < attn::CONVERTERS) {
-#pragma unroll 1
-        for (int i = 0; i < 2; ++i) {
-            const AttnOperand k = {a.mk[i] + k_at, a.k + k_at, (uint32_t)k_row}, q = {a.mq[i] + q_at, a.q + q_at, (uint32_t)q_row};
-            attn_convert<false, false, VEC>(s, turn, k, rows, q, rows, a.k_dim, i);
-        }
-        // far part and near part in turn
-        const int tiles = (a.v_dim + attn::ROWS - 1) / attn::ROWS;
-#pragma unroll 1
-        for (int n = 0; n < 4 * tiles; ++n) {
-            const bool near = n & 1;
-            const int i = n >= 2 * tiles, v0 = (n / 2 - i * tiles) * attn::ROWS;
-            if (n == 1) turn.ok = turn.ok && attn_wait_warp(s.weights, 0, s);
-            AttnOperand left, right;
-            left.mask = (near ? a.mv[i] + v_at : a.ms[i] + s_at) + v0;
-            left.open = (near ? a.v + v_at : a.s + s_at) + v0;
-            left.step = near ? (uint32_t)v_row : (uint32_t)a.v_dim;
-            right.mask = near ? a.pm[i] + w_at : a.mq[i] + q_at;
-            right.open = near ? a.p + w_at : a.q + q_at;
-            right.step = near ? w_row : (uint32_t)q_row;
-            attn_convert<true, false, VEC>(s, turn, left, min(attn::ROWS, a.v_dim - v0), right, rows, near ? rows : a.k_dim, i);
-        }
-    } else {
-#pragma unroll 1
-        for (int i = 0; i < 2; ++i) {
-            const u64 *const qk = a.qk[i] + p_at, *const mp = a.mp[i] + p_at;
-            u64 *const Ep = a.Ep[i] + p_at, *const p = a.p + w_at, *const pm = a.pm[i] + w_at;
-            attn_drain<2>(s, turn, rows, rows, [&](int k, int key, int r) { return key > r ? nullptr : (k ? mp : qk) + (r * p_row + key); },
-                          [&](int key, int r) { return i && key <= r ? p[r * w_row + key] : 0ull; }, [&](int key, int r, u64 z, const u64* words, u64 own) {
-                if (key > r) return;
-                const u64 e = attn_rescale(attn_rescale(z + words[0], i, a.f) * __ldg(w + r - key), i, a.f) - words[1];
-                Ep[r * p_row + key] = e;
-                pm[r * w_row + key] = words[1];
-                p[r * w_row + key] = own + e;                // the exchange
+    }, [&](int n, const uint8_t* step) {
+        if (warp_row >= rows) return;
+        // (a key behind all of a warp's rows has no weight)
+        if (n < far || (n - far) / 2 * attn::DEPTH < warp_row + attn::WARP) attn_multiply<false, true>(step, sums);
+        if (n == far - 1) {
+            const u64* const qs = (second ? a.qs[1] : a.qs[0]) + o_at;
+            const u64* const pv = (second ? a.pv[1] : a.pv[0]) + o_at;
+            const u64* const w = a.decay + (size_t)h * (a.C + 1) + 1;
+            sums.each([&](int e, int r, int col, ulonglong2 z) {
+                if (r >= rows || col >= cols) return;
+                const uint32_t o = r * o_row + col;
+                const ulonglong2 x = attn_load2<VEC>(qs + o), y = attn_load2<VEC>(pv + o);
+                const u64 weight = __ldg(w + r);
+                kept[e * attn::THREADS] = make_ulonglong2(y.x + weight * attn_rescale(z.x + x.x, second, a.f), y.y + weight * attn_rescale(z.y + x.y, second, a.f));
+            });
+            sums.clear();
+        } else if (n == far + near - 1) {
+            u64* const O = (second ? a.O[1] : a.O[0]) + o_at;
+            sums.each([&](int e, int r, int col, ulonglong2 z) {
+                if (r >= rows || col >= cols) return;
+                const ulonglong2 x = attn_add(z, kept[e * attn::THREADS]);
+                attn_send2<VEC>(O + (r * o_row + col), make_ulonglong2(attn_rescale(x.x, second, a.f), attn_rescale(x.y, second, a.f)));
             });
         }
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(ptx::smem_u32(&s.weights));
-#pragma unroll 1
-        for (int i = 0; i < 2; ++i)
-#pragma unroll 1
-            for (int v0 = 0; v0 < a.v_dim; v0 += attn::ROWS) {
-                // what the near part is added to waits in the result's place, where the same thread finds it again
-                const int wide = min(attn::ROWS, a.v_dim - v0);
-                u64* const O = a.O[i] + o_at + v0;
-                const u64 *const qs = a.qs[i] + o_at + v0, *const pv = a.pv[i] + o_at + v0;
-                attn_drain<2>(s, turn, wide, rows, [&](int k, int row, int r) { return (k ? pv : qs) + (r * o_row + row); }, attn_nothing,
-                              [&](int row, int r, u64 z, const u64* words, u64) {
-                    O[r * o_row + row] = words[1] + __ldg(w + r + 1) * attn_rescale(z + words[0], i, a.f);
-                });
-                attn_drain<0>(s, turn, wide, rows, [&](int, int, int) { return (const u64*)nullptr; }, [&](int row, int r) { return O[r * o_row + row]; },
-                              [&](int row, int r, u64 z, const u64*, u64 own) { O[r * o_row + row] = attn_rescale(own + z, i, a.f); });
-            }
-    }
-    attn_tile_end(s, turn, a.error);
+    });
 }
 
 // ---------------------------------------------------------------------------
