@@ -2503,14 +2503,24 @@ bool attn_heads(int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim)
            v_dim % 2 == 0 && k_dim <= at::MAX_DIM && v_dim <= at::MAX_DIM;
 }
 bool attn_stride(int64_t stride, int64_t tokens, int64_t row) { return stride >= 0 && stride <= 1ll << 32 && (tokens == 1 || stride >= row); }
-// The workspace in words: the products d v^T of both parties; the opened states, queries, keys, decayed keys and values, all of them
-// even, V_1 of queries and decayed keys; the opened weights, their masks and V_1.
+// The workspace in bytes: the products d v^T of both parties, three sets of planes of queries, keys, decayed keys, values, states and weights each,
+// the chunks.
 struct AttnRoom {
-    int64_t kv, q, k, v, p;
-    AttnRoom(int64_t tokens, int64_t chunks, int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim, int64_t chunk)
-        : kv(chunks * kv_heads * k_dim * v_dim), q(tokens * q_heads * k_dim), k(tokens * kv_heads * k_dim), v(tokens * kv_heads * v_dim),
-          p(tokens * q_heads * (chunk + chunk % 2)) {}
-    size_t bytes() const { return kv ? (size_t)(3 * kv + 2 * q + 3 * k + v + 3 * p) * sizeof(u64) : 0; }
+    int64_t kv, q, k, d, v, s, p, found;
+    AttnRoom(int64_t chunks, int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim, int64_t chunk) {
+        namespace at = comet::attn;
+        const int64_t rows = at::up16((int)chunk), ks = at::up16((int)k_dim), vs = at::up16((int)v_dim), t = at::blocks((int)chunk), kb = at::blocks((int)k_dim);
+        kv = chunks * kv_heads * k_dim * v_dim * (int64_t)sizeof(u64);
+        q = chunks * q_heads * kb * rows * at::ROW_BYTES;
+        k = chunks * kv_heads * kb * rows * at::ROW_BYTES;
+        d = chunks * kv_heads * t * ks * at::ROW_BYTES;
+        v = chunks * kv_heads * t * vs * at::ROW_BYTES;
+        s = chunks * kv_heads * kb * vs * at::ROW_BYTES;
+        p = chunks * q_heads * t * rows * at::ROW_BYTES;
+        found = chunks * (int64_t)sizeof(int2);
+        kv = (kv + 255) / 256 * 256;
+    }
+    size_t bytes() const { return (size_t)(2 * kv + 3 * (q + k + d + v + s + p) + found); }
 };
 
 bool attn_sizes(int64_t tokens, int64_t chunks, int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim, int64_t chunk) {
@@ -2551,7 +2561,7 @@ extern "C" int comet_linear_attention_workspace(int32_t tokens, int32_t chunks, 
                                                 int32_t chunk, int64_t* bytes_out) {
     if (!bytes_out) return COMET_ERR_INVALID_ARG;
     if (!attn_sizes(tokens, chunks, q_heads, kv_heads, k_dim, v_dim, chunk)) return COMET_ERR_SHAPE;
-    *bytes_out = (int64_t)AttnRoom(tokens, chunks, q_heads, kv_heads, k_dim, v_dim, chunk).bytes();
+    *bytes_out = (int64_t)AttnRoom(chunks, q_heads, kv_heads, k_dim, v_dim, chunk).bytes();
     return COMET_OK;
 }
 
@@ -2584,7 +2594,7 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
     const bool in_place = g->state[0] && g->state[0] == g->state_out[0] && g->state[1] == g->state_out[1];
     if (pair_halved(g->state) || (!in_place && !span_pairs({{g->state, st, true}}, spans))) return COMET_ERR_INVALID_ARG;
     if (outputs_overlap(spans.data(), outputs, (int)spans.size())) return COMET_ERR_INVALID_ARG;
-    const AttnRoom room(T, n, Hq, Hk, Dk, Dv, g->chunk);
+    const AttnRoom room(n, Hq, Hk, Dk, Dv, g->chunk);
     const size_t need = room.bytes();
     if (need && !g->workspace) return COMET_ERR_INVALID_ARG;
     if (g->workspace_bytes < (int64_t)need) return COMET_ERR_SHAPE;
@@ -2595,14 +2605,18 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
     give(a.qk, g->qk); give(a.pv, g->pv); give(a.qs, g->qs); give(a.dv, g->dv); give(a.S0, g->state);
     give(a.Eq, g->Eq); give(a.Ek, g->Ek); give(a.Ev, g->Ev); give(a.Ed, g->Ed); give(a.Ep, g->Ep); give(a.Es, g->Es); give(a.O, g->O);
     give(a.S1, g->state_out);
-    u64* piece = static_cast<u64*>(g->workspace);
-    auto take = [&](int64_t words) {
-        u64* const p = piece;
-        piece += words;
+    uint8_t* piece = static_cast<uint8_t*>(g->workspace);
+    auto take = [&](int64_t bytes) {
+        uint8_t* const p = piece;
+        piece += bytes;
         return p;
     };
-    a.kv[0] = take(room.kv); a.kv[1] = take(room.kv); a.s = take(room.kv); a.q = take(room.q); a.k = take(room.k); a.d = take(room.k);
-    a.v = take(room.v); a.q1 = take(room.q); a.d1 = take(room.k); a.p = take(room.p); a.pm[0] = take(room.p); a.pm[1] = take(room.p);
+    for (u64*& kv : a.kv) kv = reinterpret_cast<u64*>(take(room.kv));
+    auto planes = [&](comet::AttnPlanes& to, int64_t bytes) {
+        for (uint8_t*& set : to.set) set = take(bytes);
+    };
+    planes(a.q, room.q); planes(a.k, room.k); planes(a.d, room.d); planes(a.v, room.v); planes(a.s, room.s); planes(a.p, room.p);
+    a.found = reinterpret_cast<int2*>(take(room.found));
     a.decay = reinterpret_cast<const u64*>(g->decay);
     a.starts = g->starts;
     a.bad_starts = g->bad_starts_flag;
@@ -2624,21 +2638,21 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
         for (const u64* p : {a.mq[i], a.mk[i], a.mv[i], a.md[i], a.mp[i], a.ms[i], a.S0[i], (const u64*)a.Eq[i], (const u64*)a.Ek[i], (const u64*)a.Ev[i],
                              (const u64*)a.Ed[i], (const u64*)a.Ep[i], (const u64*)a.Es[i], (const u64*)a.S1[i], (const u64*)a.O[i], a.qk[i], a.pv[i], a.qs[i], a.dv[i]})
             vec = vec && aligned16(p);
-    const int pieces = ceil_div(a.k_dim * a.v_dim, 2 * at::THREADS);
+    // the states' threads: 8 of every block of 32 rows, 8 of 16 columns
+    const int pieces = ceil_div(8 * at::blocks(a.k_dim) * at::up16(a.v_dim) / 2, at::STATE_THREADS), slabs = 2 * at::blocks(a.C);
+    auto grid = [&](int64_t items) { return dim3((unsigned)(items < dev.sm_count ? items : dev.sm_count)); };
     cudaError_t err = cudaSuccess;
-    const int slabs = ceil_div(a.C, at::SLAB), k_tiles = ceil_div(a.k_dim, at::ROWS), v_tiles = ceil_div(a.v_dim, at::COLS), s_tiles = ceil_div(a.C, at::COLS);
-    const int keys_ctas = (int)(n * Hk) * k_tiles * v_tiles;
     if (n) err = launch_chained(vec ? comet::attn_open_kernel<true> : comet::attn_open_kernel<false>, dim3((unsigned)(n * slabs), (unsigned)(Hk + Hq)),
                                 dim3(at::THREADS), 0, stream, nullptr, a, slabs);
     if (err == cudaSuccess && n)
-        err = launch_chained(vec ? comet::attn_products_kernel<true> : comet::attn_products_kernel<false>, dim3((unsigned)(keys_ctas + n * Hq * s_tiles)),
-                             dim3(at::THREADS), at::TILE_SMEM, stream, nullptr, a, keys_ctas, k_tiles, v_tiles, s_tiles);
+        err = launch_chained(vec ? comet::attn_products_kernel<true> : comet::attn_products_kernel<false>, grid(n * (Hk + Hq)), dim3(at::TILE_THREADS),
+                             at::TILE_SMEM, stream, nullptr, a);
     if (err == cudaSuccess)
         err = launch_chained(vec ? comet::attn_state_kernel<true> : comet::attn_state_kernel<false>, dim3((unsigned)(g->sequences * Hk * pieces)),
-                             dim3(at::THREADS), 0, stream, nullptr, a, pieces);
+                             dim3(at::STATE_THREADS), 0, stream, nullptr, a, pieces);
     if (err == cudaSuccess && n)
-        err = launch_chained(vec ? comet::attn_rows_kernel<true> : comet::attn_rows_kernel<false>, dim3((unsigned)(n * Hq * v_tiles * 2)), dim3(at::THREADS),
-                             at::TILE_SMEM, stream, nullptr, a, v_tiles);
+        err = launch_chained(vec ? comet::attn_rows_kernel<true> : comet::attn_rows_kernel<false>, grid(2 * n * Hq), dim3(at::TILE_THREADS), at::TILE_SMEM,
+                             stream, nullptr, a);
     if (err != cudaSuccess) cudaGetLastError();
     return err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
 }

@@ -6,7 +6,8 @@
 //     d_s = tr(w[L - 1 - s] k_s);                     S <- tr(w[L] S + sum_s d_s v_s^T)
 //   single tokens:  S <- tr(w S + k v^T),  o = tr(q S)
 // Four kernels for a prompt: all values that need no product are opened (open); the products d v^T of all chunks and key heads and the weights P
-// of all chunks and query heads (products); the states from chunk to chunk, a word a thread (state); the rows of O (rows).
+// of all chunks and query heads (products); the states from chunk to chunk, a word a thread (state); the rows of O (rows).  What enters a product is
+// cut into bytes by the kernel that has it in registers anyway, once, so that those of the products only copy, multiply and add.
 #pragma once
 #include <cstdint>
 #include <type_traits>
@@ -21,15 +22,24 @@ namespace comet {
 namespace attn {
 constexpr int MAX_CHUNK = 64, MAX_DIM = 256;
 constexpr int THREADS = 256;
-constexpr int ROWS = 64, COLS = 32, DEPTH = 32;      // of a tile of a product; contraction indices of a step
-constexpr int WARP = 16;                             // rows and columns of a warp's part
-constexpr int LEFT_BYTES = ROWS * DEPTH * 8, STEP_BYTES = LEFT_BYTES + COLS * DEPTH * 8;
-constexpr int STEPS = 4;                             // in shared memory
-constexpr int KEPT = 8;                              // words that a thread keeps from one product to the next
-constexpr int TILE_SMEM = STEPS * STEP_BYTES + KEPT * THREADS * 8;
-constexpr int SLAB = 16;                             // rows of a chunk that a CTA opens
+constexpr int LEFT = 128, RIGHT = 64;                // rows of a tile's operands at most
+constexpr int KC = limb::KC, ROW_BYTES = limb::PLANES * KC;          // of a block of planes: 32 contraction indices
+constexpr int SLOTS = 3, LEFT_BYTES = LEFT * ROW_BYTES, SLOT_BYTES = LEFT_BYTES + RIGHT * ROW_BYTES;
+constexpr int DRAINERS = 8, PRODUCER = DRAINERS, ISSUER = DRAINERS + 1, TILE_THREADS = 32 * (ISSUER + 1), DRAIN_THREADS = 32 * DRAINERS;
+constexpr int ACC_COLS = limb::PLANES * RIGHT;
+constexpr int TILE_SMEM = SLOTS * SLOT_BYTES + RIGHT * LEFT * 8 + 128;
+constexpr int SLAB = 16;                             // tokens that a CTA opens
+constexpr int STATE_THREADS = 128;
+__host__ __device__ constexpr int up16(int n) { return (n + 15) / 16 * 16; }
+__host__ __device__ constexpr int blocks(int n) { return (n + KC - 1) / KC; }
 }  // namespace attn
 
+// Blocks of limb planes (kernels_limb.cuh) of an operand: the opened value, party 0's and party 1's mask, or for the operand of a product that takes
+// it V_i = mask + i * opened (Eq. 1).  A block has 32 contraction indices of up to 128 rows (left operands: values and states; keys have up to
+// 64) or 64 (right ones), rounded up to 16, so that a block's planes lie side by side whatever its rows are.  Contraction indices are in their order.
+struct AttnPlanes {
+    uint8_t* set[3];
+};
 struct AttnArgs {
     const u64* Q[2]; const u64* K[2]; const u64* V[2];                   // token t at t * stride, heads behind one another
     const u64* mq[2]; const u64* mk[2]; const u64* mv[2]; const u64* md[2]; const u64* mp[2]; const u64* ms[2];
@@ -39,9 +49,8 @@ struct AttnArgs {
     u64* O[2];
     u64* S1[2];
     u64* kv[2];                                                          // [chunks][kv_heads][k_dim][v_dim]: sum d v^T at scale 2f
-    u64* q; u64* k; u64* v; u64* d; u64* s;                              // opened values, as their messages lie
-    u64* q1; u64* d1;                                                    // V_1 of Eq. 1: party 1's mask and the opened value
-    u64* p; u64* pm[2];                                                  // opened weights, party 0's mask, V_1; zero off the triangle
+    AttnPlanes q, k, d, v, s, p;
+    int2* found;                                                         // [chunks]: first token, tokens
     const u64* decay;                                                    // [kv_heads][C + 1]
     const int32_t* starts;
     int32_t* bad_starts;
@@ -129,481 +138,570 @@ __device__ __forceinline__ ulonglong2 attn_sub(ulonglong2 x, ulonglong2 y) { ret
 __device__ __forceinline__ ulonglong2 attn_add(ulonglong2 x, ulonglong2 y) { return make_ulonglong2(x.x + y.x, x.y + y.y); }
 __device__ __forceinline__ u64 attn_rescale(u64 v, int party, int f) { return party ? 0ull - norm_shift(0ull - v, f) : norm_shift(v, f); }
 
-// ---------------------------------------------------------------------------
-// Products.  A CTA works out tiles of ROWS x COLS words of Z_i = (triple) + E B_i + V_i F, V_i = A_i + i E (Eq. 1), on the int8 tensor cores: a word is
-// eight bytes, x = sum_p x_p 2^(8p), and of the 64 products of bytes the 36 with p + q <= 7 matter mod 2^64, summed up by p + q in eight 32-bit
-// accumulators (kernels_limb.cuh has why 32 bits are enough).
-//
-// The words come to shared memory by asynchronous copies, STEPS steps of 32 indices of one product ahead; a warp cuts the words of its 16 rows and 16
-// columns into bytes in registers, 72 instructions of 16 x 8 x 32 a step.  Which byte of an operand's registers is which contraction index does not
-// matter as long as both operands agree: lane t of four has the indices 8j + 2t, 8j + 2t + 1, j < 4, words that lie side by side.
-// ---------------------------------------------------------------------------
-template <bool VEC>
-__device__ __forceinline__ void attn_copy2(uint32_t to, const u64* from, int words) {        // those behind the words are zero
-    if (VEC) {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(8 * words) : "memory");
-    } else {
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(from), "r"(words > 0 ? 8 : 0) : "memory");
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to + 8), "l"(words > 1 ? from + 1 : from), "r"(words > 1 ? 8 : 0) : "memory");
-    }
+// Where blocks lie, in bytes from a set's begin.  q, k, p: rows are tokens, room for up16(C) of them; d, v, s: rows are k_dim in tiles of 64, or v_dim
+// in tiles of 128.
+__device__ __forceinline__ size_t attn_token_block(int ch, int blocks, int b, int C) { return ((size_t)ch * blocks + b) * attn::up16(C) * attn::ROW_BYTES; }
+__device__ __forceinline__ size_t attn_dim_block(int ch, int blocks, int b, int dim, int row0, int tile) {
+    const int wide = attn::up16(dim);
+    return ((size_t)ch * blocks * wide + (size_t)row0 * blocks + (size_t)b * min(tile, wide - row0)) * attn::ROW_BYTES;
+}
+// Four words of a row, indices 4 quad and on, into a block of `rows` rows.
+__device__ __forceinline__ void attn_emit(uint8_t* block, int rows, int row, int quad, const u64 (&w)[4]) {
+    limb_emit4(block + (row >> 3) * 256 + (quad >> 2) * 128 + (row & 7) * 16 + (quad & 3) * 4, rows * attn::KC, w);
+}
+__device__ __forceinline__ void attn_emit(uint8_t* block, int rows, int row, int quad, u64 w0, u64 w1, u64 w2, u64 w3) {
+    const u64 w[4] = {w0, w1, w2, w3};
+    attn_emit(block, rows, row, quad, w);
 }
 
-// An operand's part of a step, N rows or columns.  Its words lie `step` words from row to row; of a DEEP operand, whose rows lie side by side, from
-// index to index.  In shared memory pieces change places so that the reads below meet no bank twice: of a row, whose 256 bytes eight lanes read in
-// turns of 64, those halves of 128 bytes that its number says; of an index of a deep operand, of which sixteen lanes read four words of four
-// indices, the pieces of 32 bytes.
-template <bool DEEP, int N>
-struct AttnSide {
-    static_assert(N % 16 == 0, "whole passes");
-    __device__ __forceinline__ static uint32_t place(int row, int piece) {           // of a pair of words
-        return DEEP ? row * (N * 8) + (((piece >> 1) ^ ((row >> 1) & 3)) << 5) + ((piece & 1) << 4)
-                    : row * 256 + (((piece >> 2) ^ (row & 1)) << 6) + ((piece & 3) << 4);
-    }
-    // `size` of the N rows are the operand's, `depth` of the 32 indices
-    template <bool VEC>
-    __device__ __forceinline__ static void copy(uint32_t to, const u64* x, uint32_t step, int size, int depth) {
-        constexpr int PIECES = DEEP ? N / 2 : 16, LINES = DEEP ? attn::DEPTH : N, PASS = attn::THREADS / PIECES;
-        const int piece = threadIdx.x % PIECES, first = threadIdx.x / PIECES;
-        const int lines = DEEP ? depth : size, words = max(0, min(2, (DEEP ? size : depth) - 2 * piece));
-#pragma unroll
-        for (int l = first; l < LINES; l += PASS) {
-            const int n = l < lines ? words : 0;
-            attn_copy2<VEC>(to + place(l, piece), n ? x + (l * step + 2 * piece) : x, n);
-        }
-    }
-    // The eight words of row `row` of lane t of four, cut into bytes: planes[p][h] byte p of the words 4h .. 4h + 3.
-    __device__ __forceinline__ static void bytes(const uint8_t* from, int row, int t, uint32_t (&planes)[limb::PLANES][2]) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            u64 w[4];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (DEEP) {
-                    const uint8_t* const at = from + (16 * h + 8 * j + 2 * t) * (N * 8) + (((row >> 2) ^ t) << 5) + ((row & 3) << 3);
-                    w[2 * j] = *reinterpret_cast<const u64*>(at);
-                    w[2 * j + 1] = *reinterpret_cast<const u64*>(at + N * 8);
-                } else {
-                    const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(from + row * 256 + (((2 * h + j) ^ (row & 1)) << 6) + (t << 4));
-                    w[2 * j] = v.x;
-                    w[2 * j + 1] = v.y;
-                }
-            }
-            limb_transpose4((uint32_t)w[0], (uint32_t)w[1], (uint32_t)w[2], (uint32_t)w[3], planes[0][h], planes[1][h], planes[2][h], planes[3][h]);
-            limb_transpose4((uint32_t)(w[0] >> 32), (uint32_t)(w[1] >> 32), (uint32_t)(w[2] >> 32), (uint32_t)(w[3] >> 32), planes[4][h], planes[5][h],
-                            planes[6][h], planes[7][h]);
-        }
-    }
-};
-
-// A warp's sums: [half of the columns][p + q][register of the instruction].
-struct AttnSums {
-    uint32_t d[2][limb::PLANES][4];
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int p = 0; p < limb::PLANES; ++p)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) d[n][p][j] = 0u;
-    }
-    // Pairs of words of a row: f(which of the thread's four pairs, row, column, pair)
-    template <typename F>
-    __device__ __forceinline__ void each(F&& f) const {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = (warp >> 1) * attn::WARP + (lane >> 2), col = (warp & 1) * attn::WARP + 2 * (lane & 3);
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                u64 z[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int e = 2 * h + j;
-                    z[j] = limb_recombine(d[n][0][e], d[n][1][e], d[n][2][e], d[n][3][e], d[n][4][e], d[n][5][e], d[n][6][e], d[n][7][e]);
-                }
-                f(2 * n + h, row + 8 * h, col + 8 * n, make_ulonglong2(z[0], z[1]));
-            }
-    }
-};
-__device__ __forceinline__ void attn_mma(uint32_t (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.u8.u8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-template <bool DEEP_LEFT, bool DEEP_RIGHT>
-__device__ __forceinline__ void attn_multiply(const uint8_t* step, AttnSums& sums) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, row = (warp >> 1) * attn::WARP + g, col = (warp & 1) * attn::WARP + g;
-    uint32_t a[2][limb::PLANES][2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) AttnSide<DEEP_LEFT, attn::ROWS>::bytes(step, row + 8 * h, t, a[h]);
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-        uint32_t b[limb::PLANES][2];
-        AttnSide<DEEP_RIGHT, attn::COLS>::bytes(step + attn::LEFT_BYTES, col + 8 * n, t, b);
-#pragma unroll
-        for (int p = 0; p < limb::PLANES; ++p)
-#pragma unroll
-            for (int q = 0; p + q < limb::PLANES; ++q) attn_mma(sums.d[n][p + q], a[0][p][0], a[1][p][0], a[0][p][1], a[1][p][1], b[q][0], b[q][1]);
-    }
-}
-// Steps 0 .. steps - 1 of a CTA: copy(step, where) asks for a step's words, work(step, where) uses them.
-template <typename C, typename W>
-__device__ __forceinline__ void attn_steps(uint8_t* smem, int steps, C&& copy, W&& work) {
-    const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem);
-#pragma unroll
-    for (int n = 0; n < attn::STEPS - 1; ++n) {
-        if (n < steps) copy(n, base + n * attn::STEP_BYTES);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-#pragma unroll 1
-    for (int n = 0; n < steps; ++n) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(attn::STEPS - 2) : "memory");
-        __syncthreads();                                     // the step is there, and the one before has been used by all
-        const int ahead = n + attn::STEPS - 1;
-        if (ahead < steps) copy(ahead, base + ahead % attn::STEPS * attn::STEP_BYTES);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        work(n, smem + n % attn::STEPS * attn::STEP_BYTES);
-    }
-}
-__device__ __forceinline__ int attn_blocks(int depth) { return (depth + attn::DEPTH - 1) / attn::DEPTH; }
-
-// The pairs of words of `rows` rows of `cols`, two at a time a thread: load(n, row, column) for both, then finish(n, row, column).
-template <typename L, typename F>
-__device__ __forceinline__ void attn_pairs(int rows, int cols, L&& load, F&& finish) {
-    const int half = cols / 2, all = rows * half;
-    for (int t = threadIdx.x; t < all; t += 2 * attn::THREADS) {
-        int r[2], j[2];
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int u = t + n * attn::THREADS;
-            r[n] = u < all ? u / half : -1;
-            j[n] = 2 * (u - r[n] * half);
-            if (r[n] >= 0) load(n, r[n], j[n]);
-        }
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-            if (r[n] >= 0) finish(n, r[n], j[n]);
-    }
-}
-
-// Messages of q, or of k, v and d, of a head and SLAB rows of a chunk, and the opened values; zeros where no weight is sent.  Bound by memory.
+// Messages of q, or of k, v and d, of a head and SLAB tokens of a chunk, and the planes of what they open; zeros where no weight is sent.  Bound by
+// memory: 4 words in and 5 out of every word of q and k, 8 and 10 of d, v.  q and k: eight lanes a row's 32 words, four words each.  v and
+// d, whose contraction runs over the tokens: four tokens x two words a thread, sixteen tokens x sixteen words a warp.
 template <bool VEC>
 __global__ void __launch_bounds__(attn::THREADS, 2)
 attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
     pdl_wait();
     pdl_launch_dependents();
-    const int c = blockIdx.x / slabs, r0 = (blockIdx.x - c * slabs) * attn::SLAB;
+    const int c = blockIdx.x / slabs, t0 = (blockIdx.x - c * slabs) * attn::SLAB;
     const AttnChunk at = attn_find(a, c);
-    const int rows = min(attn::SLAB, at.len - r0), first = at.first + r0;
-    if (rows <= 0) return;
+    if (blockIdx.x == c * slabs && blockIdx.y == 0 && threadIdx.x == 0) a.found[c] = make_int2(at.first, at.len);
+    const int blocks = attn::blocks(a.C), rows16 = attn::up16(at.len), rows = min(attn::SLAB, at.len - t0), first = at.first + t0;
+    if (t0 >= attn::blocks(at.len) * attn::KC) return;
+    const int f = a.f;
+    // rows of queries or keys: messages, and the planes of the opened value, party 0's mask, party 1's or V_1
+    auto open_rows = [&](const u64* const x[2], long long stride, const u64* const m[2], u64* const msg[2], const AttnPlanes& to, int heads, int head, bool sum) {
+        const int quads = attn::blocks(a.k_dim) * 8;
+        const size_t o0 = ((size_t)first * heads + head) * a.k_dim;
+        for (int t = threadIdx.x; t < rows * quads; t += attn::THREADS) {
+            const int r = t / quads, quad = t - r * quads;
+            const size_t o = o0 + (size_t)r * heads * a.k_dim + 4 * quad;
+            const long long from = (long long)(first + r) * stride + (long long)head * a.k_dim + 4 * quad;
+            ulonglong2 e[2][2], mask[2][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    e[i][h] = mask[i][h] = make_ulonglong2(0ull, 0ull);
+                    if (4 * quad + 2 * h < a.k_dim) {
+                        e[i][h] = attn_input2(x[i] + from + 2 * h, a.in_vec);
+                        mask[i][h] = attn_load2<VEC>(m[i] + o + 2 * h);
+                    }
+                }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    e[i][h] = attn_sub(e[i][h], mask[i][h]);
+                    if (4 * quad + 2 * h < a.k_dim) attn_send2<VEC>(msg[i] + o + 2 * h, e[i][h]);
+                }
+            const ulonglong2 y0 = attn_add(e[0][0], e[1][0]), y1 = attn_add(e[0][1], e[1][1]);             // the exchange
+            if (sum) {
+                mask[1][0] = attn_add(mask[1][0], y0);
+                mask[1][1] = attn_add(mask[1][1], y1);
+            }
+            const size_t block = attn_token_block(c * heads + head, quads / 8, quad / 8, a.C);
+            attn_emit(to.set[0] + block, rows16, t0 + r, quad & 7, y0.x, y0.y, y1.x, y1.y);
+            attn_emit(to.set[1] + block, rows16, t0 + r, quad & 7, mask[0][0].x, mask[0][0].y, mask[0][1].x, mask[0][1].y);
+            attn_emit(to.set[2] + block, rows16, t0 + r, quad & 7, mask[1][0].x, mask[1][0].y, mask[1][1].x, mask[1][1].y);
+        }
+    };
+    // values or decayed keys, `dim` words a token in tiles of `tile`; tokens behind the last count as zero
+    auto open_dims = [&](const u64* const x[2], long long stride, const u64* const m[2], u64* const msg[2], const AttnPlanes& to, int dim, int tile,
+                         int head, const u64* w, bool sum) {
+        const int half = attn::up16(dim) / 2;
+        const size_t o0 = ((size_t)first * a.kv_heads + head) * dim, row = (size_t)a.kv_heads * dim;
+        for (int t = threadIdx.x; t < 4 * half; t += attn::THREADS) {
+            const int quad = (t >> 3) & 3, j = 2 * ((t & 7) + (t >> 5) * 8);
+            ulonglong2 e[2][4], mask[2][4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int r = 4 * quad + k;
+                    e[i][k] = mask[i][k] = make_ulonglong2(0ull, 0ull);
+                    if (r < rows && j < dim) {
+                        e[i][k] = attn_input2(x[i] + (long long)(first + r) * stride + (long long)head * dim + j, a.in_vec);
+                        mask[i][k] = attn_load2<VEC>(m[i] + o0 + r * row + j);
+                    }
+                }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = 4 * quad + k;
+                const bool live = r < rows && j < dim;
+                const u64 weight = w && r < rows ? __ldg(w - r) : 1ull;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (w) e[i][k] = make_ulonglong2(attn_rescale(e[i][k].x * weight, i, f), attn_rescale(e[i][k].y * weight, i, f));
+                    e[i][k] = attn_sub(e[i][k], mask[i][k]);
+                    if (live) attn_send2<VEC>(msg[i] + o0 + r * row + j, e[i][k]);
+                }
+                e[0][k] = attn_add(e[0][k], e[1][k]);                                                      // the exchange
+                if (sum) mask[1][k] = attn_add(mask[1][k], e[0][k]);
+            }
+            const int row0 = j / tile * tile, wide = min(tile, attn::up16(dim) - row0), token = t0 / 4 + quad;
+            const size_t block = attn_dim_block(c * a.kv_heads + head, blocks, token / 8, dim, row0, tile);
+            auto emit = [&](int n, const ulonglong2 (&v)[4]) {
+                attn_emit(to.set[n] + block, wide, j - row0, token & 7, v[0].x, v[1].x, v[2].x, v[3].x);
+                attn_emit(to.set[n] + block, wide, j - row0 + 1, token & 7, v[0].y, v[1].y, v[2].y, v[3].y);
+            };
+            emit(0, e[0]);
+            emit(1, mask[0]);
+            emit(2, mask[1]);
+        }
+    };
     if ((int)blockIdx.y < a.kv_heads) {
         const int h = blockIdx.y;
-        const size_t k_row = (size_t)a.kv_heads * a.k_dim, v_row = (size_t)a.kv_heads * a.v_dim;
-        const size_t k_at = first * k_row + (size_t)h * a.k_dim, v_at = first * v_row + (size_t)h * a.v_dim;
-        const u64* const w = a.decay + (size_t)h * (a.C + 1) + at.len - 1 - r0;
-        ulonglong2 x[2][2], mk[2][2], md[2][2];
-        attn_pairs(rows, a.k_dim, [&](int n, int r, int j) {
-            const size_t o = k_at + r * k_row + j, x_at = (size_t)(first + r) * a.k_stride + (size_t)h * a.k_dim + j;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                x[n][i] = attn_input2(a.K[i] + x_at, a.in_vec);
-                mk[n][i] = attn_load2<VEC>(a.mk[i] + o);
-                md[n][i] = attn_load2<VEC>(a.md[i] + o);
-            }
-        }, [&](int n, int r, int j) {
-            const size_t o = k_at + r * k_row + j;
-            const u64 weight = __ldg(w - r);
-            ulonglong2 e[2], g[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                e[i] = attn_sub(x[n][i], mk[n][i]);
-                g[i] = attn_sub(make_ulonglong2(attn_rescale(x[n][i].x * weight, i, a.f), attn_rescale(x[n][i].y * weight, i, a.f)), md[n][i]);
-                attn_send2<VEC>(a.Ek[i] + o, e[i]);
-                attn_send2<VEC>(a.Ed[i] + o, g[i]);
-            }
-            const ulonglong2 d = attn_add(g[0], g[1]);               // the exchange
-            attn_store2<VEC>(a.k + o, attn_add(e[0], e[1]));
-            attn_store2<VEC>(a.d + o, d);
-            attn_store2<VEC>(a.d1 + o, attn_add(md[n][1], d));
-        });
-        attn_pairs(rows, a.v_dim, [&](int n, int r, int j) {
-            const size_t o = v_at + r * v_row + j, x_at = (size_t)(first + r) * a.v_stride + (size_t)h * a.v_dim + j;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                x[n][i] = attn_input2(a.V[i] + x_at, a.in_vec);
-                mk[n][i] = attn_load2<VEC>(a.mv[i] + o);
-            }
-        }, [&](int n, int r, int j) {
-            const size_t o = v_at + r * v_row + j;
-            ulonglong2 e[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                e[i] = attn_sub(x[n][i], mk[n][i]);
-                attn_send2<VEC>(a.Ev[i] + o, e[i]);
-            }
-            attn_store2<VEC>(a.v + o, attn_add(e[0], e[1]));         // the exchange
-        });
+        open_rows(a.K, a.k_stride, a.mk, a.Ek, a.k, a.kv_heads, h, false);
+        open_dims(a.K, a.k_stride, a.md, a.Ed, a.d, a.k_dim, attn::RIGHT, h, a.decay + (size_t)h * (a.C + 1) + at.len - 1 - t0, true);
+        open_dims(a.V, a.v_stride, a.mv, a.Ev, a.v, a.v_dim, attn::LEFT, h, nullptr, false);
     } else {
-        const int h = blockIdx.y - a.kv_heads, wide_C = a.C + (a.C & 1);
-        const size_t q_row = (size_t)a.q_heads * a.k_dim, p_row = (size_t)a.q_heads * a.C, w_row = (size_t)a.q_heads * wide_C;
-        const size_t q_at = first * q_row + (size_t)h * a.k_dim, p_at = first * p_row + (size_t)h * a.C, w_at = first * w_row + (size_t)h * wide_C;
-        ulonglong2 x[2][2], m[2][2];
-        attn_pairs(rows, a.k_dim, [&](int n, int r, int j) {
-            const size_t o = q_at + r * q_row + j, x_at = (size_t)(first + r) * a.q_stride + (size_t)h * a.k_dim + j;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                x[n][i] = attn_input2(a.Q[i] + x_at, a.in_vec);
-                m[n][i] = attn_load2<VEC>(a.mq[i] + o);
-            }
-        }, [&](int n, int r, int j) {
-            const size_t o = q_at + r * q_row + j;
-            ulonglong2 e[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                e[i] = attn_sub(x[n][i], m[n][i]);
-                attn_send2<VEC>(a.Eq[i] + o, e[i]);
-            }
-            const ulonglong2 q = attn_add(e[0], e[1]);               // the exchange
-            attn_store2<VEC>(a.q + o, q);
-            attn_store2<VEC>(a.q1 + o, attn_add(m[n][1], q));
-        });
+        const int h = blockIdx.y - a.kv_heads;
+        open_rows(a.Q, a.q_stride, a.mq, a.Eq, a.q, a.q_heads, h, true);
         // off the triangle nothing is sent
-        for (int t = threadIdx.x; t < rows * wide_C; t += attn::THREADS) {
-            const int r = t / wide_C, k = t - r * wide_C;
-            if (k <= r0 + r) continue;
-            const size_t o = w_at + r * w_row + k;
-            a.p[o] = a.pm[0][o] = a.pm[1][o] = 0ull;
-            if (k < a.C) a.Ep[0][p_at + r * p_row + k] = a.Ep[1][p_at + r * p_row + k] = 0ull;
+        const size_t p_row = (size_t)a.q_heads * a.C, p_at = first * p_row + (size_t)h * a.C;
+        for (int t = threadIdx.x; t < rows * a.C; t += attn::THREADS) {
+            const int r = t / a.C, k = t - r * a.C;
+            if (k > t0 + r) a.Ep[0][p_at + r * p_row + k] = a.Ep[1][p_at + r * p_row + k] = 0ull;
         }
     }
 }
 
-// A tile of the sum of d v^T of a chunk and key head, [k_dim][v_dim], of one party after the other.
-template <bool VEC>
-__device__ __forceinline__ void attn_keys(const AttnArgs& a, uint8_t* smem, const AttnChunk& at, int c, int h, int k0, int v0) {
-    const uint32_t k_row = (uint32_t)a.kv_heads * a.k_dim, v_row = (uint32_t)a.kv_heads * a.v_dim;
-    const size_t k_at = (size_t)at.first * k_row + (size_t)h * a.k_dim + k0, v_at = (size_t)at.first * v_row + (size_t)h * a.v_dim + v0;
-    const size_t out = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim + (size_t)k0 * a.v_dim + v0;
-    const int rows = min(attn::ROWS, a.k_dim - k0), cols = min(attn::COLS, a.v_dim - v0), half = 2 * attn_blocks(at.len);
-    AttnSums sums;
-    sums.clear();
-    attn_steps(smem, 2 * half, [&](int n, uint32_t to) {
-        const int i = n >= half, k = (n - i * half) / 2 * attn::DEPTH;
-        const bool first = n % 2 == 0;                       // V_i F, then E B_i
-        const u64* const d = (first ? i ? a.d1 : a.md[0] : a.d) + k_at;
-        const u64* const v = (first ? a.v : i ? a.mv[1] : a.mv[0]) + v_at;
-        AttnSide<true, attn::ROWS>::copy<VEC>(to, d + (size_t)k * k_row, k_row, rows, at.len - k);
-        AttnSide<true, attn::COLS>::copy<VEC>(to + attn::LEFT_BYTES, v + (size_t)k * v_row, v_row, cols, at.len - k);
-    }, [&](int n, const uint8_t* step) {
-        attn_multiply<true, true>(step, sums);
-        if ((n + 1) % half) return;
-        const u64* const dv = (n < half ? a.dv[0] : a.dv[1]) + out;
-        u64* const kv = (n < half ? a.kv[0] : a.kv[1]) + out;
-        sums.each([&](int, int row, int col, ulonglong2 z) {
-            if (row >= rows || col >= cols) return;
-            const int o = row * a.v_dim + col;
-            attn_store2<VEC>(kv + o, attn_add(z, attn_load2<VEC>(dv + o)));
-        });
-        sums.clear();
-    });
-}
-// A tile of the weights of a chunk and query head: P of all rows and the keys from s0 on.
-template <bool VEC>
-__device__ __forceinline__ void attn_weights(const AttnArgs& a, uint8_t* smem, const AttnChunk& at, int hq, int s0) {
-    const int h = hq / (a.q_heads / a.kv_heads), rows = at.len, keys = min(attn::COLS, rows - s0), half = 2 * attn_blocks(a.k_dim);
-    const int wide_C = a.C + (a.C & 1);                      // of the opened weights' rows, which begin on 16-byte boundaries
-    const uint32_t q_row = (uint32_t)a.q_heads * a.k_dim, k_row = (uint32_t)a.kv_heads * a.k_dim, p_row = (uint32_t)a.q_heads * a.C;
-    const uint32_t w_row = (uint32_t)a.q_heads * wide_C;
-    const size_t q_at = (size_t)at.first * q_row + (size_t)hq * a.k_dim, k_at = (size_t)(at.first + s0) * k_row + (size_t)h * a.k_dim;
-    const size_t p_at = (size_t)at.first * p_row + (size_t)hq * a.C, w_at = (size_t)at.first * w_row + (size_t)hq * wide_C;
-    const u64* const w = a.decay + (size_t)h * (a.C + 1);
-    const bool pairs = VEC && a.C % 2 == 0;
-    ulonglong2* const kept = reinterpret_cast<ulonglong2*>(smem + attn::STEPS * attn::STEP_BYTES) + threadIdx.x;
-    const int warp = threadIdx.x >> 5;
-    // off the triangle, or behind the rows: nothing to work out
-    const bool idle = s0 + (warp & 1) * attn::WARP > (warp >> 1) * attn::WARP + attn::WARP - 1 || (warp >> 1) * attn::WARP >= rows;
-    AttnSums sums;
-    sums.clear();
-    attn_steps(smem, 2 * half, [&](int n, uint32_t to) {
-        const int i = n >= half, k = (n - i * half) / 2 * attn::DEPTH;
-        const bool first = n % 2 == 0;
-        const u64* const q = (first ? i ? a.q1 : a.mq[0] : a.q) + q_at + k;
-        const u64* const x = (first ? a.k : i ? a.mk[1] : a.mk[0]) + k_at + k;
-        AttnSide<false, attn::ROWS>::copy<VEC>(to, q, q_row, rows, a.k_dim - k);
-        AttnSide<false, attn::COLS>::copy<VEC>(to + attn::LEFT_BYTES, x, k_row, keys, a.k_dim - k);
-    }, [&](int n, const uint8_t* step) {
-        if (idle) return;
-        attn_multiply<false, false>(step, sums);
-        if ((n + 1) % half) return;
-        const bool second = n >= half;
-        const u64* const qk = (second ? a.qk[1] : a.qk[0]) + p_at;
-        const u64* const mp = (second ? a.mp[1] : a.mp[0]) + p_at;
-        u64* const Ep = (second ? a.Ep[1] : a.Ep[0]) + p_at;
-        u64* const pm = (second ? a.pm[1] : a.pm[0]) + w_at;
-        // (the second word of a pair may lie off the triangle, where everything is zero, and behind an odd row's end)
-        sums.each([&](int e, int r, int col, ulonglong2 z) {
-            const int key = s0 + col;
-            if (key > r || r >= rows) return;
-            const bool both = key < r;
-            const uint32_t o = r * p_row + key, to = r * w_row + key;
-            auto load = [&](const u64* x) { return pairs ? attn_load2<true>(x + o) : make_ulonglong2(__ldcs(x + o), both ? __ldcs(x + o + 1) : 0ull); };
-            const ulonglong2 x = load(qk);
-            ulonglong2 m = load(mp);
-            if (!both) m.y = 0ull;
-            const u64 one = attn_rescale(attn_rescale(z.x + x.x, second, a.f) * __ldg(w + r - key), second, a.f) - m.x;
-            u64 two = 0ull;
-            if (both) two = attn_rescale(attn_rescale(z.y + x.y, second, a.f) * __ldg(w + r - key - 1), second, a.f) - m.y;
-            if (pairs) attn_send2<true>(Ep + o, make_ulonglong2(one, two));
-            else {
-                Ep[o] = one;
-                if (both) Ep[o + 1] = two;
-            }
-            if (!second) {
-                kept[e * attn::THREADS] = make_ulonglong2(one, two);
-            } else {
-                const ulonglong2 open = attn_add(kept[e * attn::THREADS], make_ulonglong2(one, two));    // the exchange
-                *reinterpret_cast<ulonglong2*>(a.p + w_at + to) = open;
-                m = attn_add(m, open);
-            }
-            *reinterpret_cast<ulonglong2*>(pm + to) = m;
-        });
-        sums.clear();
-    });
-}
-template <bool VEC>
-__global__ void __launch_bounds__(attn::THREADS, 2)
-attn_products_kernel(const __grid_constant__ AttnArgs a, int keys_ctas, int k_tiles, int v_tiles, int s_tiles) {
-    extern __shared__ __align__(128) uint8_t attn_smem[];
-    pdl_wait();
-    pdl_launch_dependents();
-    if ((int)blockIdx.x < keys_ctas) {
-        const int tiles = k_tiles * v_tiles, ch = blockIdx.x / tiles, tile = blockIdx.x - ch * tiles, c = ch / a.kv_heads, kt = tile / v_tiles;
-        const AttnChunk at = attn_find(a, c);
-        if (at.len) attn_keys<VEC>(a, attn_smem, at, c, ch - c * a.kv_heads, kt * attn::ROWS, (tile - kt * v_tiles) * attn::COLS);
-    } else {
-        const int b = blockIdx.x - keys_ctas, ch = b / s_tiles, s0 = (b - ch * s_tiles) * attn::COLS, c = ch / a.q_heads;
-        const AttnChunk at = attn_find(a, c);
-        if (s0 < at.len) attn_weights<VEC>(a, attn_smem, at, ch - c * a.q_heads, s0);
-    }
+// ---------------------------------------------------------------------------
+// Products: tiles of up to 128 x 64 words of Z_i - C_i = E B_i + V_i F (Eq. 1) on the int8 tensor cores.  A warp copies blocks of planes to shared memory,
+// a warp issues the MMAs, eight warps read the sums out of tensor memory to shared memory, which gives tensor memory back for the next tile, and
+// add them to what comes from memory.  Left operands are keys, values or states, right ones queries, weights or decayed keys; a left operand
+// of less than 128 rows has rows behind it that are whatever lies there, whose sums are never looked at.
+// ---------------------------------------------------------------------------
+struct AttnOperand {
+    const uint8_t* open; const uint8_t* own;             // the first blocks; V_i or the party's mask
+    uint32_t bytes, step;                                // of a block; from block to block
+};
+struct AttnTile {
+    AttnOperand left, right;
+    int blocks, rows, cols;                              // rows and columns of the result that are looked at
+    bool add;                                            // to what the tile before left in shared memory
+};
+struct AttnShared {
+    uint64_t full[attn::SLOTS], empty[attn::SLOTS], acc_full, acc_empty;
+    uint32_t tmem;
+    int abort_flag;
+};
+// Pointers of either party.
+template <typename T>
+__device__ __forceinline__ T* attn_of(T* const (&x)[2], int i) { return i ? x[1] : x[0]; }
+__device__ __forceinline__ AttnOperand attn_operand(const AttnPlanes& p, int i, size_t at, int rows) {
+    return {p.set[0] + at, (i ? p.set[2] : p.set[1]) + at, (uint32_t)(rows * attn::ROW_BYTES), (uint32_t)(rows * attn::ROW_BYTES)};
 }
 
-// The state from chunk to chunk of a sequence and key head, two words of both parties a thread; says whether the starts were in order.
+// All tiles of a CTA: items blockIdx.x, blockIdx.x + gridDim.x, ..., of an item's `tiles(item)` the tiles tile(item, n); drain(item, n, tile, sums) by the
+// draining warps, with the sums at words[column * LEFT + row].  Every role goes through all of them in the same order.
+template <typename N, typename T, typename D>
+__device__ __forceinline__ void attn_tiles(uint8_t* raw, int items, int* error, N&& tiles, T&& tile, D&& drain) {
+    using namespace attn;
+    __shared__ AttnShared s;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t* const planes = raw + ((0u - ptx::smem_u32(raw)) & 127u);
+    u64* const words = reinterpret_cast<u64*>(planes + SLOTS * SLOT_BYTES);
+    if (threadIdx.x == 0) {
+        for (int k = 0; k < SLOTS; ++k) {
+            ptx::mbar_init(ptx::smem_u32(&s.full[k]), 1);
+            ptx::mbar_init(ptx::smem_u32(&s.empty[k]), 1);
+        }
+        ptx::mbar_init(ptx::smem_u32(&s.acc_full), 1);
+        ptx::mbar_init(ptx::smem_u32(&s.acc_empty), DRAIN_THREADS);
+        s.abort_flag = 0;
+        ptx::fence_barrier_init();
+    }
+    __syncwarp();
+    if (warp == ISSUER) {
+        ptx::tmem_alloc(ptx::smem_u32(&s.tmem), ACC_COLS);
+        ptx::tmem_relinquish();
+    }
+    ptx::fence_before_sync();
+    __syncthreads();
+    ptx::fence_after_sync();
+    const uint32_t tmem = s.tmem, full0 = ptx::smem_u32(&s.full[0]), empty0 = ptx::smem_u32(&s.empty[0]), planes0 = ptx::smem_u32(planes);
+    if (warp == PRODUCER) {
+        if (ptx::elect_one()) {
+            int slot = 0, issued = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int item = blockIdx.x; item < items && ok; item += gridDim.x)
+                for (int n = 0, count = tiles(item); n < count && ok; ++n) {
+                    const AttnTile x = tile(item, n);
+                    for (int b = 0; b < 2 * x.blocks; ++b) {
+                        ok = limb_wait(empty0 + 8 * slot, phase ^ 1u, &s.abort_flag);
+                        if (!ok) break;
+                        const uint32_t bar = full0 + 8 * slot, to = planes0 + slot * SLOT_BYTES;
+                        const size_t k = b >> 1;
+                        ptx::mbar_expect_tx(bar, x.left.bytes + x.right.bytes);
+                        ptx::bulk_g2s(to, (b & 1 ? x.left.own : x.left.open) + k * x.left.step, x.left.bytes, bar);
+                        ptx::bulk_g2s(to + LEFT_BYTES, (b & 1 ? x.right.open : x.right.own) + k * x.right.step, x.right.bytes, bar);
+                        ++issued;
+                        if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+                    }
+                }
+            if (!ok) {
+                // gave up: let the copies already in flight land before the CTA leaves
+                for (int j = 1; j <= min(issued, SLOTS); ++j) {
+                    int k = slot - j;
+                    uint32_t ph = phase;
+                    if (k < 0) { k += SLOTS; ph ^= 1u; }
+                    const long long t0 = clock64();
+                    while (!ptx::mbar_try_wait(full0 + 8 * k, ph) && clock64() - t0 < 20000000ll) {}
+                }
+            }
+        }
+    } else if (warp == ISSUER) {
+        if (ptx::elect_one()) {
+            constexpr uint32_t IDESC = (2u << 4) | ((uint32_t)(LEFT >> 4) << 24);
+            const uint32_t acc_full = ptx::smem_u32(&s.acc_full), acc_empty = ptx::smem_u32(&s.acc_empty), left0 = limb_desc_lo(planes0);
+            int slot = 0, issued = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            bool ok = true;
+            for (int item = blockIdx.x; item < items && ok; item += gridDim.x)
+                for (int n = 0, count = tiles(item); n < count && ok; ++n) {
+                    const AttnTile x = tile(item, n);
+                    const uint32_t cols = x.right.bytes / ROW_BYTES, plane = x.left.bytes / (16 * limb::PLANES);
+                    ok = limb_wait(acc_empty, acc_phase ^ 1u, &s.abort_flag);
+                    if (!ok) break;
+                    ptx::fence_after_sync();
+                    for (int b = 0; b < 2 * x.blocks; ++b) {
+                        ok = limb_wait(full0 + 8 * slot, phase, &s.abort_flag);
+                        if (!ok) break;
+                        ptx::fence_after_sync();
+                        const uint32_t left = left0 + (slot * SLOT_BYTES >> 4), right = left + (LEFT_BYTES >> 4), first = b > 0 ? 1u : 0u;
+#pragma unroll
+                        for (int i = 0; i < limb::PLANES; ++i) {
+                            // left plane p meets right planes 0 .. 7 - p, whose sums lie side by side; wide and narrow instructions alternate, plane 0,
+                            // which overwrites all sums, first
+                            const int p = i & 1 ? limb::PLANES - 1 - (i >> 1) : i >> 1;
+                            const uint32_t wide = cols * (limb::PLANES - p), at = left + p * plane, to = tmem + cols * p, acc = p == 0 ? first : 1u;
+                            if (wide > 256) {
+                                ptx::mma_i8_keep_a(to, at, LIMB_DESC_HI, right, LIMB_DESC_HI, IDESC | (256u >> 3 << 17), acc);
+                                ptx::mma_i8_reuse_a(to + 256, at, LIMB_DESC_HI, right + (256 * KC >> 4), LIMB_DESC_HI, IDESC | ((wide - 256) >> 3 << 17), acc);
+                            } else {
+                                ptx::mma_i8(to, at, LIMB_DESC_HI, right, LIMB_DESC_HI, IDESC | (wide >> 3 << 17), acc);
+                            }
+                        }
+                        ptx::mma_commit(empty0 + 8 * slot);
+                        ++issued;
+                        if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+                    }
+                    if (!ok) break;
+                    ptx::mma_commit(acc_full);
+                    acc_phase ^= 1u;
+                }
+            // the last reports of the tensor core have to find this CTA's memory
+            for (int j = 1; j <= min(issued, SLOTS) && ok; ++j) {
+                int k = slot - j;
+                uint32_t ph = phase;
+                if (k < 0) { k += SLOTS; ph ^= 1u; }
+                ok = limb_wait(empty0 + 8 * k, ph, &s.abort_flag);
+            }
+        }
+    } else {
+        auto meet = [&] {
+            __syncwarp();                                // (a warp comes to a barrier as a whole)
+            asm volatile("bar.sync 1, %0;" ::"n"(DRAIN_THREADS) : "memory");
+        };
+        uint32_t acc_phase = 0;
+        bool ok = true;
+        const int quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+        for (int item = blockIdx.x; item < items; item += gridDim.x)
+            for (int n = 0, count = tiles(item); n < count; ++n) {
+                const AttnTile x = tile(item, n);
+                const int cols = x.right.bytes / ROW_BYTES;
+                ok = ok && limb_wait_warp(ptx::smem_u32(&s.acc_full), acc_phase, &s.abort_flag);
+                acc_phase ^= 1u;
+                meet();                                  // the words before have been used
+                if (ok) {
+                    ptx::fence_after_sync();
+                    if (quarter * 32 < x.rows)
+                        for (int c = (warp >> 2) * 8; c < x.cols; c += 16) {
+                            uint32_t d[limb::PLANES][8];
+#pragma unroll
+                            for (int p = 0; p < limb::PLANES; ++p) ptx::tmem_ld8(lanes + cols * p + c, d[p]);
+                            ptx::tmem_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                u64* const to = words + (c + j) * LEFT + row;
+                                *to = limb_recombine(d[0][j], d[1][j], d[2][j], d[3][j], d[4][j], d[5][j], d[6][j], d[7][j]) + (x.add ? *to : 0ull);
+                            }
+                            __syncwarp();
+                        }
+                    ptx::fence_before_sync();
+                    ptx::mbar_arrive(ptx::smem_u32(&s.acc_empty));
+                }
+                meet();
+                drain(item, n, x, words);
+            }
+    }
+    __syncwarp();
+    ptx::fence_before_sync();
+    __syncthreads();
+    if (threadIdx.x == 0 && s.abort_flag) {
+        *error = 1;
+        __threadfence_system();
+    }
+    __syncwarp();
+    if (warp == ISSUER) {
+        ptx::fence_after_sync();
+        ptx::tmem_dealloc(tmem, ACC_COLS);
+    }
+}
+// Pairs of rows of a tile's sums, U columns of a thread's at a time: load(row, column, U words) for all of them, then done(row, column, sums, U words).
+template <int WORDS, int U, typename L, typename F>
+__device__ __forceinline__ void attn_finish(u64* words, int rows, int cols, L&& load, F&& done) {
+    const int wide = rows > attn::LEFT / 2 ? 6 : 5, row = 2 * (threadIdx.x & ((1 << wide) - 1)), step = attn::DRAIN_THREADS >> wide;
+    if (row < rows)
+#pragma unroll 1
+        for (int c = threadIdx.x >> wide; c < cols; c += U * step) {
+            ulonglong2 x[U][WORDS];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < WORDS; ++k) x[u][k] = c + u * step < cols ? load(row, c + u * step, k) : make_ulonglong2(0ull, 0ull);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c + u * step < cols) done(row, c + u * step, reinterpret_cast<ulonglong2*>(words + (c + u * step) * attn::LEFT + row), x[u]);
+        }
+}
+
+// Items: chunks and key heads, the sums of d v^T, tiles of party, v_dim and k_dim; then chunks and query heads, the weights, a tile a party.
 template <bool VEC>
-__global__ void __launch_bounds__(attn::THREADS)
+__global__ void __launch_bounds__(attn::TILE_THREADS, 1)
+attn_products_kernel(const __grid_constant__ AttnArgs a) {
+    extern __shared__ uint8_t attn_smem[];
+    pdl_wait();
+    pdl_launch_dependents();
+    using namespace attn;
+    const int key_items = a.chunks * a.kv_heads, v_tiles = (a.v_dim + LEFT - 1) / LEFT, k_tiles = (a.k_dim + RIGHT - 1) / RIGHT;
+    const int t_blocks = blocks(a.C), k_blocks = blocks(a.k_dim);
+    attn_tiles(attn_smem, key_items + a.chunks * a.q_heads, a.error, [&](int item) {
+        const int c = item < key_items ? item / a.kv_heads : (item - key_items) / a.q_heads;
+        return a.found[c].y == 0 ? 0 : item < key_items ? 2 * v_tiles * k_tiles : 2;
+    }, [&](int item, int n) {
+        AttnTile x;
+        x.add = false;
+        if (item < key_items) {
+            const int i = n & 1, vk = n >> 1, vt = vk / k_tiles, v0 = vt * LEFT, k0 = (vk - vt * k_tiles) * RIGHT, len = a.found[item / a.kv_heads].y;
+            x.left = attn_operand(a.v, i, attn_dim_block(item, t_blocks, 0, a.v_dim, v0, LEFT), min(LEFT, up16(a.v_dim) - v0));
+            x.right = attn_operand(a.d, i, attn_dim_block(item, t_blocks, 0, a.k_dim, k0, RIGHT), min(RIGHT, up16(a.k_dim) - k0));
+            x.blocks = blocks(len);
+            x.rows = min(LEFT, a.v_dim - v0);
+            x.cols = min(RIGHT, a.k_dim - k0);
+        } else {
+            const int ch = item - key_items, c = ch / a.q_heads, hq = ch - c * a.q_heads, len = a.found[c].y;
+            // (room between the blocks for up16(C) rows)
+            x.left = attn_operand(a.k, n, attn_token_block(c * a.kv_heads + hq / (a.q_heads / a.kv_heads), k_blocks, 0, a.C), up16(len));
+            x.right = attn_operand(a.q, n, attn_token_block(ch, k_blocks, 0, a.C), up16(len));
+            x.left.step = x.right.step = up16(a.C) * ROW_BYTES;
+            x.blocks = k_blocks;
+            x.rows = x.cols = len;
+        }
+        return x;
+    }, [&](int item, int n, const AttnTile& x, u64* words) {
+        if (item < key_items) {
+            const int i = n & 1, vk = n >> 1, vt = vk / k_tiles, v0 = vt * LEFT, k0 = (vk - vt * k_tiles) * RIGHT;
+            const size_t at = (size_t)item * a.k_dim * a.v_dim + (size_t)k0 * a.v_dim + v0;
+            const u64* const dv = attn_of(a.dv, i) + at;
+            u64* const kv = attn_of(a.kv, i) + at;
+            attn_finish<1, 8>(words, x.rows, x.cols, [&](int row, int col, int) { return attn_load2<VEC>(dv + (col * a.v_dim + row)); },
+                              [&](int row, int col, const ulonglong2* z, const ulonglong2* y) { attn_store2<VEC>(kv + (col * a.v_dim + row), attn_add(*z, y[0])); });
+            return;
+        }
+        const int ch = item - key_items, c = ch / a.q_heads, hq = ch - c * a.q_heads, h = hq / (a.q_heads / a.kv_heads), i = n, f = a.f;
+        const int2 found = a.found[c];
+        const uint32_t p_row = (uint32_t)a.q_heads * a.C;
+        const size_t p_at = (size_t)found.x * p_row + (size_t)hq * a.C;
+        const u64* const qk = attn_of(a.qk, i) + p_at;
+        const u64* const mp = attn_of(a.mp, i) + p_at;
+        u64* const Ep = attn_of(a.Ep, i) + p_at;
+        const u64* const w = a.decay + (size_t)h * (a.C + 1);
+        const bool pairs = VEC && a.C % 2 == 0;
+        const int t_used = blocks(found.y), quads = 8 * t_used;
+        for (int t = threadIdx.x; t < found.y * quads; t += DRAIN_THREADS) {
+            const int r = t / quads, quad = t - r * quads, key0 = 4 * quad;
+            u64 z[4], m[4], e[4];
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+                const int key = key0 + j;
+                const uint32_t o = r * p_row + key;
+                ulonglong2 x0 = make_ulonglong2(0ull, 0ull), x1 = x0, y = x0;
+                if (key <= r) {                          // (the second word of a pair may lie off the triangle, and behind an odd row's end)
+                    x0 = pairs ? attn_load2<true>(qk + o) : make_ulonglong2(__ldcs(qk + o), key < r ? __ldcs(qk + o + 1) : 0ull);
+                    x1 = pairs ? attn_load2<true>(mp + o) : make_ulonglong2(__ldcs(mp + o), key < r ? __ldcs(mp + o + 1) : 0ull);
+                    y = *reinterpret_cast<const ulonglong2*>(words + r * LEFT + key);
+                }
+                z[j] = x0.x + y.x; z[j + 1] = x0.y + y.y;
+                m[j] = x1.x;       m[j + 1] = key < r ? x1.y : 0ull;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int key = key0 + j;
+                e[j] = 0ull;
+                if (key <= r) e[j] = attn_rescale(attn_rescale(z[j], i, f) * __ldg(w + r - key), i, f) - m[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+                const int key = key0 + j;
+                const uint32_t o = r * p_row + key;
+                if (key > r) continue;
+                if (pairs) attn_send2<true>(Ep + o, make_ulonglong2(e[j], e[j + 1]));
+                else {
+                    Ep[o] = e[j];
+                    if (key < r) Ep[o + 1] = e[j + 1];
+                }
+            }
+            // party 0's words wait behind the tile's rows, of which there are 64 at most, for the same thread
+            u64* const kept = words + r * LEFT + LEFT / 2 + key0;
+            const size_t block = attn_token_block(ch, t_blocks, quad >> 3, a.C);
+            const int rows16 = up16(found.y);
+            if (i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    e[j] += kept[j];                     // the exchange
+                    m[j] += e[j];
+                }
+                attn_emit(a.p.set[0] + block, rows16, r, quad & 7, e);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) kept[j] = e[j];
+            }
+            attn_emit((i ? a.p.set[2] : a.p.set[1]) + block, rows16, r, quad & 7, m);
+        }
+    });
+}
+
+// The state from chunk to chunk of a sequence and key head, 4 x 2 words of both parties a thread; says whether the starts were in order.
+template <bool VEC>
+__global__ void __launch_bounds__(attn::STATE_THREADS, 3)
 attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
     __shared__ int before;
     pdl_wait();
     pdl_launch_dependents();
     const int j = blockIdx.x / (a.kv_heads * pieces), rest = blockIdx.x - j * a.kv_heads * pieces, h = rest / pieces;
-    const int word = 2 * ((rest - h * pieces) * attn::THREADS + threadIdx.x), words = a.k_dim * a.v_dim;
+    const int t = (rest - h * pieces) * attn::STATE_THREADS + threadIdx.x, k_blocks = attn::blocks(a.k_dim), wide = attn::up16(a.v_dim);
     if (threadIdx.x == 0) before = 0;
     __syncthreads();
     const bool checks = blockIdx.x == 0;
     int sum = 0, begin;
     bool bad = false;
-    for (int s = threadIdx.x; s < (checks ? a.sequences : j); s += attn::THREADS) {
+    for (int s = threadIdx.x; s < (checks ? a.sequences : j); s += attn::STATE_THREADS) {
         sum += (attn_length(a, s, &begin) + a.C - 1) / a.C;
-        const int end = __ldg(a.starts + s + 1);
+        const int end = a.starts[s + 1];
         bad |= begin < 0 || end < begin || end > a.tokens;
     }
     if (sum) atomicAdd(&before, sum);
     if (bad && checks && a.bad_starts) *a.bad_starts = 1;
     __syncthreads();
     if (checks && threadIdx.x == 0 && before != a.chunks && a.bad_starts) *a.bad_starts = 1;
-    if (word >= words) return;
+    // a warp has four groups of four rows, eight pairs of columns: 128-byte pieces of the state, 16 bytes of eight rows of a plane
+    const int groups = wide / 16, wt = t >> 5, quad = (wt / groups) * 4 + (t >> 3 & 3), col = (wt % groups) * 16 + 2 * (t & 7);
+    if (quad >= 8 * k_blocks) return;
+    const int words = a.k_dim * a.v_dim, row = 4 * quad, word = row * a.v_dim + col;
+    const bool in = col < a.v_dim;
     const size_t at = ((size_t)j * a.kv_heads + h) * words + word, step = (size_t)a.kv_heads * words;
     const u64* const w = a.decay + (size_t)h * (a.C + 1);
     int c = checks ? 0 : before, left = attn_length(a, j, &begin);
     const int end = min(a.chunks, c + (left + a.C - 1) / a.C);
-    ulonglong2 S[2], kv[2], ms[2];
+    ulonglong2 S[2][4], kv[2][4], ms[2][4];
     size_t o = ((size_t)c * a.kv_heads + h) * words + word;
+    auto live = [&](int k) { return in && row + k < a.k_dim; };
     auto load = [&] {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            kv[i] = attn_load2<VEC>(a.kv[i] + o);
-            ms[i] = attn_keep2<VEC>(a.ms[i] + o);
-        }
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                kv[i][k] = live(k) ? attn_load2<VEC>(a.kv[i] + o + k * a.v_dim) : make_ulonglong2(0ull, 0ull);
+                ms[i][k] = live(k) ? attn_load2<VEC>(a.ms[i] + o + k * a.v_dim) : make_ulonglong2(0ull, 0ull);
+            }
     };
     if (c < end) load();
 #pragma unroll
-    for (int i = 0; i < 2; ++i) S[i] = a.S0[i] ? attn_load2<VEC>(a.S0[i] + at) : make_ulonglong2(0ull, 0ull);
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) S[i][k] = a.S0[i] && live(k) ? attn_load2<VEC>(a.S0[i] + at + k * a.v_dim) : make_ulonglong2(0ull, 0ull);
+    const int row0 = col / attn::LEFT * attn::LEFT, rows = min(attn::LEFT, wide - row0);
     for (; c < end; ++c, left -= a.C) {
         const u64 weight = __ldg(w + min(left, a.C));
-        ulonglong2 e[2];
+        ulonglong2 e[2][4];
         const size_t here = o;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            e[i] = attn_sub(S[i], ms[i]);
-            S[i] = make_ulonglong2(attn_rescale(weight * S[i].x + kv[i].x, i, a.f), attn_rescale(weight * S[i].y + kv[i].y, i, a.f));
-        }
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                e[i][k] = attn_sub(S[i][k], ms[i][k]);
+                S[i][k] = make_ulonglong2(attn_rescale(weight * S[i][k].x + kv[i][k].x, i, a.f), attn_rescale(weight * S[i][k].y + kv[i][k].y, i, a.f));
+                if (live(k)) attn_send2<VEC>(a.Es[i] + here + k * a.v_dim, e[i][k]);
+            }
+        const size_t block = attn_dim_block(c * a.kv_heads + h, k_blocks, quad >> 3, a.v_dim, row0, attn::LEFT);
+        auto emit = [&](int n, const ulonglong2 (&v)[4]) {
+            attn_emit(a.s.set[n] + block, rows, col - row0, quad & 7, v[0].x, v[1].x, v[2].x, v[3].x);
+            attn_emit(a.s.set[n] + block, rows, col - row0 + 1, quad & 7, v[0].y, v[1].y, v[2].y, v[3].y);
+        };
+        emit(1, ms[0]);
+        emit(2, ms[1]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) e[0][k] = attn_add(e[0][k], e[1][k]);        // the exchange
+        emit(0, e[0]);
         o += step;
         if (c + 1 < end) load();
-#pragma unroll
-        for (int i = 0; i < 2; ++i) attn_send2<VEC>(a.Es[i] + here, e[i]);
-        attn_store2<VEC>(a.s + here, attn_add(e[0], e[1]));              // the exchange
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) attn_store2<VEC>(a.S1[i] + at, S[i]);
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (live(k)) attn_store2<VEC>(a.S1[i] + at + k * a.v_dim, S[i][k]);
 }
 
-// A tile of the rows of O of a chunk, query head and party: the far part w[r + 1] tr(q S), then the near part P v.
+// Items: chunks, query heads and parties, the rows of O: for every tile of v_dim the far part w[r + 1] tr(q S), then the near part P v.
 template <bool VEC>
-__global__ void __launch_bounds__(attn::THREADS, 2)
-attn_rows_kernel(const __grid_constant__ AttnArgs a, int v_tiles) {
-    extern __shared__ __align__(128) uint8_t attn_smem[];
+__global__ void __launch_bounds__(attn::TILE_THREADS, 1)
+attn_rows_kernel(const __grid_constant__ AttnArgs a) {
+    extern __shared__ uint8_t attn_smem[];
     pdl_wait();
     pdl_launch_dependents();
-    const int tile = blockIdx.x / 2, ch = tile / v_tiles, c = ch / a.q_heads, hq = ch - c * a.q_heads, h = hq / (a.q_heads / a.kv_heads);
-    const int v0 = (tile - ch * v_tiles) * attn::COLS;
-    const bool second = blockIdx.x % 2;                      // party
-    const AttnChunk at = attn_find(a, c);
-    if (at.len == 0) return;
-    const int rows = at.len, cols = min(attn::COLS, a.v_dim - v0), far = 2 * attn_blocks(a.k_dim), near = 2 * attn_blocks(rows), wide_C = a.C + (a.C & 1);
-    const uint32_t q_row = (uint32_t)a.q_heads * a.k_dim, v_row = (uint32_t)a.kv_heads * a.v_dim, o_row = (uint32_t)a.q_heads * a.v_dim;
-    const uint32_t w_row = (uint32_t)a.q_heads * wide_C;
-    const size_t q_at = (size_t)at.first * q_row + (size_t)hq * a.k_dim, v_at = (size_t)at.first * v_row + (size_t)h * a.v_dim + v0;
-    const size_t s_at = ((size_t)c * a.kv_heads + h) * a.k_dim * a.v_dim + v0;
-    const size_t w_at = (size_t)at.first * w_row + (size_t)hq * wide_C, o_at = (size_t)at.first * o_row + (size_t)hq * a.v_dim + v0;
-    ulonglong2* const kept = reinterpret_cast<ulonglong2*>(attn_smem + attn::STEPS * attn::STEP_BYTES) + threadIdx.x;
-    const int warp_row = (threadIdx.x >> 6) * attn::WARP;
-    AttnSums sums;
-    sums.clear();
-    attn_steps(attn_smem, far + near, [&](int n, uint32_t to) {
-        const bool first = n % 2 == 0;
-        if (n < far) {
-            const int k = n / 2 * attn::DEPTH;
-            const u64* const q = (first ? second ? a.q1 : a.mq[0] : a.q) + q_at + k;
-            const u64* const S = (first ? a.s : second ? a.ms[1] : a.ms[0]) + s_at + (size_t)k * a.v_dim;
-            AttnSide<false, attn::ROWS>::copy<VEC>(to, q, q_row, rows, a.k_dim - k);
-            AttnSide<true, attn::COLS>::copy<VEC>(to + attn::LEFT_BYTES, S, a.v_dim, cols, a.k_dim - k);
+    using namespace attn;
+    const int v_tiles = (a.v_dim + LEFT - 1) / LEFT, t_blocks = blocks(a.C), k_blocks = blocks(a.k_dim);
+    attn_tiles(attn_smem, 2 * a.chunks * a.q_heads, a.error, [&](int item) { return a.found[(item >> 1) / a.q_heads].y == 0 ? 0 : 2 * v_tiles; },
+               [&](int item, int n) {
+        const int i = item & 1, ch = item >> 1, c = ch / a.q_heads, hq = ch - c * a.q_heads, kv = c * a.kv_heads + hq / (a.q_heads / a.kv_heads);
+        const int v0 = (n >> 1) * LEFT, len = a.found[c].y, wide = min(LEFT, up16(a.v_dim) - v0);
+        AttnTile x;
+        x.add = n & 1;
+        if (n & 1) {
+            x.left = attn_operand(a.v, i, attn_dim_block(kv, t_blocks, 0, a.v_dim, v0, LEFT), wide);
+            x.right = attn_operand(a.p, i, attn_token_block(ch, t_blocks, 0, a.C), up16(len));
+            x.blocks = blocks(len);
         } else {
-            const int k = (n - far) / 2 * attn::DEPTH;
-            const u64* const p = (first ? second ? a.pm[1] : a.pm[0] : a.p) + w_at + k;
-            const u64* const v = (first ? a.v : second ? a.mv[1] : a.mv[0]) + v_at + (size_t)k * v_row;
-            // (the opened weights' rows are longer than an odd number of keys by a word, zero)
-            AttnSide<false, attn::ROWS>::copy<VEC>(to, p, w_row, rows, rows - k);
-            AttnSide<true, attn::COLS>::copy<VEC>(to + attn::LEFT_BYTES, v, v_row, cols, rows - k);
+            x.left = attn_operand(a.s, i, attn_dim_block(kv, k_blocks, 0, a.v_dim, v0, LEFT), wide);
+            x.right = attn_operand(a.q, i, attn_token_block(ch, k_blocks, 0, a.C), up16(len));
+            x.blocks = k_blocks;
         }
-    }, [&](int n, const uint8_t* step) {
-        if (warp_row >= rows) return;
-        // (a key behind all of a warp's rows has no weight)
-        if (n < far || (n - far) / 2 * attn::DEPTH < warp_row + attn::WARP) attn_multiply<false, true>(step, sums);
-        if (n == far - 1) {
-            const u64* const qs = (second ? a.qs[1] : a.qs[0]) + o_at;
-            const u64* const pv = (second ? a.pv[1] : a.pv[0]) + o_at;
-            const u64* const w = a.decay + (size_t)h * (a.C + 1) + 1;
-            sums.each([&](int e, int r, int col, ulonglong2 z) {
-                if (r >= rows || col >= cols) return;
-                const uint32_t o = r * o_row + col;
-                const ulonglong2 x = attn_load2<VEC>(qs + o), y = attn_load2<VEC>(pv + o);
-                const u64 weight = __ldg(w + r);
-                kept[e * attn::THREADS] = make_ulonglong2(y.x + weight * attn_rescale(z.x + x.x, second, a.f), y.y + weight * attn_rescale(z.y + x.y, second, a.f));
+        x.right.step = up16(a.C) * ROW_BYTES;
+        x.rows = min(LEFT, a.v_dim - v0);
+        x.cols = len;
+        return x;
+    }, [&](int item, int n, const AttnTile& x, u64* words) {
+        const int i = item & 1, ch = item >> 1, c = ch / a.q_heads, hq = ch - c * a.q_heads, h = hq / (a.q_heads / a.kv_heads), f = a.f;
+        const uint32_t o_row = (uint32_t)a.q_heads * a.v_dim;
+        const size_t at = (size_t)a.found[c].x * o_row + (size_t)hq * a.v_dim + (n >> 1) * LEFT;
+        if (n & 1) {
+            u64* const O = attn_of(a.O, i) + at;
+            attn_finish<1, 1>(words, x.rows, x.cols, [&](int, int, int) { return make_ulonglong2(0ull, 0ull); }, [&](int row, int r, const ulonglong2* z, const ulonglong2*) {
+                attn_send2<VEC>(O + (r * o_row + row), make_ulonglong2(attn_rescale(z->x, i, f), attn_rescale(z->y, i, f)));
             });
-            sums.clear();
-        } else if (n == far + near - 1) {
-            u64* const O = (second ? a.O[1] : a.O[0]) + o_at;
-            sums.each([&](int e, int r, int col, ulonglong2 z) {
-                if (r >= rows || col >= cols) return;
-                const ulonglong2 x = attn_add(z, kept[e * attn::THREADS]);
-                attn_send2<VEC>(O + (r * o_row + col), make_ulonglong2(attn_rescale(x.x, second, a.f), attn_rescale(x.y, second, a.f)));
+        } else {
+            const u64* const qs = attn_of(a.qs, i) + at;
+            const u64* const pv = attn_of(a.pv, i) + at;
+            const u64* const w = a.decay + (size_t)h * (a.C + 1) + 1;
+            attn_finish<2, 4>(words, x.rows, x.cols, [&](int row, int r, int k) { return attn_load2<VEC>((k ? pv : qs) + (r * o_row + row)); },
+                              [&](int, int r, ulonglong2* z, const ulonglong2* y) {
+                const u64 weight = __ldg(w + r);
+                *z = make_ulonglong2(y[1].x + weight * attn_rescale(z->x + y[0].x, i, f), y[1].y + weight * attn_rescale(z->y + y[0].y, i, f));
             });
         }
     });
