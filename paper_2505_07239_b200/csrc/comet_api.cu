@@ -2638,17 +2638,17 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
         for (const u64* p : {a.mq[i], a.mk[i], a.mv[i], a.md[i], a.mp[i], a.ms[i], a.S0[i], (const u64*)a.Eq[i], (const u64*)a.Ek[i], (const u64*)a.Ev[i],
                              (const u64*)a.Ed[i], (const u64*)a.Ep[i], (const u64*)a.Es[i], (const u64*)a.S1[i], (const u64*)a.O[i], a.qk[i], a.pv[i], a.qs[i], a.dv[i]})
             vec = vec && aligned16(p);
-    // the states' threads: 8 of every block of 32 rows, 8 of 16 columns
-    const int pieces = ceil_div(8 * at::blocks(a.k_dim) * at::up16(a.v_dim) / 2, at::STATE_THREADS), slabs = 2 * at::blocks(a.C);
+    // the states' threads: 8 of every block of 32 rows
+    const int pieces = ceil_div(8 * at::blocks(a.k_dim) * at::up16(a.v_dim), at::STATE_THREADS), slabs = 2 * at::blocks(a.C);
     auto grid = [&](int64_t items) { return dim3((unsigned)(items < dev.sm_count ? items : dev.sm_count)); };
     cudaError_t err = cudaSuccess;
-    if (n) err = launch_chained(vec ? comet::attn_open_kernel<true> : comet::attn_open_kernel<false>, dim3((unsigned)(n * slabs), (unsigned)(Hk + Hq)),
+    if (n) err = launch_chained(vec ? comet::attn_open_kernel<true> : comet::attn_open_kernel<false>, dim3((unsigned)(n * slabs), (unsigned)(3 * Hk + Hq)),
                                 dim3(at::THREADS), 0, stream, nullptr, a, slabs);
     if (err == cudaSuccess && n)
         err = launch_chained(vec ? comet::attn_products_kernel<true> : comet::attn_products_kernel<false>, grid(n * (Hk + Hq)), dim3(at::TILE_THREADS),
                              at::TILE_SMEM, stream, nullptr, a);
     if (err == cudaSuccess)
-        err = launch_chained(vec ? comet::attn_state_kernel<true> : comet::attn_state_kernel<false>, dim3((unsigned)(g->sequences * Hk * pieces)),
+        err = launch_chained(comet::attn_state_kernel, dim3((unsigned)(g->sequences * Hk * pieces)),
                              dim3(at::STATE_THREADS), 0, stream, nullptr, a, pieces);
     if (err == cudaSuccess && n)
         err = launch_chained(vec ? comet::attn_rows_kernel<true> : comet::attn_rows_kernel<false>, grid(2 * n * Hq), dim3(at::TILE_THREADS), at::TILE_SMEM,

@@ -154,9 +154,9 @@ __device__ __forceinline__ void attn_emit(uint8_t* block, int rows, int row, int
     attn_emit(block, rows, row, quad, w);
 }
 
-// Messages of q, or of k, v and d, of a head and SLAB tokens of a chunk, and the planes of what they open; zeros where no weight is sent.  Bound by
+// Messages of k, d, v or q of a head and SLAB tokens of a chunk, and the planes of what they open; zeros where no weight is sent.  Bound by
 // memory: 4 words in and 5 out of every word of q and k, 8 and 10 of d, v.  q and k: eight lanes a row's 32 words, four words each.  v and
-// d, whose contraction runs over the tokens: four tokens x two words a thread, sixteen tokens x sixteen words a warp.
+// d, whose contraction runs over the tokens: four tokens of a word a thread, sixteen tokens x eight words a warp, 64 bytes of a token, 128 of a plane.
 template <bool VEC>
 __global__ void __launch_bounds__(attn::THREADS, 2)
 attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
@@ -208,54 +208,50 @@ attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
     // values or decayed keys, `dim` words a token in tiles of `tile`; tokens behind the last count as zero
     auto open_dims = [&](const u64* const x[2], long long stride, const u64* const m[2], u64* const msg[2], const AttnPlanes& to, int dim, int tile,
                          int head, const u64* w, bool sum) {
-        const int half = attn::up16(dim) / 2;
+        const int all = attn::up16(dim);
         const size_t o0 = ((size_t)first * a.kv_heads + head) * dim, row = (size_t)a.kv_heads * dim;
-        for (int t = threadIdx.x; t < 4 * half; t += attn::THREADS) {
-            const int quad = (t >> 3) & 3, j = 2 * ((t & 7) + (t >> 5) * 8);
-            ulonglong2 e[2][4], mask[2][4];
+        for (int t = threadIdx.x; t < 4 * all; t += attn::THREADS) {
+            const int quad = (t >> 3) & 3, j = (t & 7) + (t >> 5) * 8;
+            u64 e[2][4], mask[2][4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int r = 4 * quad + k;
-                    e[i][k] = mask[i][k] = make_ulonglong2(0ull, 0ull);
+                    e[i][k] = mask[i][k] = 0ull;
                     if (r < rows && j < dim) {
-                        e[i][k] = attn_input2(x[i] + (long long)(first + r) * stride + (long long)head * dim + j, a.in_vec);
-                        mask[i][k] = attn_load2<VEC>(m[i] + o0 + r * row + j);
+                        e[i][k] = __ldcs(x[i] + (long long)(first + r) * stride + (long long)head * dim + j);
+                        mask[i][k] = __ldcs(m[i] + o0 + r * row + j);
                     }
                 }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int r = 4 * quad + k;
-                const bool live = r < rows && j < dim;
                 const u64 weight = w && r < rows ? __ldg(w - r) : 1ull;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    if (w) e[i][k] = make_ulonglong2(attn_rescale(e[i][k].x * weight, i, f), attn_rescale(e[i][k].y * weight, i, f));
-                    e[i][k] = attn_sub(e[i][k], mask[i][k]);
-                    if (live) attn_send2<VEC>(msg[i] + o0 + r * row + j, e[i][k]);
+                    if (w) e[i][k] = attn_rescale(e[i][k] * weight, i, f);
+                    e[i][k] -= mask[i][k];
+                    if (r < rows && j < dim) __stcs(msg[i] + o0 + r * row + j, e[i][k]);
                 }
-                e[0][k] = attn_add(e[0][k], e[1][k]);                                                      // the exchange
-                if (sum) mask[1][k] = attn_add(mask[1][k], e[0][k]);
+                e[0][k] += e[1][k];                                                                        // the exchange
+                if (sum) mask[1][k] += e[0][k];
             }
-            const int row0 = j / tile * tile, wide = min(tile, attn::up16(dim) - row0), token = t0 / 4 + quad;
+            const int row0 = j / tile * tile, wide = min(tile, all - row0), token = t0 / 4 + quad;
             const size_t block = attn_dim_block(c * a.kv_heads + head, blocks, token / 8, dim, row0, tile);
-            auto emit = [&](int n, const ulonglong2 (&v)[4]) {
-                attn_emit(to.set[n] + block, wide, j - row0, token & 7, v[0].x, v[1].x, v[2].x, v[3].x);
-                attn_emit(to.set[n] + block, wide, j - row0 + 1, token & 7, v[0].y, v[1].y, v[2].y, v[3].y);
-            };
-            emit(0, e[0]);
-            emit(1, mask[0]);
-            emit(2, mask[1]);
+            attn_emit(to.set[0] + block, wide, j - row0, token & 7, e[0]);
+            attn_emit(to.set[1] + block, wide, j - row0, token & 7, mask[0]);
+            attn_emit(to.set[2] + block, wide, j - row0, token & 7, mask[1]);
         }
     };
-    if ((int)blockIdx.y < a.kv_heads) {
-        const int h = blockIdx.y;
+    const int what = min(3, (int)blockIdx.y / a.kv_heads), h = blockIdx.y - what * a.kv_heads;
+    if (what == 0) {
         open_rows(a.K, a.k_stride, a.mk, a.Ek, a.k, a.kv_heads, h, false);
+    } else if (what == 1) {
         open_dims(a.K, a.k_stride, a.md, a.Ed, a.d, a.k_dim, attn::RIGHT, h, a.decay + (size_t)h * (a.C + 1) + at.len - 1 - t0, true);
+    } else if (what == 2) {
         open_dims(a.V, a.v_stride, a.mv, a.Ev, a.v, a.v_dim, attn::LEFT, h, nullptr, false);
     } else {
-        const int h = blockIdx.y - a.kv_heads;
         open_rows(a.Q, a.q_stride, a.mq, a.Eq, a.q, a.q_heads, h, true);
         // off the triangle nothing is sent
         const size_t p_row = (size_t)a.q_heads * a.C, p_at = first * p_row + (size_t)h * a.C;
@@ -293,10 +289,19 @@ __device__ __forceinline__ AttnOperand attn_operand(const AttnPlanes& p, int i, 
     return {p.set[0] + at, (i ? p.set[2] : p.set[1]) + at, (uint32_t)(rows * attn::ROW_BYTES), (uint32_t)(rows * attn::ROW_BYTES)};
 }
 
-// All tiles of a CTA: items blockIdx.x, blockIdx.x + gridDim.x, ..., of an item's `tiles(item)` the tiles tile(item, n); drain(item, n, tile, sums) by the
-// draining warps, with the sums at words[column * LEFT + row].  Every role goes through all of them in the same order.
-template <typename N, typename T, typename D>
-__device__ __forceinline__ void attn_tiles(uint8_t* raw, int items, int* error, N&& tiles, T&& tile, D&& drain) {
+// Asks the L2 for `rows` rows of `words` words, `step` words apart: the draining warps, for what they add to the sums while the products run.
+__device__ __forceinline__ void attn_ask(const u64* p, int words, int rows, uint32_t step) {
+    const int lines = (words + 15) / 16;
+    for (int t = threadIdx.x; t < lines * rows; t += attn::DRAIN_THREADS) {
+        const int r = t / lines;
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(p + (r * step + 16 * (t - r * lines))));
+    }
+}
+
+// All tiles of a CTA: items blockIdx.x, blockIdx.x + gridDim.x, ..., of an item's `tiles(item)` the tiles tile(item, n); ask(item, n, tile) and then
+// drain(item, n, tile, sums) by the draining warps, with the sums at words[column * LEFT + row].  Every role goes through all of them in the same order.
+template <typename N, typename T, typename A, typename D>
+__device__ __forceinline__ void attn_tiles(uint8_t* raw, int items, int* error, N&& tiles, T&& tile, A&& ask, D&& drain) {
     using namespace attn;
     __shared__ AttnShared s;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -413,6 +418,7 @@ __device__ __forceinline__ void attn_tiles(uint8_t* raw, int items, int* error, 
             for (int n = 0, count = tiles(item); n < count; ++n) {
                 const AttnTile x = tile(item, n);
                 const int cols = x.right.bytes / ROW_BYTES;
+                ask(item, n, x);
                 ok = ok && limb_wait_warp(ptx::smem_u32(&s.acc_full), acc_phase, &s.abort_flag);
                 acc_phase ^= 1u;
                 meet();                                  // the words before have been used
@@ -502,6 +508,17 @@ attn_products_kernel(const __grid_constant__ AttnArgs a) {
             x.rows = x.cols = len;
         }
         return x;
+    }, [&](int item, int n, const AttnTile& x) {
+        if (item < key_items) {
+            const int vk = n >> 1, vt = vk / k_tiles;
+            attn_ask(attn_of(a.dv, n & 1) + ((size_t)item * a.k_dim * a.v_dim + (size_t)(vk - vt * k_tiles) * RIGHT * a.v_dim + vt * LEFT), x.rows, x.cols, a.v_dim);
+        } else {
+            const int ch = item - key_items, c = ch / a.q_heads;
+            const uint32_t p_row = (uint32_t)a.q_heads * a.C;
+            const size_t p_at = (size_t)a.found[c].x * p_row + (size_t)(ch - c * a.q_heads) * a.C;
+            attn_ask(attn_of(a.qk, n) + p_at, x.rows, x.rows, p_row);
+            attn_ask(attn_of(a.mp, n) + p_at, x.rows, x.rows, p_row);
+        }
     }, [&](int item, int n, const AttnTile& x, u64* words) {
         if (item < key_items) {
             const int i = n & 1, vk = n >> 1, vt = vk / k_tiles, v0 = vt * LEFT, k0 = (vk - vt * k_tiles) * RIGHT;
@@ -575,9 +592,8 @@ attn_products_kernel(const __grid_constant__ AttnArgs a) {
     });
 }
 
-// The state from chunk to chunk of a sequence and key head, 4 x 2 words of both parties a thread; says whether the starts were in order.
-template <bool VEC>
-__global__ void __launch_bounds__(attn::STATE_THREADS, 3)
+// The state from chunk to chunk of a sequence and key head, four words of a column and both parties a thread; says whether the starts were in order.
+__global__ void __launch_bounds__(attn::STATE_THREADS)
 attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
     __shared__ int before;
     pdl_wait();
@@ -598,63 +614,61 @@ attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
     if (bad && checks && a.bad_starts) *a.bad_starts = 1;
     __syncthreads();
     if (checks && threadIdx.x == 0 && before != a.chunks && a.bad_starts) *a.bad_starts = 1;
-    // a warp has four groups of four rows, eight pairs of columns: 128-byte pieces of the state, 16 bytes of eight rows of a plane
-    const int groups = wide / 16, wt = t >> 5, quad = (wt / groups) * 4 + (t >> 3 & 3), col = (wt % groups) * 16 + 2 * (t & 7);
+    // a warp has four groups of four rows, eight columns: 64 bytes of a row, 128 of a plane
+    const int groups = wide / 8, wt = t >> 5, quad = (wt / groups) * 4 + (t >> 3 & 3), col = (wt % groups) * 8 + (t & 7);
     if (quad >= 8 * k_blocks) return;
     const int words = a.k_dim * a.v_dim, row = 4 * quad, word = row * a.v_dim + col;
-    const bool in = col < a.v_dim;
     const size_t at = ((size_t)j * a.kv_heads + h) * words + word, step = (size_t)a.kv_heads * words;
     const u64* const w = a.decay + (size_t)h * (a.C + 1);
     int c = checks ? 0 : before, left = attn_length(a, j, &begin);
     const int end = min(a.chunks, c + (left + a.C - 1) / a.C);
-    ulonglong2 S[2][4], kv[2][4], ms[2][4];
+    u64 S[2][4], kv[2][4], ms[2][4];
     size_t o = ((size_t)c * a.kv_heads + h) * words + word;
-    auto live = [&](int k) { return in && row + k < a.k_dim; };
+    auto live = [&](int k) { return col < a.v_dim && row + k < a.k_dim; };
     auto load = [&] {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                kv[i][k] = live(k) ? attn_load2<VEC>(a.kv[i] + o + k * a.v_dim) : make_ulonglong2(0ull, 0ull);
-                ms[i][k] = live(k) ? attn_load2<VEC>(a.ms[i] + o + k * a.v_dim) : make_ulonglong2(0ull, 0ull);
+                kv[i][k] = live(k) ? __ldcs(a.kv[i] + o + k * a.v_dim) : 0ull;
+                ms[i][k] = live(k) ? __ldcs(a.ms[i] + o + k * a.v_dim) : 0ull;
             }
     };
     if (c < end) load();
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) S[i][k] = a.S0[i] && live(k) ? attn_load2<VEC>(a.S0[i] + at + k * a.v_dim) : make_ulonglong2(0ull, 0ull);
+        for (int k = 0; k < 4; ++k) S[i][k] = a.S0[i] && live(k) ? __ldcs(a.S0[i] + at + k * a.v_dim) : 0ull;
     const int row0 = col / attn::LEFT * attn::LEFT, rows = min(attn::LEFT, wide - row0);
     for (; c < end; ++c, left -= a.C) {
         const u64 weight = __ldg(w + min(left, a.C));
-        ulonglong2 e[2][4];
-        const size_t here = o;
+        const size_t here = o, block = attn_dim_block(c * a.kv_heads + h, k_blocks, quad >> 3, a.v_dim, row0, attn::LEFT);
+        attn_emit(a.s.set[1] + block, rows, col - row0, quad & 7, ms[0]);
+        attn_emit(a.s.set[2] + block, rows, col - row0, quad & 7, ms[1]);
+        u64 e[2][4];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                e[i][k] = attn_sub(S[i][k], ms[i][k]);
-                S[i][k] = make_ulonglong2(attn_rescale(weight * S[i][k].x + kv[i][k].x, i, a.f), attn_rescale(weight * S[i][k].y + kv[i][k].y, i, a.f));
-                if (live(k)) attn_send2<VEC>(a.Es[i] + here + k * a.v_dim, e[i][k]);
+                e[i][k] = S[i][k] - ms[i][k];
+                S[i][k] = attn_rescale(weight * S[i][k] + kv[i][k], i, a.f);
             }
-        const size_t block = attn_dim_block(c * a.kv_heads + h, k_blocks, quad >> 3, a.v_dim, row0, attn::LEFT);
-        auto emit = [&](int n, const ulonglong2 (&v)[4]) {
-            attn_emit(a.s.set[n] + block, rows, col - row0, quad & 7, v[0].x, v[1].x, v[2].x, v[3].x);
-            attn_emit(a.s.set[n] + block, rows, col - row0 + 1, quad & 7, v[0].y, v[1].y, v[2].y, v[3].y);
-        };
-        emit(1, ms[0]);
-        emit(2, ms[1]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) e[0][k] = attn_add(e[0][k], e[1][k]);        // the exchange
-        emit(0, e[0]);
         o += step;
         if (c + 1 < end) load();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (live(k)) __stcs(a.Es[i] + here + k * a.v_dim, e[i][k]);
+            e[0][k] += e[1][k];                              // the exchange
+        }
+        attn_emit(a.s.set[0] + block, rows, col - row0, quad & 7, e[0]);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            if (live(k)) attn_store2<VEC>(a.S1[i] + at + k * a.v_dim, S[i][k]);
+            if (live(k)) a.S1[i][at + k * a.v_dim] = S[i][k];
 }
 
 // Items: chunks, query heads and parties, the rows of O: for every tile of v_dim the far part w[r + 1] tr(q S), then the near part P v.
@@ -685,6 +699,13 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a) {
         x.rows = min(LEFT, a.v_dim - v0);
         x.cols = len;
         return x;
+    }, [&](int item, int n, const AttnTile& x) {
+        if (n & 1) return;
+        const int ch = item >> 1, c = ch / a.q_heads;
+        const uint32_t o_row = (uint32_t)a.q_heads * a.v_dim;
+        const size_t at = (size_t)a.found[c].x * o_row + (size_t)(ch - c * a.q_heads) * a.v_dim + (n >> 1) * LEFT;
+        attn_ask(attn_of(a.qs, item & 1) + at, x.rows, x.cols, o_row);
+        attn_ask(attn_of(a.pv, item & 1) + at, x.rows, x.cols, o_row);
     }, [&](int item, int n, const AttnTile& x, u64* words) {
         const int i = item & 1, ch = item >> 1, c = ch / a.q_heads, hq = ch - c * a.q_heads, h = hq / (a.q_heads / a.kv_heads), f = a.f;
         const uint32_t o_row = (uint32_t)a.q_heads * a.v_dim;
