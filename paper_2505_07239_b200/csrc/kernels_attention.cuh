@@ -25,7 +25,7 @@ constexpr int THREADS = 256;
 constexpr int LEFT = 128, RIGHT = 64;                // rows of a tile's operands at most
 constexpr int KC = limb::KC, ROW_BYTES = limb::PLANES * KC;          // of a block of planes: 32 contraction indices
 constexpr int SLOTS = 3, LEFT_BYTES = LEFT * ROW_BYTES, SLOT_BYTES = LEFT_BYTES + RIGHT * ROW_BYTES;
-constexpr int DRAINERS = 8, PRODUCER = DRAINERS, ISSUER = DRAINERS + 1, TILE_THREADS = 32 * (ISSUER + 1), DRAIN_THREADS = 32 * DRAINERS;
+constexpr int DRAINERS = 16, PRODUCER = DRAINERS, ISSUER = DRAINERS + 1, TILE_THREADS = 32 * (ISSUER + 1), DRAIN_THREADS = 32 * DRAINERS;
 constexpr int ACC_COLS = limb::PLANES * RIGHT;
 constexpr int TILE_SMEM = SLOTS * SLOT_BYTES + RIGHT * LEFT * 8 + 128;
 constexpr int SLAB = 16;                             // tokens that a CTA opens
@@ -110,11 +110,6 @@ __device__ __forceinline__ ulonglong2 attn_load2(const u64* p) {         // word
     return make_ulonglong2(__ldcs(p), __ldcs(p + 1));
 }
 template <bool VEC>
-__device__ __forceinline__ ulonglong2 attn_keep2(const u64* p) {         // words that the same kernel reads again
-    if (VEC) return *reinterpret_cast<const ulonglong2*>(p);
-    return make_ulonglong2(p[0], p[1]);
-}
-template <bool VEC>
 __device__ __forceinline__ void attn_send2(u64* p, ulonglong2 v) {       // a message or result: nobody here reads it
     if (VEC) {
         __stcs(reinterpret_cast<ulonglong2*>(p), v);
@@ -134,7 +129,6 @@ __device__ __forceinline__ void attn_store2(u64* p, ulonglong2 v) {
 }
 
 __device__ __forceinline__ ulonglong2 attn_input2(const u64* p, int vec) { return vec ? attn_load2<true>(p) : attn_load2<false>(p); }
-__device__ __forceinline__ ulonglong2 attn_sub(ulonglong2 x, ulonglong2 y) { return make_ulonglong2(x.x - y.x, x.y - y.y); }
 __device__ __forceinline__ ulonglong2 attn_add(ulonglong2 x, ulonglong2 y) { return make_ulonglong2(x.x + y.x, x.y + y.y); }
 __device__ __forceinline__ u64 attn_rescale(u64 v, int party, int f) { return party ? 0ull - norm_shift(0ull - v, f) : norm_shift(v, f); }
 
@@ -145,23 +139,34 @@ __device__ __forceinline__ size_t attn_dim_block(int ch, int blocks, int b, int 
     const int wide = attn::up16(dim);
     return ((size_t)ch * blocks * wide + (size_t)row0 * blocks + (size_t)b * min(tile, wide - row0)) * attn::ROW_BYTES;
 }
-// Four words of a row, indices 4 quad and on, into a block of `rows` rows.
-__device__ __forceinline__ void attn_emit(uint8_t* block, int rows, int row, int quad, const u64 (&w)[4]) {
-    limb_emit4(block + (row >> 3) * 256 + (quad >> 2) * 128 + (row & 7) * 16 + (quad & 3) * 4, rows * attn::KC, w);
+// Words of a row, `n` of them from index `first` on (a multiple of n), into a block of `rows` rows: n bytes a plane at once.
+__device__ __forceinline__ uint8_t* attn_spot(uint8_t* block, int row, int first) {
+    return block + (row >> 3) * 256 + (first >> 4) * 128 + (row & 7) * 16 + (first & 15);
 }
-__device__ __forceinline__ void attn_emit(uint8_t* block, int rows, int row, int quad, u64 w0, u64 w1, u64 w2, u64 w3) {
-    const u64 w[4] = {w0, w1, w2, w3};
-    attn_emit(block, rows, row, quad, w);
+__device__ __forceinline__ void attn_bytes(const u64* w, uint32_t (&p)[limb::PLANES]) {
+    limb_transpose4((uint32_t)w[0], (uint32_t)w[1], (uint32_t)w[2], (uint32_t)w[3], p[0], p[1], p[2], p[3]);
+    limb_transpose4((uint32_t)(w[0] >> 32), (uint32_t)(w[1] >> 32), (uint32_t)(w[2] >> 32), (uint32_t)(w[3] >> 32), p[4], p[5], p[6], p[7]);
+}
+__device__ __forceinline__ void attn_emit(uint8_t* block, int rows, int row, int first, const u64 (&w)[4]) {
+    limb_emit4(attn_spot(block, row, first), rows * attn::KC, w);
+}
+__device__ __forceinline__ void attn_emit(uint8_t* block, int rows, int row, int first, const u64 (&w)[8]) {
+    uint32_t lo[limb::PLANES], hi[limb::PLANES];
+    attn_bytes(w, lo);
+    attn_bytes(w + 4, hi);
+    uint8_t* const to = attn_spot(block, row, first);
+#pragma unroll
+    for (int p = 0; p < limb::PLANES; ++p) *reinterpret_cast<uint2*>(to + p * rows * attn::KC) = make_uint2(lo[p], hi[p]);
 }
 
 // Messages of k, d, v or q of a head and SLAB tokens of a chunk, and the planes of what they open; zeros where no weight is sent.  Bound by
-// memory: 4 words in and 5 out of every word of q and k, 8 and 10 of d, v.  q and k: eight lanes a row's 32 words, four words each.  v and
-// d, whose contraction runs over the tokens: four tokens of a word a thread, sixteen tokens x eight words a warp, 64 bytes of a token, 128 of a plane.
+// memory: of a word and party two in, one out as a message, and three sets of planes for both parties.  q and k: eight words of a row a thread, four
+// threads a row's 32 words.  v and d, whose contraction runs over the tokens: eight tokens of a word a thread, sixteen tokens x sixteen words a
+// warp, 128 bytes of a token.  Eight bytes a plane at once either way, 256 bytes a warp, whole sectors.
 template <bool VEC>
 __global__ void __launch_bounds__(attn::THREADS, 2)
 attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
     pdl_wait();
-    pdl_launch_dependents();
     const int c = blockIdx.x / slabs, t0 = (blockIdx.x - c * slabs) * attn::SLAB;
     const AttnChunk at = attn_find(a, c);
     if (blockIdx.x == c * slabs && blockIdx.y == 0 && threadIdx.x == 0) a.found[c] = make_int2(at.first, at.len);
@@ -169,40 +174,44 @@ attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
     if (t0 >= attn::blocks(at.len) * attn::KC) return;
     const int f = a.f;
     // rows of queries or keys: messages, and the planes of the opened value, party 0's mask, party 1's or V_1
-    auto open_rows = [&](const u64* const x[2], long long stride, const u64* const m[2], u64* const msg[2], const AttnPlanes& to, int heads, int head, bool sum) {
-        const int quads = attn::blocks(a.k_dim) * 8;
+    auto open_rows = [&](const u64* const x[2], long long stride, const u64* const m[2], u64* const msg[2], const AttnPlanes& to, int heads, int head, bool query) {
+        const int parts = attn::blocks(a.k_dim) * 4;
         const size_t o0 = ((size_t)first * heads + head) * a.k_dim;
-        for (int t = threadIdx.x; t < rows * quads; t += attn::THREADS) {
-            const int r = t / quads, quad = t - r * quads;
-            const size_t o = o0 + (size_t)r * heads * a.k_dim + 4 * quad;
-            const long long from = (long long)(first + r) * stride + (long long)head * a.k_dim + 4 * quad;
-            ulonglong2 e[2][2], mask[2][2];
+        for (int t = threadIdx.x; t < rows * parts; t += attn::THREADS) {
+            const int r = t / parts, part = t - r * parts;
+            const size_t o = o0 + (size_t)r * heads * a.k_dim + 8 * part;
+            const long long from = (long long)(first + r) * stride + (long long)head * a.k_dim + 8 * part;
+            u64 e[2][8], mask[2][8];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 8; h += 2)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    e[i][h] = mask[i][h] = make_ulonglong2(0ull, 0ull);
-                    if (4 * quad + 2 * h < a.k_dim) {
-                        e[i][h] = attn_input2(x[i] + from + 2 * h, a.in_vec);
-                        mask[i][h] = attn_load2<VEC>(m[i] + o + 2 * h);
+                    ulonglong2 v = make_ulonglong2(0ull, 0ull), k = v;
+                    if (8 * part + h < a.k_dim) {
+                        v = attn_input2(x[i] + from + h, a.in_vec);
+                        k = attn_load2<VEC>(m[i] + o + h);
                     }
+                    e[i][h] = v.x; e[i][h + 1] = v.y;
+                    mask[i][h] = k.x; mask[i][h + 1] = k.y;
                 }
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 8; h += 2) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    e[i][h] = attn_sub(e[i][h], mask[i][h]);
-                    if (4 * quad + 2 * h < a.k_dim) attn_send2<VEC>(msg[i] + o + 2 * h, e[i][h]);
+                    e[i][h] -= mask[i][h];
+                    e[i][h + 1] -= mask[i][h + 1];
+                    if (8 * part + h < a.k_dim) attn_send2<VEC>(msg[i] + o + h, make_ulonglong2(e[i][h], e[i][h + 1]));
                 }
-            const ulonglong2 y0 = attn_add(e[0][0], e[1][0]), y1 = attn_add(e[0][1], e[1][1]);             // the exchange
-            if (sum) {
-                mask[1][0] = attn_add(mask[1][0], y0);
-                mask[1][1] = attn_add(mask[1][1], y1);
+#pragma unroll
+                for (int n = h; n < h + 2; ++n) {
+                    e[0][n] += e[1][n];                                                                    // the exchange
+                    if (query) mask[1][n] += e[0][n];
+                }
             }
-            const size_t block = attn_token_block(c * heads + head, quads / 8, quad / 8, a.C);
-            attn_emit(to.set[0] + block, rows16, t0 + r, quad & 7, y0.x, y0.y, y1.x, y1.y);
-            attn_emit(to.set[1] + block, rows16, t0 + r, quad & 7, mask[0][0].x, mask[0][0].y, mask[0][1].x, mask[0][1].y);
-            attn_emit(to.set[2] + block, rows16, t0 + r, quad & 7, mask[1][0].x, mask[1][0].y, mask[1][1].x, mask[1][1].y);
+            const size_t block = attn_token_block(c * heads + head, parts / 4, part / 4, a.C);
+            attn_emit(to.set[0] + block, rows16, t0 + r, part % 4 * 8, e[0]);
+            attn_emit(to.set[1] + block, rows16, t0 + r, part % 4 * 8, mask[0]);
+            attn_emit(to.set[2] + block, rows16, t0 + r, part % 4 * 8, mask[1]);
         }
     };
     // values or decayed keys, `dim` words a token in tiles of `tile`; tokens behind the last count as zero
@@ -210,14 +219,14 @@ attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
                          int head, const u64* w, bool sum) {
         const int all = attn::up16(dim);
         const size_t o0 = ((size_t)first * a.kv_heads + head) * dim, row = (size_t)a.kv_heads * dim;
-        for (int t = threadIdx.x; t < 4 * all; t += attn::THREADS) {
-            const int quad = (t >> 3) & 3, j = (t & 7) + (t >> 5) * 8;
-            u64 e[2][4], mask[2][4];
+        for (int t = threadIdx.x; t < 2 * all; t += attn::THREADS) {
+            const int r0 = (t >> 4 & 1) * 8, j = (t & 15) + (t >> 5) * 16;
+            u64 e[2][8], mask[2][8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < 8; ++k)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const int r = 4 * quad + k;
+                    const int r = r0 + k;
                     e[i][k] = mask[i][k] = 0ull;
                     if (r < rows && j < dim) {
                         e[i][k] = __ldcs(x[i] + (long long)(first + r) * stride + (long long)head * dim + j);
@@ -225,8 +234,8 @@ attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
                     }
                 }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int r = 4 * quad + k;
+            for (int k = 0; k < 8; ++k) {
+                const int r = r0 + k;
                 const u64 weight = w && r < rows ? __ldg(w - r) : 1ull;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
@@ -237,11 +246,11 @@ attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
                 e[0][k] += e[1][k];                                                                        // the exchange
                 if (sum) mask[1][k] += e[0][k];
             }
-            const int row0 = j / tile * tile, wide = min(tile, all - row0), token = t0 / 4 + quad;
-            const size_t block = attn_dim_block(c * a.kv_heads + head, blocks, token / 8, dim, row0, tile);
-            attn_emit(to.set[0] + block, wide, j - row0, token & 7, e[0]);
-            attn_emit(to.set[1] + block, wide, j - row0, token & 7, mask[0]);
-            attn_emit(to.set[2] + block, wide, j - row0, token & 7, mask[1]);
+            const int row0 = j / tile * tile, wide = min(tile, all - row0), token = t0 + r0;
+            const size_t block = attn_dim_block(c * a.kv_heads + head, blocks, token / attn::KC, dim, row0, tile);
+            attn_emit(to.set[0] + block, wide, j - row0, token % attn::KC, e[0]);
+            attn_emit(to.set[1] + block, wide, j - row0, token % attn::KC, mask[0]);
+            attn_emit(to.set[2] + block, wide, j - row0, token % attn::KC, mask[1]);
         }
     };
     const int what = min(3, (int)blockIdx.y / a.kv_heads), h = blockIdx.y - what * a.kv_heads;
@@ -425,7 +434,7 @@ __device__ __forceinline__ void attn_tiles(uint8_t* raw, int items, int* error, 
                 if (ok) {
                     ptx::fence_after_sync();
                     if (quarter * 32 < x.rows)
-                        for (int c = (warp >> 2) * 8; c < x.cols; c += 16) {
+                        for (int c = (warp >> 2) * 8; c < x.cols; c += 2 * DRAINERS) {
                             uint32_t d[limb::PLANES][8];
 #pragma unroll
                             for (int p = 0; p < limb::PLANES; ++p) ptx::tmem_ld8(lanes + cols * p + c, d[p]);
@@ -481,7 +490,6 @@ __global__ void __launch_bounds__(attn::TILE_THREADS, 1)
 attn_products_kernel(const __grid_constant__ AttnArgs a) {
     extern __shared__ uint8_t attn_smem[];
     pdl_wait();
-    pdl_launch_dependents();
     using namespace attn;
     const int key_items = a.chunks * a.kv_heads, v_tiles = (a.v_dim + LEFT - 1) / LEFT, k_tiles = (a.k_dim + RIGHT - 1) / RIGHT;
     const int t_blocks = blocks(a.C), k_blocks = blocks(a.k_dim);
@@ -582,12 +590,12 @@ attn_products_kernel(const __grid_constant__ AttnArgs a) {
                     e[j] += kept[j];                     // the exchange
                     m[j] += e[j];
                 }
-                attn_emit(a.p.set[0] + block, rows16, r, quad & 7, e);
+                attn_emit(a.p.set[0] + block, rows16, r, 4 * (quad & 7), e);
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) kept[j] = e[j];
             }
-            attn_emit((i ? a.p.set[2] : a.p.set[1]) + block, rows16, r, quad & 7, m);
+            attn_emit((i ? a.p.set[2] : a.p.set[1]) + block, rows16, r, 4 * (quad & 7), m);
         }
     });
 }
@@ -597,7 +605,6 @@ __global__ void __launch_bounds__(attn::STATE_THREADS)
 attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
     __shared__ int before;
     pdl_wait();
-    pdl_launch_dependents();
     const int j = blockIdx.x / (a.kv_heads * pieces), rest = blockIdx.x - j * a.kv_heads * pieces, h = rest / pieces;
     const int t = (rest - h * pieces) * attn::STATE_THREADS + threadIdx.x, k_blocks = attn::blocks(a.k_dim), wide = attn::up16(a.v_dim);
     if (threadIdx.x == 0) before = 0;
@@ -643,8 +650,8 @@ attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
     for (; c < end; ++c, left -= a.C) {
         const u64 weight = __ldg(w + min(left, a.C));
         const size_t here = o, block = attn_dim_block(c * a.kv_heads + h, k_blocks, quad >> 3, a.v_dim, row0, attn::LEFT);
-        attn_emit(a.s.set[1] + block, rows, col - row0, quad & 7, ms[0]);
-        attn_emit(a.s.set[2] + block, rows, col - row0, quad & 7, ms[1]);
+        attn_emit(a.s.set[1] + block, rows, col - row0, 4 * (quad & 7), ms[0]);
+        attn_emit(a.s.set[2] + block, rows, col - row0, 4 * (quad & 7), ms[1]);
         u64 e[2][4];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -662,7 +669,7 @@ attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
                 if (live(k)) __stcs(a.Es[i] + here + k * a.v_dim, e[i][k]);
             e[0][k] += e[1][k];                              // the exchange
         }
-        attn_emit(a.s.set[0] + block, rows, col - row0, quad & 7, e[0]);
+        attn_emit(a.s.set[0] + block, rows, col - row0, 4 * (quad & 7), e[0]);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -677,7 +684,6 @@ __global__ void __launch_bounds__(attn::TILE_THREADS, 1)
 attn_rows_kernel(const __grid_constant__ AttnArgs a) {
     extern __shared__ uint8_t attn_smem[];
     pdl_wait();
-    pdl_launch_dependents();
     using namespace attn;
     const int v_tiles = (a.v_dim + LEFT - 1) / LEFT, t_blocks = blocks(a.C), k_blocks = blocks(a.k_dim);
     attn_tiles(attn_smem, 2 * a.chunks * a.q_heads, a.error, [&](int item) { return a.found[(item >> 1) / a.q_heads].y == 0 ? 0 : 2 * v_tiles; },
@@ -769,7 +775,6 @@ attn_step_kernel(const __grid_constant__ AttnStepArgs a) {
     const int col = 2 * (mine ? pair : 0);
     const size_t k_at = (size_t)bh * a.k_dim, v_at = (size_t)bh * a.v_dim, q_at = k_at * group, o_at = v_at * group, s_at = k_at * a.v_dim + col;
     pdl_wait();
-    pdl_launch_dependents();
     // a row's words: state, product, mask
     ulonglong2 S[2], kv[2], ms[2];
     auto load = [&](int r) {

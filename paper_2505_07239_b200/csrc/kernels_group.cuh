@@ -291,7 +291,6 @@ group_tile_kernel(const __grid_constant__ GroupArgs a) {
     const bool live = sub < groups;
     const int group = first + (live ? sub : 0);
     pdl_wait();
-    pdl_launch_dependents();
     GroupOwn<W, ACC> own;
     u64 sum[2], sq[2];
     own.open(a, group, quad, quads, live, places + threadIdx.x * W, blockDim.x, sum);
@@ -358,7 +357,6 @@ group_cluster_kernel(const __grid_constant__ GroupArgs a) {
     // (a CTA's shared memory is written to by the others when it has begun)
     if (cluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     pdl_wait();
-    pdl_launch_dependents();
     GroupOwn<W, ACC> own;
     u64 sum[2], sq[2];
     own.open(a, group, (int)(rank * blockDim.x + threadIdx.x), (int)(cluster * blockDim.x), true, places + threadIdx.x * W, blockDim.x, sum);
@@ -483,7 +481,6 @@ template <int W>
 __global__ void __launch_bounds__(group::SLAB_THREADS)
 group_sum_kernel(const __grid_constant__ GroupArgs a) {
     pdl_wait();
-    pdl_launch_dependents();
     const GroupSlab s = group_slab<W>(a);
     u64 sum[2] = {0ull, 0ull};
     if (s.channel >= 0) {
@@ -508,7 +505,6 @@ __global__ void __launch_bounds__(group::SLAB_THREADS)
 group_open_kernel(const __grid_constant__ GroupArgs a) {
     __shared__ u64 means[group::SLAB_GROUPS][2];
     pdl_wait();
-    pdl_launch_dependents();
     const GroupSlab s = group_slab<W>(a);
     for (int k = threadIdx.x; k < 2 * s.groups; k += blockDim.x) {
         const u64 t = a.sums[((size_t)s.sample * a.groups + s.group0) * 2 + k];
@@ -555,7 +551,6 @@ group_apply_kernel(const __grid_constant__ GroupArgs a) {
     u64* const words = reinterpret_cast<u64*>(group_smem);               // [party][group][count], party 1's negated
     u64* const opened = words + 2 * a.tile_groups * count;               // [party][group][sent]
     pdl_wait();
-    pdl_launch_dependents();
     const GroupSlab s = group_slab<W>(a);
     const size_t first = (size_t)s.sample * a.groups + s.group0;
     for (int k = threadIdx.x; k < s.groups * count; k += blockDim.x) {
