@@ -2720,8 +2720,8 @@ bool group_sizes(int64_t samples, int64_t positions, int64_t channels, int64_t g
     return positions <= 1 << 24 && positions * (channels / groups) <= 1 << 24 && samples * groups <= 1 << 24;
 }
 // How long groups are cut: tiles of whole groups, up to SLAB_GROUPS of them and as many channels as a CTA has threads of `wide` words, or parts of
-// one group; slabs of positions until there are eight CTAs an SM.
-void group_slabs(comet::GroupArgs& a, int samples, int wide, int sm_count) {
+// one group; slabs of positions until there are eight CTAs an SM, or for the last pass as many as run at once.
+void group_slabs(comet::GroupArgs& a, int samples, int wide, int sm_count, bool apply) {
     namespace gr = comet::group;
     const int most = gr::SLAB_THREADS * wide;
     a.parts = ceil_div(a.per, most);
@@ -2736,7 +2736,8 @@ void group_slabs(comet::GroupArgs& a, int samples, int wide, int sm_count) {
         a.units = gr::SLAB_THREADS;
     }
     a.subs = std::max(1, gr::SLAB_THREADS / a.units);
-    const int64_t columns = (int64_t)samples * a.tiles, want = std::max<int64_t>(1, ((int64_t)sm_count * 8 + columns - 1) / columns);
+    const int64_t columns = (int64_t)samples * a.tiles, once = (int64_t)sm_count * (gr::SLAB_APPLY / (ceil_div(a.units * a.subs, 32) * 32));
+    const int64_t want = std::max<int64_t>(1, apply ? once / columns : ((int64_t)sm_count * 8 + columns - 1) / columns);
     a.slab = (int)std::max<int64_t>(a.subs, (a.positions + want - 1) / want);
     a.slab = ceil_div(a.slab, a.subs) * a.subs;
     a.slabs = ceil_div(a.positions, a.slab);
@@ -2861,15 +2862,17 @@ extern "C" int comet_group_norm(void* cuda_stream, const comet_group_norm_args* 
                               (const void*)a.VW[i], (const void*)a.R[i], (const void*)a.Q[i], (const void*)a.N[i]})
             vec = vec && aligned16(p);
     if (a.count <= GROUP_HELD) return launch_group(a, vec, stream);
-    group_slabs(a, g->samples, vec ? 2 : 1, dev.sm_count);
-    const int64_t blocks = S * a.tiles * a.slabs;
-    if (blocks > 0x7fffffffll) return COMET_ERR_SHAPE;
+    group_slabs(a, g->samples, vec ? 2 : 1, dev.sm_count, false);
+    comet::GroupArgs last = a;
+    group_slabs(last, g->samples, vec ? 2 : 1, dev.sm_count, true);
+    const int64_t blocks = S * a.tiles * a.slabs, last_blocks = S * a.tiles * last.slabs;
+    if (blocks > 0x7fffffffll || last_blocks > 0x7fffffffll) return COMET_ERR_SHAPE;
     const dim3 grid((unsigned)blocks), block(ceil_div(a.units * a.subs, 32) * 32);
     const size_t words = (size_t)a.tile_groups * nm::row_bytes(a.root.steps);
     cudaError_t err = cudaMemsetAsync(a.sums, 0, (size_t)need, stream);
     if (err == cudaSuccess) err = launch_chained(vec ? comet::group_sum_kernel<2> : comet::group_sum_kernel<1>, grid, block, 0, stream, nullptr, a);
     if (err == cudaSuccess) err = launch_chained(vec ? comet::group_open_kernel<2> : comet::group_open_kernel<1>, grid, block, 0, stream, nullptr, a);
-    if (err == cudaSuccess) err = launch_chained(vec ? comet::group_apply_kernel<2> : comet::group_apply_kernel<1>, grid, block, words, stream, nullptr, a);
+    if (err == cudaSuccess) err = launch_chained(vec ? comet::group_apply_kernel<2> : comet::group_apply_kernel<1>, dim3((unsigned)last_blocks), block, words, stream, nullptr, last);
     if (err != cudaSuccess) cudaGetLastError();
     return err == cudaSuccess ? COMET_OK : COMET_ERR_CUDA;
 }

@@ -7,7 +7,11 @@
 //   single tokens:  S <- tr(w S + k v^T),  o = tr(q S)
 // Four kernels for a prompt: all values that need no product are opened (open); the products d v^T of all chunks and key heads and the weights P
 // of all chunks and query heads (products); the states from chunk to chunk, a word a thread (state); the rows of O (rows).  What enters a product is
-// cut into bytes by the kernel that has it in registers anyway, once, so that those of the products only copy, multiply and add.
+// cut into bytes by the kernel that has it in registers anyway, once, so that those of the products only copy, multiply and add.  (The bytes are
+// as many as the words: the same traffic, and no warp of a product's kernel converts.  512 tokens x 32 heads x 128, "the case" below: words cut
+// into bytes by warps beside the issuer 438 us, by every warp for its own mma.sync 679, this 371, of which memory's floor is 108.)
+// None of these kernels lets the next one's CTAs in before its end (pdl_launch_dependents): they would hold registers and shared memory of SMs that
+// still have work, where the kernel that opens the next pass's values holds most.  With it 468 us.
 #pragma once
 #include <cstdint>
 #include <type_traits>
@@ -163,6 +167,7 @@ __device__ __forceinline__ void attn_emit(uint8_t* block, int rows, int row, int
 // memory: of a word and party two in, one out as a message, and three sets of planes for both parties.  q and k: eight words of a row a thread, four
 // threads a row's 32 words.  v and d, whose contraction runs over the tokens: eight tokens of a word a thread, sixteen tokens x sixteen words a
 // warp, 128 bytes of a token.  Eight bytes a plane at once either way, 256 bytes a warp, whole sectors.
+// The case: 118 us, 570 MB; four bytes a plane at once took 135 us, a third CTA an SM (80 registers) 135 as well.
 template <bool VEC>
 __global__ void __launch_bounds__(attn::THREADS, 2)
 attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
@@ -273,9 +278,11 @@ attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
 
 // ---------------------------------------------------------------------------
 // Products: tiles of up to 128 x 64 words of Z_i - C_i = E B_i + V_i F (Eq. 1) on the int8 tensor cores.  A warp copies blocks of planes to shared memory,
-// a warp issues the MMAs, eight warps read the sums out of tensor memory to shared memory, which gives tensor memory back for the next tile, and
+// a warp issues the MMAs, sixteen warps read the sums out of tensor memory to shared memory, which gives tensor memory back for the next tile, and
 // add them to what comes from memory.  Left operands are keys, values or states, right ones queries, weights or decayed keys; a left operand
-// of less than 128 rows has rows behind it that are whatever lies there, whose sums are never looked at.
+// of less than 128 rows has rows behind it that are whatever lies there, whose sums are never looked at.  Sixteen warps read and add, since what
+// they add comes from memory: the case took 2 % longer with eight.  One CTA an SM: the eight accumulators of 64 columns are all of an SM's tensor
+// memory, so a tile's products wait until the sums before them have gone to shared memory.
 // ---------------------------------------------------------------------------
 struct AttnOperand {
     const uint8_t* open; const uint8_t* own;             // the first blocks; V_i or the party's mask
@@ -484,7 +491,8 @@ __device__ __forceinline__ void attn_finish(u64* words, int rows, int cols, L&& 
         }
 }
 
-// Items: chunks and key heads, the sums of d v^T, tiles of party, v_dim and k_dim; then chunks and query heads, the weights, a tile a party.
+// Items: chunks and key heads, the sums of d v^T, tiles of party, v_dim and k_dim; then chunks and query heads, the weights, a tile a party.  Both only
+// need what was opened, so they share a launch: 97 us for the case, tensor pipe 42 %, 410 MB.
 template <bool VEC>
 __global__ void __launch_bounds__(attn::TILE_THREADS, 1)
 attn_products_kernel(const __grid_constant__ AttnArgs a) {
@@ -601,6 +609,9 @@ attn_products_kernel(const __grid_constant__ AttnArgs a) {
 }
 
 // The state from chunk to chunk of a sequence and key head, four words of a column and both parties a thread; says whether the starts were in order.
+// Bound by memory: the next chunk's words are on their way while this one's are worked on.  49 us for the case, 290 MB (5.9 TB/s).  Carried along by
+// the kernel of the products, tile by tile in shared memory, it saved the 134 MB of sums, but left few warps an SM to wait for memory: 152 us for both, where
+// the two kernels take 146.
 __global__ void __launch_bounds__(attn::STATE_THREADS)
 attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
     __shared__ int before;
@@ -678,7 +689,8 @@ attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
             if (live(k)) a.S1[i][at + k * a.v_dim] = S[i][k];
 }
 
-// Items: chunks, query heads and parties, the rows of O: for every tile of v_dim the far part w[r + 1] tr(q S), then the near part P v.
+// Items: chunks, query heads and parties, the rows of O: for every tile of v_dim the far part w[r + 1] tr(q S), then the near part P v, which is added to what
+// the far part left in shared memory.  80 us for the case, tensor pipe 40 %, 360 MB.
 template <bool VEC>
 __global__ void __launch_bounds__(attn::TILE_THREADS, 1)
 attn_rows_kernel(const __grid_constant__ AttnArgs a) {

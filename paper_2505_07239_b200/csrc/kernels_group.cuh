@@ -16,7 +16,7 @@
 namespace comet {
 
 namespace group {
-constexpr int SLAB_THREADS = 256, SLAB_GROUPS = 32;  // at most, of a CTA that has a slab of long groups; its groups
+constexpr int SLAB_THREADS = 256, SLAB_GROUPS = 32, SLAB_APPLY = 768;  // at most, of a CTA that has a slab of long groups; its groups
 constexpr int TILE_THREADS = 128, TILE_WORDS = 4 * TILE_THREADS, TILE_GROUPS = 16, TILE_CTAS = 5;
 constexpr int CLUSTER_THREADS = 256, MAX_CLUSTER = 8, CLUSTER_CTAS = 2;
 constexpr int TABLE = 1024;                          // channels of a group that a CTA keeps the products of root and gain of
@@ -541,9 +541,10 @@ group_open_kernel(const __grid_constant__ GroupArgs a) {
     group_gather(a, s, a.sums + 2 * (size_t)a.all, sq);
 }
 
-// Every CTA works out the roots of its groups, a pair of lanes each; then every thread the scale of its column.
+// Every CTA works out the roots of its groups, a pair of lanes each; then every thread the scale of its column.  A chain of products that takes some
+// microseconds before the first word: so there are no more CTAs than run at once (SLAB_APPLY threads an SM).
 template <int W>
-__global__ void __launch_bounds__(group::SLAB_THREADS)
+__global__ void __launch_bounds__(group::SLAB_THREADS, group::SLAB_APPLY / group::SLAB_THREADS)
 group_apply_kernel(const __grid_constant__ GroupArgs a) {
     extern __shared__ __align__(16) uint8_t group_smem[];
     __shared__ u64 roots[group::SLAB_GROUPS];
