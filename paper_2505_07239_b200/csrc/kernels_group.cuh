@@ -275,7 +275,8 @@ struct GroupOwn {
 };
 
 // Groups of up to TILE_WORDS words: a CTA has as many as its threads cover, four words a thread; one warp works out their means and roots, a pair
-// of lanes a group.
+// of lanes a group.  512 tokens x 32 heads of 128 with activation: 91 us, 0.66 of the measured copy rate; a CTA's five sit on an SM, and the chain of a
+// root's products, some 7 us, is what they cover for one another.
 template <int W>
 __global__ void __launch_bounds__(group::TILE_THREADS, group::TILE_CTAS)
 group_tile_kernel(const __grid_constant__ GroupArgs a) {
@@ -431,7 +432,8 @@ group_cluster_kernel(const __grid_constant__ GroupArgs a) {
 
 // ---------------------------------------------------------------------------
 // Groups that fit no cluster: three passes over slabs of positions, the sums of a group gathered by 64-bit additions, which are exact in any
-// order.  What the second and third pass read again is the L2's where it fits.
+// order.  What the second and third pass read again is the L2's where it fits.  4096 positions x 320 channels in 32 groups: 11 + 15 + 38 us by themselves, 60 a
+// pass; 8 x 1024 x 640 in 32: 19 + 45 + 122, 191.  Of 16 arrays that have to move 6 move twice.
 // A CTA has a slab of a tile of channels, whole groups or a part of one, a thread a column of W channels of it in every `subs`-th position.
 // ---------------------------------------------------------------------------
 struct GroupSlab {
