@@ -624,7 +624,7 @@ attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
     int sum = 0, begin;
     bool bad = false;
     for (int s = threadIdx.x; s < (checks ? a.sequences : j); s += attn::STATE_THREADS) {
-        sum += (attn_length(a, s, &begin) + a.C - 1) / a.C;
+        sum = min(sum + (attn_length(a, s, &begin) + a.C - 1) / a.C, a.chunks + 1);      // (starts out of order may have more than an int of chunks)
         const int end = a.starts[s + 1];
         bad |= begin < 0 || end < begin || end > a.tokens;
     }

@@ -251,6 +251,22 @@ def test_another_number_of_chunks(cb, n):  # noqa: F811
         assert np.array_equal(got["s"][i], ref["s"][i][:n])
 
 
+def test_starts_with_more_chunks_than_an_int_counts(cb):  # noqa: F811
+    """Starts that go back and forth over 2^20 tokens, chunks of one: 2^31 of them and more, of which four are asked for."""
+    T, n, times = 1 << 20, 4, 2100
+    case = ring_prompt(9, [0, n], 1, 1, 2, 2, 1, 16, tokens=T)
+    ref = attention.linear_attention(**case)
+    many = pair(9, "more", 2 * times - 1, 1, 2, 2)
+    for i in (0, 1):
+        many[i][0] = case["state"][i][0]
+    got, flag = run_raw(cb, dict(case, starts=[0, T] * times, state=many))
+    assert flag == 1
+    for i in (0, 1):
+        assert np.array_equal(got["O"][i][:n], ref["O"][i][:n]) and (got["O"][i][n:] == 77).all()
+        assert np.array_equal(got["s"][i], ref["s"][i])
+        assert np.array_equal(got["S"][i][0], ref["S"][i][0]) and np.array_equal(got["S"][i][1:], many[i][1:])
+
+
 def test_state_in_place(cb):  # noqa: F811
     case = ring_step(12, 4, 4, 2, 64, 48, 16)
     ref = attention.linear_attention_step(**case)
