@@ -604,14 +604,15 @@ int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args* args);
  * chunk]; pv, qs, O [tokens, q_heads, v_dim]; ms, dv, Es [chunks, kv_heads, k_dim, v_dim]; state, state_out [sequences, kv_heads, k_dim,
  * v_dim]; decay [kv_heads, chunk + 1] (single tokens: [kv_heads], w[1] alone); starts [sequences + 1].  `state` may be null: zero.
  * `state_out` may be `state`, word for word; nothing else that is written may overlap another argument.
- * Rows of tokens that are in no sequence stay as they are in every result.  Where the starts are not ascending or leave the tokens, that
+ * Rows of tokens that are in no chunk, and states in Es of chunks that there are not, stay as they are in every result, or are set to zero where
+ * `zero_unwritten` is 1: for messages in memory that held something else before.  Where the starts are not ascending or leave the tokens, that
  * sequence counts as empty; where the chunks are more than `chunks` the surplus ones are not worked out; either way, and where they are
  * fewer, `bad_starts_flag` (device int32, may be null) is set to 1.  The caller clears the flag.
  * Stateless; DEVICE pointers on the current device, owned by the caller, 8-byte aligned.  The work is enqueued on `cuda_stream` (NULL =
  * default stream) and the call does not wait for it.  `workspace` is 256-byte aligned and has at least the bytes that
  * comet_linear_attention_workspace reports for these sizes; a captured call keeps its address, and calls whose work may overlap in
  * time need one each.
- * Errors: INVALID_ARG (null or unaligned pointer, overlap), SHAPE (a size below 1, but for chunks; kv_heads not a divisor of q_heads; q_heads above
+ * Errors: INVALID_ARG (null or unaligned pointer, overlap, a `zero_unwritten` that is neither 0 nor 1), SHAPE (a size below 1, but for chunks; kv_heads not a divisor of q_heads; q_heads above
  * 4096; k_dim or v_dim odd or above 256; chunk above 64; tokens, sequences or chunks above 2^20; tokens * q_heads or chunks * q_heads above 2^24; batch *
  * q_heads above 2^24; a stride below its heads' words or above 2^32; frac_bits outside [1, 31]; workspace too small), CUDA. */
 typedef struct {
@@ -645,6 +646,7 @@ typedef struct {
     int32_t* bad_starts_flag;
     void* workspace;
     int64_t workspace_bytes;
+    int32_t zero_unwritten;         /* 0 or 1                                              */
 } comet_linear_attention_args;
 int comet_linear_attention(void* cuda_stream, const comet_linear_attention_args* args);
 /* Bytes of workspace that comet_linear_attention takes for these sizes.  Errors: INVALID_ARG, SHAPE. */

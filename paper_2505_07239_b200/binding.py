@@ -80,7 +80,8 @@ class CometLinearAttentionArgs(ctypes.Structure):
         (n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride")] + [("frac_bits", ctypes.c_int32)] + [
         (n, ctypes.c_void_p) for n in ("starts", "decay")] + [(n, ctypes.c_void_p * 2) for n in (
             "Q", "K", "V", "mq", "mk", "mv", "md", "mp", "ms", "qk", "pv", "qs", "dv", "state", "Eq", "Ek", "Ev", "Ed", "Ep", "Es", "O",
-            "state_out")] + [("bad_starts_flag", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
+            "state_out")] + [("bad_starts_flag", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64),
+        ("zero_unwritten", ctypes.c_int32)]
 
 
 class CometLinearAttentionStepArgs(ctypes.Structure):
@@ -554,7 +555,7 @@ def linear_attention(Q, K, V, starts, decay, dealer: PromptDealer, frac_bits: in
     GPU, sequence j the tokens from starts[j] to before starts[j + 1].  decay: public powers [Hk, C + 1] at scale f, of exponents 0 to C; C, at most 64,
     is the length of a chunk.  state: None (zero) or a pair [sequences, Hk, Dk, Dv].
     Returns (PromptMessages, O, state behind the last tokens): new tensors, each share of a result in memory of its own; a party's messages
-    may lie together in one piece, none of the other party's words in it.  Rows of tokens in no sequence are not written.
+    may lie together in one piece, none of the other party's words in it.  Rows of tokens in no sequence, and messages of states that no chunk finds, are zero.
     """
     code, *m, O, S = _native.linear_attention(stream, Q, K, V, starts, decay, dealer, frac_bits, state, bad_starts_flag)
     if code:

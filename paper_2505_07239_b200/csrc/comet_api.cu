@@ -2574,6 +2574,7 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
     if (g->sequences * Hk > ATTN_MAX_ROWS) return COMET_ERR_SHAPE;
     if (!attn_stride(g->q_stride, T, Hq * Dk) || !attn_stride(g->k_stride, T, Hk * Dk) || !attn_stride(g->v_stride, T, Hk * Dv)) return COMET_ERR_SHAPE;
     if (g->frac_bits < 1 || g->frac_bits > 31) return COMET_ERR_SHAPE;
+    if (g->zero_unwritten != 0 && g->zero_unwritten != 1) return COMET_ERR_INVALID_ARG;
     if (!g->starts || !g->decay || reinterpret_cast<uintptr_t>(g->starts) % sizeof(int32_t) || reinterpret_cast<uintptr_t>(g->decay) % sizeof(u64) ||
         reinterpret_cast<uintptr_t>(g->bad_starts_flag) % sizeof(int32_t) || reinterpret_cast<uintptr_t>(g->workspace) % LINEAR_ALIGN || g->workspace_bytes < 0)
         return COMET_ERR_INVALID_ARG;
@@ -2640,6 +2641,7 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
             vec = vec && aligned16(p);
     // the states' threads: 8 of every block of 32 rows
     const int pieces = ceil_div(8 * at::blocks(a.k_dim) * at::up16(a.v_dim), at::STATE_THREADS), slabs = 2 * at::blocks(a.C);
+    a.clears = g->zero_unwritten ? ceil_div(a.tokens, at::WINDOW) : 0;
     auto grid = [&](int64_t items) { return dim3((unsigned)(items < dev.sm_count ? items : dev.sm_count)); };
     cudaError_t err = cudaSuccess;
     if (n) err = launch_chained(vec ? comet::attn_open_kernel<true> : comet::attn_open_kernel<false>, dim3((unsigned)(n * slabs), (unsigned)(3 * Hk + Hq)),
@@ -2648,7 +2650,7 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
         err = launch_chained(vec ? comet::attn_products_kernel<true> : comet::attn_products_kernel<false>, grid(n * (Hk + Hq)), dim3(at::TILE_THREADS),
                              at::TILE_SMEM, stream, nullptr, a);
     if (err == cudaSuccess)
-        err = launch_chained(comet::attn_state_kernel, dim3((unsigned)(g->sequences * Hk * pieces)),
+        err = launch_chained(comet::attn_state_kernel, dim3((unsigned)(g->sequences * Hk * pieces + a.clears)),
                              dim3(at::STATE_THREADS), 0, stream, nullptr, a, pieces);
     if (err == cudaSuccess && n)
         err = launch_chained(vec ? comet::attn_rows_kernel<true> : comet::attn_rows_kernel<false>, grid(2 * n * Hq), dim3(at::TILE_THREADS), at::TILE_SMEM,

@@ -34,6 +34,7 @@ constexpr int ACC_COLS = limb::PLANES * RIGHT;
 constexpr int TILE_SMEM = SLOTS * SLOT_BYTES + RIGHT * LEFT * 8 + 128;
 constexpr int SLAB = 16;                             // tokens that a CTA opens
 constexpr int STATE_THREADS = 128;
+constexpr int WINDOW = 1024;                           // tokens that a CTA looks over for rows in no chunk
 __host__ __device__ constexpr int up16(int n) { return (n + 15) / 16 * 16; }
 __host__ __device__ constexpr int blocks(int n) { return (n + KC - 1) / KC; }
 }  // namespace attn
@@ -62,6 +63,7 @@ struct AttnArgs {
     int tokens, sequences, q_heads, kv_heads, k_dim, v_dim, C, chunks, f;
     int in_vec;                                                          // 16-byte accesses of Q, K and V
     int* error;                                                          // set where a wait ran out
+    int clears;                                                          // CTAs of the kernel of states that set to zero what nobody writes
 };
 
 // Tokens of sequence j, which begin at *begin: none where the starts are not ascending or leave the tokens.
@@ -608,6 +610,43 @@ attn_products_kernel(const __grid_constant__ AttnArgs a) {
     });
 }
 
+// Rows of tokens in no chunk, and messages of states that no chunk finds, are set to zero: CTA `part` of a.clears has a window of tokens and every
+// a.clears-th of such states.
+__device__ __forceinline__ void attn_clear(const AttnArgs& a, int part) {
+    using namespace attn;
+    __shared__ uint32_t covered[WINDOW / 32];
+    __shared__ int there;                                // chunks that there are: the first ones
+    const int tid = threadIdx.x, t0 = part * WINDOW, tokens = min(WINDOW, a.tokens - t0);
+    for (int k = tid; k < WINDOW / 32; k += STATE_THREADS) covered[k] = 0u;
+    if (tid == 0) there = 0;
+    __syncthreads();
+    int mine = 0;
+    for (int c = tid; c < a.chunks; c += STATE_THREADS) {
+        const int2 found = a.found[c];
+        mine += found.y > 0;
+        const int b = max(found.x - t0, 0), e = min(found.x + found.y - t0, tokens);
+        for (int k = b >> 5; b < e && 32 * k < e; ++k)
+            atomicOr(&covered[k], (~0u << max(b - 32 * k, 0)) & (~0u >> (32 - min(e - 32 * k, 32))));
+    }
+    if (mine) atomicAdd(&there, mine);
+    __syncthreads();
+    auto zero = [&](u64* const x[2], size_t row, int words) {
+        for (int k = tid; k < words; k += STATE_THREADS) x[0][row * words + k] = x[1][row * words + k] = 0ull;
+    };
+    const int q = a.q_heads * a.k_dim, k = a.kv_heads * a.k_dim, v = a.kv_heads * a.v_dim, p = a.q_heads * a.C, o = a.q_heads * a.v_dim;
+    for (int w = 0; 32 * w < tokens; ++w)
+        for (uint32_t left = ~covered[w] & (~0u >> (32 - min(tokens - 32 * w, 32))); left; left &= left - 1) {
+            const size_t t = t0 + 32 * w + __ffs(left) - 1;
+            zero(a.Eq, t, q);
+            zero(a.Ek, t, k);
+            zero(a.Ed, t, k);
+            zero(a.Ev, t, v);
+            zero(a.Ep, t, p);
+            zero(a.O, t, o);
+        }
+    for (int c = there + part; c < a.chunks; c += a.clears) zero(a.Es, c, k * a.v_dim);
+}
+
 // The state from chunk to chunk of a sequence and key head, four words of a column and both parties a thread; says whether the starts were in order.
 // Bound by memory: the next chunk's words are on their way while this one's are worked on.  49 us for the case, 290 MB (5.9 TB/s).  Carried along by
 // the kernel of the products, tile by tile in shared memory, it saved the 134 MB of sums, but left few warps an SM to wait for memory: 152 us for both, where
@@ -616,11 +655,16 @@ __global__ void __launch_bounds__(attn::STATE_THREADS)
 attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
     __shared__ int before;
     pdl_wait();
-    const int j = blockIdx.x / (a.kv_heads * pieces), rest = blockIdx.x - j * a.kv_heads * pieces, h = rest / pieces;
+    const int block = (int)blockIdx.x - a.clears;        // (the others are the first ones to begin)
+    if (block < 0) {
+        attn_clear(a, blockIdx.x);
+        return;
+    }
+    const int j = block / (a.kv_heads * pieces), rest = block - j * a.kv_heads * pieces, h = rest / pieces;
     const int t = (rest - h * pieces) * attn::STATE_THREADS + threadIdx.x, k_blocks = attn::blocks(a.k_dim), wide = attn::up16(a.v_dim);
     if (threadIdx.x == 0) before = 0;
     __syncthreads();
-    const bool checks = blockIdx.x == 0;
+    const bool checks = block == 0;
     int sum = 0, begin;
     bool bad = false;
     for (int s = threadIdx.x; s < (checks ? a.sequences : j); s += attn::STATE_THREADS) {

@@ -748,6 +748,7 @@ PyObject* linear_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
         if (!fits_int32({T, sequences, Hq, Hk, Dk, Dv, C, chunks, frac})) return done(COMET_ERR_SHAPE);
         g.tokens = (int32_t)T; g.sequences = (int32_t)sequences; g.q_heads = (int32_t)Hq; g.kv_heads = (int32_t)Hk;
         g.k_dim = (int32_t)Dk; g.v_dim = (int32_t)Dv; g.chunk = (int32_t)C; g.chunks = (int32_t)chunks; g.frac_bits = (int32_t)frac;
+        g.zero_unwritten = 1;                                // (new memory holds what its last owner left there)
         std::optional<c10::Stream> on;
         if (!stream_of(args[0], x.device(), &on)) return nullptr;
         const OnStream guard(x.device(), *on);
