@@ -606,7 +606,8 @@ int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args* args);
  * `state_out` may be `state`, word for word; nothing else that is written may overlap another argument.
  * Rows of tokens that are in no chunk, and states in Es of chunks that there are not, stay as they are in every result, or are set to zero where
  * `zero_unwritten` is 1: for messages in memory that held something else before.  Where the starts are not ascending or leave the tokens, that
- * sequence counts as empty; where the chunks are more than `chunks` the surplus ones are not worked out; either way, and where they are
+ * sequence counts as empty; where the chunks are more than `chunks`, or sequences that overlap have more tokens together than there are, the
+ * surplus ones are not worked out; either way, and where they are
  * fewer, `bad_starts_flag` (device int32, may be null) is set to 1.  The caller clears the flag.
  * Stateless; DEVICE pointers on the current device, owned by the caller, 8-byte aligned.  The work is enqueued on `cuda_stream` (NULL =
  * default stream) and the call does not wait for it.  `workspace` is 256-byte aligned and has at least the bytes that

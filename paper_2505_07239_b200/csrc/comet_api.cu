@@ -2504,20 +2504,23 @@ bool attn_heads(int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim)
 }
 bool attn_stride(int64_t stride, int64_t tokens, int64_t row) { return stride >= 0 && stride <= 1ll << 32 && (tokens == 1 || stride >= row); }
 // The workspace in bytes: the products d v^T of both parties, three sets of planes of queries, keys, decayed keys, values, states and weights each,
-// the chunks.
+// the chunks.  A chunk's rows are rounded up to 16 and its blocks of 32 tokens to whole ones, so all chunks of `tokens` tokens have
+// (tokens + 15 chunks) / 16 sixteens of rows and (tokens + 31 chunks) / 32 blocks at most, and no more than whole chunks would.
 struct AttnRoom {
-    int64_t kv, q, k, d, v, s, p, found;
-    AttnRoom(int64_t chunks, int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim, int64_t chunk) {
+    int64_t kv, q, k, d, v, s, p, found, sixteens, token_blocks;
+    AttnRoom(int64_t tokens, int64_t chunks, int64_t q_heads, int64_t kv_heads, int64_t k_dim, int64_t v_dim, int64_t chunk) {
         namespace at = comet::attn;
-        const int64_t rows = at::up16((int)chunk), ks = at::up16((int)k_dim), vs = at::up16((int)v_dim), t = at::blocks((int)chunk), kb = at::blocks((int)k_dim);
+        sixteens = std::min(chunks * (at::up16((int)chunk) / 16), (tokens + 15 * chunks) / 16);
+        token_blocks = std::min(chunks * at::blocks((int)chunk), (tokens + 31 * chunks) / 32);
+        const int64_t rows = 16 * sixteens, ks = at::up16((int)k_dim), vs = at::up16((int)v_dim), t = at::blocks((int)chunk), kb = at::blocks((int)k_dim);
         kv = chunks * kv_heads * k_dim * v_dim * (int64_t)sizeof(u64);
-        q = chunks * q_heads * kb * rows * at::ROW_BYTES;
-        k = chunks * kv_heads * kb * rows * at::ROW_BYTES;
-        d = chunks * kv_heads * t * ks * at::ROW_BYTES;
-        v = chunks * kv_heads * t * vs * at::ROW_BYTES;
+        q = q_heads * kb * rows * at::ROW_BYTES;
+        k = kv_heads * kb * rows * at::ROW_BYTES;
+        d = kv_heads * token_blocks * ks * at::ROW_BYTES;
+        v = kv_heads * token_blocks * vs * at::ROW_BYTES;
         s = chunks * kv_heads * kb * vs * at::ROW_BYTES;
-        p = chunks * q_heads * t * rows * at::ROW_BYTES;
-        found = chunks * (int64_t)sizeof(int2);
+        p = q_heads * t * rows * at::ROW_BYTES;
+        found = chunks * (int64_t)sizeof(int4);
         kv = (kv + 255) / 256 * 256;
     }
     size_t bytes() const { return (size_t)(2 * kv + 3 * (q + k + d + v + s + p) + found); }
@@ -2561,7 +2564,7 @@ extern "C" int comet_linear_attention_workspace(int32_t tokens, int32_t chunks, 
                                                 int32_t chunk, int64_t* bytes_out) {
     if (!bytes_out) return COMET_ERR_INVALID_ARG;
     if (!attn_sizes(tokens, chunks, q_heads, kv_heads, k_dim, v_dim, chunk)) return COMET_ERR_SHAPE;
-    *bytes_out = (int64_t)AttnRoom(chunks, q_heads, kv_heads, k_dim, v_dim, chunk).bytes();
+    *bytes_out = (int64_t)AttnRoom(tokens, chunks, q_heads, kv_heads, k_dim, v_dim, chunk).bytes();
     return COMET_OK;
 }
 
@@ -2595,7 +2598,7 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
     const bool in_place = g->state[0] && g->state[0] == g->state_out[0] && g->state[1] == g->state_out[1];
     if (pair_halved(g->state) || (!in_place && !span_pairs({{g->state, st, true}}, spans))) return COMET_ERR_INVALID_ARG;
     if (outputs_overlap(spans.data(), outputs, (int)spans.size())) return COMET_ERR_INVALID_ARG;
-    const AttnRoom room(n, Hq, Hk, Dk, Dv, g->chunk);
+    const AttnRoom room(T, n, Hq, Hk, Dk, Dv, g->chunk);
     const size_t need = room.bytes();
     if (need && !g->workspace) return COMET_ERR_INVALID_ARG;
     if (g->workspace_bytes < (int64_t)need) return COMET_ERR_SHAPE;
@@ -2617,7 +2620,9 @@ extern "C" int comet_linear_attention(void* cuda_stream, const comet_linear_atte
         for (uint8_t*& set : to.set) set = take(bytes);
     };
     planes(a.q, room.q); planes(a.k, room.k); planes(a.d, room.d); planes(a.v, room.v); planes(a.s, room.s); planes(a.p, room.p);
-    a.found = reinterpret_cast<int2*>(take(room.found));
+    a.found = reinterpret_cast<int4*>(take(room.found));
+    a.row_room = (int)room.sixteens;
+    a.block_room = (int)room.token_blocks;
     a.decay = reinterpret_cast<const u64*>(g->decay);
     a.starts = g->starts;
     a.bad_starts = g->bad_starts_flag;

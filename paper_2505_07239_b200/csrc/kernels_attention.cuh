@@ -42,6 +42,7 @@ __host__ __device__ constexpr int blocks(int n) { return (n + KC - 1) / KC; }
 // Blocks of limb planes (kernels_limb.cuh) of an operand: the opened value, party 0's and party 1's mask, or for the operand of a product that takes
 // it V_i = mask + i * opened (Eq. 1).  A block has 32 contraction indices of up to 128 rows (left operands: values and states; keys have up to
 // 64) or 64 (right ones), rounded up to 16, so that a block's planes lie side by side whatever its rows are.  Contraction indices are in their order.
+// Planes of tokens lie behind those of the chunks before, whose rows and blocks are counted: a chunk of one token takes one block's room, not a whole chunk's.
 struct AttnPlanes {
     uint8_t* set[3];
 };
@@ -55,12 +56,13 @@ struct AttnArgs {
     u64* S1[2];
     u64* kv[2];                                                          // [chunks][kv_heads][k_dim][v_dim]: sum d v^T at scale 2f
     AttnPlanes q, k, d, v, s, p;
-    int2* found;                                                         // [chunks]: first token, tokens
+    int4* found;                                                         // [chunks]: first token, tokens, rows (in sixteens) and blocks of those before
     const u64* decay;                                                    // [kv_heads][C + 1]
     const int32_t* starts;
     int32_t* bad_starts;
     long long q_stride, k_stride, v_stride;
     int tokens, sequences, q_heads, kv_heads, k_dim, v_dim, C, chunks, f;
+    int row_room, block_room;                                            // sixteens of rows and blocks of all chunks that there is room for
     int in_vec;                                                          // 16-byte accesses of Q, K and V
     int* error;                                                          // set where a wait ran out
     int clears;                                                          // CTAs of the kernel of states that set to zero what nobody writes
@@ -73,38 +75,48 @@ __device__ __forceinline__ int attn_length(const AttnArgs& a, int j, int* begin)
     return b >= 0 && b <= e && e <= a.tokens ? e - b : 0;
 }
 
-struct AttnChunk {
-    int seq, first, len;                                                 // len 0: there is no such chunk
-};
-
-// Chunk `want` of all sequences', by all threads of a CTA.
-__device__ __forceinline__ AttnChunk attn_find(const AttnArgs& a, int want) {
-    __shared__ AttnChunk found;
-    __shared__ int sums[attn::THREADS / 32];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-    if (tid == 0) found = {0, 0, 0};
-    for (int j0 = 0, base = 0; j0 < a.sequences && base <= want; j0 += blockDim.x) {
+// Chunk `want` of all sequences', by all threads of a CTA; no tokens where there is no such chunk, or no room for it (sequences that overlap may have more
+// tokens together than there are).
+__device__ __forceinline__ int4 attn_find(const AttnArgs& a, int want) {
+    __shared__ int4 found;
+    __shared__ int sums[attn::THREADS / 32][3];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) found = make_int4(0, 0, 0, 0);
+    int base[3] = {0, 0, 0};                             // chunks, their rows in sixteens, their blocks
+    for (int j0 = 0; j0 < a.sequences && base[0] <= want; j0 += attn::THREADS) {
+        const int warps = (min(a.sequences - j0, attn::THREADS) + 31) / 32;              // that have any
         const int j = j0 + tid;
         int begin = 0, len = 0;
         if (j < a.sequences) len = attn_length(a, j, &begin);
-        const int n = (len + a.C - 1) / a.C;
-        int up = n;
+        const int full = len / a.C, rest = len - full * a.C;
+        const int own[3] = {full + (rest > 0), full * (attn::up16(a.C) / 16) + attn::up16(rest) / 16, full * attn::blocks(a.C) + attn::blocks(rest)};
+        int up[3] = {own[0], own[1], own[2]};
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int t = __shfl_up_sync(0xffffffffu, up, o);
-            if (lane >= o) up += t;
-        }
+        for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                const int t = __shfl_up_sync(0xffffffffu, up[k], o);
+                if (lane >= o) up[k] += t;
+            }
         __syncthreads();
-        if (lane == 31) sums[warp] = up;
+        if (lane == 31)
+#pragma unroll
+            for (int k = 0; k < 3; ++k) sums[warp][k] = up[k];
         __syncthreads();
-        int before = base, total = 0;
-        for (int w = 0; w < warps; ++w) {
-            before += w < warp ? sums[w] : 0;
-            total += sums[w];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) up[k] += base[k] - own[k];
+        for (int w = 0; w < warps; ++w)
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                const int t = sums[w][k];
+                up[k] += w < warp ? t : 0;
+                base[k] += t;
+            }
+        const int mine = want - up[0];
+        if (mine >= 0 && mine < own[0]) {
+            const int n = min(a.C, len - mine * a.C), rows = up[1] + mine * (attn::up16(a.C) / 16), blocks = up[2] + mine * attn::blocks(a.C);
+            if (rows + attn::up16(n) / 16 <= a.row_room && blocks + attn::blocks(n) <= a.block_room) found = make_int4(begin + mine * a.C, n, rows, blocks);
         }
-        const int mine = want - (before + up - n);
-        if (mine >= 0 && mine < n) found = {j, begin + mine * a.C, min(a.C, len - mine * a.C)};
-        base += total;
     }
     __syncthreads();
     return found;
@@ -138,13 +150,17 @@ __device__ __forceinline__ ulonglong2 attn_input2(const u64* p, int vec) { retur
 __device__ __forceinline__ ulonglong2 attn_add(ulonglong2 x, ulonglong2 y) { return make_ulonglong2(x.x + y.x, x.y + y.y); }
 __device__ __forceinline__ u64 attn_rescale(u64 v, int party, int f) { return party ? 0ull - norm_shift(0ull - v, f) : norm_shift(v, f); }
 
-// Where blocks lie, in bytes from a set's begin.  q, k, p: rows are tokens, room for up16(C) of them; d, v, s: rows are k_dim in tiles of 64, or v_dim
-// in tiles of 128.
-__device__ __forceinline__ size_t attn_token_block(int ch, int blocks, int b, int C) { return ((size_t)ch * blocks + b) * attn::up16(C) * attn::ROW_BYTES; }
-__device__ __forceinline__ size_t attn_dim_block(int ch, int blocks, int b, int dim, int row0, int tile) {
-    const int wide = attn::up16(dim);
-    return ((size_t)ch * blocks * wide + (size_t)row0 * blocks + (size_t)b * min(tile, wide - row0)) * attn::ROW_BYTES;
+// Where blocks lie, in bytes from a set's begin.  q, k, p: rows are a chunk's tokens, a head has up to `blocks` blocks; d, v, s: rows are k_dim in tiles of
+// 64, or v_dim in tiles of 128, and a head has `blocks` blocks behind the `before` of others.
+__device__ __forceinline__ size_t attn_token_block(const int4& found, int heads, int head, int blocks, int b) {
+    return ((size_t)found.z * 16 * heads * blocks + (size_t)(head * blocks + b) * attn::up16(found.y)) * attn::ROW_BYTES;
 }
+__device__ __forceinline__ size_t attn_dim_block(size_t before, int blocks, int b, int dim, int row0, int tile) {
+    const int wide = attn::up16(dim);
+    return (before * wide + (size_t)row0 * blocks + (size_t)b * min(tile, wide - row0)) * attn::ROW_BYTES;
+}
+// Blocks of a key head's values or decayed keys start behind this many.
+__device__ __forceinline__ size_t attn_before(const int4& found, int heads, int head) { return (size_t)found.w * heads + head * attn::blocks(found.y); }
 // Words of a row, `n` of them from index `first` on (a multiple of n), into a block of `rows` rows: n bytes a plane at once.
 __device__ __forceinline__ uint8_t* attn_spot(uint8_t* block, int row, int first) {
     return block + (row >> 3) * 256 + (first >> 4) * 128 + (row & 7) * 16 + (first & 15);
@@ -175,15 +191,15 @@ __global__ void __launch_bounds__(attn::THREADS, 2)
 attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
     pdl_wait();
     const int c = blockIdx.x / slabs, t0 = (blockIdx.x - c * slabs) * attn::SLAB;
-    const AttnChunk at = attn_find(a, c);
-    if (blockIdx.x == c * slabs && blockIdx.y == 0 && threadIdx.x == 0) a.found[c] = make_int2(at.first, at.len);
-    const int blocks = attn::blocks(a.C), rows16 = attn::up16(at.len), rows = min(attn::SLAB, at.len - t0), first = at.first + t0;
-    if (t0 >= attn::blocks(at.len) * attn::KC) return;
+    const int4 at = attn_find(a, c);
+    if (blockIdx.x == c * slabs && blockIdx.y == 0 && threadIdx.x == 0) a.found[c] = at;
+    const int blocks = attn::blocks(at.y), rows16 = attn::up16(at.y), rows = min(attn::SLAB, at.y - t0), first = at.x + t0;
+    if (t0 >= blocks * attn::KC) return;
     const int f = a.f;
     // rows of queries or keys: messages, and the planes of the opened value, party 0's mask, party 1's or V_1
     auto open_rows = [&](const u64* const x[2], long long stride, const u64* const m[2], u64* const msg[2], const AttnPlanes& to, int heads, int head, bool query) {
         const int parts = attn::blocks(a.k_dim) * 4;
-        const size_t o0 = ((size_t)first * heads + head) * a.k_dim;
+        const size_t o0 = ((size_t)first * heads + head) * a.k_dim, block0 = attn_token_block(at, heads, head, parts / 4, 0);
         for (int t = threadIdx.x; t < rows * parts; t += attn::THREADS) {
             const int r = t / parts, part = t - r * parts;
             const size_t o = o0 + (size_t)r * heads * a.k_dim + 8 * part;
@@ -215,7 +231,7 @@ attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
                     if (query) mask[1][n] += e[0][n];
                 }
             }
-            const size_t block = attn_token_block(c * heads + head, parts / 4, part / 4, a.C);
+            const size_t block = block0 + (size_t)(part / 4 * rows16 * attn::ROW_BYTES);
             attn_emit(to.set[0] + block, rows16, t0 + r, part % 4 * 8, e[0]);
             attn_emit(to.set[1] + block, rows16, t0 + r, part % 4 * 8, mask[0]);
             attn_emit(to.set[2] + block, rows16, t0 + r, part % 4 * 8, mask[1]);
@@ -254,7 +270,7 @@ attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
                 if (sum) mask[1][k] += e[0][k];
             }
             const int row0 = j / tile * tile, wide = min(tile, all - row0), token = t0 + r0;
-            const size_t block = attn_dim_block(c * a.kv_heads + head, blocks, token / attn::KC, dim, row0, tile);
+            const size_t block = attn_dim_block(attn_before(at, a.kv_heads, head), blocks, token / attn::KC, dim, row0, tile);
             attn_emit(to.set[0] + block, wide, j - row0, token % attn::KC, e[0]);
             attn_emit(to.set[1] + block, wide, j - row0, token % attn::KC, mask[0]);
             attn_emit(to.set[2] + block, wide, j - row0, token % attn::KC, mask[1]);
@@ -264,7 +280,7 @@ attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
     if (what == 0) {
         open_rows(a.K, a.k_stride, a.mk, a.Ek, a.k, a.kv_heads, h, false);
     } else if (what == 1) {
-        open_dims(a.K, a.k_stride, a.md, a.Ed, a.d, a.k_dim, attn::RIGHT, h, a.decay + (size_t)h * (a.C + 1) + at.len - 1 - t0, true);
+        open_dims(a.K, a.k_stride, a.md, a.Ed, a.d, a.k_dim, attn::RIGHT, h, a.decay + (size_t)h * (a.C + 1) + at.y - 1 - t0, true);
     } else if (what == 2) {
         open_dims(a.V, a.v_stride, a.mv, a.Ev, a.v, a.v_dim, attn::LEFT, h, nullptr, false);
     } else {
@@ -288,7 +304,7 @@ attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
 // ---------------------------------------------------------------------------
 struct AttnOperand {
     const uint8_t* open; const uint8_t* own;             // the first blocks; V_i or the party's mask
-    uint32_t bytes, step;                                // of a block; from block to block
+    uint32_t bytes;                                      // of a block; the next one lies behind it
 };
 struct AttnTile {
     AttnOperand left, right;
@@ -304,7 +320,7 @@ struct AttnShared {
 template <typename T>
 __device__ __forceinline__ T* attn_of(T* const (&x)[2], int i) { return i ? x[1] : x[0]; }
 __device__ __forceinline__ AttnOperand attn_operand(const AttnPlanes& p, int i, size_t at, int rows) {
-    return {p.set[0] + at, (i ? p.set[2] : p.set[1]) + at, (uint32_t)(rows * attn::ROW_BYTES), (uint32_t)(rows * attn::ROW_BYTES)};
+    return {p.set[0] + at, (i ? p.set[2] : p.set[1]) + at, (uint32_t)(rows * attn::ROW_BYTES)};
 }
 
 // Asks the L2 for `rows` rows of `words` words, `step` words apart: the draining warps, for what they add to the sums while the products run.
@@ -358,8 +374,8 @@ __device__ __forceinline__ void attn_tiles(uint8_t* raw, int items, int* error, 
                         const uint32_t bar = full0 + 8 * slot, to = planes0 + slot * SLOT_BYTES;
                         const size_t k = b >> 1;
                         ptx::mbar_expect_tx(bar, x.left.bytes + x.right.bytes);
-                        ptx::bulk_g2s(to, (b & 1 ? x.left.own : x.left.open) + k * x.left.step, x.left.bytes, bar);
-                        ptx::bulk_g2s(to + LEFT_BYTES, (b & 1 ? x.right.open : x.right.own) + k * x.right.step, x.right.bytes, bar);
+                        ptx::bulk_g2s(to, (b & 1 ? x.left.own : x.left.open) + k * x.left.bytes, x.left.bytes, bar);
+                        ptx::bulk_g2s(to + LEFT_BYTES, (b & 1 ? x.right.open : x.right.own) + k * x.right.bytes, x.right.bytes, bar);
                         ++issued;
                         if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
                     }
@@ -510,20 +526,21 @@ attn_products_kernel(const __grid_constant__ AttnArgs a) {
         AttnTile x;
         x.add = false;
         if (item < key_items) {
-            const int i = n & 1, vk = n >> 1, vt = vk / k_tiles, v0 = vt * LEFT, k0 = (vk - vt * k_tiles) * RIGHT, len = a.found[item / a.kv_heads].y;
-            x.left = attn_operand(a.v, i, attn_dim_block(item, t_blocks, 0, a.v_dim, v0, LEFT), min(LEFT, up16(a.v_dim) - v0));
-            x.right = attn_operand(a.d, i, attn_dim_block(item, t_blocks, 0, a.k_dim, k0, RIGHT), min(RIGHT, up16(a.k_dim) - k0));
-            x.blocks = blocks(len);
+            const int i = n & 1, vk = n >> 1, vt = vk / k_tiles, v0 = vt * LEFT, k0 = (vk - vt * k_tiles) * RIGHT, c = item / a.kv_heads;
+            const int4 found = a.found[c];
+            const size_t before = attn_before(found, a.kv_heads, item - c * a.kv_heads);
+            x.blocks = blocks(found.y);
+            x.left = attn_operand(a.v, i, attn_dim_block(before, x.blocks, 0, a.v_dim, v0, LEFT), min(LEFT, up16(a.v_dim) - v0));
+            x.right = attn_operand(a.d, i, attn_dim_block(before, x.blocks, 0, a.k_dim, k0, RIGHT), min(RIGHT, up16(a.k_dim) - k0));
             x.rows = min(LEFT, a.v_dim - v0);
             x.cols = min(RIGHT, a.k_dim - k0);
         } else {
-            const int ch = item - key_items, c = ch / a.q_heads, hq = ch - c * a.q_heads, len = a.found[c].y;
-            // (room between the blocks for up16(C) rows)
-            x.left = attn_operand(a.k, n, attn_token_block(c * a.kv_heads + hq / (a.q_heads / a.kv_heads), k_blocks, 0, a.C), up16(len));
-            x.right = attn_operand(a.q, n, attn_token_block(ch, k_blocks, 0, a.C), up16(len));
-            x.left.step = x.right.step = up16(a.C) * ROW_BYTES;
+            const int ch = item - key_items, c = ch / a.q_heads, hq = ch - c * a.q_heads;
+            const int4 found = a.found[c];
+            x.left = attn_operand(a.k, n, attn_token_block(found, a.kv_heads, hq / (a.q_heads / a.kv_heads), k_blocks, 0), up16(found.y));
+            x.right = attn_operand(a.q, n, attn_token_block(found, a.q_heads, hq, k_blocks, 0), up16(found.y));
             x.blocks = k_blocks;
-            x.rows = x.cols = len;
+            x.rows = x.cols = found.y;
         }
         return x;
     }, [&](int item, int n, const AttnTile& x) {
@@ -548,16 +565,18 @@ attn_products_kernel(const __grid_constant__ AttnArgs a) {
             return;
         }
         const int ch = item - key_items, c = ch / a.q_heads, hq = ch - c * a.q_heads, h = hq / (a.q_heads / a.kv_heads), i = n, f = a.f;
-        const int2 found = a.found[c];
+        const int4 found = a.found[c];
+        const int len = found.y, rows16 = up16(len);
         const uint32_t p_row = (uint32_t)a.q_heads * a.C;
         const size_t p_at = (size_t)found.x * p_row + (size_t)hq * a.C;
+        const uint32_t row0 = (uint32_t)(found.z * 16 * a.q_heads + hq * rows16) * t_blocks;     // of the planes (chunks x heads are 2^24 at most)
         const u64* const qk = attn_of(a.qk, i) + p_at;
         const u64* const mp = attn_of(a.mp, i) + p_at;
         u64* const Ep = attn_of(a.Ep, i) + p_at;
         const u64* const w = a.decay + (size_t)h * (a.C + 1);
         const bool pairs = VEC && a.C % 2 == 0;
-        const int t_used = blocks(found.y), quads = 8 * t_used;
-        for (int t = threadIdx.x; t < found.y * quads; t += DRAIN_THREADS) {
+        const int quads = 8 * blocks(len);
+        for (int t = threadIdx.x; t < len * quads; t += DRAIN_THREADS) {
             const int r = t / quads, quad = t - r * quads, key0 = 4 * quad;
             u64 z[4], m[4], e[4];
 #pragma unroll
@@ -592,8 +611,7 @@ attn_products_kernel(const __grid_constant__ AttnArgs a) {
             }
             // party 0's words wait behind the tile's rows, of which there are 64 at most, for the same thread
             u64* const kept = words + r * LEFT + LEFT / 2 + key0;
-            const size_t block = attn_token_block(ch, t_blocks, quad >> 3, a.C);
-            const int rows16 = up16(found.y);
+            const size_t block = (size_t)(row0 + (quad >> 3) * rows16) * ROW_BYTES;
             if (i) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -622,7 +640,7 @@ __device__ __forceinline__ void attn_clear(const AttnArgs& a, int part) {
     __syncthreads();
     int mine = 0;
     for (int c = tid; c < a.chunks; c += STATE_THREADS) {
-        const int2 found = a.found[c];
+        const int4 found = a.found[c];
         mine += found.y > 0;
         const int b = max(found.x - t0, 0), e = min(found.x + found.y - t0, tokens);
         for (int k = b >> 5; b < e && 32 * k < e; ++k)
@@ -682,12 +700,14 @@ attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
     const int words = a.k_dim * a.v_dim, row = 4 * quad, word = row * a.v_dim + col;
     const size_t at = ((size_t)j * a.kv_heads + h) * words + word, step = (size_t)a.kv_heads * words;
     const u64* const w = a.decay + (size_t)h * (a.C + 1);
-    int c = checks ? 0 : before, left = attn_length(a, j, &begin);
-    const int end = min(a.chunks, c + (left + a.C - 1) / a.C);
+    int c = checks ? 0 : before;
+    const int end = min(a.chunks, c + (attn_length(a, j, &begin) + a.C - 1) / a.C);
     u64 S[2][4], kv[2][4], ms[2][4];
     size_t o = ((size_t)c * a.kv_heads + h) * words + word;
     auto live = [&](int k) { return col < a.v_dim && row + k < a.k_dim; };
-    auto load = [&] {
+    int len = 0;                                         // of the chunk; none where it had no room: then it and those behind it are not worked out
+    auto load = [&](int chunk) {
+        len = a.found[chunk].y;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -696,15 +716,15 @@ attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
                 ms[i][k] = live(k) ? __ldcs(a.ms[i] + o + k * a.v_dim) : 0ull;
             }
     };
-    if (c < end) load();
+    if (c < end) load(c);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int k = 0; k < 4; ++k) S[i][k] = a.S0[i] && live(k) ? __ldcs(a.S0[i] + at + k * a.v_dim) : 0ull;
     const int row0 = col / attn::LEFT * attn::LEFT, rows = min(attn::LEFT, wide - row0);
-    for (; c < end; ++c, left -= a.C) {
-        const u64 weight = __ldg(w + min(left, a.C));
-        const size_t here = o, block = attn_dim_block(c * a.kv_heads + h, k_blocks, quad >> 3, a.v_dim, row0, attn::LEFT);
+    for (; c < end && len > 0; ++c) {
+        const u64 weight = __ldg(w + len);
+        const size_t here = o, block = attn_dim_block(((size_t)c * a.kv_heads + h) * k_blocks, k_blocks, quad >> 3, a.v_dim, row0, attn::LEFT);
         attn_emit(a.s.set[1] + block, rows, col - row0, 4 * (quad & 7), ms[0]);
         attn_emit(a.s.set[2] + block, rows, col - row0, 4 * (quad & 7), ms[1]);
         u64 e[2][4];
@@ -716,7 +736,7 @@ attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
                 S[i][k] = attn_rescale(weight * S[i][k] + kv[i][k], i, a.f);
             }
         o += step;
-        if (c + 1 < end) load();
+        if (c + 1 < end) load(c + 1);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
 #pragma unroll
@@ -744,22 +764,22 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a) {
     const int v_tiles = (a.v_dim + LEFT - 1) / LEFT, t_blocks = blocks(a.C), k_blocks = blocks(a.k_dim);
     attn_tiles(attn_smem, 2 * a.chunks * a.q_heads, a.error, [&](int item) { return a.found[(item >> 1) / a.q_heads].y == 0 ? 0 : 2 * v_tiles; },
                [&](int item, int n) {
-        const int i = item & 1, ch = item >> 1, c = ch / a.q_heads, hq = ch - c * a.q_heads, kv = c * a.kv_heads + hq / (a.q_heads / a.kv_heads);
-        const int v0 = (n >> 1) * LEFT, len = a.found[c].y, wide = min(LEFT, up16(a.v_dim) - v0);
+        const int i = item & 1, ch = item >> 1, c = ch / a.q_heads, hq = ch - c * a.q_heads, h = hq / (a.q_heads / a.kv_heads);
+        const int v0 = (n >> 1) * LEFT, wide = min(LEFT, up16(a.v_dim) - v0);
+        const int4 found = a.found[c];
         AttnTile x;
         x.add = n & 1;
         if (n & 1) {
-            x.left = attn_operand(a.v, i, attn_dim_block(kv, t_blocks, 0, a.v_dim, v0, LEFT), wide);
-            x.right = attn_operand(a.p, i, attn_token_block(ch, t_blocks, 0, a.C), up16(len));
-            x.blocks = blocks(len);
+            x.blocks = blocks(found.y);
+            x.left = attn_operand(a.v, i, attn_dim_block(attn_before(found, a.kv_heads, h), x.blocks, 0, a.v_dim, v0, LEFT), wide);
+            x.right = attn_operand(a.p, i, attn_token_block(found, a.q_heads, hq, t_blocks, 0), up16(found.y));
         } else {
-            x.left = attn_operand(a.s, i, attn_dim_block(kv, k_blocks, 0, a.v_dim, v0, LEFT), wide);
-            x.right = attn_operand(a.q, i, attn_token_block(ch, k_blocks, 0, a.C), up16(len));
             x.blocks = k_blocks;
+            x.left = attn_operand(a.s, i, attn_dim_block(((size_t)c * a.kv_heads + h) * k_blocks, k_blocks, 0, a.v_dim, v0, LEFT), wide);
+            x.right = attn_operand(a.q, i, attn_token_block(found, a.q_heads, hq, k_blocks, 0), up16(found.y));
         }
-        x.right.step = up16(a.C) * ROW_BYTES;
         x.rows = min(LEFT, a.v_dim - v0);
-        x.cols = len;
+        x.cols = found.y;
         return x;
     }, [&](int item, int n, const AttnTile& x) {
         if (n & 1) return;
