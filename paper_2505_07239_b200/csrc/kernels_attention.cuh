@@ -6,7 +6,8 @@
 //     d_s = tr(w[L - 1 - s] k_s);                     S <- tr(w[L] S + sum_s d_s v_s^T)
 //   single tokens:  S <- tr(w S + k v^T),  o = tr(q S)
 // Four kernels for a prompt: all values that need no product are opened (open); the products d v^T of all chunks and key heads and the weights P
-// of all chunks and query heads (products); the states from chunk to chunk, a word a thread (state); the rows of O (rows).  What enters a product is
+// of all chunks and query heads (products); the states from chunk to chunk, a word a thread (state); the rows of O (rows).  Before them, where it pays, one
+// that lists the chunks (list).  What enters a product is
 // cut into bytes by the kernel that has it in registers anyway, once, so that those of the products only copy, multiply and add.  (The bytes are
 // as many as the words: the same traffic, and no warp of a product's kernel converts.  512 tokens x 32 heads x 128, "the case" below: words cut
 // into bytes by warps beside the issuer 438 us, by every warp for its own mma.sync 679, this 371, of which memory's floor is 108.)
@@ -34,6 +35,7 @@ constexpr int ACC_COLS = limb::PLANES * RIGHT;
 constexpr int TILE_SMEM = SLOTS * SLOT_BYTES + RIGHT * LEFT * 8 + 128;
 constexpr int SLAB = 16;                             // tokens that a CTA opens
 constexpr int STATE_THREADS = 128;
+constexpr int NOBODY = 1 << 20;                          // behind the last sequence, of which there are no more
 constexpr int WINDOW = 1024;                           // tokens that a CTA looks over for rows in no chunk
 __host__ __device__ constexpr int up16(int n) { return (n + 15) / 16 * 16; }
 __host__ __device__ constexpr int blocks(int n) { return (n + KC - 1) / KC; }
@@ -56,7 +58,8 @@ struct AttnArgs {
     u64* S1[2];
     u64* kv[2];                                                          // [chunks][kv_heads][k_dim][v_dim]: sum d v^T at scale 2f
     AttnPlanes q, k, d, v, s, p;
-    int4* found;                                                         // [chunks]: first token, tokens, rows (in sixteens) and blocks of those before
+    int4* found;                                                         // [chunks]: first token, 128 x sequence + tokens, rows (in sixteens) and blocks of those before
+    int listed;                                                          // whether it is there before the values are opened
     const u64* decay;                                                    // [kv_heads][C + 1]
     const int32_t* starts;
     int32_t* bad_starts;
@@ -75,15 +78,27 @@ __device__ __forceinline__ int attn_length(const AttnArgs& a, int j, int* begin)
     return b >= 0 && b <= e && e <= a.tokens ? e - b : 0;
 }
 
-// Chunk `want` of all sequences', by all threads of a CTA; no tokens where there is no such chunk, or no room for it (sequences that overlap may have more
-// tokens together than there are).
-__device__ __forceinline__ int4 attn_find(const AttnArgs& a, int want) {
-    __shared__ int4 found;
+struct AttnChunk {
+    int4 at;                                             // as in `found`, but y the tokens: none where there is no such chunk, or no room for it
+    int owner;                                           // its sequence
+};
+__device__ __forceinline__ AttnChunk attn_no_chunk() { return {make_int4(0, 0, 0, 0), attn::NOBODY}; }
+__device__ __forceinline__ void attn_put(const AttnArgs& a, int c, const AttnChunk& x) { a.found[c] = make_int4(x.at.x, x.owner * 128 + x.at.y, x.at.z, x.at.w); }
+__device__ __forceinline__ int4 attn_chunk(const AttnArgs& a, int c) {
+    int4 at = a.found[c];
+    at.y &= 127;
+    return at;
+}
+__device__ __forceinline__ int attn_owner(const AttnArgs& a, int c) { return a.found[c].y >> 7; }
+
+// Chunks first to last of all sequences', by all threads of a CTA: emit(number, chunk) by whichever thread has its sequence.  Sequences that overlap may have more
+// tokens together than there is room for.
+template <typename F>
+__device__ __forceinline__ void attn_scan(const AttnArgs& a, int first, int last, F&& emit) {
     __shared__ int sums[attn::THREADS / 32][3];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid == 0) found = make_int4(0, 0, 0, 0);
     int base[3] = {0, 0, 0};                             // chunks, their rows in sixteens, their blocks
-    for (int j0 = 0; j0 < a.sequences && base[0] <= want; j0 += attn::THREADS) {
+    for (int j0 = 0; j0 < a.sequences && base[0] <= last; j0 += attn::THREADS) {
         const int warps = (min(a.sequences - j0, attn::THREADS) + 31) / 32;              // that have any
         const int j = j0 + tid;
         int begin = 0, len = 0;
@@ -112,14 +127,33 @@ __device__ __forceinline__ int4 attn_find(const AttnArgs& a, int want) {
                 up[k] += w < warp ? t : 0;
                 base[k] += t;
             }
-        const int mine = want - up[0];
-        if (mine >= 0 && mine < own[0]) {
-            const int n = min(a.C, len - mine * a.C), rows = up[1] + mine * (attn::up16(a.C) / 16), blocks = up[2] + mine * attn::blocks(a.C);
-            if (rows + attn::up16(n) / 16 <= a.row_room && blocks + attn::blocks(n) <= a.block_room) found = make_int4(begin + mine * a.C, n, rows, blocks);
+        for (int c = max(first, up[0]); c <= min(last, up[0] + own[0] - 1); ++c) {
+            const int mine = c - up[0], n = min(a.C, len - mine * a.C), rows = up[1] + mine * (attn::up16(a.C) / 16), blocks = up[2] + mine * attn::blocks(a.C);
+            const bool room = rows + attn::up16(n) / 16 <= a.row_room && blocks + attn::blocks(n) <= a.block_room;
+            emit(c, AttnChunk{room ? make_int4(begin + mine * a.C, n, rows, blocks) : make_int4(0, 0, 0, 0), j});
         }
     }
+}
+
+// Chunk `want`, to all threads of a CTA.
+__device__ __forceinline__ AttnChunk attn_find(const AttnArgs& a, int want) {
+    __shared__ AttnChunk found;
+    if (threadIdx.x == 0) found = attn_no_chunk();
+    __syncthreads();
+    attn_scan(a, want, want, [&](int, const AttnChunk& c) { found = c; });
     __syncthreads();
     return found;
+}
+
+// The list of all chunks (AttnArgs::listed): a CTA has as many chunks as threads.  65536 prompts of one token, one head of 2: 11 ms; with every CTA that
+// opens values looking through all sequences for itself 181.
+__global__ void __launch_bounds__(attn::THREADS)
+attn_list_kernel(const __grid_constant__ AttnArgs a) {
+    pdl_wait();
+    const int first = blockIdx.x * attn::THREADS, last = min(first + attn::THREADS, a.chunks) - 1, c = first + threadIdx.x;
+    if (c <= last) attn_put(a, c, attn_no_chunk());
+    __syncthreads();
+    attn_scan(a, first, last, [&](int k, const AttnChunk& x) { attn_put(a, k, x); });
 }
 
 template <bool VEC>
@@ -191,8 +225,14 @@ __global__ void __launch_bounds__(attn::THREADS, 2)
 attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
     pdl_wait();
     const int c = blockIdx.x / slabs, t0 = (blockIdx.x - c * slabs) * attn::SLAB;
-    const int4 at = attn_find(a, c);
-    if (blockIdx.x == c * slabs && blockIdx.y == 0 && threadIdx.x == 0) a.found[c] = at;
+    int4 at;
+    if (a.listed) {
+        at = attn_chunk(a, c);
+    } else {
+        const AttnChunk found = attn_find(a, c);
+        at = found.at;
+        if (blockIdx.x == c * slabs && blockIdx.y == 0 && threadIdx.x == 0) attn_put(a, c, found);
+    }
     const int blocks = attn::blocks(at.y), rows16 = attn::up16(at.y), rows = min(attn::SLAB, at.y - t0), first = at.x + t0;
     if (t0 >= blocks * attn::KC) return;
     const int f = a.f;
@@ -521,13 +561,13 @@ attn_products_kernel(const __grid_constant__ AttnArgs a) {
     const int t_blocks = blocks(a.C), k_blocks = blocks(a.k_dim);
     attn_tiles(attn_smem, key_items + a.chunks * a.q_heads, a.error, [&](int item) {
         const int c = item < key_items ? item / a.kv_heads : (item - key_items) / a.q_heads;
-        return a.found[c].y == 0 ? 0 : item < key_items ? 2 * v_tiles * k_tiles : 2;
+        return attn_chunk(a, c).y == 0 ? 0 : item < key_items ? 2 * v_tiles * k_tiles : 2;
     }, [&](int item, int n) {
         AttnTile x;
         x.add = false;
         if (item < key_items) {
             const int i = n & 1, vk = n >> 1, vt = vk / k_tiles, v0 = vt * LEFT, k0 = (vk - vt * k_tiles) * RIGHT, c = item / a.kv_heads;
-            const int4 found = a.found[c];
+            const int4 found = attn_chunk(a, c);
             const size_t before = attn_before(found, a.kv_heads, item - c * a.kv_heads);
             x.blocks = blocks(found.y);
             x.left = attn_operand(a.v, i, attn_dim_block(before, x.blocks, 0, a.v_dim, v0, LEFT), min(LEFT, up16(a.v_dim) - v0));
@@ -536,7 +576,7 @@ attn_products_kernel(const __grid_constant__ AttnArgs a) {
             x.cols = min(RIGHT, a.k_dim - k0);
         } else {
             const int ch = item - key_items, c = ch / a.q_heads, hq = ch - c * a.q_heads;
-            const int4 found = a.found[c];
+            const int4 found = attn_chunk(a, c);
             x.left = attn_operand(a.k, n, attn_token_block(found, a.kv_heads, hq / (a.q_heads / a.kv_heads), k_blocks, 0), up16(found.y));
             x.right = attn_operand(a.q, n, attn_token_block(found, a.q_heads, hq, k_blocks, 0), up16(found.y));
             x.blocks = k_blocks;
@@ -565,7 +605,7 @@ attn_products_kernel(const __grid_constant__ AttnArgs a) {
             return;
         }
         const int ch = item - key_items, c = ch / a.q_heads, hq = ch - c * a.q_heads, h = hq / (a.q_heads / a.kv_heads), i = n, f = a.f;
-        const int4 found = a.found[c];
+        const int4 found = attn_chunk(a, c);
         const int len = found.y, rows16 = up16(len);
         const uint32_t p_row = (uint32_t)a.q_heads * a.C;
         const size_t p_at = (size_t)found.x * p_row + (size_t)hq * a.C;
@@ -640,7 +680,7 @@ __device__ __forceinline__ void attn_clear(const AttnArgs& a, int part) {
     __syncthreads();
     int mine = 0;
     for (int c = tid; c < a.chunks; c += STATE_THREADS) {
-        const int4 found = a.found[c];
+        const int4 found = attn_chunk(a, c);
         mine += found.y > 0;
         const int b = max(found.x - t0, 0), e = min(found.x + found.y - t0, tokens);
         for (int k = b >> 5; b < e && 32 * k < e; ++k)
@@ -671,7 +711,6 @@ __device__ __forceinline__ void attn_clear(const AttnArgs& a, int part) {
 // the two kernels take 146.
 __global__ void __launch_bounds__(attn::STATE_THREADS)
 attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
-    __shared__ int before;
     pdl_wait();
     const int block = (int)blockIdx.x - a.clears;        // (the others are the first ones to begin)
     if (block < 0) {
@@ -680,34 +719,34 @@ attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
     }
     const int j = block / (a.kv_heads * pieces), rest = block - j * a.kv_heads * pieces, h = rest / pieces;
     const int t = (rest - h * pieces) * attn::STATE_THREADS + threadIdx.x, k_blocks = attn::blocks(a.k_dim), wide = attn::up16(a.v_dim);
-    if (threadIdx.x == 0) before = 0;
-    __syncthreads();
-    const bool checks = block == 0;
-    int sum = 0, begin;
-    bool bad = false;
-    for (int s = threadIdx.x; s < (checks ? a.sequences : j); s += attn::STATE_THREADS) {
-        sum = min(sum + (attn_length(a, s, &begin) + a.C - 1) / a.C, a.chunks + 1);      // (starts out of order may have more than an int of chunks)
-        const int end = a.starts[s + 1];
-        bad |= begin < 0 || end < begin || end > a.tokens;
+    // the sequence's first chunk: the first one whose owner it, or a later one, is
+    int c = 0, top = a.chunks;
+    while (c < top) {
+        const int step = (top - c + attn::STATE_THREADS - 1) / attn::STATE_THREADS, at = c + threadIdx.x * step;
+        const int n = __syncthreads_count(at < top && attn_owner(a, at) < j);
+        if (n == 0) break;
+        top = min(top, c + n * step);
+        c += (n - 1) * step + 1;
     }
-    if (sum) atomicAdd(&before, sum);
-    if (bad && checks && a.bad_starts) *a.bad_starts = 1;
-    __syncthreads();
-    if (checks && threadIdx.x == 0 && before != a.chunks && a.bad_starts) *a.bad_starts = 1;
+    int begin;
+    const int own = (attn_length(a, j, &begin) + a.C - 1) / a.C, end = min(a.chunks, c + own);
+    if (rest == 0 && threadIdx.x == 0 && a.bad_starts) {
+        const int last = a.starts[j + 1];
+        // out of order; more chunks than there are to be; fewer
+        if (begin < 0 || last < begin || last > a.tokens || c + own > a.chunks || (j == 0 && a.chunks > 0 && attn_owner(a, a.chunks - 1) == attn::NOBODY)) *a.bad_starts = 1;
+    }
     // a warp has four groups of four rows, eight columns: 64 bytes of a row, 128 of a plane
     const int groups = wide / 8, wt = t >> 5, quad = (wt / groups) * 4 + (t >> 3 & 3), col = (wt % groups) * 8 + (t & 7);
     if (quad >= 8 * k_blocks) return;
     const int words = a.k_dim * a.v_dim, row = 4 * quad, word = row * a.v_dim + col;
     const size_t at = ((size_t)j * a.kv_heads + h) * words + word, step = (size_t)a.kv_heads * words;
     const u64* const w = a.decay + (size_t)h * (a.C + 1);
-    int c = checks ? 0 : before;
-    const int end = min(a.chunks, c + (attn_length(a, j, &begin) + a.C - 1) / a.C);
     u64 S[2][4], kv[2][4], ms[2][4];
     size_t o = ((size_t)c * a.kv_heads + h) * words + word;
     auto live = [&](int k) { return col < a.v_dim && row + k < a.k_dim; };
     int len = 0;                                         // of the chunk; none where it had no room: then it and those behind it are not worked out
     auto load = [&](int chunk) {
-        len = a.found[chunk].y;
+        len = attn_chunk(a, chunk).y;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -762,11 +801,11 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a) {
     pdl_wait();
     using namespace attn;
     const int v_tiles = (a.v_dim + LEFT - 1) / LEFT, t_blocks = blocks(a.C), k_blocks = blocks(a.k_dim);
-    attn_tiles(attn_smem, 2 * a.chunks * a.q_heads, a.error, [&](int item) { return a.found[(item >> 1) / a.q_heads].y == 0 ? 0 : 2 * v_tiles; },
+    attn_tiles(attn_smem, 2 * a.chunks * a.q_heads, a.error, [&](int item) { return attn_chunk(a, (item >> 1) / a.q_heads).y == 0 ? 0 : 2 * v_tiles; },
                [&](int item, int n) {
         const int i = item & 1, ch = item >> 1, c = ch / a.q_heads, hq = ch - c * a.q_heads, h = hq / (a.q_heads / a.kv_heads);
         const int v0 = (n >> 1) * LEFT, wide = min(LEFT, up16(a.v_dim) - v0);
-        const int4 found = a.found[c];
+        const int4 found = attn_chunk(a, c);
         AttnTile x;
         x.add = n & 1;
         if (n & 1) {
