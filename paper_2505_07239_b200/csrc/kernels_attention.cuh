@@ -400,6 +400,10 @@ __device__ __forceinline__ void attn_tiles(uint8_t* raw, int items, int* error, 
     __syncthreads();
     ptx::fence_after_sync();
     const uint32_t tmem = s.tmem, full0 = ptx::smem_u32(&s.full[0]), empty0 = ptx::smem_u32(&s.empty[0]), planes0 = ptx::smem_u32(planes);
+    auto settle = [](uint32_t bar, uint32_t parity) {     // a limit of its own: the abort flag is up
+        const long long t0 = clock64();
+        while (!ptx::mbar_try_wait(bar, parity) && clock64() - t0 < 20000000ll) {}
+    };
     if (warp == PRODUCER) {
         if (ptx::elect_one()) {
             int slot = 0, issued = 0;
@@ -420,15 +424,12 @@ __device__ __forceinline__ void attn_tiles(uint8_t* raw, int items, int* error, 
                         if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
                     }
                 }
-            if (!ok) {
-                // gave up: let the copies already in flight land before the CTA leaves
-                for (int j = 1; j <= min(issued, SLOTS); ++j) {
-                    int k = slot - j;
-                    uint32_t ph = phase;
-                    if (k < 0) { k += SLOTS; ph ^= 1u; }
-                    const long long t0 = clock64();
-                    while (!ptx::mbar_try_wait(full0 + 8 * k, ph) && clock64() - t0 < 20000000ll) {}
-                }
+            // gave up: let the copies already in flight land before the CTA leaves
+            for (int j = 1; j <= min(issued, SLOTS) && !ok; ++j) {
+                int k = slot - j;
+                uint32_t ph = phase;
+                if (k < 0) { k += SLOTS; ph ^= 1u; }
+                settle(full0 + 8 * k, ph);
             }
         }
     } else if (warp == ISSUER) {
@@ -437,7 +438,7 @@ __device__ __forceinline__ void attn_tiles(uint8_t* raw, int items, int* error, 
             const uint32_t acc_full = ptx::smem_u32(&s.acc_full), acc_empty = ptx::smem_u32(&s.acc_empty), left0 = limb_desc_lo(planes0);
             int slot = 0, issued = 0;
             uint32_t phase = 0, acc_phase = 0;
-            bool ok = true;
+            bool ok = true, sums = false;
             for (int item = blockIdx.x; item < items && ok; item += gridDim.x)
                 for (int n = 0, count = tiles(item); n < count && ok; ++n) {
                     const AttnTile x = tile(item, n);
@@ -469,15 +470,18 @@ __device__ __forceinline__ void attn_tiles(uint8_t* raw, int items, int* error, 
                     }
                     if (!ok) break;
                     ptx::mma_commit(acc_full);
+                    sums = true;
                     acc_phase ^= 1u;
                 }
-            // the last reports of the tensor core have to find this CTA's memory
-            for (int j = 1; j <= min(issued, SLOTS) && ok; ++j) {
+            // the last reports of the tensor core have to find this CTA's memory, also where somebody gave up (else the draining warps have seen those of sums)
+            for (int j = 1; j <= min(issued, SLOTS); ++j) {
                 int k = slot - j;
                 uint32_t ph = phase;
                 if (k < 0) { k += SLOTS; ph ^= 1u; }
-                ok = limb_wait(empty0 + 8 * k, ph, &s.abort_flag);
+                if (ok) ok = limb_wait(empty0 + 8 * k, ph, &s.abort_flag);
+                if (!ok) settle(empty0 + 8 * k, ph);
             }
+            if (!ok && sums) settle(acc_full, acc_phase ^ 1u);
         }
     } else {
         auto meet = [&] {
