@@ -607,15 +607,19 @@ int comet_norm_rotate(void* cuda_stream, const comet_norm_rotate_args* args);
  * Rows of tokens that are in no chunk, and states in Es of chunks that there are not, stay as they are in every result, or are set to zero where
  * `zero_unwritten` is 1: for messages in memory that held something else before.  Where the starts are not ascending or leave the tokens, that
  * sequence counts as empty; where the chunks are more than `chunks`, or sequences that overlap have more tokens together than there are, the
- * surplus ones are not worked out; either way, and where they are
- * fewer, `bad_starts_flag` (device int32, may be null) is set to 1.  The caller clears the flag.
+ * surplus ones are not worked out; either way, and where they are fewer, `bad_starts_flag` (device int32, may be null) is set to 1.  The caller
+ * clears the flag.
  * Stateless; DEVICE pointers on the current device, owned by the caller, 8-byte aligned.  The work is enqueued on `cuda_stream` (NULL =
  * default stream) and the call does not wait for it.  `workspace` is 256-byte aligned and has at least the bytes that
  * comet_linear_attention_workspace reports for these sizes; a captured call keeps its address, and calls whose work may overlap in
  * time need one each.
- * Errors: INVALID_ARG (null or unaligned pointer, overlap, a `zero_unwritten` that is neither 0 nor 1), SHAPE (a size below 1, but for chunks; kv_heads not a divisor of q_heads; q_heads above
- * 4096; k_dim or v_dim odd or above 256; chunk above 64; tokens, sequences or chunks above 2^20; tokens * q_heads or chunks * q_heads above 2^24; batch *
- * q_heads above 2^24; a stride below its heads' words or above 2^32; frac_bits outside [1, 31]; workspace too small), CUDA. */
+ * The waits of a prompt's kernels are bounded (about two seconds, which no working launch comes near): after one that ran out the words of Ep, O, Es and
+ * the states are not to be trusted, and comet_static_status says so.  The first call of either on a device makes settings once; make it outside
+ * stream capture.
+ * Errors: INVALID_ARG (null or unaligned pointer, overlap, a `zero_unwritten` that is neither 0 nor 1), SHAPE (a size below 1, but for chunks;
+ * kv_heads not a divisor of q_heads; q_heads above 4096; k_dim or v_dim odd or above 256; chunk above 64; tokens, sequences, chunks or batch
+ * above 2^20; tokens * q_heads, chunks * q_heads, sequences * kv_heads or batch * q_heads above 2^24; a stride above 2^32, negative or, of more
+ * than one token, below its heads' words; frac_bits outside [1, 31]; workspace too small), CUDA. */
 typedef struct {
     int32_t tokens, sequences, q_heads, kv_heads, k_dim, v_dim, chunk, chunks;
     int64_t q_stride, k_stride, v_stride;
@@ -694,7 +698,7 @@ int comet_linear_attention_step(void* cuda_stream, const comet_linear_attention_
  * groups, ...]; gain, gain_mask, bias, G [channels]; T, VW, D [samples, channels].
  * Stateless; DEVICE pointers on the current device, owned by the caller, 8-byte aligned; what is written must not overlap any other
  * argument.  The work is enqueued on `cuda_stream` and the call does not wait for it.  `workspace` is 256-byte aligned and has at least the
- * bytes that comet_group_norm_workspace reports for these sizes on this device (often none); a captured call keeps its address, and calls
+ * bytes that comet_group_norm_workspace reports for these sizes (often none); a captured call keeps its address, and calls
  * whose work may overlap in time need one each.  The first call on a device makes settings once; make it outside stream capture.
  * Errors: INVALID_ARG (null or unaligned pointer, overlap, a gain without its bias, a `quadratic` that is neither 0 nor 1), SHAPE
  * (a size below 1, channels not a multiple of groups, a group of more than 2^24 words, more than 2^24 groups of all samples, channels above
@@ -728,7 +732,7 @@ typedef struct {
     int64_t workspace_bytes;
 } comet_group_norm_args;
 int comet_group_norm(void* cuda_stream, const comet_group_norm_args* args);
-/* Bytes of workspace that comet_group_norm takes for these sizes on the current device.  Errors: INVALID_ARG, SHAPE, CUDA. */
+/* Bytes of workspace that comet_group_norm takes for these sizes.  Errors: INVALID_ARG, SHAPE. */
 int comet_group_norm_workspace(int32_t samples, int32_t positions, int32_t channels, int32_t groups, int64_t* bytes_out);
 
 /* ---------------------------------------------------------------------------
@@ -787,8 +791,8 @@ int comet_beaver_matmul_static(void* cuda_stream, const uint64_t* const X[2], co
                                const uint64_t* const Y[2], const uint64_t* const B[2], const uint64_t* const C[2],
                                uint64_t* const Z[2], int32_t T, int32_t K, int32_t N);
 
-/* Waits for `cuda_stream` and reports whether a comet_beaver_matmul_static or comet_linear call
- * on the current device gave up on a bounded wait since this was last asked:
+/* Waits for `cuda_stream` and reports whether a comet_beaver_matmul_static, comet_linear or
+ * comet_linear_attention call on the current device gave up on a bounded wait since this was last asked:
  * COMET_OK, COMET_ERR_TIMEOUT (the results since then are not to be trusted) or
  * COMET_ERR_CUDA.  The report is given once.  Allocates nothing. */
 int comet_static_status(void* cuda_stream);

@@ -356,8 +356,8 @@ def beaver_matmul_static(X, A, Y, B, C, Z, stream: Optional[torch.cuda.Stream] =
 
 
 def static_status(stream: Optional[torch.cuda.Stream] = None) -> int:
-    """Waits for the stream; ERR_TIMEOUT if a beaver_matmul_static or linear call on the current device gave up on a bounded
-    wait since this was last asked (comet_static_status), else 0 = ok."""
+    """Waits for the stream; ERR_TIMEOUT if a beaver_matmul_static, linear or linear_attention call on the current device gave up on a
+    bounded wait since this was last asked (comet_static_status), else 0 = ok."""
     return _lib.comet_static_status(ctypes.c_void_p(stream.cuda_stream if stream is not None else 0))
 
 
