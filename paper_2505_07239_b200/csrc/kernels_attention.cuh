@@ -219,7 +219,7 @@ __device__ __forceinline__ void attn_emit(uint8_t* block, int rows, int row, int
 // memory: of a word and party two in, one out as a message, and three sets of planes for both parties.  q and k: eight words of a row a thread, four
 // threads a row's 32 words.  v and d, whose contraction runs over the tokens: eight tokens of a word a thread, sixteen tokens x sixteen words a
 // warp, 128 bytes of a token.  Eight bytes a plane at once either way, 256 bytes a warp, whole sectors.
-// The case: 118 us, 570 MB; four bytes a plane at once took 135 us, a third CTA an SM (80 registers) 135 as well.
+// The case: 114 us, 570 MB; four bytes a plane at once took 135 us, a third CTA an SM (80 registers) 135 as well.
 template <bool VEC>
 __global__ void __launch_bounds__(attn::THREADS, 2)
 attn_open_kernel(const __grid_constant__ AttnArgs a, int slabs) {
@@ -554,7 +554,7 @@ __device__ __forceinline__ void attn_finish(u64* words, int rows, int cols, L&& 
 }
 
 // Items: chunks and key heads, the sums of d v^T, tiles of party, v_dim and k_dim; then chunks and query heads, the weights, a tile a party.  Both only
-// need what was opened, so they share a launch: 97 us for the case, tensor pipe 42 %, 410 MB.
+// need what was opened, so they share a launch: 97 to 102 us for the case, tensor pipe 36 to 42 %, 410 MB.
 template <bool VEC>
 __global__ void __launch_bounds__(attn::TILE_THREADS, 1)
 attn_products_kernel(const __grid_constant__ AttnArgs a) {
@@ -710,9 +710,9 @@ __device__ __forceinline__ void attn_clear(const AttnArgs& a, int part) {
 }
 
 // The state from chunk to chunk of a sequence and key head, four words of a column and both parties a thread; says whether the starts were in order.
-// Bound by memory: the next chunk's words are on their way while this one's are worked on.  49 us for the case, 290 MB (5.9 TB/s).  Carried along by
+// Bound by memory: the next chunk's words are on their way while this one's are worked on.  50 us for the case, 290 MB (5.8 TB/s).  Carried along by
 // the kernel of the products, tile by tile in shared memory, it saved the 134 MB of sums, but left few warps an SM to wait for memory: 152 us for both, where
-// the two kernels take 146.
+// the two kernels took 146.
 __global__ void __launch_bounds__(attn::STATE_THREADS)
 attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
     pdl_wait();
@@ -797,7 +797,7 @@ attn_state_kernel(const __grid_constant__ AttnArgs a, int pieces) {
 }
 
 // Items: chunks, query heads and parties, the rows of O: for every tile of v_dim the far part w[r + 1] tr(q S), then the near part P v, which is added to what
-// the far part left in shared memory.  80 us for the case, tensor pipe 40 %, 360 MB.
+// the far part left in shared memory.  81 to 84 us for the case, tensor pipe 34 to 40 %, 360 MB.
 template <bool VEC>
 __global__ void __launch_bounds__(attn::TILE_THREADS, 1)
 attn_rows_kernel(const __grid_constant__ AttnArgs a) {
@@ -858,7 +858,7 @@ attn_rows_kernel(const __grid_constant__ AttnArgs a) {
 // and the new state out.  A CTA has both parties' words of a slice of a state's columns, a thread one pair of columns in every
 // row_groups-th row, so every word passes once through the thread that exchanges it; q and k lie in shared memory, what they
 // are multiplied with as they are needed.  The sums of o are added up over the row groups at the end.  32 sequences x 32 heads of 128 x 128: 237 us, 0.88
-// of the measured copy rate; a few heads 16 us, most of which is the launch and one trip to memory behind another.
+// of the measured copy rate; one sequence of 12 heads of 64 5.5 us, seven of 10 heads on 2 of 80 x 96 9.7 (the call, 16, is the host's).
 // ---------------------------------------------------------------------------
 struct AttnStepArgs {
     const u64* Q[2]; const u64* K[2]; const u64* V[2];
